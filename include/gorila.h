@@ -341,6 +341,156 @@ int gorila_ps_apply(float* theta_plus, float* accum, int64_t n, const float* gra
                     const uint8_t* keep, const int64_t* grad_version, int64_t* ps_version,
                     int64_t max_delay, float lr, float eps, uint8_t* applied_out, gorila_ctx* ctx);
 
+/* ---- A recurrent core on the network's features (partially observed games) ----
+ *
+ * Operators for sequences of feature rows: learners train on replayed sequences
+ * that hold episode starts, actors take one step at a time with a state kept for
+ * every environment.  Conventions beyond those at the top of this file:
+ *  - `dtype` (GORILA_F32 or GORILA_BF16) is the type of the rows: inputs, outputs
+ *    and their gradients.  Parameters, parameter gradients, states and scales are
+ *    fp32; sums are formed in fp32.
+ *  - Inputs with strides: element c of step t of sequence b is at
+ *    b * batch_stride + t * step_stride + c (in elements; any strides, the inner
+ *    dimensions contiguous).  Outputs are contiguous.  Any alignment of the
+ *    element type is accepted; 4 elements' alignment (of bases and strides) is faster.
+ *  - reset [batch][length] u8 (may be NULL): nonzero = this step begins an episode,
+ *    and nothing of earlier steps reaches it or any later one, whatever their
+ *    values (infinities and NaN included).
+ *  - slot [rows] int32 (may be NULL: row i uses slot i): which of `slots` states row
+ *    i of a single-step call uses.  Rows that name one slot twice race.  A slot out
+ *    of range reads a zero state, writes none and sets the sticky device error
+ *    (GORILA_ERANGE from gorila_ctx_check); it needs a context with a workspace
+ *    (GORILA_EWORKSPACE).
+ *  - Calls that use the workspace say so; after them the values behind
+ *    gorila_learner_td are gone.
+ *  - Zero rows, sequences or steps are a no-op that still writes the outputs that
+ *    have elements (a carried state, zero parameter gradients). */
+
+/* Norm with the residual's addition, over `rows` rows of `width` (1 .. 65536):
+ *   total = x + residual, rounded to dtype (residual NULL: total = x),
+ *   rho = 1 / sqrt(mean(total^2) + eps),   y = total * rho * weight.
+ * Row i of x is at x + i * x_stride elements, of residual at residual + i *
+ * residual_stride.  total, y [rows, width], rstd [rows] = rho fp32; total may be
+ * NULL, and so may rstd.  EINVAL for eps < 0. */
+int gorila_add_rmsnorm(const void* x, int64_t x_stride, const void* residual,
+                       int64_t residual_stride, const float* weight, int64_t rows, int32_t width,
+                       int32_t dtype, float eps, void* y, void* total, float* rstd,
+                       gorila_ctx* ctx);
+/* The same with 8-bit rows out: u = total * weight, m = max |u| of the row,
+ * codes = round to nearest even of u * (127 / m) (int8; each operation one fp32
+ * operation rounded once), scale [rows] = rho * (m / 127), so codes * scale
+ * stands for y.  A row of zeros has codes and scale 0; a row that is not finite
+ * has codes 0 and a NaN scale. */
+int gorila_add_rmsnorm_codes(const void* x, int64_t x_stride, const void* residual,
+                             int64_t residual_stride, const float* weight, int64_t rows,
+                             int32_t width, int32_t dtype, float eps, int8_t* codes, float* scale,
+                             void* total, gorila_ctx* ctx);
+/* Gradients: with dy and dtotal (NULL: none) those that reach y and total,
+ *   dx = dtotal + rho * weight * dy - total * rho^3 * mean(weight * dy * total)
+ * [rows, width] (of x and of residual alike) and dweight [width] =
+ * sum over rows of dy * total * rho.  Uses
+ * gorila_add_rmsnorm_workspace_bytes(width) of the workspace. */
+size_t gorila_add_rmsnorm_workspace_bytes(int32_t width);
+int gorila_add_rmsnorm_backward(const void* dy, int64_t dy_stride, const void* dtotal,
+                                int64_t dtotal_stride, const void* total, const float* rstd,
+                                const float* weight, int64_t rows, int32_t width, int32_t dtype,
+                                void* dx, float* dweight, gorila_ctx* ctx);
+
+/* Short causal convolution of every channel with its own `taps` (2 .. 4) weights:
+ *   v[t][c] = bias[c] + sum_j weight[c][j] * e[t - taps + 1 + j][c],
+ *   y = v * sigmoid(v) (silu = 1) or v (silu = 0),
+ * with e the steps before the sequence (window [batch][taps-1][channels] of
+ * dtype, oldest first; NULL: zeros), then x; a tap with an episode start after
+ * it, up to t, counts as zero.  window_out (may be NULL, may not be window) is
+ * the window for the steps that follow.  bias may be NULL. */
+typedef struct {
+    int32_t dtype, batch, length, channels, taps, silu;
+    const void* x;
+    int64_t x_batch_stride, x_step_stride;
+    const float* weight;      /* [channels][taps] */
+    const float* bias;        /* [channels] */
+    const uint8_t* reset;     /* [batch][length] */
+    const void* window;
+} gorila_causal_conv_args;
+int gorila_causal_conv(const gorila_causal_conv_args* args, void* y, void* window_out,
+                       gorila_ctx* ctx);
+/* Gradients for dy and dwindow_out (NULL: none): dx [batch][length][channels],
+ * dweight, dbias (NULL if there is no bias), dwindow (may be NULL).  Uses
+ * gorila_causal_conv_workspace_bytes(channels, taps) of the workspace. */
+size_t gorila_causal_conv_workspace_bytes(int32_t channels, int32_t taps);
+int gorila_causal_conv_backward(const gorila_causal_conv_args* args, const void* dy,
+                                int64_t dy_batch_stride, int64_t dy_step_stride,
+                                const void* dwindow_out, void* dx, float* dweight, float* dbias,
+                                void* dwindow, gorila_ctx* ctx);
+/* One step of `batch` rows (length 1): row i's window is window_pool[slot[i]]
+ * ([slots][taps-1][channels] of dtype), updated in place; args->window is unused. */
+int gorila_causal_conv_step(const gorila_causal_conv_args* args, void* window_pool, int64_t slots,
+                            const int32_t* slot, void* y, gorila_ctx* ctx);
+
+/* Selective scan: `heads` heads of head_dim channels with a state of state_dim
+ * each; head h reads the b and c of group h / (heads / groups).
+ *   d = softplus(dt + dt_bias[h]),   a = exp(-exp(a_log[h]) * d), 0 at a reset,
+ *   S_t = a_t S_{t-1} + d_t x_t b_t^T   (head_dim x state_dim, from `state`),
+ *   y_t = S_t c_t + skip[h] x_t.
+ * x [batch][length][heads][head_dim], dt [batch][length][heads], b and c
+ * [batch][length][groups][state_dim], y as x; state and state_out
+ * [batch][heads][head_dim][state_dim] (NULL: zeros / not wanted; state_out may be
+ * state).  head_dim and state_dim 1 .. 128 (else GORILA_EUNSUPPORTED).  Uses
+ * gorila_scan_workspace_bytes(..., backward) of the workspace (0: none). */
+typedef struct {
+    int32_t dtype, batch, length, heads, head_dim, groups, state_dim, reserved;
+    const void* x;
+    int64_t x_batch_stride, x_step_stride;
+    const void* dt;
+    int64_t dt_batch_stride, dt_step_stride;
+    const void* b;
+    int64_t b_batch_stride, b_step_stride;
+    const void* c;
+    int64_t c_batch_stride, c_step_stride;
+    const float* a_log;       /* [heads] */
+    const float* dt_bias;     /* [heads] */
+    const float* skip;        /* [heads] */
+    const uint8_t* reset;     /* [batch][length] */
+    const float* state;
+} gorila_scan_args;
+size_t gorila_scan_workspace_bytes(int32_t batch, int32_t length, int32_t heads, int32_t head_dim,
+                                   int32_t groups, int32_t state_dim, int32_t backward);
+int gorila_scan(const gorila_scan_args* args, void* y, float* state_out, gorila_ctx* ctx);
+/* Gradients for dy and dstate_out (NULL: none) of every input: dx, ddt, db, dc as
+ * their inputs (contiguous), da_log, ddt_bias, dskip [heads], dstate (may be NULL).
+ * Nothing but the inputs is kept from the forward call. */
+int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t dy_batch_stride,
+                         int64_t dy_step_stride, const float* dstate_out, void* dx, void* ddt,
+                         void* db, void* dc, float* da_log, float* ddt_bias, float* dskip,
+                         float* dstate, gorila_ctx* ctx);
+/* One step of `batch` rows (length 1): row i's state is state_pool[slot[i]]
+ * ([slots][heads][head_dim][state_dim]), updated in place; args->state is unused. */
+int gorila_scan_step(const gorila_scan_args* args, float* state_pool, int64_t slots,
+                     const int32_t* slot, void* y, gorila_ctx* ctx);
+
+/* 4-bit weights with group scales: w[o][k] stands for scales[o][k / group] *
+ * (code - 8), code 0 .. 15.  codes [outputs][16 * ceil(inputs / 32)] bytes (whole
+ * runs of 32 codes, what lies past `inputs` is never read as a weight): code k in
+ * byte k / 2, even k in the low half.  scales [outputs][ceil(inputs / group)] fp32.
+ * group is 32, 64 or 128.  codes 16-byte aligned.
+ *
+ * gorila_quantize_weights makes them from weights [outputs][inputs] (dtype): m =
+ * max |w| of the group, scale = m / 7, code = 8 + round to nearest even of w *
+ * (7 / m) (a group of zeros: scale 0, codes 8; a group that is not finite: NaN
+ * scale, codes 8). */
+int gorila_quantize_weights(const void* weights, int64_t weights_stride, int32_t outputs,
+                            int32_t inputs, int32_t dtype, int32_t group, uint8_t* codes,
+                            float* scales, gorila_ctx* ctx);
+/* y[i][o] = sum_k x[i][k] w[o][k] for `rows` rows (row i of x at x + i *
+ * x_stride elements).  x_dtype GORILA_F32 or GORILA_BF16 (y of the same type), or
+ * GORILA_CODES: int8 rows with x_scale [rows] (as gorila_add_rmsnorm_codes makes
+ * them), y fp32.  Made for the few rows of actors; any number of rows is
+ * accepted. */
+enum { GORILA_CODES = 2 };
+int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_t x_dtype,
+                   int64_t rows, const uint8_t* codes, const float* scales, int32_t outputs,
+                   int32_t inputs, int32_t group, void* y, gorila_ctx* ctx);
+
 #ifdef __cplusplus
 }
 #endif

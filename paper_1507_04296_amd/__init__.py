@@ -33,6 +33,11 @@ EXPORTS = (
     "gorila_ctx_timing_begin", "gorila_ctx_timing_end", "gorila_stage_name",
     "gorila_loss_filter", "gorila_ps_apply", "gorila_replay_insert", "gorila_epsilon",
     "gorila_params_sync", "gorila_learner_td", "gorila_act_noalloc",
+    "gorila_add_rmsnorm", "gorila_add_rmsnorm_codes", "gorila_add_rmsnorm_workspace_bytes",
+    "gorila_add_rmsnorm_backward", "gorila_causal_conv", "gorila_causal_conv_workspace_bytes",
+    "gorila_causal_conv_backward", "gorila_causal_conv_step", "gorila_scan_workspace_bytes",
+    "gorila_scan", "gorila_scan_backward", "gorila_scan_step", "gorila_quantize_weights",
+    "gorila_qmatvec",
 )
 NOALLOC_MAX_STATES = 256  # GORILA_NOALLOC_MAX_STATES
 
@@ -98,6 +103,8 @@ def lib() -> ctypes.CDLL:
         "gorila_learner_td": (ctypes.c_int, [vp, vp, vp, vp]),
         "gorila_act_noalloc": (ctypes.c_int, [P, vp, i32, f32, u64, vp, vp, vp]),
     }
+    from .sequence import SIGNATURES
+    sig.update(SIGNATURES)
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
         fn.restype, fn.argtypes = res, args
@@ -140,11 +147,12 @@ class Context:
     """A gorila_ctx bound to a torch-allocated device workspace.
 
     The workspace is sized for calls with batch <= max_batch (learner step) or
-    n <= 2 * max_batch states (forward / act); max_batch = 0 makes a context
-    without one (for gorila_act_noalloc and the calls that need none)."""
+    n <= 2 * max_batch states (forward / act), and for sequence operators that need
+    up to min_bytes; max_batch = 0 makes a context without one (for
+    gorila_act_noalloc and the calls that need none)."""
 
     def __init__(self, max_batch: int, n_actions: int, groups: int = 1, device=None,
-                 dtype: int = GORILA_F32):
+                 dtype: int = GORILA_F32, min_bytes: int = 0):
         import torch
         self.device = torch.device(device if device is not None else "cuda")
         if max_batch == 0:  # a context without a workspace (gorila_act_noalloc)
@@ -153,6 +161,7 @@ class Context:
             self.ws_bytes = workspace_bytes(max_batch, n_actions, dtype, groups)
             if self.ws_bytes == 0:
                 raise ValueError("invalid workspace request")
+            self.ws_bytes = max(self.ws_bytes, int(min_bytes))
         with torch.cuda.device(self.device):
             if self.ws_bytes:
                 self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
@@ -458,3 +467,16 @@ def gather(ctx: Context, replay: Replay, idx):
 
 
 INF = math.inf
+
+_SEQUENCE = ("add_rmsnorm", "add_rmsnorm_codes", "add_rmsnorm_workspace_bytes", "add_rmsnorm_backward",
+             "causal_conv", "causal_conv_workspace_bytes", "causal_conv_backward", "causal_conv_step",
+             "scan", "scan_workspace_bytes", "scan_backward", "scan_step", "quantize_weights", "qmatvec")
+
+
+def __getattr__(name: str):
+    """The sequence operators (sequence.py) as names of the package, loaded at first use."""
+    if name in _SEQUENCE:
+        from . import sequence
+        value = globals()[name] = getattr(sequence, name)
+        return value
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -9,6 +9,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "seq.h"
 
 using namespace gorila;
 
@@ -331,6 +332,25 @@ int noalloc_scratch(int dev, hipStream_t st, char** out) {
 }
 
 }  // namespace
+
+namespace gorila {
+
+const size_t WS_FIXED_BYTES = WS_HEAD + ZERO_BYTES;
+
+int ctx_view(gorila_ctx* ctx, size_t need, CtxView& out) {
+    const int rc = check_ctx(ctx);
+    if (rc) return rc;
+    const bool has = ctx->ws && ctx->ws_bytes >= WS_FIXED_BYTES;
+    if (need && (!has || need > ctx->ws_bytes - WS_FIXED_BYTES)) return GORILA_EWORKSPACE;
+    if (need) ctx->td_valid = false;  // the call overwrites a learner call's rows
+    out.stream = ctx->stream;
+    out.cus = ctx->cus;
+    out.ws = has ? ctx->ws + WS_FIXED_BYTES : nullptr;
+    out.err = has ? (unsigned*)ctx->ws : nullptr;
+    return GORILA_OK;
+}
+
+}  // namespace gorila
 
 extern "C" {
 

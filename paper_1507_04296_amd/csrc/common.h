@@ -25,6 +25,7 @@ namespace gorila {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 // the same, and four bf16 bit patterns, at any element's address
 typedef float f32x4a __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint16_t u16x4a __attribute__((ext_vector_type(4), aligned(2)));

@@ -1,0 +1,1058 @@
+// The selective scan (gorila_scan, _backward, _step).
+//
+// With log-decays g_t = log a_t, G_t their running sum inside a chunk of Q steps,
+// v_t = d_t x_t, and the state S before the chunk, one head's chunk is
+//   y_t = sum_{s <= t} e^(G_t - G_s) (c_t . b_s) v_s + e^(G_t) S c_t + skip x_t,
+//   S'  = e^(G_Q) S + sum_s e^(G_Q - G_s) v_s b_s^T,
+// matrix products of Q x Q, Q x state and head_dim x state, formed on
+// v_mfma_f32_16x16x4_f32 from LDS.  An episode start cuts the chunk: a pair (t, s)
+// counts only where both are in one episode, S only for the steps before the first
+// start.  Backward, with R the gradient that reaches the state after the chunk and
+// F_ts = e^(G_t - G_s) (dy_t . x_s), M_ts = e^(G_t - G_s) (c_t . b_s),
+//   dv_s = sum_t M_ts dy_t + w_s R b_s,            w_s = e^(G_Q - G_s)
+//   dc_t = sum_s F_ts d_s b_s + e^(G_t) S^T dy_t,
+//   db_s = d_s q_s,  q_s = sum_t F_ts c_t + w_s R^T x_s,
+//   R'   = e^(G_Q) R + sum_t e^(G_t) dy_t c_t^T,
+// and the gradient of g_t is the sum over all that passes from before t to t and
+// after: pairs s < t <= u inside the chunk (F_us d_s (c_u . b_s)), the state before
+// to the steps from t on, the steps before t to the state behind, and the state
+// before to the state behind.  (The shorter sum_{u >= t} (c_u . dc_u - b_u . db_u)
+// + <R, S'> is the same number, but cancels what does not pass t: with large step
+// sizes its error is thousands of times the gradient's.)
+//
+// A workgroup of four waves walks the chunks of one segment of one (sequence,
+// head, 64 channels), the state in registers (a wave holds 16 channels).  Where
+// there are few of those, sequences are cut into segments whose states are formed
+// first (state_kernel), joined (join_kernel), and walked again side by side.
+//
+// Masked products multiply by zero, which is no mask for infinities and NaN, so a
+// chunk that holds any is walked one step at a time.
+#include "seq.h"
+
+namespace gorila {
+namespace {
+
+constexpr int Q = 32;    // steps a chunk
+constexpr int PW = 64;   // channels a workgroup
+constexpr int LP = PW + 4, LQ = Q + 4;  // LDS row lengths: 16 lanes' quads on all banks
+constexpr float LOG2E = 1.44269504088896341f;
+
+struct ScanView {
+    const void *x, *dt, *b, *c, *dy;
+    int64_t xb, xt, dtb, dtt, bb, bt, cb, ct, dyb, dyt;
+    const float *a_log, *dt_bias, *skip, *state;
+    const uint8_t* reset;
+    int B, T, H, P, G, N;
+    int ptiles, vh;       // 64-channel tiles of a head; heads * ptiles
+    int nch, cps, nseg;   // chunks, chunks a segment, segments
+    void* y;
+    float* state_out;
+    // segments' states [B][nseg][vh][PW][NP] and decays [B][nseg][vh] (< 0: an
+    // episode starts in it)
+    float *seg_s, *seg_r, *seg_a;
+    // backward
+    const float* dstate_out;
+    float *chunk_s;             // states before the chunks [B][nch][vh][PW][NP]
+    float *pdb, *pdc;           // [B][T][vh][N]
+    float *pdt;                 // [B][T][vh]
+    float *ppar;                // [B][nseg][vh][3]
+    void* dx;
+    float* dstate;
+};
+
+// Position of a workgroup: (sequence, segment, head, channels).
+struct Place {
+    int b, seg, v, h, p0, pw, grp;
+    __device__ Place(const ScanView& s, int id) {
+        v = id % s.vh;
+        const int r = id / s.vh;
+        seg = r % s.nseg;
+        b = r / s.nseg;
+        h = v / s.ptiles;
+        p0 = (v % s.ptiles) * PW;
+        pw = s.P - p0 < PW ? s.P - p0 : PW;
+        grp = h / (s.H / s.G);
+    }
+};
+
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+// Operands of 16 rows (columns) and 16 reduction indices: lane l holds row l % 16
+// and indices 4 (l / 16) .. +3.  kfrag: the reduction runs along the LDS rows.
+__device__ __forceinline__ f32x4 kfrag(const float* s, int ld, int row0, int k0, int l) {
+    return *(const f32x4*)(s + (row0 + (l & 15)) * ld + k0 + 4 * (l >> 4));
+}
+__device__ __forceinline__ f32x4 rfrag(const float* s, int ld, int k0, int col0, int l) {
+    const float* p = s + (k0 + 4 * (l >> 4)) * ld + col0 + (l & 15);
+    return f32x4{p[0], p[ld], p[2 * ld], p[3 * ld]};
+}
+
+// Q rows of COLS columns on their way from memory to LDS; rows past len and
+// columns past cols are zeros.
+template <int COLS, bool VEC, class T>
+struct Rows {
+    static constexpr int QUADS = COLS * Q / 4, R = (QUADS + 255) / 256;
+    f32x4 v[R];
+    __device__ __forceinline__ void load(const T* base, int64_t stride, int t0, int len, int cols, int tid) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int e = tid + 256 * i, row = e / (COLS / 4), col = e % (COLS / 4) * 4;
+            const bool in = row < len && col < cols;
+            v[i] = row_load<VEC>(base + (in ? (int64_t)(t0 + row) * stride + col : 0), in ? cols - col : 0);
+        }
+    }
+    // Adds 0 to bad, or NaN where a value is not finite.
+    __device__ __forceinline__ void store(float* lds, int ld, int tid, float& bad) const {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int e = tid + 256 * i, row = e / (COLS / 4), col = e % (COLS / 4) * 4;
+            if (QUADS % 256 == 0 || e < QUADS) *(f32x4*)(lds + row * ld + col) = v[i];
+            bad += (v[i][0] * 0.0f + v[i][1] * 0.0f) + (v[i][2] * 0.0f + v[i][3] * 0.0f);
+        }
+    }
+};
+
+// Step sizes, running log2-decays and episode numbers of a chunk.  A running sum is
+// kept as a whole number and a rest within +-1/2, so that the difference of two of
+// them is exact to 2^-23 however large both have grown: one sum in fp32 would lose
+// what few small steps after a large one differ by.
+struct Steps {
+    float d[Q], sig[Q], dec[Q];  // step size, d step size / d dt, own log2-decay
+    float gi[Q], gf[Q];          // sum of dec: whole number, rest
+    int ep[Q];                   // -1: past the end
+    float end_gi, end_gf;
+    int end_ep;
+};
+__device__ __forceinline__ float pow2(float v) { return __builtin_amdgcn_exp2f(v); }
+constexpr float LEAST_LOG2 = -65536.0f;  // 2^this is zero, and sums of Q of it are whole numbers below 2^24
+struct StepRegs {
+    float dt;
+    int reset;
+    template <class T>
+    __device__ __forceinline__ void load(const T* dt_base, int64_t stride, const uint8_t* rs, int t0, int len, int l) {
+        const bool in = l < len;
+        dt = in ? row_value(dt_base[(int64_t)(t0 + l) * stride]) : 0.0f;
+        reset = in && rs ? rs[t0 + l] != 0 : 0;
+    }
+    // By the lanes of one wave (lanes past Q take part and store nothing).
+    __device__ __forceinline__ void store(Steps& s, float bias, float rate2, int len, int l, float& bad) const {
+        const float v = dt + bias;
+        const float e = expf(-fabsf(v));
+        float d = fmaxf(v, 0.0f) + log1pf(e);
+        if (v != v) d = v;
+        if (l >= len) d = 0.0f;
+        float dec = rate2 * d;
+        if (dec < LEAST_LOG2) dec = LEAST_LOG2;
+        float gi = rintf(dec), gf = dec - gi;
+        int ep = reset;
+#pragma unroll
+        for (int o = 1; o < Q; o <<= 1) {
+            const float iu = __shfl_up(gi, o, 64), fu = __shfl_up(gf, o, 64);
+            const int eu = __shfl_up(ep, o, 64);
+            if (l >= o) {
+                gf += fu;
+                const float r = rintf(gf);
+                gi += iu + r;
+                gf -= r;
+                ep += eu;
+            }
+        }
+        if (l == Q - 1) {
+            s.end_gi = gi;
+            s.end_gf = gf;
+            s.end_ep = ep;
+        }
+        if (l < Q) {
+            s.d[l] = d;
+            s.gi[l] = gi;
+            s.gf[l] = gf;
+            s.ep[l] = l < len ? ep : -1;
+            s.dec[l] = dec;
+            s.sig[l] = l < len ? (v >= 0.0f ? 1.0f : e) / (1.0f + e) : 0.0f;
+            bad += d * 0.0f;
+        }
+    }
+};
+// e^(G_t) and e^(G_end - G_s).
+__device__ __forceinline__ float from_start(const Steps& s, int t) { return pow2(s.gi[t] + s.gf[t]); }
+__device__ __forceinline__ float to_end(const Steps& s, int t) { return pow2((s.end_gi - s.gi[t]) + (s.end_gf - s.gf[t])); }
+
+// acc (rows: state, columns: 16 channels from 16 w) = decay * acc + sum over steps
+// of weight * m[step][state] * ch[step][channel].  AFTER: the state after the
+// chunk from the one before (weights w_s d_s); else the gradient before it from the
+// one after (weights e^G).
+template <int NT, bool AFTER>
+__device__ __forceinline__ void walk(f32x4 (&acc)[NT], const float* m, int ldm, const float* ch, const Steps& st, int w, int l) {
+    const int eq = st.end_ep;
+    const float all = pow2(st.end_gi + st.end_gf);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = eq == 0 ? acc[n] * all : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (!AFTER && st.ep[0] != 0) return;  // an episode starts with the chunk
+#pragma unroll
+    for (int kb = 0; kb < Q / 16; ++kb) {
+        const int k0 = 16 * kb + 4 * (l >> 4);
+        f32x4 v = rfrag(ch, LP, 16 * kb, 16 * w, l);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] *= AFTER ? (st.ep[k0 + j] == eq ? to_end(st, k0 + j) * st.d[k0 + j] : 0.0f) : (st.ep[k0 + j] == 0 ? from_start(st, k0 + j) : 0.0f);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] = mma(rfrag(m, ldm, 16 * kb, 16 * n, l), v, acc[n]);
+    }
+}
+
+// Registers <-> state arrays [channel][state], of `pn` states a channel in memory.
+template <int NT, bool VEC>
+__device__ __forceinline__ void load_state(f32x4 (&acc)[NT], const float* s, int ld, int pw, int n_in, int w, int l) {
+    const int p = 16 * w + (l & 15);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int n0 = 16 * n + 4 * (l >> 4);
+        const bool in = s && p < pw && n0 < n_in;
+        acc[n] = row_load<VEC>(in ? s + (int64_t)p * ld + n0 : s, in ? n_in - n0 : 0);
+    }
+}
+template <int NT, bool VEC>
+__device__ __forceinline__ void store_state(const f32x4 (&acc)[NT], float* s, int ld, int pw, int n_in, int w, int l) {
+    const int p = 16 * w + (l & 15);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int n0 = 16 * n + 4 * (l >> 4);
+        if (p < pw && n0 < n_in) row_store<VEC>(s + (int64_t)p * ld + n0, acc[n], n_in - n0);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ const T* of(const void* p, int64_t off) { return (const T*)p + off; }
+
+// Forward over one segment.
+template <class T, int NP, bool VEC>
+__global__ __launch_bounds__(256, 2) void scan_kernel(ScanView s) {
+    constexpr int NT = NP / 16, LN = NP + 4;
+    __shared__ __align__(16) float sc[Q * LN], sb[Q * LN], sx[Q * LP], ss[PW * LN], sm[Q * LQ];
+    __shared__ __align__(16) Steps st;
+    __shared__ int flag;
+    const Place at(s, blockIdx.x);
+    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lg = l >> 4, lc = l & 15;
+    const float rate2 = -expf(s.a_log[at.h]) * LOG2E, bias = s.dt_bias[at.h], skip = s.skip[at.h];
+    const T* x = of<T>(s.x, at.b * s.xb + (int64_t)at.h * s.P + at.p0);
+    const T* bm = of<T>(s.b, at.b * s.bb + (int64_t)at.grp * s.N);
+    const T* cm = of<T>(s.c, at.b * s.cb + (int64_t)at.grp * s.N);
+    const T* dt = of<T>(s.dt, at.b * s.dtb + at.h);
+    const uint8_t* rs = s.reset ? s.reset + (int64_t)at.b * s.T : nullptr;
+    T* y = (T*)s.y + ((int64_t)at.b * s.T * s.H + at.h) * s.P + at.p0;
+    const int64_t yt = (int64_t)s.H * s.P;
+    const int64_t state0 = (((int64_t)at.b * s.H + at.h) * s.P + at.p0) * s.N;
+
+    f32x4 S[NT];
+    if (s.nseg > 1)
+        load_state<NT, true>(S, s.seg_s + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * PW * NP, NP, PW, NP, w, l);
+    else
+        load_state<NT, VEC>(S, s.state ? s.state + state0 : nullptr, s.N, at.pw, s.N, w, l);
+    if (tid == 0) flag = 0;
+    const int c0 = at.seg * s.cps, c1 = c0 + s.cps < s.nch ? c0 + s.cps : s.nch;
+
+    Rows<PW, VEC, T> rx;
+    Rows<NP, VEC, T> rb, rc;
+    StepRegs rd;
+    auto load = [&](int t0, int len) {
+        rx.load(x, s.xt, t0, len, at.pw, tid);
+        rb.load(bm, s.bt, t0, len, s.N, tid);
+        rc.load(cm, s.ct, t0, len, s.N, tid);
+        if (w == 3) rd.load(dt, s.dtt, rs, t0, len, l);
+    };
+    auto stage = [&](int len) {
+        float bad = 0.0f;
+        rx.store(sx, LP, tid, bad);
+        rb.store(sb, LN, tid, bad);
+        rc.store(sc, LN, tid, bad);
+        if (w == 3) rd.store(st, bias, rate2, len, l, bad);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) *(f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg) = S[n];
+        if (bad != bad) flag = 1;
+    };
+    if (c0 < c1) load(c0 * Q, s.T - c0 * Q < Q ? s.T - c0 * Q : Q);
+    for (int c = c0; c < c1; ++c) {
+        const int t0 = c * Q, len = s.T - t0 < Q ? s.T - t0 : Q;
+        __syncthreads();
+        stage(len);
+        __syncthreads();
+        const bool single = flag != 0;
+        const int next = s.T - t0 - Q < Q ? s.T - t0 - Q : Q;
+        if (!single && c + 1 < c1) load(t0 + Q, next);
+        for (int u = 0; u < (single ? len : 1); ++u) {
+            const int tu = t0 + u, lu = single ? 1 : len;
+            if (single) {
+                __syncthreads();
+                load(tu, 1);
+                stage(1);
+                __syncthreads();
+            }
+            // what the state gives: rows = channels, columns = steps
+            f32x4 acc[Q / 16];
+#pragma unroll
+            for (int i = 0; i < Q / 16; ++i) {
+                acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[i] = mma(kfrag(ss, LN, 16 * w, 16 * n, l), kfrag(sc, LN, 16 * i, 16 * n, l), acc[i]);
+                const int t = 16 * i + lc;
+                acc[i] = st.ep[t] == 0 ? acc[i] * from_start(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            if (w < 3) {  // decay * (c_t . b_s) * d_s of one of the three tiles with s <= t
+                const int si = w >> 1, ti = w > 0;
+                f32x4 m{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
+                const int t = 16 * ti + lc, q0 = 16 * si + 4 * lg;
+                const float ti_ = st.gi[t], tf = st.gf[t];
+                const int et = st.ep[t];
+                const f32x4 gi = *(const f32x4*)(st.gi + q0), gf = *(const f32x4*)(st.gf + q0), d = *(const f32x4*)(st.d + q0);
+                const i32x4 ep = *(const i32x4*)(st.ep + q0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool same = t == q0 + j, on = t > q0 + j && ep[j] == et;
+                    m[j] = same ? m[j] * d[j] : on ? m[j] * (pow2((ti_ - gi[j]) + (tf - gf[j])) * d[j]) : 0.0f;
+                }
+                *(f32x4*)(sm + t * LQ + q0) = m;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < Q / 16; ++i) {
+#pragma unroll
+                for (int k = 0; k <= i; ++k) acc[i] = mma(rfrag(sx, LP, 16 * k, 16 * w, l), kfrag(sm, LQ, 16 * i, 16 * k, l), acc[i]);
+                const int t = 16 * i + lc, p = 16 * w + 4 * lg;
+                if (t < lu && p < at.pw)
+                    row_store<VEC>(y + (int64_t)(tu + t) * yt + p, acc[i] + skip * *(const f32x4*)(sx + t * LP + p), at.pw - p);
+            }
+            walk<NT, true>(S, sb, LN, sx, st, w, l);
+        }
+        if (single) {
+            __syncthreads();
+            if (tid == 0) flag = 0;
+            if (c + 1 < c1) load(t0 + Q, next);
+        }
+    }
+    if (s.state_out && at.seg == s.nseg - 1) store_state<NT, VEC>(S, s.state_out + state0, s.N, at.pw, s.N, w, l);
+}
+
+// What one segment adds to the state behind it (REV = false: from x and b) or to
+// the gradient of the state before it (REV = true: from dy and c), and its decay.
+template <class T, int NP, bool VEC, bool REV>
+__global__ __launch_bounds__(256, 2) void state_kernel(ScanView s) {
+    constexpr int NT = NP / 16, LN = NP + 4;
+    __shared__ __align__(16) float sb[Q * LN], sx[Q * LP];
+    __shared__ __align__(16) Steps st;
+    __shared__ int flag;
+    const Place at(s, blockIdx.x);
+    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
+    const float rate2 = -expf(s.a_log[at.h]) * LOG2E, bias = s.dt_bias[at.h];
+    const int64_t xt = REV ? s.dyt : s.xt, bt = REV ? s.ct : s.bt;
+    const T* x = of<T>(REV ? s.dy : s.x, at.b * (REV ? s.dyb : s.xb) + (int64_t)at.h * s.P + at.p0);
+    const T* bm = of<T>(REV ? s.c : s.b, at.b * (REV ? s.cb : s.bb) + (int64_t)at.grp * s.N);
+    const T* dt = of<T>(s.dt, at.b * s.dtb + at.h);
+    const uint8_t* rs = s.reset ? s.reset + (int64_t)at.b * s.T : nullptr;
+    f32x4 S[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) S[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (tid == 0) flag = 0;
+    const int c0 = at.seg * s.cps, c1 = c0 + s.cps < s.nch ? c0 + s.cps : s.nch;
+    float decay = 1.0f;
+    bool starts = false;
+
+    Rows<PW, VEC, T> rx;
+    Rows<NP, VEC, T> rb;
+    StepRegs rd;
+    auto load = [&](int t0, int len) {
+        rx.load(x, xt, t0, len, at.pw, tid);
+        rb.load(bm, bt, t0, len, s.N, tid);
+        if (w == 3) rd.load(dt, s.dtt, rs, t0, len, l);
+    };
+    auto stage = [&](int len) {
+        float bad = 0.0f;
+        rx.store(sx, LP, tid, bad);
+        rb.store(sb, LN, tid, bad);
+        if (w == 3) rd.store(st, bias, rate2, len, l, bad);
+        if (bad != bad) flag = 1;
+    };
+    auto first = [&](int i) { return REV ? c1 - 1 - i : c0 + i; };
+    auto length = [&](int c) { return s.T - c * Q < Q ? s.T - c * Q : Q; };
+    if (c0 < c1) load(first(0) * Q, length(first(0)));
+    for (int i = 0; i < c1 - c0; ++i) {
+        const int t0 = first(i) * Q, len = length(first(i));
+        __syncthreads();
+        stage(len);
+        __syncthreads();
+        const bool single = flag != 0;
+        if (!single && i + 1 < c1 - c0) load(first(i + 1) * Q, length(first(i + 1)));
+        decay *= pow2(st.end_gi + st.end_gf);
+        starts |= st.end_ep != 0;
+        for (int u = 0; u < (single ? len : 1); ++u) {
+            if (single) {
+                __syncthreads();
+                load(REV ? t0 + len - 1 - u : t0 + u, 1);
+                stage(1);
+                __syncthreads();
+            }
+            walk<NT, !REV>(S, sb, LN, sx, st, w, l);
+        }
+        if (single) {
+            __syncthreads();
+            if (tid == 0) flag = 0;
+            if (i + 1 < c1 - c0) load(first(i + 1) * Q, length(first(i + 1)));
+        }
+    }
+    const int64_t o = ((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v;
+    store_state<NT, true>(S, (REV ? s.seg_r : s.seg_s) + o * PW * NP, NP, PW, NP, w, l);
+    if (!REV && tid == 0) s.seg_a[o] = starts ? -1.0f : decay;
+}
+
+// Turns what each segment adds into the state before it (blockIdx.y = 0) or the
+// gradient behind it (1), in place, one thread an element.
+template <int NP, bool VEC>
+__global__ __launch_bounds__(256) void join_kernel(ScanView s) {
+    const int e = (blockIdx.x % (PW * NP / 256)) * 256 + threadIdx.x, o = blockIdx.x / (PW * NP / 256);
+    const int v = o % s.vh, b = o / s.vh, h = v / s.ptiles, p = (v % s.ptiles) * PW + e / NP, n = e % NP;
+    const bool rev = blockIdx.y != 0;
+    const float* from = rev ? s.dstate_out : s.state;
+    float* seg = (rev ? s.seg_r : s.seg_s) + ((int64_t)b * s.nseg * s.vh + v) * PW * NP + e;
+    const float* dec = s.seg_a + (int64_t)b * s.nseg * s.vh + v;
+    const int64_t step = (int64_t)s.vh * PW * NP;
+    float cur = from && p < s.P && n < s.N ? from[(((int64_t)b * s.H + h) * s.P + p) * s.N + n] : 0.0f;
+    for (int i = 0; i < s.nseg; ++i) {
+        const int k = rev ? s.nseg - 1 - i : i;
+        const float own = seg[k * step], a = dec[k * s.vh];
+        seg[k * step] = cur;
+        cur = a < 0.0f ? own : a * cur + own;
+    }
+}
+
+// Backward over one segment: forward once for the states before its chunks, then
+// back.
+template <class T, int NP, bool VEC>
+__global__ __launch_bounds__(256, NP > 64 ? 1 : 2) void scan_backward_kernel(ScanView s) {
+    constexpr int NT = NP / 16, LN = NP + 4;
+    __shared__ __align__(16) float sc[Q * LN], sb[Q * LN], sx[Q * LP], sdy[Q * LP], ss[PW * LN], sr[PW * LN];
+    __shared__ __align__(16) float sm[Q * LQ], sf[Q * LQ];
+    __shared__ __align__(16) Steps st;
+    __shared__ float hc[NT][Q], qb[NT][Q], kb[NT][Q], pairs[3][Q], inner[4], red[4];
+    __shared__ int flag;
+    const Place at(s, blockIdx.x);
+    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lg = l >> 4, lc = l & 15;
+    const float rate2 = -expf(s.a_log[at.h]) * LOG2E, bias = s.dt_bias[at.h], skip = s.skip[at.h];
+    const T* x = of<T>(s.x, at.b * s.xb + (int64_t)at.h * s.P + at.p0);
+    const T* dy = of<T>(s.dy, at.b * s.dyb + (int64_t)at.h * s.P + at.p0);
+    const T* bm = of<T>(s.b, at.b * s.bb + (int64_t)at.grp * s.N);
+    const T* cm = of<T>(s.c, at.b * s.cb + (int64_t)at.grp * s.N);
+    const T* dt = of<T>(s.dt, at.b * s.dtb + at.h);
+    const uint8_t* rs = s.reset ? s.reset + (int64_t)at.b * s.T : nullptr;
+    T* dx = (T*)s.dx + ((int64_t)at.b * s.T * s.H + at.h) * s.P + at.p0;
+    const int64_t yt = (int64_t)s.H * s.P;
+    const int64_t state0 = (((int64_t)at.b * s.H + at.h) * s.P + at.p0) * s.N;
+    const int64_t seg0 = (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * PW * NP;
+    float* chunk_s = s.chunk_s + ((int64_t)at.b * s.nch * s.vh + at.v) * PW * NP;
+    const int64_t chunk_step = (int64_t)s.vh * PW * NP;
+    const int c0 = at.seg * s.cps, c1 = c0 + s.cps < s.nch ? c0 + s.cps : s.nch;
+    auto length = [&](int c) { return s.T - c * Q < Q ? s.T - c * Q : Q; };
+
+    Rows<PW, VEC, T> rx, ry;
+    Rows<NP, VEC, T> rb, rc;
+    StepRegs rd;
+    f32x4 R[NT];
+    float decay_sum = 0.0f, bias_sum = 0.0f, skip_sum = 0.0f;  // of the three parameters' gradients
+    if (tid == 0) flag = 0;
+    auto load_in = [&](int t0, int len) {
+        rx.load(x, s.xt, t0, len, at.pw, tid);
+        rb.load(bm, s.bt, t0, len, s.N, tid);
+        if (w == 3) rd.load(dt, s.dtt, rs, t0, len, l);
+    };
+    auto stage_in = [&](int len) {
+        float bad = 0.0f;
+        rx.store(sx, LP, tid, bad);
+        rb.store(sb, LN, tid, bad);
+        if (w == 3) rd.store(st, bias, rate2, len, l, bad);
+        if (bad != bad) flag = 1;
+    };
+    {
+        f32x4 S[NT];
+        if (s.nseg > 1)
+            load_state<NT, true>(S, s.seg_s + seg0, NP, PW, NP, w, l);
+        else
+            load_state<NT, VEC>(S, s.state ? s.state + state0 : nullptr, s.N, at.pw, s.N, w, l);
+        if (c0 < c1) load_in(c0 * Q, length(c0));
+        for (int c = c0; c < c1; ++c) {
+            const int t0 = c * Q, len = length(c);
+            store_state<NT, true>(S, chunk_s + c * chunk_step, NP, PW, NP, w, l);
+            __syncthreads();
+            stage_in(len);
+            __syncthreads();
+            const bool single = flag != 0;
+            if (!single && c + 1 < c1) load_in(t0 + Q, length(c + 1));
+            for (int u = 0; u < (single ? len : 1); ++u) {
+                if (single) {
+                    __syncthreads();
+                    load_in(t0 + u, 1);
+                    stage_in(1);
+                    __syncthreads();
+                }
+                walk<NT, true>(S, sb, LN, sx, st, w, l);
+            }
+            if (single) {
+                __syncthreads();
+                if (tid == 0) flag = 0;
+                if (c + 1 < c1) load_in(t0 + Q, length(c + 1));
+            }
+        }
+        if (s.nseg > 1)
+            load_state<NT, true>(R, s.seg_r + seg0, NP, PW, NP, w, l);
+        else
+            load_state<NT, VEC>(R, s.dstate_out ? s.dstate_out + state0 : nullptr, s.N, at.pw, s.N, w, l);
+    }
+
+    auto load = [&](int t0, int len) {
+        load_in(t0, len);
+        ry.load(dy, s.dyt, t0, len, at.pw, tid);
+        rc.load(cm, s.ct, t0, len, s.N, tid);
+    };
+    auto stage = [&](int len) {
+        float bad = 0.0f;
+        stage_in(len);
+        ry.store(sdy, LP, tid, bad);
+        rc.store(sc, LN, tid, bad);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) *(f32x4*)(sr + (16 * w + lc) * LN + 16 * n + 4 * lg) = R[n];
+        if (bad != bad) flag = 1;
+    };
+    // one chunk (or step) of lu steps from tu, staged, with the state before it in S
+    auto back = [&](int tu, int lu) {
+        if (w < 3) {
+            const int si = w >> 1, ti = w > 0;
+            f32x4 m{0.0f, 0.0f, 0.0f, 0.0f}, f = m;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
+#pragma unroll
+            for (int n = 0; n < PW / 16; ++n) f = mma(kfrag(sx, LP, 16 * si, 16 * n, l), kfrag(sdy, LP, 16 * ti, 16 * n, l), f);
+            const int t = 16 * ti + lc, q0 = 16 * si + 4 * lg;
+            const float ti_ = st.gi[t], tf = st.gf[t];
+            const int et = st.ep[t];
+            const f32x4 gi = *(const f32x4*)(st.gi + q0), gf = *(const f32x4*)(st.gf + q0);
+            const i32x4 ep = *(const i32x4*)(st.ep + q0);
+            f32x4 pre;  // sums over s up to q0 + j of what passes from s to t
+            float run = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float dec = pow2((ti_ - gi[j]) + (tf - gf[j]));
+                const bool same = t == q0 + j, on = t > q0 + j && ep[j] == et;
+                const float fd = f[j] * dec;
+                run += on ? m[j] * fd * st.d[q0 + j] : 0.0f;
+                pre[j] = run;
+                m[j] = same ? m[j] : on ? m[j] * dec : 0.0f;
+                f[j] = same ? f[j] : on ? fd : 0.0f;
+            }
+            *(f32x4*)(sm + t * LQ + q0) = m;
+            *(f32x4*)(sf + t * LQ + q0) = f;
+            const float up = __shfl_up(run, 16, 64);  // and of the lanes with lower s
+            float low = lg > 0 ? up : 0.0f;
+            const float up2 = __shfl_up(low + run, 32, 64);
+            if (lg > 1) low += up2;
+            pre += low;
+            if (si == ti) {
+                // step q0 + j + 1 of this half: sum over t from it on
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float v = t > q0 + j ? pre[j] : 0.0f;
+                    for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o, 64);
+                    if (lc == 0 && (q0 + j + 1) % 16) pairs[2 * si][q0 + j + 1] = v;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {  // every t is behind step q0 + j + 1
+                    float v = pre[j];
+                    for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o, 64);
+                    if (lc == 0) pairs[1][q0 + j + 1] = v;
+                }
+                float v = __shfl(pre[3], 48 + lc, 64);  // all s, and t from a step of the second half on
+                for (int o = 1; o < 16; o <<= 1) {
+                    const float up = __shfl_down(v, o, 16);
+                    if (lc + o < 16) v += up;
+                }
+                if (lg == 0 && lc > 0) pairs[1][t] = v;
+            }
+        }
+        __syncthreads();
+        const int eq = st.end_ep;
+        // dc and db: rows = state, columns = steps
+        for (int job = w; job < 2 * NT; job += 4) {
+            const int n = job >> 1, i = job & 1, t = 16 * i + lc, n0 = 16 * n + 4 * lg;
+            const float dt_ = st.d[t];
+            const int et = st.ep[t];
+            f32x4 a{0.0f, 0.0f, 0.0f, 0.0f}, q = a;
+#pragma unroll
+            for (int k = 0; k < PW / 16; ++k) {
+                a = mma(rfrag(ss, LN, 16 * k, 16 * n, l), kfrag(sdy, LP, 16 * i, 16 * k, l), a);
+                q = mma(rfrag(sr, LN, 16 * k, 16 * n, l), kfrag(sx, LP, 16 * i, 16 * k, l), q);
+            }
+            a = et == 0 ? a * from_start(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            q = et == eq ? q * to_end(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            const f32x4 cv = *(const f32x4*)(sc + t * LN + n0), bv = *(const f32x4*)(sb + t * LN + n0);
+            float h = (a[0] * cv[0] + a[1] * cv[1]) + (a[2] * cv[2] + a[3] * cv[3]);
+            float kv = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
+            for (int k = 0; k <= i; ++k) {  // steps up to this one
+                const f32x4 fd = kfrag(sf, LQ, 16 * i, 16 * k, l) * *(const f32x4*)(st.d + 16 * k + 4 * lg);
+                a = mma(rfrag(sb, LN, 16 * k, 16 * n, l), fd, a);
+            }
+            for (int k = i; k < Q / 16; ++k)  // steps from this one on
+                q = mma(rfrag(sc, LN, 16 * k, 16 * n, l), rfrag(sf, LQ, 16 * k, 16 * i, l), q);
+            float bq = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
+#pragma unroll
+            for (int o = 16; o < 64; o <<= 1) {
+                h += __shfl_xor(h, o, 64);
+                kv += __shfl_xor(kv, o, 64);
+                bq += __shfl_xor(bq, o, 64);
+            }
+            if (lg == 0) {
+                hc[n][t] = h;
+                kb[n][t] = kv;
+                qb[n][t] = bq;
+            }
+            if (t < lu && n0 < s.N) {
+                const int64_t o = (((int64_t)at.b * s.T + tu + t) * s.vh + at.v) * s.N + n0;
+                row_store<VEC>(s.pdc + o, a, s.N - n0);
+                row_store<VEC>(s.pdb + o, q * dt_, s.N - n0);
+            }
+        }
+        // dx: rows = channels, columns = steps
+#pragma unroll
+        for (int i = 0; i < Q / 16; ++i) {
+            const int t = 16 * i + lc, p = 16 * w + 4 * lg;
+            f32x4 a{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) a = mma(kfrag(sr, LN, 16 * w, 16 * n, l), kfrag(sb, LN, 16 * i, 16 * n, l), a);
+            a = st.ep[t] == eq ? a * to_end(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = i; k < Q / 16; ++k) a = mma(rfrag(sdy, LP, 16 * k, 16 * w, l), rfrag(sm, LQ, 16 * k, 16 * i, l), a);
+            const f32x4 yv = *(const f32x4*)(sdy + t * LP + p), xv = *(const f32x4*)(sx + t * LP + p);
+            skip_sum += (yv[0] * xv[0] + yv[1] * xv[1]) + (yv[2] * xv[2] + yv[3] * xv[3]);
+            if (t < lu && p < at.pw) row_store<VEC>(dx + (int64_t)(tu + t) * yt + p, a * st.d[t] + skip * yv, at.pw - p);
+        }
+        float in = 0.0f;  // <R, S>, from the state before to the one behind
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const f32x4 v = *(const f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg);
+            in += (R[n][0] * v[0] + R[n][1] * v[1]) + (R[n][2] * v[2] + R[n][3] * v[3]);
+        }
+        for (int o = 32; o; o >>= 1) in += __shfl_xor(in, o, 64);
+        if (l == 0) inner[w] = in;
+        walk<NT, false>(R, sc, LN, sdy, st, w, l);
+        __syncthreads();
+        if (w == 3) {  // the gradients of the steps' decays and sizes, lane = step
+            const int t = l & (Q - 1);
+            float h = 0.0f, k = 0.0f, q = 0.0f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                h += hc[n][t];
+                k += kb[n][t];
+                q += qb[n][t];
+            }
+            const float d = st.d[t], dec = st.dec[t], sig = st.sig[t];
+            k *= d;
+#pragma unroll
+            for (int o = 1; o < Q; o <<= 1) {  // steps from t on; steps up to t
+                const float hu = __shfl_down(h, o, Q), ku = __shfl_up(k, o, Q);
+                if (t + o < Q) h += hu;
+                if (t >= o) k += ku;
+            }
+            const float before = __shfl_up(k, 1, Q);
+            float g = h + (t > 0 ? before : 0.0f);
+            if (t > 0) g += pairs[1][t];
+            if (t > 0 && t < 16) g += pairs[0][t];
+            if (t > 16) g += pairs[2][t];
+            if (eq == 0) g += ((inner[0] + inner[1]) + (inner[2] + inner[3])) * pow2(st.end_gi + st.end_gf);
+            if (l < lu) {
+                // log a = dec / LOG2E = -exp(a_log) d
+                const float dd = (q + g * (rate2 / LOG2E)) * sig;
+                decay_sum += g * (dec / LOG2E);
+                bias_sum += dd;
+                s.pdt[((int64_t)at.b * s.T + tu + t) * s.vh + at.v] = dd;
+            }
+        }
+    };
+    if (c0 < c1) load((c1 - 1) * Q, length(c1 - 1));
+    for (int c = c1 - 1; c >= c0; --c) {
+        const int t0 = c * Q, len = length(c);
+        {
+            f32x4 S[NT];
+            load_state<NT, true>(S, chunk_s + c * chunk_step, NP, PW, NP, w, l);
+            __syncthreads();
+            stage(len);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) *(f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg) = S[n];
+        }
+        __syncthreads();
+        const bool single = flag != 0;
+        if (!single && c > c0) load(t0 - Q, Q);
+        for (int u = 0; u < (single ? len : 1); ++u) {
+            const int tu = single ? t0 + len - 1 - u : t0;
+            if (single) {  // the state before step tu, walked from the chunk's
+                f32x4 S[NT];
+                load_state<NT, true>(S, chunk_s + c * chunk_step, NP, PW, NP, w, l);
+                for (int i = t0; i < tu; ++i) {
+                    __syncthreads();
+                    load_in(i, 1);
+                    stage_in(1);
+                    __syncthreads();
+                    walk<NT, true>(S, sb, LN, sx, st, w, l);
+                }
+                __syncthreads();
+                load(tu, 1);
+                stage(1);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) *(f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg) = S[n];
+                __syncthreads();
+            }
+            back(tu, single ? 1 : len);
+        }
+        if (single) {
+            __syncthreads();
+            if (tid == 0) flag = 0;
+            if (c > c0) load(t0 - Q, Q);
+        }
+    }
+    if (s.dstate && at.seg == 0) store_state<NT, VEC>(R, s.dstate + state0, s.N, at.pw, s.N, w, l);
+    for (int o = 32; o; o >>= 1) {
+        skip_sum += __shfl_xor(skip_sum, o, 64);
+        decay_sum += __shfl_xor(decay_sum, o, 64);
+        bias_sum += __shfl_xor(bias_sum, o, 64);
+    }
+    if (l == 0) red[w] = skip_sum;
+    __syncthreads();
+    if (tid == 192) {
+        float* o = s.ppar + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * 3;
+        o[0] = decay_sum;
+        o[1] = bias_sum;
+        o[2] = (red[0] + red[1]) + (red[2] + red[3]);
+    }
+}
+
+// Sums the workgroups' parts, in order: of db and dc over the heads of a group,
+// of ddt over a head's tiles (blockIdx.y = 0), and of the parameters over sequences
+// and segments (blockIdx.y = 1: a wave a head).
+template <class T>
+__global__ __launch_bounds__(256) void scan_reduce_kernel(ScanView s, T* db, T* dc, T* ddt, float* da_log, float* ddt_bias,
+                                                          float* dskip) {
+    if (blockIdx.y == 1) {
+        const int h = blockIdx.x * 4 + (threadIdx.x >> 6), l = threadIdx.x & 63;
+        if (h >= s.H) return;
+        float a[3] = {0.0f, 0.0f, 0.0f};
+        const int parts = s.B * s.nseg * s.ptiles;
+        for (int i = l; i < parts; i += 64) {
+            const float* p = s.ppar + ((int64_t)(i / s.ptiles) * s.vh + h * s.ptiles + i % s.ptiles) * 3;
+            a[0] += p[0];
+            a[1] += p[1];
+            a[2] += p[2];
+        }
+        for (int o = 32; o; o >>= 1)
+            for (int j = 0; j < 3; ++j) a[j] += __shfl_xor(a[j], o, 64);
+        if (l == 0) {
+            da_log[h] = a[0];
+            ddt_bias[h] = a[1];
+            dskip[h] = a[2];
+        }
+        return;
+    }
+    const int64_t rows = (int64_t)s.B * s.T, per = (int64_t)s.G * s.N, total = rows * per;
+    const int heads = s.vh / s.G;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
+        const int64_t row = e / per;
+        const int g = (int)(e % per) / s.N, n = (int)(e % per) % s.N;
+        const int64_t o = (row * s.vh + (int64_t)g * heads) * s.N + n;
+        float b = 0.0f, c = 0.0f;
+        for (int i = 0; i < heads; ++i) {
+            b += s.pdb[o + (int64_t)i * s.N];
+            c += s.pdc[o + (int64_t)i * s.N];
+        }
+        db[e] = row_round<T>(b);
+        dc[e] = row_round<T>(c);
+    }
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * s.H; e += (int64_t)gridDim.x * 256) {
+        float d = 0.0f;
+        for (int i = 0; i < s.ptiles; ++i) d += s.pdt[e * s.ptiles + i];
+        ddt[e] = row_round<T>(d);
+    }
+}
+
+// One step of a row and head: memory bound on the state, read and written once.  A
+// workgroup takes 256 / L channels at a time, L = lanes of a channel's states.
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void scan_step_kernel(ScanView s, float* pool, int64_t slots, const int32_t* slot, int lanes,
+                                                        int pblocks, unsigned* err) {
+    constexpr int V = VEC ? 4 : 1;
+    const int id = blockIdx.x, pb = id % pblocks, h = id / pblocks % s.H, row = id / pblocks / s.H;
+    const int grp = h / (s.H / s.G), l = threadIdx.x % lanes;
+    const T* x = of<T>(s.x, row * s.xb + (int64_t)h * s.P);
+    const T* bm = of<T>(s.b, row * s.bb + (int64_t)grp * s.N);
+    const T* cm = of<T>(s.c, row * s.cb + (int64_t)grp * s.N);
+    const float v = row_value(of<T>(s.dt, row * s.dtb)[h]) + s.dt_bias[h];
+    float d = fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v)));
+    if (v != v) d = v;
+    const float a = expf(-expf(s.a_log[h]) * d), skip = s.skip[h];
+    bool reset = s.reset && s.reset[row];
+    int64_t at = slot ? slot[row] : row;
+    const bool out = at < 0 || at >= slots;
+    if (out) {
+        if (threadIdx.x == 0 && err) atomicOr(err, ERR_IDX_RANGE);
+        reset = true;
+        at = 0;
+    }
+    float* st = pool + (at * s.H + h) * (int64_t)s.P * s.N;
+    T* y = (T*)s.y + ((int64_t)row * s.H + h) * s.P;
+    const int per = (s.P + pblocks - 1) / pblocks, p1 = (pb + 1) * per < s.P ? (pb + 1) * per : s.P;
+    for (int p = pb * per + threadIdx.x / lanes; p < p1; p += 256 / lanes) {
+        const float xv = row_value(x[p]), dxv = d * xv;
+        float sum = 0.0f;
+        for (int n = l * V; n < s.N; n += lanes * V) {
+            float* e = st + (int64_t)p * s.N + n;
+            float o[V], bv[V], cv[V];
+            if (VEC) {
+                const f32x4 ov = reset ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : *(const f32x4*)e, b4 = row_load4(bm + n), c4 = row_load4(cm + n);
+                for (int j = 0; j < V; ++j) o[j] = ov[j], bv[j] = b4[j], cv[j] = c4[j];
+            } else {
+                o[0] = reset ? 0.0f : *e;
+                bv[0] = row_value(bm[n]);
+                cv[0] = row_value(cm[n]);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                o[j] = reset ? dxv * bv[j] : fmaf(a, o[j], dxv * bv[j]);
+                sum = fmaf(o[j], cv[j], sum);
+            }
+            if (!out) {
+                if (VEC) *(f32x4*)e = f32x4{o[0], o[V > 1 ? 1 : 0], o[V > 2 ? 2 : 0], o[V > 3 ? 3 : 0]};
+                else *e = o[0];
+            }
+        }
+        for (int m = lanes >> 1; m; m >>= 1) sum += __shfl_xor(sum, m, 64);
+        if (l == 0) y[p] = row_round<T>(fmaf(skip, xv, sum));
+    }
+}
+
+// ---- host ----
+
+int padded_state(int n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
+
+// Segments a sequence is cut into: none where the (sequence, head, channels) fill
+// the chip, else enough for two workgroups a compute unit, of one chunk at least.
+struct Cut {
+    int ptiles, vh, nch, cps, nseg;
+    Cut(int B, int T, int H, int P) {
+        ptiles = (P + PW - 1) / PW;
+        vh = H * ptiles;
+        nch = (T + Q - 1) / Q;
+        const int64_t groups = (int64_t)B * vh;
+        const int want = groups > 0 && groups < 512 ? (int)((512 + groups - 1) / groups) : 1;
+        nseg = want < nch ? want : nch;
+        if (nseg < 1) nseg = 1;
+        cps = nch > 0 ? (nch + nseg - 1) / nseg : 1;
+        nseg = nch > 0 ? (nch + cps - 1) / cps : 1;
+    }
+};
+struct ScanPlan {
+    size_t seg_s, seg_r, seg_a, chunk_s, pdb, pdc, pdt, ppar, total;
+    ScanPlan(const Cut& k, int B, int T, int N, bool backward) {
+        size_t o = 0;
+        auto take = [&](size_t floats) { size_t at = o; o += (floats * 4 + 255) / 256 * 256; return at; };
+        const size_t state = (size_t)PW * padded_state(N), segs = (size_t)B * k.nseg * k.vh, rows = (size_t)B * T * k.vh;
+        seg_s = take(k.nseg > 1 ? segs * state : 0);
+        seg_a = take(k.nseg > 1 ? segs : 0);
+        seg_r = take(backward && k.nseg > 1 ? segs * state : 0);
+        chunk_s = take(backward ? (size_t)B * k.nch * k.vh * state : 0);
+        pdb = take(backward ? rows * N : 0);
+        pdc = take(backward ? rows * N : 0);
+        pdt = take(backward ? rows : 0);
+        ppar = take(backward ? segs * 3 : 0);
+        total = o;
+    }
+};
+
+constexpr int MAX_WIDTH = 128, MAX_STATE = 128;
+
+// The view of valid arguments; `step`: strides along the steps are not used.
+int scan_view(const gorila_scan_args* a, bool step, ScanView& v, bool& vec) {
+    if (!a || !row_dtype(a->dtype) || a->batch < 0 || a->length < 0 || a->heads < 1 || a->groups < 1) return GORILA_EINVAL;
+    if (a->heads % a->groups || a->head_dim < 1 || a->state_dim < 1) return GORILA_EINVAL;
+    if (a->head_dim > MAX_WIDTH || a->state_dim > MAX_STATE || a->heads > 65536) return GORILA_EUNSUPPORTED;
+    if ((int64_t)a->batch * a->length > INT32_MAX) return GORILA_EUNSUPPORTED;
+    if (!a->a_log || !a->dt_bias || !a->skip) return GORILA_EINVAL;
+    if (a->batch > 0 && a->length > 0 && (!a->x || !a->dt || !a->b || !a->c)) return GORILA_EINVAL;
+    const int e = dtype_bytes(a->dtype);
+    for (const void* p : {a->x, a->dt, a->b, a->c})
+        if (!at_element(p, e)) return GORILA_EINVAL;
+    for (const void* p : {a->a_log, a->dt_bias, a->skip, a->state})
+        if (!at_element(p, 4)) return GORILA_EINVAL;
+    v = ScanView{};
+    v.x = a->x, v.dt = a->dt, v.b = a->b, v.c = a->c;
+    v.xb = a->x_batch_stride, v.xt = a->x_step_stride, v.dtb = a->dt_batch_stride, v.dtt = a->dt_step_stride;
+    v.bb = a->b_batch_stride, v.bt = a->b_step_stride, v.cb = a->c_batch_stride, v.ct = a->c_step_stride;
+    v.a_log = a->a_log, v.dt_bias = a->dt_bias, v.skip = a->skip, v.state = a->state, v.reset = a->reset;
+    v.B = a->batch, v.T = a->length, v.H = a->heads, v.P = a->head_dim, v.G = a->groups, v.N = a->state_dim;
+    const int64_t strides = v.xb | v.bb | v.cb | (step ? 0 : v.xt | v.bt | v.ct);
+    vec = !((v.P | v.N) & 3) && !(strides & 3) && at_four(a->x, e) && at_four(a->b, e) && at_four(a->c, e) && at_four(a->state, 4);
+    return GORILA_OK;
+}
+
+void cut_view(ScanView& v, const Cut& k) {
+    v.ptiles = k.ptiles, v.vh = k.vh, v.nch = k.nch, v.cps = k.cps, v.nseg = k.nseg;
+}
+
+template <class F>
+void by_state(int n, F&& f) {
+    switch (padded_state(n)) {
+        case 16: f(std::integral_constant<int, 16>{}); break;
+        case 32: f(std::integral_constant<int, 32>{}); break;
+        case 64: f(std::integral_constant<int, 64>{}); break;
+        default: f(std::integral_constant<int, 128>{}); break;
+    }
+}
+// Calls f(row type, padded state, whether quads are aligned) as constants.
+template <class F>
+void by_kind(int dtype, int n, bool vec, F&& f) {
+    by_state(n, [&](auto np) {
+        if (dtype == GORILA_F32) vec ? f(float{}, np, std::true_type{}) : f(float{}, np, std::false_type{});
+        else vec ? f(uint16_t{}, np, std::true_type{}) : f(uint16_t{}, np, std::false_type{});
+    });
+}
+
+bool grid_fits(int64_t blocks) { return blocks <= INT32_MAX; }
+
+}  // namespace
+}  // namespace gorila
+
+using namespace gorila;
+
+extern "C" {
+
+size_t gorila_scan_workspace_bytes(int32_t batch, int32_t length, int32_t heads, int32_t head_dim, int32_t groups,
+                                   int32_t state_dim, int32_t backward) {
+    if (batch < 0 || length < 0 || heads < 1 || heads > 65536 || groups < 1 || heads % groups) return 0;
+    if (head_dim < 1 || head_dim > MAX_WIDTH || state_dim < 1 || state_dim > MAX_STATE) return 0;
+    const size_t own = ScanPlan(Cut(batch, length, heads, head_dim), batch, length, state_dim, backward != 0).total;
+    return own ? WS_FIXED_BYTES + own : 0;
+}
+
+int gorila_scan(const gorila_scan_args* args, void* y, float* state_out, gorila_ctx* ctx) {
+    ScanView v;
+    CtxView c;
+    bool vec;
+    int rc = ctx_view(ctx, 0, c);
+    if (rc || (rc = scan_view(args, false, v, vec))) return rc;
+    if (v.B == 0 || (v.T == 0 && !state_out)) return GORILA_OK;
+    if ((v.T > 0 && !y) || !at_element(y, dtype_bytes(args->dtype)) || !at_element(state_out, 4)) return GORILA_EINVAL;
+    const Cut k(v.B, v.T, v.H, v.P);
+    const ScanPlan p(k, v.B, v.T, v.N, false);
+    cut_view(v, k);
+    const int64_t blocks = (int64_t)v.B * v.nseg * v.vh;
+    if (!grid_fits(blocks * (PW * MAX_STATE / 256))) return GORILA_EUNSUPPORTED;
+    if ((rc = ctx_view(ctx, p.total, c))) return rc;
+    vec = vec && at_four(y, dtype_bytes(args->dtype)) && at_four(state_out, 4);
+    v.y = y;
+    v.state_out = state_out;
+    v.seg_s = (float*)(c.ws + p.seg_s);
+    v.seg_a = (float*)(c.ws + p.seg_a);
+    by_kind(args->dtype, v.N, vec, [&](auto t, auto np, auto al) {
+        using T = decltype(t);
+        constexpr int NP = decltype(np)::value;
+        constexpr bool VEC = decltype(al)::value;
+        if (v.nseg > 1) {
+            state_kernel<T, NP, VEC, false><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+            join_kernel<NP, VEC><<<dim3((unsigned)(v.B * v.vh * (PW * NP / 256)), 1), 256, 0, c.stream>>>(v);
+        }
+        scan_kernel<T, NP, VEC><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+    });
+    return launched();
+}
+
+int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t dy_batch_stride, int64_t dy_step_stride,
+                         const float* dstate_out, void* dx, void* ddt, void* db, void* dc, float* da_log, float* ddt_bias,
+                         float* dskip, float* dstate, gorila_ctx* ctx) {
+    ScanView v;
+    CtxView c;
+    bool vec;
+    int rc = ctx_view(ctx, 0, c);
+    if (rc || (rc = scan_view(args, false, v, vec))) return rc;
+    const int e = dtype_bytes(args->dtype);
+    if (!da_log || !ddt_bias || !dskip) return GORILA_EINVAL;
+    if (v.B > 0 && v.T > 0 && (!dy || !dx || !ddt || !db || !dc)) return GORILA_EINVAL;
+    for (const void* p : {dy, (const void*)dx, (const void*)ddt, (const void*)db, (const void*)dc})
+        if (!at_element(p, e)) return GORILA_EINVAL;
+    for (const float* p : {dstate_out, (const float*)da_log, (const float*)ddt_bias, (const float*)dskip, (const float*)dstate})
+        if (!at_element(p, 4)) return GORILA_EINVAL;
+    const Cut k(v.B, v.T, v.H, v.P);
+    const ScanPlan p(k, v.B, v.T, v.N, true);
+    cut_view(v, k);
+    const int64_t blocks = (int64_t)v.B * v.nseg * v.vh;
+    if (!grid_fits(blocks * (PW * MAX_STATE / 256))) return GORILA_EUNSUPPORTED;
+    if ((rc = ctx_view(ctx, p.total, c))) return rc;
+    vec = vec && !((dy_batch_stride | dy_step_stride) & 3) && at_four(dy, e) && at_four(dx, e) && at_four(dstate_out, 4) && at_four(dstate, 4);
+    v.dy = dy;
+    v.dyb = dy_batch_stride;
+    v.dyt = dy_step_stride;
+    v.dstate_out = dstate_out;
+    v.dx = dx;
+    v.dstate = dstate;
+    auto ws = [&](size_t o) { return (float*)(c.ws + o); };
+    v.seg_s = ws(p.seg_s), v.seg_a = ws(p.seg_a), v.seg_r = ws(p.seg_r), v.chunk_s = ws(p.chunk_s);
+    v.pdb = ws(p.pdb), v.pdc = ws(p.pdc), v.pdt = ws(p.pdt), v.ppar = ws(p.ppar);
+    by_kind(args->dtype, v.N, vec, [&](auto t, auto np, auto al) {
+        using T = decltype(t);
+        constexpr int NP = decltype(np)::value;
+        constexpr bool VEC = decltype(al)::value;
+        if (blocks > 0) {
+            if (v.nseg > 1) {
+                state_kernel<T, NP, VEC, false><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+                state_kernel<T, NP, VEC, true><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+                join_kernel<NP, VEC><<<dim3((unsigned)(v.B * v.vh * (PW * NP / 256)), 2), 256, 0, c.stream>>>(v);
+            }
+            scan_backward_kernel<T, NP, VEC><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+        }
+        const int64_t per = ((int64_t)v.B * v.T * v.G * v.N + 255) / 256, heads = (v.H + 3) / 4;
+        const unsigned gx = (unsigned)(per > 8192 ? 8192 : per);
+        scan_reduce_kernel<T><<<dim3(gx > heads ? gx : (unsigned)heads, 2), 256, 0, c.stream>>>(v, (T*)db, (T*)dc, (T*)ddt, da_log,
+                                                                                              ddt_bias, dskip);
+    });
+    return launched();
+}
+
+int gorila_scan_step(const gorila_scan_args* args, float* state_pool, int64_t slots, const int32_t* slot, void* y,
+                     gorila_ctx* ctx) {
+    ScanView v;
+    CtxView c;
+    bool vec;
+    int rc = ctx_view(ctx, 0, c);
+    if (rc || (rc = scan_view(args, true, v, vec))) return rc;
+    if (v.T != 1 || slots < 0) return GORILA_EINVAL;
+    if (v.B == 0) return GORILA_OK;
+    if (!state_pool || !y || !at_element(state_pool, 4) || !at_element(y, dtype_bytes(args->dtype)) || !at_element(slot, 4))
+        return GORILA_EINVAL;
+    if (slot ? !c.err : slots < v.B) return slot ? GORILA_EWORKSPACE : GORILA_EINVAL;
+    vec = vec && at_four(state_pool, 4);
+    v.y = y;
+    // lanes of a channel: its quads, up to a wave; channels over more workgroups
+    // while there are fewer of them than compute units
+    int lanes = 1;
+    while (lanes < 64 && lanes * (vec ? 4 : 1) < v.N) lanes <<= 1;
+    const int most = (v.P * lanes + 255) / 256;
+    int pblocks = 1;
+    while (pblocks < most && (int64_t)v.B * v.H * pblocks < 2 * c.cus) pblocks <<= 1;
+    if (pblocks > most) pblocks = most;
+    const int64_t blocks = (int64_t)v.B * v.H * pblocks;
+    if (!grid_fits(blocks)) return GORILA_EUNSUPPORTED;
+    auto go = [&](auto t, auto al) {
+        scan_step_kernel<decltype(t), decltype(al)::value><<<(unsigned)blocks, 256, 0, c.stream>>>(v, state_pool, slots, slot, lanes, pblocks, c.err);
+    };
+    if (args->dtype == GORILA_F32) vec ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});
+    else vec ? go(uint16_t{}, std::true_type{}) : go(uint16_t{}, std::false_type{});
+    return launched();
+}
+
+}  // extern "C"
