@@ -175,8 +175,6 @@ SplitWs split_ws(gorila_ctx* c, const Plan& p) {
     return sw;
 }
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
 int check_launch() {
     return hipGetLastError() == hipSuccess ? GORILA_OK : GORILA_EHIP;
 }

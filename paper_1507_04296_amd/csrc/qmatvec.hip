@@ -164,7 +164,7 @@ int gorila_quantize_weights(const void* weights, int64_t weights_stride, int32_t
     if (inputs > INT32_MAX - 128) return GORILA_EUNSUPPORTED;
     if (outputs == 0) return GORILA_OK;
     const int e = dtype_bytes(dtype);
-    if (!weights || !codes || !scales || !at_element(weights, e) || !aligned_codes(codes) || !at_element(scales, 4)) return GORILA_EINVAL;
+    if (!weights || !codes || !scales || !at_element(weights, e) || !aligned16(codes) || !at_element(scales, 4)) return GORILA_EINVAL;
     const int chunks = (inputs + 31) / 32, groups = (inputs + group - 1) / group;
     const int64_t lanes = (int64_t)outputs * groups * (group / 4);
     if ((lanes + 255) / 256 > INT32_MAX) return GORILA_EUNSUPPORTED;
@@ -190,7 +190,7 @@ int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_
     if (rows == 0 || outputs == 0) return GORILA_OK;
     const int e = x_dtype == GORILA_CODES ? 1 : dtype_bytes(x_dtype);
     if (!x || !codes || !scales || !y || (x_dtype == GORILA_CODES && !x_scale)) return GORILA_EINVAL;
-    if (!at_element(x, e) || !aligned_codes(codes) || !at_element(scales, 4) || !at_element(x_scale, 4) ||
+    if (!at_element(x, e) || !aligned16(codes) || !at_element(scales, 4) || !at_element(x_scale, 4) ||
         !at_element(y, x_dtype == GORILA_BF16 ? 2 : 4))
         return GORILA_EINVAL;
     if (inputs > INT32_MAX - 128 || rows > 65535) return GORILA_EUNSUPPORTED;

@@ -66,7 +66,7 @@ __device__ __forceinline__ void row_store(T* p, f32x4 v, int n) {
 }
 
 inline int dtype_bytes(int dtype) { return dtype == GORILA_BF16 ? 2 : 4; }
-inline bool aligned_codes(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool row_dtype(int dtype) { return dtype == GORILA_F32 || dtype == GORILA_BF16; }
 // Whether an address is one of an element of `bytes`, or of four of them.
 inline bool at_element(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
