@@ -155,6 +155,9 @@ class Context:
                  dtype: int = GORILA_F32, min_bytes: int = 0):
         import torch
         self.device = torch.device(device if device is not None else "cuda")
+        self._raw_stream = torch._C._cuda_getCurrentRawStream
+        self._current_device = torch.cuda.current_device
+        self._bound = None  # the stream that the context has
         if max_batch == 0:  # a context without a workspace (gorila_act_noalloc)
             self.ws_bytes, self.workspace = 0, None
         else:
@@ -174,14 +177,14 @@ class Context:
         """The handle of torch's current stream on the context's device.  Read
         from the native accessor: building a torch.cuda.Stream object for it
         took 3.2 of a call's 9.2 us of host time (replay insert), this 0.1."""
-        import torch
         index = self.device.index
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if index is None else index)
+        return self._raw_stream(self._current_device() if index is None else index)
 
     def bind_stream(self):
-        rc = lib().gorila_ctx_set_stream(self.handle, self._stream())
-        if rc != 0:
-            _check(rc, "gorila_ctx_set_stream")
+        stream = self._stream()
+        if stream != self._bound or self.handle is None:
+            _check(lib().gorila_ctx_set_stream(self.handle, stream), "gorila_ctx_set_stream")
+            self._bound = stream
         return self.handle
 
     def check(self) -> None:

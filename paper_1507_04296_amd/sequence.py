@@ -64,44 +64,55 @@ def _dtype(x) -> int:
     return dt
 
 
-def _at(ctx, t, name: str, shape, dtype, strided: int = 0):
-    """Address of an optional tensor of `shape` and `dtype` on the context's device.
-    The dimensions from `strided` on are contiguous; the leading ones have strides of
-    their own."""
+def _like(t):
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _at(index: int, t, name: str, shape, dtype, strided: int = 0):
+    """Address of an optional tensor of `shape` and `dtype` on device `index`.  The
+    dimensions from `strided` on are contiguous; the leading ones have strides of
+    their own.  (Host time is what a single step costs, so the accepting path is short.)"""
     if t is None:
         return None
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.device.type != ctx.device.type or (ctx.device.index is not None and t.device.index != ctx.device.index):
-        raise ValueError(f"{name} must be on {ctx.device}, got {t.device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on device {index}, got {t.device}")
     if not t.is_contiguous():
         run = 1
         for d in range(t.dim() - 1, strided - 1, -1):
-            if t.stride(d) != run and t.shape[d] > 1:
-                raise ValueError(f"{name} must be contiguous from dimension {strided} on")
-            run *= t.shape[d]
+            if t.shape[d] > 1:
+                if t.stride(d) != run:
+                    raise ValueError(f"{name} must be contiguous from dimension {strided} on")
+                run *= t.shape[d]
     return t.data_ptr()
+
+
+def _device(ctx) -> int:
+    index = ctx.device.index
+    return torch.cuda.current_device() if index is None else index
 
 
 # ---- norm ----
 
 def _norm_in(ctx, x, weight, residual):
     _want(x.dim() == 2, "x must be [rows, width]")
+    dev = _device(ctx)
     rows, width = x.shape
     dt = _dtype(x)
-    px = _at(ctx, x, "x", x.shape, x.dtype, 1)
-    pr = _at(ctx, residual, "residual", x.shape, x.dtype, 1)
+    px = _at(dev, x, "x", x.shape, x.dtype, 1)
+    pr = _at(dev, residual, "residual", x.shape, x.dtype, 1)
     return (px, x.stride(0), pr, 0 if residual is None else residual.stride(0),
-            _at(ctx, weight, "weight", (width,), torch.float32), rows, width, dt)
+            _at(dev, weight, "weight", (width,), torch.float32), rows, width, dt)
 
 
 def add_rmsnorm(ctx, x, weight, residual=None, eps: float = 1e-6):
     """y, total, rstd of total = x + residual (x itself without one) and y = its norm times weight."""
     a = _norm_in(ctx, x, weight, residual)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    total = torch.empty_like(y) if residual is not None or not x.is_contiguous() else None
+    y = _like(x)
+    total = _like(x) if residual is not None or not x.is_contiguous() else None
     rstd = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
     _check(lib().gorila_add_rmsnorm(*a, eps, y.data_ptr(), None if total is None else total.data_ptr(), rstd.data_ptr(),
                                     ctx.bind_stream()), "gorila_add_rmsnorm")
@@ -112,7 +123,7 @@ def add_rmsnorm_codes(ctx, x, weight, residual=None, eps: float = 1e-6):
     """codes (int8), scale, total: codes * scale[:, None] stands for add_rmsnorm's y."""
     a = _norm_in(ctx, x, weight, residual)
     codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    total = torch.empty(x.shape, dtype=x.dtype, device=x.device) if residual is not None or not x.is_contiguous() else None
+    total = _like(x) if residual is not None or not x.is_contiguous() else None
     scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
     _check(lib().gorila_add_rmsnorm_codes(*a, eps, codes.data_ptr(), scale.data_ptr(),
                                           None if total is None else total.data_ptr(), ctx.bind_stream()),
@@ -127,16 +138,17 @@ def add_rmsnorm_workspace_bytes(width: int) -> int:
 def add_rmsnorm_backward(ctx, dy, total, rstd, weight, dtotal=None):
     """dx (of x and of residual), dweight for the gradients that reach y and total."""
     _want(total.dim() == 2, "total must be [rows, width]")
+    dev = _device(ctx)
     rows, width = total.shape
     dt = _dtype(total)
-    pdy = _at(ctx, dy, "dy", total.shape, total.dtype, 1)
-    pdt = _at(ctx, dtotal, "dtotal", total.shape, total.dtype, 1)
-    pt = _at(ctx, total, "total", total.shape, total.dtype)
-    dx = torch.empty(total.shape, dtype=total.dtype, device=total.device)
+    pdy = _at(dev, dy, "dy", total.shape, total.dtype, 1)
+    pdt = _at(dev, dtotal, "dtotal", total.shape, total.dtype, 1)
+    pt = _at(dev, total, "total", total.shape, total.dtype)
+    dx = _like(total)
     dweight = torch.empty(width, dtype=torch.float32, device=total.device)
     _check(lib().gorila_add_rmsnorm_backward(
         pdy, dy.stride(0), pdt, 0 if dtotal is None else dtotal.stride(0), pt,
-        _at(ctx, rstd, "rstd", (rows,), torch.float32), _at(ctx, weight, "weight", (width,), torch.float32), rows, width, dt,
+        _at(dev, rstd, "rstd", (rows,), torch.float32), _at(dev, weight, "weight", (width,), torch.float32), rows, width, dt,
         dx.data_ptr(), dweight.data_ptr(), ctx.bind_stream()), "gorila_add_rmsnorm_backward")
     return dx, dweight
 
@@ -146,19 +158,19 @@ def add_rmsnorm_backward(ctx, dy, total, rstd, weight, dtotal=None):
 def _conv_args(ctx, x, weight, bias, reset, window, silu):
     _want(x.dim() == 3, "x must be [batch, length, channels]")
     batch, length, channels = x.shape
-    dt = _dtype(x)
+    dt, dev = _dtype(x), _device(ctx)
     _want(weight.dim() == 2 and weight.shape[0] == channels, "weight must be [channels, taps]")
     taps = weight.shape[1]
     return _ConvArgs(
-        dt, batch, length, channels, taps, 1 if silu else 0, _at(ctx, x, "x", x.shape, x.dtype, 2), x.stride(0), x.stride(1),
-        _at(ctx, weight, "weight", weight.shape, torch.float32), _at(ctx, bias, "bias", (channels,), torch.float32),
-        _at(ctx, reset, "reset", (batch, length), torch.uint8), _at(ctx, window, "window", (batch, taps - 1, channels), x.dtype))
+        dt, batch, length, channels, taps, 1 if silu else 0, _at(dev, x, "x", x.shape, x.dtype, 2), x.stride(0), x.stride(1),
+        _at(dev, weight, "weight", weight.shape, torch.float32), _at(dev, bias, "bias", (channels,), torch.float32),
+        _at(dev, reset, "reset", (batch, length), torch.uint8), _at(dev, window, "window", (batch, taps - 1, channels), x.dtype))
 
 
 def causal_conv(ctx, x, weight, bias=None, reset=None, window=None, silu: bool = True):
     """y [batch, length, channels] and the window [batch, taps - 1, channels] for the steps that follow."""
     a = _conv_args(ctx, x, weight, bias, reset, window, silu)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _like(x)
     out = torch.empty((a.batch, max(0, a.taps - 1), a.channels), dtype=x.dtype, device=x.device)
     _check(lib().gorila_causal_conv(a, y.data_ptr(), out.data_ptr(), ctx.bind_stream()), "gorila_causal_conv")
     return y, out
@@ -170,13 +182,13 @@ def causal_conv_workspace_bytes(channels: int, taps: int) -> int:
 
 def causal_conv_backward(ctx, dy, x, weight, bias=None, reset=None, window=None, silu: bool = True, dwindow_out=None):
     """dx, dweight, dbias, dwindow (the last two None without a bias or window)."""
-    a = _conv_args(ctx, x, weight, bias, reset, window, silu)
-    pdy = _at(ctx, dy, "dy", x.shape, x.dtype, 2)
-    pdw = _at(ctx, dwindow_out, "dwindow_out", (a.batch, a.taps - 1, a.channels), x.dtype)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    a, dev = _conv_args(ctx, x, weight, bias, reset, window, silu), _device(ctx)
+    pdy = _at(dev, dy, "dy", x.shape, x.dtype, 2)
+    pdw = _at(dev, dwindow_out, "dwindow_out", (a.batch, a.taps - 1, a.channels), x.dtype)
+    dx = _like(x)
     dweight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
     dbias = None if bias is None else torch.empty_like(dweight[:, 0], memory_format=torch.contiguous_format)
-    dwindow = None if window is None else torch.empty(window.shape, dtype=x.dtype, device=x.device)
+    dwindow = None if window is None else _like(window)
     _check(lib().gorila_causal_conv_backward(
         a, pdy, dy.stride(0), dy.stride(1), pdw, dx.data_ptr(), dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
         None if dwindow is None else dwindow.data_ptr(), ctx.bind_stream()), "gorila_causal_conv_backward")
@@ -188,14 +200,14 @@ def causal_conv_step(ctx, x, window_pool, weight, bias=None, slot=None, reset=No
     _want(x.dim() == 2, "x must be [rows, channels]")
     rows, channels = x.shape
     _want(weight.dim() == 2 and weight.shape[0] == channels, "weight must be [channels, taps]")
-    taps, slots = weight.shape[1], window_pool.shape[0]
+    taps, slots, dev = weight.shape[1], window_pool.shape[0], _device(ctx)
     a = _ConvArgs(
-        _dtype(x), rows, 1, channels, taps, 1 if silu else 0, _at(ctx, x, "x", x.shape, x.dtype, 1), x.stride(0), 0,
-        _at(ctx, weight, "weight", weight.shape, torch.float32), _at(ctx, bias, "bias", (channels,), torch.float32),
-        _at(ctx, reset, "reset", (rows,), torch.uint8), None)
-    pool = _at(ctx, window_pool, "window_pool", (slots, taps - 1, channels), x.dtype)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _check(lib().gorila_causal_conv_step(a, pool, slots, _at(ctx, slot, "slot", (rows,), torch.int32), y.data_ptr(),
+        _dtype(x), rows, 1, channels, taps, 1 if silu else 0, _at(dev, x, "x", x.shape, x.dtype, 1), x.stride(0), 0,
+        _at(dev, weight, "weight", weight.shape, torch.float32), _at(dev, bias, "bias", (channels,), torch.float32),
+        _at(dev, reset, "reset", (rows,), torch.uint8), None)
+    pool = _at(dev, window_pool, "window_pool", (slots, taps - 1, channels), x.dtype)
+    y = _like(x)
+    _check(lib().gorila_causal_conv_step(a, pool, slots, _at(dev, slot, "slot", (rows,), torch.int32), y.data_ptr(),
                                          ctx.bind_stream()), "gorila_causal_conv_step")
     return y
 
@@ -204,6 +216,7 @@ def causal_conv_step(ctx, x, window_pool, weight, bias=None, slot=None, reset=No
 
 def _scan_args(ctx, x, dt, b, c, a_log, dt_bias, skip, reset, state):
     """x [..., heads, head_dim]; one leading dimension (single steps) or two."""
+    dev = _device(ctx)
     lead = x.dim() - 2
     step = lead == 1
     shape, typ = x.shape, x.dtype
@@ -215,13 +228,13 @@ def _scan_args(ctx, x, dt, b, c, a_log, dt_bias, skip, reset, state):
     xs, ds, bs, cs = x.stride(), dt.stride(), b.stride(), c.stride()
     return _ScanArgs(
         _dtype(x), batch, length, heads, width, groups, n, 0,
-        _at(ctx, x, "x", shape, typ, lead), xs[0], 0 if step else xs[1],
-        _at(ctx, dt, "dt", shape[:lead] + par, typ, lead), ds[0], 0 if step else ds[1],
-        _at(ctx, b, "b", shape[:lead] + (groups, n), typ, lead), bs[0], 0 if step else bs[1],
-        _at(ctx, c, "c", shape[:lead] + (groups, n), typ, lead), cs[0], 0 if step else cs[1],
-        _at(ctx, a_log, "a_log", par, torch.float32), _at(ctx, dt_bias, "dt_bias", par, torch.float32),
-        _at(ctx, skip, "skip", par, torch.float32), _at(ctx, reset, "reset", shape[:lead], torch.uint8),
-        _at(ctx, state, "state", (batch, heads, width, n), torch.float32))
+        _at(dev, x, "x", shape, typ, lead), xs[0], 0 if step else xs[1],
+        _at(dev, dt, "dt", shape[:lead] + par, typ, lead), ds[0], 0 if step else ds[1],
+        _at(dev, b, "b", shape[:lead] + (groups, n), typ, lead), bs[0], 0 if step else bs[1],
+        _at(dev, c, "c", shape[:lead] + (groups, n), typ, lead), cs[0], 0 if step else cs[1],
+        _at(dev, a_log, "a_log", par, torch.float32), _at(dev, dt_bias, "dt_bias", par, torch.float32),
+        _at(dev, skip, "skip", par, torch.float32), _at(dev, reset, "reset", shape[:lead], torch.uint8),
+        _at(dev, state, "state", (batch, heads, width, n), torch.float32))
 
 
 def scan_workspace_bytes(batch: int, length: int, heads: int, head_dim: int, groups: int, state_dim: int,
@@ -234,7 +247,7 @@ def scan(ctx, x, dt, b, c, a_log, dt_bias, skip, reset=None, state=None):
     [batch, heads, head_dim, state_dim]); state: the one before the first (None: zeros)."""
     _want(x.dim() == 4, "x must be [batch, length, heads, head_dim]")
     a = _scan_args(ctx, x, dt, b, c, a_log, dt_bias, skip, reset, state)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _like(x)
     out = torch.empty((a.batch, a.heads, a.head_dim, a.state_dim), dtype=torch.float32, device=x.device)
     _check(lib().gorila_scan(a, y.data_ptr(), out.data_ptr(), ctx.bind_stream()), "gorila_scan")
     return y, out
@@ -243,15 +256,13 @@ def scan(ctx, x, dt, b, c, a_log, dt_bias, skip, reset=None, state=None):
 def scan_backward(ctx, dy, x, dt, b, c, a_log, dt_bias, skip, reset=None, state=None, dstate_out=None):
     """dx, ddt, db, dc, da_log, ddt_bias, dskip, dstate (None without a state)."""
     _want(x.dim() == 4, "x must be [batch, length, heads, head_dim]")
-    a = _scan_args(ctx, x, dt, b, c, a_log, dt_bias, skip, reset, state)
-    pdy = _at(ctx, dy, "dy", x.shape, x.dtype, 2)
-    pds = _at(ctx, dstate_out, "dstate_out", (a.batch, a.heads, a.head_dim, a.state_dim), torch.float32)
-    dev, typ = x.device, x.dtype
-    dx, ddt = torch.empty(x.shape, dtype=typ, device=dev), torch.empty(dt.shape, dtype=typ, device=dev)
-    db, dc = torch.empty(b.shape, dtype=typ, device=dev), torch.empty(c.shape, dtype=typ, device=dev)
-    par = torch.empty((3, a.heads), dtype=torch.float32, device=dev)
+    a, dev = _scan_args(ctx, x, dt, b, c, a_log, dt_bias, skip, reset, state), _device(ctx)
+    pdy = _at(dev, dy, "dy", x.shape, x.dtype, 2)
+    pds = _at(dev, dstate_out, "dstate_out", (a.batch, a.heads, a.head_dim, a.state_dim), torch.float32)
+    dx, ddt, db, dc = _like(x), _like(dt), _like(b), _like(c)
+    par = torch.empty((3, a.heads), dtype=torch.float32, device=x.device)
     da_log, ddt_bias, dskip = par[0], par[1], par[2]
-    dstate = None if state is None else torch.empty(state.shape, dtype=torch.float32, device=dev)
+    dstate = None if state is None else _like(state)
     p0, row = par.data_ptr(), 4 * a.heads
     _check(lib().gorila_scan_backward(
         a, pdy, dy.stride(0), dy.stride(1), pds, dx.data_ptr(), ddt.data_ptr(), db.data_ptr(), dc.data_ptr(), p0, p0 + row,
@@ -262,11 +273,11 @@ def scan_backward(ctx, dy, x, dt, b, c, a_log, dt_bias, skip, reset=None, state=
 def scan_step(ctx, x, dt, b, c, a_log, dt_bias, skip, state_pool, slot=None, reset=None):
     """One step of every row of x [rows, heads, head_dim]; state_pool [slots, heads, head_dim, state_dim] is updated."""
     _want(x.dim() == 3, "x must be [rows, heads, head_dim]")
-    a = _scan_args(ctx, x, dt, b, c, a_log, dt_bias, skip, reset, None)
+    a, dev = _scan_args(ctx, x, dt, b, c, a_log, dt_bias, skip, reset, None), _device(ctx)
     slots = state_pool.shape[0]
-    pool = _at(ctx, state_pool, "state_pool", (slots, a.heads, a.head_dim, a.state_dim), torch.float32)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    _check(lib().gorila_scan_step(a, pool, slots, _at(ctx, slot, "slot", (a.batch,), torch.int32), y.data_ptr(),
+    pool = _at(dev, state_pool, "state_pool", (slots, a.heads, a.head_dim, a.state_dim), torch.float32)
+    y = _like(x)
+    _check(lib().gorila_scan_step(a, pool, slots, _at(dev, slot, "slot", (a.batch,), torch.int32), y.data_ptr(),
                                   ctx.bind_stream()), "gorila_scan_step")
     return y
 
@@ -277,11 +288,12 @@ def quantize_weights(ctx, weights, group: int = 64):
     """codes (uint8 [outputs, 16 * ceil(inputs / 32)]), scales [outputs, ceil(inputs / group)] of [outputs, inputs]."""
     _want(weights.dim() == 2, "weights must be [outputs, inputs]")
     outputs, inputs = weights.shape
+    dev = _device(ctx)
     _want(group in (32, 64, 128), "group must be 32, 64 or 128")
     codes = torch.empty((outputs, 16 * -(-inputs // 32)), dtype=torch.uint8, device=weights.device)
     scales = torch.empty((outputs, -(-inputs // group)), dtype=torch.float32, device=weights.device)
     _check(lib().gorila_quantize_weights(
-        _at(ctx, weights, "weights", weights.shape, weights.dtype, 1), weights.stride(0), outputs, inputs, _dtype(weights), group,
+        _at(dev, weights, "weights", weights.shape, weights.dtype, 1), weights.stride(0), outputs, inputs, _dtype(weights), group,
         codes.data_ptr(), scales.data_ptr(), ctx.bind_stream()), "gorila_quantize_weights")
     return codes, scales
 
@@ -290,7 +302,7 @@ def qmatvec(ctx, x, codes, scales, group: int = 64, x_scale=None):
     """y [rows, outputs] of x [rows, inputs] and 4-bit weights; int8 x with x_scale [rows] gives float32."""
     _want(x.dim() == 2 and codes.dim() == 2, "x must be [rows, inputs], codes [outputs, bytes]")
     rows, inputs = x.shape
-    outputs = codes.shape[0]
+    outputs, dev = codes.shape[0], _device(ctx)
     _want(group in (32, 64, 128), "group must be 32, 64 or 128")
     if x.dtype == torch.int8:
         _want(x_scale is not None, "int8 rows need x_scale")
@@ -300,8 +312,8 @@ def qmatvec(ctx, x, codes, scales, group: int = 64, x_scale=None):
         dt, typ = _dtype(x), x.dtype
     y = torch.empty((rows, outputs), dtype=typ, device=x.device)
     _check(lib().gorila_qmatvec(
-        _at(ctx, x, "x", x.shape, x.dtype, 1), x.stride(0), _at(ctx, x_scale, "x_scale", (rows,), torch.float32), dt, rows,
-        _at(ctx, codes, "codes", (outputs, 16 * -(-inputs // 32)), torch.uint8),
-        _at(ctx, scales, "scales", (outputs, -(-inputs // group)), torch.float32), outputs, inputs, group, y.data_ptr(),
+        _at(dev, x, "x", x.shape, x.dtype, 1), x.stride(0), _at(dev, x_scale, "x_scale", (rows,), torch.float32), dt, rows,
+        _at(dev, codes, "codes", (outputs, 16 * -(-inputs // 32)), torch.uint8),
+        _at(dev, scales, "scales", (outputs, -(-inputs // group)), torch.float32), outputs, inputs, group, y.data_ptr(),
         ctx.bind_stream()), "gorila_qmatvec")
     return y
