@@ -20,13 +20,15 @@
 // + <R, S'> is the same number, but cancels what does not pass t: with large step
 // sizes its error is thousands of times the gradient's.)
 //
-// A workgroup of four waves walks the chunks of one segment of one (sequence,
-// head, 64 channels), the state in registers (a wave holds 16 channels).  Where
+// A workgroup of eight waves walks the chunks of one segment of one (sequence,
+// head, 64 channels), the state in registers: wave w holds 16 channels (w % 4) and
+// half of their states (w / 4).  Where
 // there are few of those, sequences are cut into segments whose states are formed
 // first (state_kernel), joined (join_kernel), and walked again side by side.
 //
 // Masked products multiply by zero, which is no mask for infinities and NaN, so a
 // chunk that holds any is walked one step at a time.
+#include "planes.h"
 #include "seq.h"
 
 namespace gorila {
@@ -34,6 +36,7 @@ namespace {
 
 constexpr int Q = 32;    // steps a chunk
 constexpr int PW = 64;   // channels a workgroup
+constexpr int THREADS = 512;
 constexpr int LP = PW + 4, LQ = Q + 4;  // LDS row lengths: 16 lanes' quads on all banks
 constexpr float LOG2E = 1.44269504088896341f;
 
@@ -90,27 +93,50 @@ __device__ __forceinline__ f32x4 rfrag(const float* s, int ld, int k0, int col0,
     return f32x4{p[0], p[ld], p[2 * ld], p[3 * ld]};
 }
 
-// Q rows of COLS columns on their way from memory to LDS; rows past len and
-// columns past cols are zeros.
+// Q rows of COLS columns on their way from memory to LDS, as they are in memory; rows
+// past len and columns past cols are zeros.
+template <class T, bool VEC> struct Quad {
+    f32x4 v;
+    __device__ __forceinline__ void load(const T* p, int n) { v = row_load<VEC>(p, n); }
+    __device__ __forceinline__ f32x4 get() const { return v; }
+};
+template <> struct Quad<uint16_t, true> {
+    uint2 v;
+    __device__ __forceinline__ void load(const uint16_t* p, int n) {
+        v = uint2{0, 0};
+        if (n > 0) v = *(const uint2*)p;
+    }
+    __device__ __forceinline__ f32x4 get() const {
+        return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+    }
+};
 template <int COLS, bool VEC, class T>
 struct Rows {
-    static constexpr int QUADS = COLS * Q / 4, R = (QUADS + 255) / 256;
-    f32x4 v[R];
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int t0, int len, int cols, int tid) {
+    static constexpr int QUADS = COLS * Q / 4, R = (QUADS + THREADS - 1) / THREADS;
+    Quad<T, VEC> v[R];
+    const T* p[R];
+    int cols;
+    static __device__ __forceinline__ int row(int i) { return (threadIdx.x + THREADS * i) / (COLS / 4); }
+    static __device__ __forceinline__ int col(int i) { return (threadIdx.x + THREADS * i) % (COLS / 4) * 4; }
+    __device__ __forceinline__ Rows(const T* base, int64_t stride, int n) : cols(n) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) p[i] = base + (col(i) < n ? row(i) * stride + col(i) : 0);
+    }
+    // off: elements from step 0 to the first step
+    __device__ __forceinline__ void load(int64_t off, int len) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int e = tid + 256 * i, row = e / (COLS / 4), col = e % (COLS / 4) * 4;
-            const bool in = row < len && col < cols;
-            v[i] = row_load<VEC>(base + (in ? (int64_t)(t0 + row) * stride + col : 0), in ? cols - col : 0);
+            const bool in = row(i) < len && col(i) < cols;
+            v[i].load(in ? p[i] + off : p[i], in ? cols - col(i) : 0);
         }
     }
     // Adds 0 to bad, or NaN where a value is not finite.
-    __device__ __forceinline__ void store(float* lds, int ld, int tid, float& bad) const {
+    __device__ __forceinline__ void store(float* lds, int ld, float& bad) const {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const int e = tid + 256 * i, row = e / (COLS / 4), col = e % (COLS / 4) * 4;
-            if (QUADS % 256 == 0 || e < QUADS) *(f32x4*)(lds + row * ld + col) = v[i];
-            bad += (v[i][0] * 0.0f + v[i][1] * 0.0f) + (v[i][2] * 0.0f + v[i][3] * 0.0f);
+            const f32x4 f = v[i].get();
+            if (QUADS % THREADS == 0 || (int)threadIdx.x + THREADS * i < QUADS) *(f32x4*)(lds + row(i) * ld + col(i)) = f;
+            bad += (f[0] * 0.0f + f[1] * 0.0f) + (f[2] * 0.0f + f[3] * 0.0f);
         }
     }
 };
@@ -120,11 +146,15 @@ struct Rows {
 // them is exact to 2^-23 however large both have grown: one sum in fp32 would lose
 // what few small steps after a large one differ by.
 struct Steps {
-    float d[Q], sig[Q], dec[Q];  // step size, d step size / d dt, own log2-decay
-    float gi[Q], gf[Q];          // sum of dec: whole number, rest
-    int ep[Q];                   // -1: past the end
-    float end_gi, end_gf;
-    int end_ep;
+    float d[Q];            // step size
+    float gi[Q], gf[Q];    // sum of the log2-decays: whole number, rest
+    float from[Q], to[Q];  // e^G_t from the state before, e^(G_end - G_t) to the one behind; 0 in another episode
+    int ep[Q];             // -1: past the end
+    float all;             // from the state before to the one behind
+    int starts;            // an episode starts in it
+};
+struct GradSteps : Steps {
+    float sig[Q], dec[Q];  // d step size / d dt, own log2-decay
 };
 __device__ __forceinline__ float pow2(float v) { return __builtin_amdgcn_exp2f(v); }
 constexpr float LEAST_LOG2 = -65536.0f;  // 2^this is zero, and sums of Q of it are whole numbers below 2^24
@@ -138,7 +168,8 @@ struct StepRegs {
         reset = in && rs ? rs[t0 + l] != 0 : 0;
     }
     // By the lanes of one wave (lanes past Q take part and store nothing).
-    __device__ __forceinline__ void store(Steps& s, float bias, float rate2, int len, int l, float& bad) const {
+    template <class S>
+    __device__ __forceinline__ void store(S& s, float bias, float rate2, int len, int l, float& bad) const {
         const float v = dt + bias;
         const float e = expf(-fabsf(v));
         float d = fmaxf(v, 0.0f) + log1pf(e);
@@ -160,251 +191,293 @@ struct StepRegs {
                 ep += eu;
             }
         }
-        if (l == Q - 1) {
-            s.end_gi = gi;
-            s.end_gf = gf;
-            s.end_ep = ep;
-        }
+        const float end_gi = __shfl(gi, Q - 1, 64), end_gf = __shfl(gf, Q - 1, 64);
+        const int end_ep = __shfl(ep, Q - 1, 64);
         if (l < Q) {
+            const bool in = l < len;
             s.d[l] = d;
             s.gi[l] = gi;
             s.gf[l] = gf;
-            s.ep[l] = l < len ? ep : -1;
-            s.dec[l] = dec;
-            s.sig[l] = l < len ? (v >= 0.0f ? 1.0f : e) / (1.0f + e) : 0.0f;
+            s.ep[l] = in ? ep : -1;
+            s.from[l] = in && ep == 0 ? pow2(gi + gf) : 0.0f;
+            s.to[l] = in && ep == end_ep ? pow2((end_gi - gi) + (end_gf - gf)) : 0.0f;
+            if constexpr (std::is_same<S, GradSteps>::value) {
+                s.dec[l] = dec;
+                s.sig[l] = in ? (v >= 0.0f ? 1.0f : e) / (1.0f + e) : 0.0f;
+            }
             bad += d * 0.0f;
+        }
+        if (l == 0) {
+            s.all = end_ep == 0 ? pow2(end_gi + end_gf) : 0.0f;
+            s.starts = end_ep != 0;
         }
     }
 };
-// e^(G_t) and e^(G_end - G_s).
-__device__ __forceinline__ float from_start(const Steps& s, int t) { return pow2(s.gi[t] + s.gf[t]); }
-__device__ __forceinline__ float to_end(const Steps& s, int t) { return pow2((s.end_gi - s.gi[t]) + (s.end_gf - s.gf[t])); }
+// v times a factor of a Steps, where a zero one is a mask whatever v is.
+__device__ __forceinline__ f32x4 masked(f32x4 v, float f) { return f != 0.0f ? v * f : f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 
-// acc (rows: state, columns: 16 channels from 16 w) = decay * acc + sum over steps
-// of weight * m[step][state] * ch[step][channel].  AFTER: the state after the
-// chunk from the one before (weights w_s d_s); else the gradient before it from the
-// one after (weights e^G).
-template <int NT, bool AFTER>
-__device__ __forceinline__ void walk(f32x4 (&acc)[NT], const float* m, int ldm, const float* ch, const Steps& st, int w, int l) {
-    const int eq = st.end_ep;
-    const float all = pow2(st.end_gi + st.end_gf);
+// State tiles of a wave: the half h of NT (all of one).
+template <int NT> struct Half {
+    static constexpr int TILES = NT > 1 ? NT / 2 : 1;
+    static __device__ __forceinline__ int first(int h) { return h * TILES; }
+    static __device__ __forceinline__ bool on(int h) { return NT > 1 || h == 0; }
+};
+
+// acc (rows: states from m on, columns: 16 channels from ch on) = decay * acc + sum
+// over steps of weight * m[step][state] * ch[step][channel].  AFTER: the state after
+// the chunk from the one before (weights w_s d_s); else the gradient before it from
+// the one after (weights e^G).
+template <int TILES, bool AFTER>
+__device__ __forceinline__ void walk(f32x4 (&acc)[TILES], const float* m, int ldm, const float* ch, const Steps& st, int l) {
+    const float all = st.all;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = eq == 0 ? acc[n] * all : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < TILES; ++n) acc[n] = masked(acc[n], all);
     if (!AFTER && st.ep[0] != 0) return;  // an episode starts with the chunk
 #pragma unroll
     for (int kb = 0; kb < Q / 16; ++kb) {
         const int k0 = 16 * kb + 4 * (l >> 4);
-        f32x4 v = rfrag(ch, LP, 16 * kb, 16 * w, l);
+        f32x4 v = rfrag(ch, LP, 16 * kb, 0, l);
+        v *= AFTER ? *(const f32x4*)(st.to + k0) * *(const f32x4*)(st.d + k0) : *(const f32x4*)(st.from + k0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] *= AFTER ? (st.ep[k0 + j] == eq ? to_end(st, k0 + j) * st.d[k0 + j] : 0.0f) : (st.ep[k0 + j] == 0 ? from_start(st, k0 + j) : 0.0f);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = mma(rfrag(m, ldm, 16 * kb, 16 * n, l), v, acc[n]);
+        for (int n = 0; n < TILES; ++n) acc[n] = mma(rfrag(m, ldm, 16 * kb, 16 * n, l), v, acc[n]);
     }
 }
 
-// Registers <-> state arrays [channel][state], of `pn` states a channel in memory.
-template <int NT, bool VEC>
-__device__ __forceinline__ void load_state(f32x4 (&acc)[NT], const float* s, int ld, int pw, int n_in, int w, int l) {
-    const int p = 16 * w + (l & 15);
+// Registers <-> state arrays [channel][state] of `ld` states a channel in memory, the
+// wave's tiles from channel p0 and state n0 on, of pw channels and n_in states in all.
+template <int TILES, bool VEC>
+__device__ __forceinline__ void load_state(f32x4 (&acc)[TILES], const float* s, int ld, int pw, int n_in, int p0, int n0, int l) {
+    const int p = p0 + (l & 15);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int n0 = 16 * n + 4 * (l >> 4);
-        const bool in = s && p < pw && n0 < n_in;
-        acc[n] = row_load<VEC>(in ? s + (int64_t)p * ld + n0 : s, in ? n_in - n0 : 0);
+    for (int i = 0; i < TILES; ++i) {
+        const int n = n0 + 16 * i + 4 * (l >> 4);
+        const bool in = s && p < pw && n < n_in;
+        acc[i] = row_load<VEC>(in ? s + (int64_t)p * ld + n : s, in ? n_in - n : 0);
     }
 }
-template <int NT, bool VEC>
-__device__ __forceinline__ void store_state(const f32x4 (&acc)[NT], float* s, int ld, int pw, int n_in, int w, int l) {
-    const int p = 16 * w + (l & 15);
+template <int TILES, bool VEC>
+__device__ __forceinline__ void store_state(const f32x4 (&acc)[TILES], float* s, int ld, int pw, int n_in, int p0, int n0, int l) {
+    const int p = p0 + (l & 15);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int n0 = 16 * n + 4 * (l >> 4);
-        if (p < pw && n0 < n_in) row_store<VEC>(s + (int64_t)p * ld + n0, acc[n], n_in - n0);
+    for (int i = 0; i < TILES; ++i) {
+        const int n = n0 + 16 * i + 4 * (l >> 4);
+        if (p < pw && n < n_in) row_store<VEC>(s + (int64_t)p * ld + n, acc[i], n_in - n);
     }
+}
+// To LDS [channel][state].
+template <int TILES>
+__device__ __forceinline__ void stage_state(const f32x4 (&acc)[TILES], float* s, int ld, int p0, int n0, int l) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) *(f32x4*)(s + (p0 + (l & 15)) * ld + n0 + 16 * i + 4 * (l >> 4)) = acc[i];
 }
 
 template <class T>
 __device__ __forceinline__ const T* of(const void* p, int64_t off) { return (const T*)p + off; }
 
+// Where a workgroup's data lie.
+template <class T> struct Data {
+    const T *x, *b, *c, *dy, *dt;
+    const uint8_t* reset;
+    int64_t state;  // of the caller's states
+    float rate2, bias;
+    __device__ Data(const ScanView& s, const Place& at) {
+        const int64_t h = (int64_t)at.h * s.P + at.p0, g = (int64_t)at.grp * s.N;
+        x = of<T>(s.x, at.b * s.xb + h);
+        dy = of<T>(s.dy, at.b * s.dyb + h);
+        b = of<T>(s.b, at.b * s.bb + g);
+        c = of<T>(s.c, at.b * s.cb + g);
+        dt = of<T>(s.dt, at.b * s.dtb + at.h);
+        reset = s.reset ? s.reset + (int64_t)at.b * s.T : nullptr;
+        state = (((int64_t)at.b * s.H + at.h) * s.P + at.p0) * s.N;
+        rate2 = -expf(s.a_log[at.h]) * LOG2E;
+        bias = s.dt_bias[at.h];
+    }
+};
+
+// Steps that are walked together: chunks, or, where a chunk holds a value that is not
+// finite, its steps one by one.
+struct Walk {
+    int begin, end;    // of the segment
+    int t, len;        // now
+    int single;        // end (backward: begin) of the chunk that is walked step by step, or -1
+    __device__ Walk(const ScanView& s, int seg) {
+        begin = seg * s.cps * Q;
+        end = begin + s.cps * Q < s.T ? begin + s.cps * Q : s.T;
+        single = -1;
+    }
+    __device__ int chunk_end(int a) const { return a + Q < end ? a + Q : end; }
+    // forward
+    __device__ bool start() { t = begin, len = chunk_end(t) - t; return t < end; }
+    __device__ void split() { single = t + len, len = 1; }
+    __device__ bool next(bool& whole) {  // whole: the chunk that was walked step by step is done
+        t += len;
+        whole = single >= 0 && t >= single;
+        if (whole) single = -1;
+        if (t >= end) return false;
+        len = single >= 0 ? 1 : chunk_end(t) - t;
+        return true;
+    }
+    // backward
+    __device__ int chunk() const { return begin + (t - begin) / Q * Q; }
+    __device__ bool start_back() { t = begin + (end > begin ? (end - begin - 1) / Q * Q : 0), len = end - t; return begin < end; }
+    __device__ void split_back() { single = t, t += len - 1, len = 1; }
+    __device__ bool next_back(bool& whole) {
+        whole = single >= 0 && t <= single;
+        if (whole) single = -1;
+        if (t <= begin) return false;
+        if (single >= 0) { t -= 1; }
+        else { t = begin + (t - 1 - begin) / Q * Q, len = Q; }
+        return true;
+    }
+};
+
 // Forward over one segment.
 template <class T, int NP, bool VEC>
-__global__ __launch_bounds__(256, 2) void scan_kernel(ScanView s) {
-    constexpr int NT = NP / 16, LN = NP + 4;
+__global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
+    constexpr int NT = NP / 16, LN = NP + 4, TILES = Half<NT>::TILES;
     __shared__ __align__(16) float sc[Q * LN], sb[Q * LN], sx[Q * LP], ss[PW * LN], sm[Q * LQ];
     __shared__ __align__(16) Steps st;
     __shared__ int flag;
     const Place at(s, blockIdx.x);
-    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lg = l >> 4, lc = l & 15;
-    const float rate2 = -expf(s.a_log[at.h]) * LOG2E, bias = s.dt_bias[at.h], skip = s.skip[at.h];
-    const T* x = of<T>(s.x, at.b * s.xb + (int64_t)at.h * s.P + at.p0);
-    const T* bm = of<T>(s.b, at.b * s.bb + (int64_t)at.grp * s.N);
-    const T* cm = of<T>(s.c, at.b * s.cb + (int64_t)at.grp * s.N);
-    const T* dt = of<T>(s.dt, at.b * s.dtb + at.h);
-    const uint8_t* rs = s.reset ? s.reset + (int64_t)at.b * s.T : nullptr;
-    T* y = (T*)s.y + ((int64_t)at.b * s.T * s.H + at.h) * s.P + at.p0;
+    const Data<T> in(s, at);
+    const int tid = threadIdx.x, l = tid & 63, lg = l >> 4, lc = l & 15;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wp = w & 3, half = w >> 2, n_own = 16 * Half<NT>::first(half);
+    const bool on = Half<NT>::on(half);
+    const float skip = s.skip[at.h];
     const int64_t yt = (int64_t)s.H * s.P;
-    const int64_t state0 = (((int64_t)at.b * s.H + at.h) * s.P + at.p0) * s.N;
+    T* y = (T*)s.y + ((int64_t)at.b * s.T * s.H + at.h) * s.P + at.p0 + (16 * half + lc) * yt + 16 * wp + 4 * lg;
 
-    f32x4 S[NT];
+    f32x4 S[TILES];
     if (s.nseg > 1)
-        load_state<NT, true>(S, s.seg_s + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * PW * NP, NP, PW, NP, w, l);
+        load_state<TILES, true>(S, s.seg_s + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * PW * NP, NP, PW, NP, 16 * wp, n_own, l);
     else
-        load_state<NT, VEC>(S, s.state ? s.state + state0 : nullptr, s.N, at.pw, s.N, w, l);
+        load_state<TILES, VEC>(S, s.state ? s.state + in.state : nullptr, s.N, at.pw, s.N, 16 * wp, n_own, l);
     if (tid == 0) flag = 0;
-    const int c0 = at.seg * s.cps, c1 = c0 + s.cps < s.nch ? c0 + s.cps : s.nch;
 
-    Rows<PW, VEC, T> rx;
-    Rows<NP, VEC, T> rb, rc;
+    Rows<PW, VEC, T> rx(in.x, s.xt, at.pw);
+    Rows<NP, VEC, T> rb(in.b, s.bt, s.N), rc(in.c, s.ct, s.N);
     StepRegs rd;
-    auto load = [&](int t0, int len) {
-        rx.load(x, s.xt, t0, len, at.pw, tid);
-        rb.load(bm, s.bt, t0, len, s.N, tid);
-        rc.load(cm, s.ct, t0, len, s.N, tid);
-        if (w == 3) rd.load(dt, s.dtt, rs, t0, len, l);
+    Walk at_t(s, at.seg);
+    auto load = [&]() {
+        rx.load(at_t.t * s.xt, at_t.len);
+        rb.load(at_t.t * s.bt, at_t.len);
+        rc.load(at_t.t * s.ct, at_t.len);
+        if (w == 7) rd.load(in.dt, s.dtt, in.reset, at_t.t, at_t.len, l);
     };
-    auto stage = [&](int len) {
+    bool more = at_t.start();
+    if (more) load();
+    while (more) {
+        __syncthreads();
         float bad = 0.0f;
-        rx.store(sx, LP, tid, bad);
-        rb.store(sb, LN, tid, bad);
-        rc.store(sc, LN, tid, bad);
-        if (w == 3) rd.store(st, bias, rate2, len, l, bad);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) *(f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg) = S[n];
+        rx.store(sx, LP, bad);
+        rb.store(sb, LN, bad);
+        rc.store(sc, LN, bad);
+        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l, bad);
+        if (on) stage_state<TILES>(S, ss, LN, 16 * wp, n_own, l);
         if (bad != bad) flag = 1;
-    };
-    if (c0 < c1) load(c0 * Q, s.T - c0 * Q < Q ? s.T - c0 * Q : Q);
-    for (int c = c0; c < c1; ++c) {
-        const int t0 = c * Q, len = s.T - t0 < Q ? s.T - t0 : Q;
         __syncthreads();
-        stage(len);
-        __syncthreads();
-        const bool single = flag != 0;
-        const int next = s.T - t0 - Q < Q ? s.T - t0 - Q : Q;
-        if (!single && c + 1 < c1) load(t0 + Q, next);
-        for (int u = 0; u < (single ? len : 1); ++u) {
-            const int tu = t0 + u, lu = single ? 1 : len;
-            if (single) {
-                __syncthreads();
-                load(tu, 1);
-                stage(1);
-                __syncthreads();
-            }
-            // what the state gives: rows = channels, columns = steps
-            f32x4 acc[Q / 16];
-#pragma unroll
-            for (int i = 0; i < Q / 16; ++i) {
-                acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int n = 0; n < NT; ++n) acc[i] = mma(kfrag(ss, LN, 16 * w, 16 * n, l), kfrag(sc, LN, 16 * i, 16 * n, l), acc[i]);
-                const int t = 16 * i + lc;
-                acc[i] = st.ep[t] == 0 ? acc[i] * from_start(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-            if (w < 3) {  // decay * (c_t . b_s) * d_s of one of the three tiles with s <= t
-                const int si = w >> 1, ti = w > 0;
-                f32x4 m{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
-                const int t = 16 * ti + lc, q0 = 16 * si + 4 * lg;
-                const float ti_ = st.gi[t], tf = st.gf[t];
-                const int et = st.ep[t];
-                const f32x4 gi = *(const f32x4*)(st.gi + q0), gf = *(const f32x4*)(st.gf + q0), d = *(const f32x4*)(st.d + q0);
-                const i32x4 ep = *(const i32x4*)(st.ep + q0);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool same = t == q0 + j, on = t > q0 + j && ep[j] == et;
-                    m[j] = same ? m[j] * d[j] : on ? m[j] * (pow2((ti_ - gi[j]) + (tf - gf[j])) * d[j]) : 0.0f;
-                }
-                *(f32x4*)(sm + t * LQ + q0) = m;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < Q / 16; ++i) {
-#pragma unroll
-                for (int k = 0; k <= i; ++k) acc[i] = mma(rfrag(sx, LP, 16 * k, 16 * w, l), kfrag(sm, LQ, 16 * i, 16 * k, l), acc[i]);
-                const int t = 16 * i + lc, p = 16 * w + 4 * lg;
-                if (t < lu && p < at.pw)
-                    row_store<VEC>(y + (int64_t)(tu + t) * yt + p, acc[i] + skip * *(const f32x4*)(sx + t * LP + p), at.pw - p);
-            }
-            walk<NT, true>(S, sb, LN, sx, st, w, l);
+        if (at_t.single < 0 && flag) {
+            at_t.split();
+            load();
+            continue;
         }
-        if (single) {
+        const int t0 = at_t.t, len = at_t.len;
+        bool whole;
+        more = at_t.next(whole);
+        if (more) load();
+        // what the state gives 16 steps: rows = channels, columns = steps
+        const int t = 16 * half + lc;
+        f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc = mma(kfrag(ss, LN, 16 * wp, 16 * n, l), kfrag(sc, LN, 16 * half, 16 * n, l), acc);
+        acc = masked(acc, st.from[t]);
+        if (w < 3) {  // decay * (c_t . b_s) * d_s of one of the three tiles with s <= t
+            const int si = w >> 1, ti = w > 0;
+            f32x4 m{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
+            const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
+            const float gi_t = st.gi[tm], gf_t = st.gf[tm];
+            const int et = st.ep[tm];
+            const f32x4 gi = *(const f32x4*)(st.gi + q0), gf = *(const f32x4*)(st.gf + q0), d = *(const f32x4*)(st.d + q0);
+            const i32x4 ep = *(const i32x4*)(st.ep + q0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool same = tm == q0 + j, behind = tm > q0 + j && ep[j] == et;
+                m[j] = same ? m[j] * d[j] : behind ? m[j] * (pow2((gi_t - gi[j]) + (gf_t - gf[j])) * d[j]) : 0.0f;
+            }
+            *(f32x4*)(sm + tm * LQ + q0) = m;
+        }
+        __syncthreads();
+        for (int k = 0; k <= half; ++k) acc = mma(rfrag(sx, LP, 16 * k, 16 * wp, l), kfrag(sm, LQ, 16 * half, 16 * k, l), acc);
+        const int p = 16 * wp + 4 * lg;
+        if (t < len && p < at.pw) row_store<VEC>(y + t0 * yt, acc + skip * *(const f32x4*)(sx + t * LP + p), at.pw - p);
+        if (on) walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, l);
+        if (whole) {
             __syncthreads();
             if (tid == 0) flag = 0;
-            if (c + 1 < c1) load(t0 + Q, next);
         }
     }
-    if (s.state_out && at.seg == s.nseg - 1) store_state<NT, VEC>(S, s.state_out + state0, s.N, at.pw, s.N, w, l);
+    if (on && s.state_out && at.seg == s.nseg - 1) store_state<TILES, VEC>(S, s.state_out + in.state, s.N, at.pw, s.N, 16 * wp, n_own, l);
 }
 
 // What one segment adds to the state behind it (REV = false: from x and b) or to
 // the gradient of the state before it (REV = true: from dy and c), and its decay.
 template <class T, int NP, bool VEC, bool REV>
-__global__ __launch_bounds__(256, 2) void state_kernel(ScanView s) {
-    constexpr int NT = NP / 16, LN = NP + 4;
+__global__ __launch_bounds__(THREADS, 4) void state_kernel(ScanView s) {
+    constexpr int NT = NP / 16, LN = NP + 4, TILES = Half<NT>::TILES;
     __shared__ __align__(16) float sb[Q * LN], sx[Q * LP];
     __shared__ __align__(16) Steps st;
     __shared__ int flag;
     const Place at(s, blockIdx.x);
-    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
-    const float rate2 = -expf(s.a_log[at.h]) * LOG2E, bias = s.dt_bias[at.h];
-    const int64_t xt = REV ? s.dyt : s.xt, bt = REV ? s.ct : s.bt;
-    const T* x = of<T>(REV ? s.dy : s.x, at.b * (REV ? s.dyb : s.xb) + (int64_t)at.h * s.P + at.p0);
-    const T* bm = of<T>(REV ? s.c : s.b, at.b * (REV ? s.cb : s.bb) + (int64_t)at.grp * s.N);
-    const T* dt = of<T>(s.dt, at.b * s.dtb + at.h);
-    const uint8_t* rs = s.reset ? s.reset + (int64_t)at.b * s.T : nullptr;
-    f32x4 S[NT];
+    const Data<T> in(s, at);
+    const int tid = threadIdx.x, l = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wp = w & 3, half = w >> 2, n_own = 16 * Half<NT>::first(half);
+    const bool on = Half<NT>::on(half);
+    f32x4 S[TILES];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) S[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < TILES; ++n) S[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (tid == 0) flag = 0;
-    const int c0 = at.seg * s.cps, c1 = c0 + s.cps < s.nch ? c0 + s.cps : s.nch;
     float decay = 1.0f;
     bool starts = false;
-
-    Rows<PW, VEC, T> rx;
-    Rows<NP, VEC, T> rb;
+    const int64_t xt = REV ? s.dyt : s.xt, bt = REV ? s.ct : s.bt;
+    Rows<PW, VEC, T> rx(REV ? in.dy : in.x, xt, at.pw);
+    Rows<NP, VEC, T> rb(REV ? in.c : in.b, bt, s.N);
     StepRegs rd;
-    auto load = [&](int t0, int len) {
-        rx.load(x, xt, t0, len, at.pw, tid);
-        rb.load(bm, bt, t0, len, s.N, tid);
-        if (w == 3) rd.load(dt, s.dtt, rs, t0, len, l);
+    Walk at_t(s, at.seg);
+    auto load = [&]() {
+        rx.load(at_t.t * xt, at_t.len);
+        rb.load(at_t.t * bt, at_t.len);
+        if (w == 7) rd.load(in.dt, s.dtt, in.reset, at_t.t, at_t.len, l);
     };
-    auto stage = [&](int len) {
+    bool more = REV ? at_t.start_back() : at_t.start();
+    if (more) load();
+    while (more) {
+        __syncthreads();
         float bad = 0.0f;
-        rx.store(sx, LP, tid, bad);
-        rb.store(sb, LN, tid, bad);
-        if (w == 3) rd.store(st, bias, rate2, len, l, bad);
+        rx.store(sx, LP, bad);
+        rb.store(sb, LN, bad);
+        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l, bad);
         if (bad != bad) flag = 1;
-    };
-    auto first = [&](int i) { return REV ? c1 - 1 - i : c0 + i; };
-    auto length = [&](int c) { return s.T - c * Q < Q ? s.T - c * Q : Q; };
-    if (c0 < c1) load(first(0) * Q, length(first(0)));
-    for (int i = 0; i < c1 - c0; ++i) {
-        const int t0 = first(i) * Q, len = length(first(i));
         __syncthreads();
-        stage(len);
-        __syncthreads();
-        const bool single = flag != 0;
-        if (!single && i + 1 < c1 - c0) load(first(i + 1) * Q, length(first(i + 1)));
-        decay *= pow2(st.end_gi + st.end_gf);
-        starts |= st.end_ep != 0;
-        for (int u = 0; u < (single ? len : 1); ++u) {
-            if (single) {
-                __syncthreads();
-                load(REV ? t0 + len - 1 - u : t0 + u, 1);
-                stage(1);
-                __syncthreads();
-            }
-            walk<NT, !REV>(S, sb, LN, sx, st, w, l);
+        if (at_t.single < 0 && flag) {
+            REV ? at_t.split_back() : at_t.split();
+            load();
+            continue;
         }
-        if (single) {
+        bool whole;
+        more = REV ? at_t.next_back(whole) : at_t.next(whole);
+        if (more) load();
+        decay *= st.all;
+        starts |= st.starts != 0;
+        if (on) walk<TILES, !REV>(S, sb + n_own, LN, sx + 16 * wp, st, l);
+        if (whole) {
             __syncthreads();
             if (tid == 0) flag = 0;
-            if (i + 1 < c1 - c0) load(first(i + 1) * Q, length(first(i + 1)));
         }
     }
     const int64_t o = ((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v;
-    store_state<NT, true>(S, (REV ? s.seg_r : s.seg_s) + o * PW * NP, NP, PW, NP, w, l);
+    if (on) store_state<TILES, true>(S, (REV ? s.seg_r : s.seg_s) + o * PW * NP, NP, PW, NP, 16 * wp, n_own, l);
     if (!REV && tid == 0) s.seg_a[o] = starts ? -1.0f : decay;
 }
 
@@ -428,130 +501,186 @@ __global__ __launch_bounds__(256) void join_kernel(ScanView s) {
     }
 }
 
+// A lane's part of a state walked without LDS from step t0 to t1, where a chunk has
+// values that are not finite (slow, and rare: kept out of the registers of the rest).
+template <int TILES> struct Tiles { f32x4 v[TILES]; };
+template <int TILES, class T>
+__device__ __noinline__ Tiles<TILES> walk_plain(Tiles<TILES> S, const T* x, int64_t xt, const T* b, int64_t bt, int n_left, const T* dt,
+                                                int64_t dtt, const uint8_t* reset, float rate2, float bias, int t0, int t1) {
+    for (int t = t0; t < t1; ++t) {
+        const float v = row_value(dt[t * dtt]) + bias;
+        float d = fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v)));
+        if (v != v) d = v;
+        const float a = pow2(rate2 * d), xv = x ? row_value(x[t * xt]) : 0.0f;
+        const bool start = reset && reset[t];
+#pragma unroll
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float add = d * xv * (16 * i + j < n_left ? row_value(b[t * bt + 16 * i + j]) : 0.0f);
+                S.v[i][j] = start ? add : fmaf(a, S.v[i][j], add);
+            }
+    }
+    return S;
+}
+
 // Backward over one segment: forward once for the states before its chunks, then
 // back.
 template <class T, int NP, bool VEC>
-__global__ __launch_bounds__(256, NP > 64 ? 1 : 2) void scan_backward_kernel(ScanView s) {
-    constexpr int NT = NP / 16, LN = NP + 4;
+__global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel(ScanView s) {
+    constexpr int NT = NP / 16, LN = NP + 4, TILES = Half<NT>::TILES;
     __shared__ __align__(16) float sc[Q * LN], sb[Q * LN], sx[Q * LP], sdy[Q * LP], ss[PW * LN], sr[PW * LN];
     __shared__ __align__(16) float sm[Q * LQ], sf[Q * LQ];
-    __shared__ __align__(16) Steps st;
-    __shared__ float hc[NT][Q], qb[NT][Q], kb[NT][Q], pairs[3][Q], inner[4], red[4];
+    __shared__ __align__(16) GradSteps st;
+    __shared__ float hc[NT][Q], qb[NT][Q], kb[NT][Q], pairs[3][Q], inner[8];
     __shared__ int flag;
     const Place at(s, blockIdx.x);
-    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lg = l >> 4, lc = l & 15;
-    const float rate2 = -expf(s.a_log[at.h]) * LOG2E, bias = s.dt_bias[at.h], skip = s.skip[at.h];
-    const T* x = of<T>(s.x, at.b * s.xb + (int64_t)at.h * s.P + at.p0);
-    const T* dy = of<T>(s.dy, at.b * s.dyb + (int64_t)at.h * s.P + at.p0);
-    const T* bm = of<T>(s.b, at.b * s.bb + (int64_t)at.grp * s.N);
-    const T* cm = of<T>(s.c, at.b * s.cb + (int64_t)at.grp * s.N);
-    const T* dt = of<T>(s.dt, at.b * s.dtb + at.h);
-    const uint8_t* rs = s.reset ? s.reset + (int64_t)at.b * s.T : nullptr;
-    T* dx = (T*)s.dx + ((int64_t)at.b * s.T * s.H + at.h) * s.P + at.p0;
+    const Data<T> in(s, at);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wp = w & 3, half = w >> 2, n_own = 16 * Half<NT>::first(half);
+    const bool on = Half<NT>::on(half);
     const int64_t yt = (int64_t)s.H * s.P;
-    const int64_t state0 = (((int64_t)at.b * s.H + at.h) * s.P + at.p0) * s.N;
     const int64_t seg0 = (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * PW * NP;
-    float* chunk_s = s.chunk_s + ((int64_t)at.b * s.nch * s.vh + at.v) * PW * NP;
+    float* chunk_s = s.chunk_s + ((int64_t)at.b * s.nch * s.vh + at.v) * PW * NP;  // of chunk 0
     const int64_t chunk_step = (int64_t)s.vh * PW * NP;
-    const int c0 = at.seg * s.cps, c1 = c0 + s.cps < s.nch ? c0 + s.cps : s.nch;
-    auto length = [&](int c) { return s.T - c * Q < Q ? s.T - c * Q : Q; };
 
-    Rows<PW, VEC, T> rx, ry;
-    Rows<NP, VEC, T> rb, rc;
+    Rows<PW, VEC, T> rx(in.x, s.xt, at.pw);
+    Rows<NP, VEC, T> rb(in.b, s.bt, s.N);
     StepRegs rd;
-    f32x4 R[NT];
+    f32x4 R[TILES];
     float decay_sum = 0.0f, bias_sum = 0.0f, skip_sum = 0.0f;  // of the three parameters' gradients
     if (tid == 0) flag = 0;
-    auto load_in = [&](int t0, int len) {
-        rx.load(x, s.xt, t0, len, at.pw, tid);
-        rb.load(bm, s.bt, t0, len, s.N, tid);
-        if (w == 3) rd.load(dt, s.dtt, rs, t0, len, l);
+    Walk at_t(s, at.seg);
+    auto load_in = [&]() {
+        rx.load(at_t.t * s.xt, at_t.len);
+        rb.load(at_t.t * s.bt, at_t.len);
+        if (w == 7) rd.load(in.dt, s.dtt, in.reset, at_t.t, at_t.len, opaque(lane));
     };
-    auto stage_in = [&](int len) {
+    auto stage_in = [&](int l) {
         float bad = 0.0f;
-        rx.store(sx, LP, tid, bad);
-        rb.store(sb, LN, tid, bad);
-        if (w == 3) rd.store(st, bias, rate2, len, l, bad);
+        rx.store(sx, LP, bad);
+        rb.store(sb, LN, bad);
+        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l, bad);
         if (bad != bad) flag = 1;
     };
+    auto plain_walk = [&](f32x4 (&S)[TILES], int t0, int t1) {
+        const int lc = lane & 15, lg = lane >> 4;
+        Tiles<TILES> v;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) v.v[i] = S[i];
+        const int p = 16 * wp + lc, n = n_own + 4 * lg;
+        v = walk_plain<TILES, T>(v, p < at.pw ? in.x + p : nullptr, s.xt, in.b + n, s.bt, s.N - n, in.dt, s.dtt, in.reset, in.rate2, in.bias, t0, t1);
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) S[i] = v.v[i];
+    };
     {
-        f32x4 S[NT];
+        f32x4 S[TILES];
         if (s.nseg > 1)
-            load_state<NT, true>(S, s.seg_s + seg0, NP, PW, NP, w, l);
+            load_state<TILES, true>(S, s.seg_s + seg0, NP, PW, NP, 16 * wp, n_own, lane);
         else
-            load_state<NT, VEC>(S, s.state ? s.state + state0 : nullptr, s.N, at.pw, s.N, w, l);
-        if (c0 < c1) load_in(c0 * Q, length(c0));
-        for (int c = c0; c < c1; ++c) {
-            const int t0 = c * Q, len = length(c);
-            store_state<NT, true>(S, chunk_s + c * chunk_step, NP, PW, NP, w, l);
-            __syncthreads();
-            stage_in(len);
-            __syncthreads();
-            const bool single = flag != 0;
-            if (!single && c + 1 < c1) load_in(t0 + Q, length(c + 1));
-            for (int u = 0; u < (single ? len : 1); ++u) {
-                if (single) {
-                    __syncthreads();
-                    load_in(t0 + u, 1);
-                    stage_in(1);
-                    __syncthreads();
-                }
-                walk<NT, true>(S, sb, LN, sx, st, w, l);
-            }
-            if (single) {
+            load_state<TILES, VEC>(S, s.state ? s.state + in.state : nullptr, s.N, at.pw, s.N, 16 * wp, n_own, lane);
+        if (at_t.start()) {
+            load_in();
+            for (;;) {
+                const int t0 = at_t.t, len = at_t.len;
+                if (on) store_state<TILES, true>(S, chunk_s + t0 / Q * chunk_step, NP, PW, NP, 16 * wp, n_own, lane);
+                bool whole;
+                if (t0 + len >= at_t.end) break;  // nobody asks for the state behind the last
                 __syncthreads();
-                if (tid == 0) flag = 0;
-                if (c + 1 < c1) load_in(t0 + Q, length(c + 1));
+                stage_in(opaque(lane));
+                __syncthreads();
+                const bool plain = flag != 0;
+                at_t.next(whole);
+                load_in();
+                if (plain) {
+                    plain_walk(S, t0, t0 + len);
+                    __syncthreads();
+                    if (tid == 0) flag = 0;
+                } else if (on) {
+                    walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, opaque(lane));
+                }
             }
         }
         if (s.nseg > 1)
-            load_state<NT, true>(R, s.seg_r + seg0, NP, PW, NP, w, l);
+            load_state<TILES, true>(R, s.seg_r + seg0, NP, PW, NP, 16 * wp, n_own, lane);
         else
-            load_state<NT, VEC>(R, s.dstate_out ? s.dstate_out + state0 : nullptr, s.N, at.pw, s.N, w, l);
+            load_state<TILES, VEC>(R, s.dstate_out ? s.dstate_out + in.state : nullptr, s.N, at.pw, s.N, 16 * wp, n_own, lane);
     }
 
-    auto load = [&](int t0, int len) {
-        load_in(t0, len);
-        ry.load(dy, s.dyt, t0, len, at.pw, tid);
-        rc.load(cm, s.ct, t0, len, s.N, tid);
+    Rows<PW, VEC, T> ry(in.dy, s.dyt, at.pw);
+    Rows<NP, VEC, T> rc(in.c, s.ct, s.N);
+    f32x4 S[TILES];
+    auto load_out = [&]() {
+        ry.load(at_t.t * s.dyt, at_t.len);
+        rc.load(at_t.t * s.ct, at_t.len);
+        load_state<TILES, true>(S, chunk_s + at_t.chunk() / Q * chunk_step, NP, PW, NP, 16 * wp, n_own, opaque(lane));
     };
-    auto stage = [&](int len) {
+    const float skip = s.skip[at.h];
+    T* dx = (T*)s.dx + ((int64_t)at.b * s.T * s.H + at.h) * s.P + at.p0;
+    const int64_t part_t = (int64_t)s.vh * s.N;
+    const int64_t part0 = ((int64_t)at.b * s.T * s.vh + at.v) * s.N;
+    auto load = [&]() {
+        load_in();
+        load_out();
+    };
+    bool more = at_t.start_back();
+    if (more) load_out();  // the last chunk's inputs are here
+    while (more) {
+        // what the lane number decides is decided again for every chunk: kept over the
+        // loop it took more scalar registers than there are
+        const int l = opaque(lane), lg = l >> 4, lc = l & 15;
+        if (at_t.single >= 0 && on) plain_walk(S, at_t.chunk(), at_t.t);
+        __syncthreads();
+        stage_in(l);
         float bad = 0.0f;
-        stage_in(len);
-        ry.store(sdy, LP, tid, bad);
-        rc.store(sc, LN, tid, bad);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) *(f32x4*)(sr + (16 * w + lc) * LN + 16 * n + 4 * lg) = R[n];
+        ry.store(sdy, LP, bad);
+        rc.store(sc, LN, bad);
+        if (on) {
+            stage_state<TILES>(R, sr, LN, 16 * wp, n_own, l);
+            stage_state<TILES>(S, ss, LN, 16 * wp, n_own, l);
+        }
         if (bad != bad) flag = 1;
-    };
-    // one chunk (or step) of lu steps from tu, staged, with the state before it in S
-    auto back = [&](int tu, int lu) {
-        if (w < 3) {
-            const int si = w >> 1, ti = w > 0;
-            f32x4 m{0.0f, 0.0f, 0.0f, 0.0f}, f = m;
+        __syncthreads();
+        if (at_t.single < 0 && flag) {
+            at_t.split_back();
+            load();
+            continue;
+        }
+        const int t0 = at_t.t, len = at_t.len;
+        bool whole;
+        more = at_t.next_back(whole);
+        if (more) load();
+        // the tiles with s <= t of M (waves 0 .. 2) and F (3 .. 5): rows = s, columns = t
+        const int tile = w < 3 ? w : w - 3, si = tile >> 1, ti = tile > 0;
+        const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
+        f32x4 f{0.0f, 0.0f, 0.0f, 0.0f};
+        if (w < 6) {
+            if (w < 3) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
+                for (int n = 0; n < NT; ++n) f = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), f);
+            } else {
 #pragma unroll
-            for (int n = 0; n < PW / 16; ++n) f = mma(kfrag(sx, LP, 16 * si, 16 * n, l), kfrag(sdy, LP, 16 * ti, 16 * n, l), f);
-            const int t = 16 * ti + lc, q0 = 16 * si + 4 * lg;
-            const float ti_ = st.gi[t], tf = st.gf[t];
-            const int et = st.ep[t];
+                for (int n = 0; n < PW / 16; ++n) f = mma(kfrag(sx, LP, 16 * si, 16 * n, l), kfrag(sdy, LP, 16 * ti, 16 * n, l), f);
+            }
+            const float gi_t = st.gi[tm], gf_t = st.gf[tm];
+            const int et = st.ep[tm];
             const f32x4 gi = *(const f32x4*)(st.gi + q0), gf = *(const f32x4*)(st.gf + q0);
             const i32x4 ep = *(const i32x4*)(st.ep + q0);
-            f32x4 pre;  // sums over s up to q0 + j of what passes from s to t
-            float run = 0.0f;
+            f32x4 g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float dec = pow2((ti_ - gi[j]) + (tf - gf[j]));
-                const bool same = t == q0 + j, on = t > q0 + j && ep[j] == et;
-                const float fd = f[j] * dec;
-                run += on ? m[j] * fd * st.d[q0 + j] : 0.0f;
-                pre[j] = run;
-                m[j] = same ? m[j] : on ? m[j] * dec : 0.0f;
-                f[j] = same ? f[j] : on ? fd : 0.0f;
+                const bool same = tm == q0 + j, behind = tm > q0 + j && ep[j] == et;
+                g[j] = same ? f[j] : behind ? f[j] * pow2((gi_t - gi[j]) + (gf_t - gf[j])) : 0.0f;
             }
-            *(f32x4*)(sm + t * LQ + q0) = m;
-            *(f32x4*)(sf + t * LQ + q0) = f;
+            *(f32x4*)((w < 3 ? sm : sf) + tm * LQ + q0) = g;
+        }
+        __syncthreads();
+        if (w >= 3 && w < 6) {  // what passes from s to t: M F d without F's decay, summed for every step between
+            const f32x4 v = *(const f32x4*)(sm + tm * LQ + q0) * f * *(const f32x4*)(st.d + q0);
+            f32x4 pre;  // sums over s up to q0 + j
+            float run = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pre[j] = run += tm > q0 + j ? v[j] : 0.0f;
             const float up = __shfl_up(run, 16, 64);  // and of the lanes with lower s
             float low = lg > 0 ? up : 0.0f;
             const float up2 = __shfl_up(low + run, 32, 64);
@@ -561,40 +690,36 @@ __global__ __launch_bounds__(256, NP > 64 ? 1 : 2) void scan_backward_kernel(Sca
                 // step q0 + j + 1 of this half: sum over t from it on
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float v = t > q0 + j ? pre[j] : 0.0f;
-                    for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o, 64);
-                    if (lc == 0 && (q0 + j + 1) % 16) pairs[2 * si][q0 + j + 1] = v;
+                    float u = tm > q0 + j ? pre[j] : 0.0f;
+                    for (int o = 8; o; o >>= 1) u += __shfl_xor(u, o, 64);
+                    if (lc == 0 && (q0 + j + 1) % 16) pairs[2 * si][q0 + j + 1] = u;
                 }
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {  // every t is behind step q0 + j + 1
-                    float v = pre[j];
-                    for (int o = 8; o; o >>= 1) v += __shfl_xor(v, o, 64);
-                    if (lc == 0) pairs[1][q0 + j + 1] = v;
+                    float u = pre[j];
+                    for (int o = 8; o; o >>= 1) u += __shfl_xor(u, o, 64);
+                    if (lc == 0) pairs[1][q0 + j + 1] = u;
                 }
-                float v = __shfl(pre[3], 48 + lc, 64);  // all s, and t from a step of the second half on
+                float u = __shfl(pre[3], 48 + lc, 64);  // all s, and t from a step of the second half on
                 for (int o = 1; o < 16; o <<= 1) {
-                    const float up = __shfl_down(v, o, 16);
-                    if (lc + o < 16) v += up;
+                    const float down = __shfl_down(u, o, 16);
+                    if (lc + o < 16) u += down;
                 }
-                if (lg == 0 && lc > 0) pairs[1][t] = v;
+                if (lg == 0 && lc > 0) pairs[1][tm] = u;
             }
         }
-        __syncthreads();
-        const int eq = st.end_ep;
         // dc and db: rows = state, columns = steps
-        for (int job = w; job < 2 * NT; job += 4) {
+        for (int job = w; job < 2 * NT; job += 8) {
             const int n = job >> 1, i = job & 1, t = 16 * i + lc, n0 = 16 * n + 4 * lg;
-            const float dt_ = st.d[t];
-            const int et = st.ep[t];
             f32x4 a{0.0f, 0.0f, 0.0f, 0.0f}, q = a;
 #pragma unroll
             for (int k = 0; k < PW / 16; ++k) {
                 a = mma(rfrag(ss, LN, 16 * k, 16 * n, l), kfrag(sdy, LP, 16 * i, 16 * k, l), a);
                 q = mma(rfrag(sr, LN, 16 * k, 16 * n, l), kfrag(sx, LP, 16 * i, 16 * k, l), q);
             }
-            a = et == 0 ? a * from_start(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            q = et == eq ? q * to_end(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            a = masked(a, st.from[t]);
+            q = masked(q, st.to[t]);
             const f32x4 cv = *(const f32x4*)(sc + t * LN + n0), bv = *(const f32x4*)(sb + t * LN + n0);
             float h = (a[0] * cv[0] + a[1] * cv[1]) + (a[2] * cv[2] + a[3] * cv[3]);
             float kv = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
@@ -616,37 +741,36 @@ __global__ __launch_bounds__(256, NP > 64 ? 1 : 2) void scan_backward_kernel(Sca
                 kb[n][t] = kv;
                 qb[n][t] = bq;
             }
-            if (t < lu && n0 < s.N) {
-                const int64_t o = (((int64_t)at.b * s.T + tu + t) * s.vh + at.v) * s.N + n0;
+            if (t < len && n0 < s.N) {
+                const int64_t o = part0 + (t0 + t) * part_t + n0;
                 row_store<VEC>(s.pdc + o, a, s.N - n0);
-                row_store<VEC>(s.pdb + o, q * dt_, s.N - n0);
+                row_store<VEC>(s.pdb + o, q * st.d[t], s.N - n0);
             }
         }
-        // dx: rows = channels, columns = steps
-#pragma unroll
-        for (int i = 0; i < Q / 16; ++i) {
-            const int t = 16 * i + lc, p = 16 * w + 4 * lg;
+        {  // dx: rows = channels, columns = steps
+            const int t = 16 * half + lc, p = 16 * wp + 4 * lg;
             f32x4 a{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int n = 0; n < NT; ++n) a = mma(kfrag(sr, LN, 16 * w, 16 * n, l), kfrag(sb, LN, 16 * i, 16 * n, l), a);
-            a = st.ep[t] == eq ? a * to_end(st, t) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = i; k < Q / 16; ++k) a = mma(rfrag(sdy, LP, 16 * k, 16 * w, l), rfrag(sm, LQ, 16 * k, 16 * i, l), a);
+            for (int n = 0; n < NT; ++n) a = mma(kfrag(sr, LN, 16 * wp, 16 * n, l), kfrag(sb, LN, 16 * half, 16 * n, l), a);
+            a = masked(a, st.to[t]);
+            for (int k = half; k < Q / 16; ++k) a = mma(rfrag(sdy, LP, 16 * k, 16 * wp, l), rfrag(sm, LQ, 16 * k, 16 * half, l), a);
             const f32x4 yv = *(const f32x4*)(sdy + t * LP + p), xv = *(const f32x4*)(sx + t * LP + p);
             skip_sum += (yv[0] * xv[0] + yv[1] * xv[1]) + (yv[2] * xv[2] + yv[3] * xv[3]);
-            if (t < lu && p < at.pw) row_store<VEC>(dx + (int64_t)(tu + t) * yt + p, a * st.d[t] + skip * yv, at.pw - p);
+            if (t < len && p < at.pw) row_store<VEC>(dx + (t0 + t) * yt + p, a * st.d[t] + skip * yv, at.pw - p);
         }
-        float in = 0.0f;  // <R, S>, from the state before to the one behind
+        float pass = 0.0f;  // <R, S>, from the state before to the one behind
+        if (on) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const f32x4 v = *(const f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg);
-            in += (R[n][0] * v[0] + R[n][1] * v[1]) + (R[n][2] * v[2] + R[n][3] * v[3]);
+            for (int n = 0; n < TILES; ++n) {
+                const f32x4 v = *(const f32x4*)(ss + (16 * wp + lc) * LN + n_own + 16 * n + 4 * lg);
+                pass += (R[n][0] * v[0] + R[n][1] * v[1]) + (R[n][2] * v[2] + R[n][3] * v[3]);
+            }
         }
-        for (int o = 32; o; o >>= 1) in += __shfl_xor(in, o, 64);
-        if (l == 0) inner[w] = in;
-        walk<NT, false>(R, sc, LN, sdy, st, w, l);
+        for (int o = 32; o; o >>= 1) pass += __shfl_xor(pass, o, 64);
+        if (l == 0) inner[w] = pass;
+        if (on) walk<TILES, false>(R, sc + n_own, LN, sdy + 16 * wp, st, l);
         __syncthreads();
-        if (w == 3) {  // the gradients of the steps' decays and sizes, lane = step
+        if (w == 7) {  // the gradients of the steps' decays and sizes, lane = step
             const int t = l & (Q - 1);
             float h = 0.0f, k = 0.0f, q = 0.0f;
 #pragma unroll
@@ -655,7 +779,7 @@ __global__ __launch_bounds__(256, NP > 64 ? 1 : 2) void scan_backward_kernel(Sca
                 k += kb[n][t];
                 q += qb[n][t];
             }
-            const float d = st.d[t], dec = st.dec[t], sig = st.sig[t];
+            const float d = st.d[t];
             k *= d;
 #pragma unroll
             for (int o = 1; o < Q; o <<= 1) {  // steps from t on; steps up to t
@@ -668,70 +792,34 @@ __global__ __launch_bounds__(256, NP > 64 ? 1 : 2) void scan_backward_kernel(Sca
             if (t > 0) g += pairs[1][t];
             if (t > 0 && t < 16) g += pairs[0][t];
             if (t > 16) g += pairs[2][t];
-            if (eq == 0) g += ((inner[0] + inner[1]) + (inner[2] + inner[3])) * pow2(st.end_gi + st.end_gf);
-            if (l < lu) {
+            if (!st.starts) g += (((inner[0] + inner[1]) + (inner[2] + inner[3])) + ((inner[4] + inner[5]) + (inner[6] + inner[7]))) * st.all;
+            if (l < len) {
                 // log a = dec / LOG2E = -exp(a_log) d
-                const float dd = (q + g * (rate2 / LOG2E)) * sig;
-                decay_sum += g * (dec / LOG2E);
+                const float dd = (q + g * (in.rate2 / LOG2E)) * st.sig[t];
+                decay_sum += g * (st.dec[t] / LOG2E);
                 bias_sum += dd;
-                s.pdt[((int64_t)at.b * s.T + tu + t) * s.vh + at.v] = dd;
+                s.pdt[((int64_t)at.b * s.T + t0 + t) * s.vh + at.v] = dd;
             }
         }
-    };
-    if (c0 < c1) load((c1 - 1) * Q, length(c1 - 1));
-    for (int c = c1 - 1; c >= c0; --c) {
-        const int t0 = c * Q, len = length(c);
-        {
-            f32x4 S[NT];
-            load_state<NT, true>(S, chunk_s + c * chunk_step, NP, PW, NP, w, l);
-            __syncthreads();
-            stage(len);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) *(f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg) = S[n];
-        }
-        __syncthreads();
-        const bool single = flag != 0;
-        if (!single && c > c0) load(t0 - Q, Q);
-        for (int u = 0; u < (single ? len : 1); ++u) {
-            const int tu = single ? t0 + len - 1 - u : t0;
-            if (single) {  // the state before step tu, walked from the chunk's
-                f32x4 S[NT];
-                load_state<NT, true>(S, chunk_s + c * chunk_step, NP, PW, NP, w, l);
-                for (int i = t0; i < tu; ++i) {
-                    __syncthreads();
-                    load_in(i, 1);
-                    stage_in(1);
-                    __syncthreads();
-                    walk<NT, true>(S, sb, LN, sx, st, w, l);
-                }
-                __syncthreads();
-                load(tu, 1);
-                stage(1);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) *(f32x4*)(ss + (16 * w + lc) * LN + 16 * n + 4 * lg) = S[n];
-                __syncthreads();
-            }
-            back(tu, single ? 1 : len);
-        }
-        if (single) {
+        if (whole) {
             __syncthreads();
             if (tid == 0) flag = 0;
-            if (c > c0) load(t0 - Q, Q);
         }
     }
-    if (s.dstate && at.seg == 0) store_state<NT, VEC>(R, s.dstate + state0, s.N, at.pw, s.N, w, l);
+    if (on && s.dstate && at.seg == 0) store_state<TILES, VEC>(R, s.dstate + in.state, s.N, at.pw, s.N, 16 * wp, n_own, lane);
     for (int o = 32; o; o >>= 1) {
         skip_sum += __shfl_xor(skip_sum, o, 64);
         decay_sum += __shfl_xor(decay_sum, o, 64);
         bias_sum += __shfl_xor(bias_sum, o, 64);
     }
-    if (l == 0) red[w] = skip_sum;
     __syncthreads();
-    if (tid == 192) {
+    if (lane == 0) inner[w] = skip_sum;
+    __syncthreads();
+    if (tid == THREADS - 64) {
         float* o = s.ppar + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * 3;
         o[0] = decay_sum;
         o[1] = bias_sum;
-        o[2] = (red[0] + red[1]) + (red[2] + red[3]);
+        o[2] = ((inner[0] + inner[1]) + (inner[2] + inner[3])) + ((inner[4] + inner[5]) + (inner[6] + inner[7]));
     }
 }
 
@@ -964,10 +1052,10 @@ int gorila_scan(const gorila_scan_args* args, void* y, float* state_out, gorila_
         constexpr int NP = decltype(np)::value;
         constexpr bool VEC = decltype(al)::value;
         if (v.nseg > 1) {
-            state_kernel<T, NP, VEC, false><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+            state_kernel<T, NP, VEC, false><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
             join_kernel<NP, VEC><<<dim3((unsigned)(v.B * v.vh * (PW * NP / 256)), 1), 256, 0, c.stream>>>(v);
         }
-        scan_kernel<T, NP, VEC><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+        scan_kernel<T, NP, VEC><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
     });
     return launched();
 }
@@ -1009,11 +1097,11 @@ int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t d
         constexpr bool VEC = decltype(al)::value;
         if (blocks > 0) {
             if (v.nseg > 1) {
-                state_kernel<T, NP, VEC, false><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
-                state_kernel<T, NP, VEC, true><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+                state_kernel<T, NP, VEC, false><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
+                state_kernel<T, NP, VEC, true><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
                 join_kernel<NP, VEC><<<dim3((unsigned)(v.B * v.vh * (PW * NP / 256)), 2), 256, 0, c.stream>>>(v);
             }
-            scan_backward_kernel<T, NP, VEC><<<(unsigned)blocks, 256, 0, c.stream>>>(v);
+            scan_backward_kernel<T, NP, VEC><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
         }
         const int64_t per = ((int64_t)v.B * v.T * v.G * v.N + 255) / 256, heads = (v.H + 3) / 4;
         const unsigned gx = (unsigned)(per > 8192 ? 8192 : per);
