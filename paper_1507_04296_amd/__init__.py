@@ -156,8 +156,8 @@ class Context:
         import torch
         self.device = torch.device(device if device is not None else "cuda")
         self._raw_stream = torch._C._cuda_getCurrentRawStream
-        self._current_device = torch.cuda.current_device
-        self._bound = None  # the stream that the context has
+        index = self.device.index
+        self.index = torch.cuda.current_device() if index is None else index
         if max_batch == 0:  # a context without a workspace (gorila_act_noalloc)
             self.ws_bytes, self.workspace = 0, None
         else:
@@ -172,19 +172,18 @@ class Context:
             _check(lib().gorila_ctx_create(ctypes.byref(h), self._stream(), _ptr(self.workspace),
                                            self.ws_bytes), "gorila_ctx_create")
         self.handle = h
+        self.address = h.value  # for the native binding
 
     def _stream(self) -> int:
         """The handle of torch's current stream on the context's device.  Read
         from the native accessor: building a torch.cuda.Stream object for it
         took 3.2 of a call's 9.2 us of host time (replay insert), this 0.1."""
-        index = self.device.index
-        return self._raw_stream(self._current_device() if index is None else index)
+        return self._raw_stream(self.index)
 
     def bind_stream(self):
-        stream = self._stream()
-        if stream != self._bound or self.handle is None:
-            _check(lib().gorila_ctx_set_stream(self.handle, stream), "gorila_ctx_set_stream")
-            self._bound = stream
+        rc = lib().gorila_ctx_set_stream(self.handle, self._stream())
+        if rc != 0:
+            _check(rc, "gorila_ctx_set_stream")
         return self.handle
 
     def check(self) -> None:
@@ -211,7 +210,7 @@ class Context:
     def close(self):
         if getattr(self, "handle", None) is not None:
             lib().gorila_ctx_destroy(self.handle)
-            self.handle = None
+            self.handle, self.address = None, 0
 
     def __del__(self):
         try:

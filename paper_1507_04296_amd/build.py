@@ -1,4 +1,4 @@
-"""Build libgorila.so for gfx950 with hipcc (in-tree, no JIT cache)."""
+"""Build libgorila.so for gfx950 with hipcc and the native binding (in-tree, no JIT cache)."""
 from __future__ import annotations
 
 import os
@@ -23,6 +23,29 @@ FLAGS = [
 ]
 
 
+# The native half of the sequence operators' binding, against the installed torch.
+BINDING = os.path.join(HERE, "_binding.so")
+
+
+def _compile_binding() -> str:
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = BINDING + ".tmp%d" % os.getpid()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(root, "include"),
+           "-I" + os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           os.path.join(CSRC, "binding.cpp"), "-o", tmp,
+           "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for binding.cpp:\n{r.stderr}")
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD_DIR, os.path.splitext(src)[0] + ".o")
     cmd = [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
@@ -35,7 +58,9 @@ def _compile(src: str) -> str:
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     with ThreadPoolExecutor(max_workers=min(len(SOURCES), 8)) as ex:
+        binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, SOURCES))
+        binding.result()
     tmp = OUT + ".tmp%d" % os.getpid()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

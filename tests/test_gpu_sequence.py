@@ -517,6 +517,11 @@ def test_nothing_is_written_past_the_outputs(g, ctx):
         buf = torch.full((n + 128,), 7.0, dtype=dtype, device="cuda")
         return buf, buf[64:64 + n]
 
+    def scan_struct(i, state):
+        rows = [v for t in (i["x"], i["dt"], i["b"], i["c"]) for v in (t.data_ptr(), t.stride(0), t.stride(1))]
+        return sq._ScanArgs(0 if i["x"].dtype == F32 else 1, B, T, H, P, G, N, 0, *rows, i["a_log"].data_ptr(), i["dt_bias"].data_ptr(),
+                            i["skip"].data_ptr(), None, None if state is None else state.data_ptr())
+
     def check(bufs):
         for buf, mid in bufs:
             n = mid.numel()
@@ -526,17 +531,17 @@ def test_nothing_is_written_past_the_outputs(g, ctx):
     B, T, H, P, G, N = 2, 37, 3, 13, 3, 9
     for dtype in (F32, BF16):
         i = scan_inputs(B, T, H, P, G, N, dtype)
-        a = sq._scan_args(ctx, *i.values(), None, None)
+        a = scan_struct(i, None)
         out = [room(B * T * H * P, dtype), room(B * H * P * N)]
         assert L.gorila_scan(a, *(m.data_ptr() for _, m in out), ctx.bind_stream()) == 0
         check(out)
         dy, st = rand(B, T, H, P, dtype=dtype, seed=9), rand(B, H, P, N, seed=8)
-        a = sq._scan_args(ctx, *i.values(), None, st)
+        a = scan_struct(i, st)
         out = [room(i[k].numel(), dtype if n < 4 else F32) for n, k in enumerate(i)] + [room(st.numel())]
         assert L.gorila_scan_backward(a, dy.data_ptr(), dy.stride(0), dy.stride(1), None, *(m.data_ptr() for _, m in out), ctx.bind_stream()) == 0
         check(out)
         x, w, b, win = rand(B, T, 11, dtype=dtype, seed=1), rand(11, 4, seed=2), rand(11, seed=3), rand(B, 3, 11, dtype=dtype, seed=4)
-        a = sq._conv_args(ctx, x, w, b, None, win, True)
+        a = sq._ConvArgs(0 if dtype == F32 else 1, B, T, 11, 4, 1, x.data_ptr(), *x.stride()[:2], w.data_ptr(), b.data_ptr(), None, win.data_ptr())
         out = [room(x.numel(), dtype), room(win.numel(), dtype)]
         assert L.gorila_causal_conv(a, *(m.data_ptr() for _, m in out), ctx.bind_stream()) == 0
         check(out)
