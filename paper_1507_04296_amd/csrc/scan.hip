@@ -152,6 +152,7 @@ struct Steps {
     int ep[Q];             // -1: past the end
     float all;             // from the state before to the one behind
     int starts;            // an episode starts in it
+    int odd;               // a step size is not finite
 };
 struct GradSteps : Steps {
     float sig[Q], dec[Q];  // d step size / d dt, own log2-decay
@@ -169,7 +170,7 @@ struct StepRegs {
     }
     // By the lanes of one wave (lanes past Q take part and store nothing).
     template <class S>
-    __device__ __forceinline__ void store(S& s, float bias, float rate2, int len, int l, float& bad) const {
+    __device__ __forceinline__ void store(S& s, float bias, float rate2, int len, int l) const {
         const float v = dt + bias;
         const float e = expf(-fabsf(v));
         float d = fmaxf(v, 0.0f) + log1pf(e);
@@ -205,14 +206,25 @@ struct StepRegs {
                 s.dec[l] = dec;
                 s.sig[l] = in ? (v >= 0.0f ? 1.0f : e) / (1.0f + e) : 0.0f;
             }
-            bad += d * 0.0f;
         }
+        const bool odd = __any(l < Q && d * 0.0f != 0.0f);
         if (l == 0) {
+            s.odd = odd;
             s.all = end_ep == 0 ? pow2(end_gi + end_gf) : 0.0f;
             s.starts = end_ep != 0;
         }
     }
 };
+// Sum over 16 lanes (all of them get it).
+__device__ __forceinline__ float sum16(float v) {
+    auto with = [&](auto ctrl) { v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
+    with(std::integral_constant<int, 0xb1>{});   // lanes swapped in pairs
+    with(std::integral_constant<int, 0x4e>{});   // pairs in fours
+    with(std::integral_constant<int, 0x141>{});  // eight mirrored
+    with(std::integral_constant<int, 0x140>{});  // sixteen mirrored
+    return v;
+}
+
 // v times a factor of a Steps, where a zero one is a mask whatever v is.
 __device__ __forceinline__ f32x4 masked(f32x4 v, float f) { return f != 0.0f ? v * f : f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 
@@ -372,11 +384,23 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
         rx.store(sx, LP, bad);
         rb.store(sb, LN, bad);
         rc.store(sc, LN, bad);
-        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l, bad);
         if (on) stage_state<TILES>(S, ss, LN, 16 * wp, n_own, l);
         if (bad != bad) flag = 1;
         __syncthreads();
-        if (at_t.single < 0 && flag) {
+        // What needs no decays, beside the decays (a long chain of a few lanes): what the
+        // state gives 16 steps (rows = channels, columns = steps), c_t . b_s of the three
+        // tiles with s <= t.
+        const int t = 16 * half + lc, si = w >> 1, ti = w > 0;
+        f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f}, m = acc;
+        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc = mma(kfrag(ss, LN, 16 * wp, 16 * n, l), kfrag(sc, LN, 16 * half, 16 * n, l), acc);
+        if (w < 3) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
+        }
+        __syncthreads();
+        if (at_t.single < 0 && (flag || st.odd)) {
             at_t.split();
             load();
             continue;
@@ -385,17 +409,8 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
         bool whole;
         more = at_t.next(whole);
         if (more) load();
-        // what the state gives 16 steps: rows = channels, columns = steps
-        const int t = 16 * half + lc;
-        f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc = mma(kfrag(ss, LN, 16 * wp, 16 * n, l), kfrag(sc, LN, 16 * half, 16 * n, l), acc);
         acc = masked(acc, st.from[t]);
-        if (w < 3) {  // decay * (c_t . b_s) * d_s of one of the three tiles with s <= t
-            const int si = w >> 1, ti = w > 0;
-            f32x4 m{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
+        if (w < 3) {  // decay * (c_t . b_s) * d_s
             const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
             const float gi_t = st.gi[tm], gf_t = st.gf[tm];
             const int et = st.ep[tm];
@@ -408,15 +423,12 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
             }
             *(f32x4*)(sm + tm * LQ + q0) = m;
         }
+        if (on) walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, l);
         __syncthreads();
         for (int k = 0; k <= half; ++k) acc = mma(rfrag(sx, LP, 16 * k, 16 * wp, l), kfrag(sm, LQ, 16 * half, 16 * k, l), acc);
         const int p = 16 * wp + 4 * lg;
         if (t < len && p < at.pw) row_store<VEC>(y + t0 * yt, acc + skip * *(const f32x4*)(sx + t * LP + p), at.pw - p);
-        if (on) walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, l);
-        if (whole) {
-            __syncthreads();
-            if (tid == 0) flag = 0;
-        }
+        if (whole && tid == 0) flag = 0;  // nobody reads it before the next chunk is staged
     }
     if (on && s.state_out && at.seg == s.nseg - 1) store_state<TILES, VEC>(S, s.state_out + in.state, s.N, at.pw, s.N, 16 * wp, n_own, l);
 }
@@ -424,11 +436,8 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
 // What one segment adds to the state behind it (REV = false: from x and b) or to
 // the gradient of the state before it (REV = true: from dy and c), and its decay.
 template <class T, int NP, bool VEC, bool REV>
-__global__ __launch_bounds__(THREADS, 4) void state_kernel(ScanView s) {
+__device__ __forceinline__ void segment_state(const ScanView& s, float* sb, float* sx, Steps* st, int& flag) {
     constexpr int NT = NP / 16, LN = NP + 4, TILES = Half<NT>::TILES;
-    __shared__ __align__(16) float sb[Q * LN], sx[Q * LP];
-    __shared__ __align__(16) Steps st;
-    __shared__ int flag;
     const Place at(s, blockIdx.x);
     const Data<T> in(s, at);
     const int tid = threadIdx.x, l = tid & 63;
@@ -450,27 +459,37 @@ __global__ __launch_bounds__(THREADS, 4) void state_kernel(ScanView s) {
         rb.load(at_t.t * bt, at_t.len);
         if (w == 7) rd.load(in.dt, s.dtt, in.reset, at_t.t, at_t.len, l);
     };
+    // Where nothing stops it, wave 7 forms the decays of the next chunk beside the walk
+    // of this one (st[turn ^ 1]).
+    int turn = 0;
+    auto steps = [&](int to) { rd.store(st[to], in.bias, in.rate2, at_t.len, l); };
     bool more = REV ? at_t.start_back() : at_t.start();
-    if (more) load();
+    if (more) {
+        load();
+        if (w == 7) steps(0);
+    }
     while (more) {
         __syncthreads();
         float bad = 0.0f;
         rx.store(sx, LP, bad);
         rb.store(sb, LN, bad);
-        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l, bad);
         if (bad != bad) flag = 1;
         __syncthreads();
-        if (at_t.single < 0 && flag) {
+        if (at_t.single < 0 && (flag || st[turn].odd)) {
             REV ? at_t.split_back() : at_t.split();
             load();
+            __syncthreads();  // everyone has read st[turn]
+            if (w == 7) steps(turn);
             continue;
         }
         bool whole;
         more = REV ? at_t.next_back(whole) : at_t.next(whole);
         if (more) load();
-        decay *= st.all;
-        starts |= st.starts != 0;
-        if (on) walk<TILES, !REV>(S, sb + n_own, LN, sx + 16 * wp, st, l);
+        decay *= st[turn].all;
+        starts |= st[turn].starts != 0;
+        if (on) walk<TILES, !REV>(S, sb + n_own, LN, sx + 16 * wp, st[turn], l);
+        if (more && w == 7) steps(turn ^ 1);
+        turn ^= 1;
         if (whole) {
             __syncthreads();
             if (tid == 0) flag = 0;
@@ -479,6 +498,15 @@ __global__ __launch_bounds__(THREADS, 4) void state_kernel(ScanView s) {
     const int64_t o = ((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v;
     if (on) store_state<TILES, true>(S, (REV ? s.seg_r : s.seg_s) + o * PW * NP, NP, PW, NP, 16 * wp, n_own, l);
     if (!REV && tid == 0) s.seg_a[o] = starts ? -1.0f : decay;
+}
+
+template <class T, int NP, bool VEC>
+__global__ __launch_bounds__(THREADS, 4) void state_kernel(ScanView s) {
+    __shared__ __align__(16) float sb[Q * (NP + 4)], sx[Q * LP];
+    __shared__ __align__(16) Steps st[2];
+    __shared__ int flag;
+    if (blockIdx.y == 0) segment_state<T, NP, VEC, false>(s, sb, sx, st, flag);
+    else segment_state<T, NP, VEC, true>(s, sb, sx, st, flag);
 }
 
 // Turns what each segment adds into the state before it (blockIdx.y = 0) or the
@@ -493,11 +521,20 @@ __global__ __launch_bounds__(256) void join_kernel(ScanView s) {
     const float* dec = s.seg_a + (int64_t)b * s.nseg * s.vh + v;
     const int64_t step = (int64_t)s.vh * PW * NP;
     float cur = from && p < s.P && n < s.N ? from[(((int64_t)b * s.H + h) * s.P + p) * s.N + n] : 0.0f;
-    for (int i = 0; i < s.nseg; ++i) {
-        const int k = rev ? s.nseg - 1 - i : i;
-        const float own = seg[k * step], a = dec[k * s.vh];
-        seg[k * step] = cur;
-        cur = a < 0.0f ? own : a * cur + own;
+    constexpr int AHEAD = 8;  // loads in flight
+    for (int i0 = 0; i0 < s.nseg; i0 += AHEAD) {
+        float own[AHEAD], a[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int at = i0 + i < s.nseg ? i0 + i : s.nseg - 1, k = rev ? s.nseg - 1 - at : at;
+            own[i] = seg[k * step], a[i] = dec[k * s.vh];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (i0 + i >= s.nseg) break;
+            seg[(rev ? s.nseg - 1 - i0 - i : i0 + i) * step] = cur;
+            cur = a[i] < 0.0f ? own[i] : a[i] * cur + own[i];
+        }
     }
 }
 
@@ -560,9 +597,9 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         float bad = 0.0f;
         rx.store(sx, LP, bad);
         rb.store(sb, LN, bad);
-        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l, bad);
         if (bad != bad) flag = 1;
     };
+    auto steps = [&](GradSteps& to, int l) { rd.store(to, in.bias, in.rate2, at_t.len, l); };
     auto plain_walk = [&](f32x4 (&S)[TILES], int t0, int t1) {
         const int lc = lane & 15, lg = lane >> 4;
         Tiles<TILES> v;
@@ -579,8 +616,13 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
             load_state<TILES, true>(S, s.seg_s + seg0, NP, PW, NP, 16 * wp, n_own, lane);
         else
             load_state<TILES, VEC>(S, s.state ? s.state + in.state : nullptr, s.N, at.pw, s.N, 16 * wp, n_own, lane);
+        // Wave 7 forms the decays of the next chunk beside the walk of this one; every
+        // other chunk's stand in sf, which is not in use yet.
+        static_assert(sizeof(GradSteps) <= sizeof sf, "a place for the steps");
         if (at_t.start()) {
             load_in();
+            if (w == 7 && at_t.len < at_t.end - at_t.t) steps(st, opaque(lane));
+            GradSteps *now = &st, *next = (GradSteps*)sf;
             for (;;) {
                 const int t0 = at_t.t, len = at_t.len;
                 if (on) store_state<TILES, true>(S, chunk_s + t0 / Q * chunk_step, NP, PW, NP, 16 * wp, n_own, lane);
@@ -589,7 +631,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                 __syncthreads();
                 stage_in(opaque(lane));
                 __syncthreads();
-                const bool plain = flag != 0;
+                const bool plain = flag != 0 || now->odd;
                 at_t.next(whole);
                 load_in();
                 if (plain) {
@@ -597,8 +639,12 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                     __syncthreads();
                     if (tid == 0) flag = 0;
                 } else if (on) {
-                    walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, opaque(lane));
+                    walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, *now, opaque(lane));
                 }
+                if (w == 7 && at_t.len < at_t.end - at_t.t) steps(*next, opaque(lane));
+                GradSteps* const other = now;
+                now = next;
+                next = other;
             }
         }
         if (s.nseg > 1)
@@ -641,7 +687,22 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         }
         if (bad != bad) flag = 1;
         __syncthreads();
-        if (at_t.single < 0 && flag) {
+        // What needs no decays, beside the decays: the tiles with s <= t of c_t . b_s
+        // (waves 0 .. 2) and dy_t . x_s (3 .. 5); rows = s, columns = t.
+        const int tile = w < 3 ? w : w - 3, si = tile >> 1, ti = tile > 0;
+        const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
+        f32x4 f{0.0f, 0.0f, 0.0f, 0.0f};
+        if (w < 3) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) f = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), f);
+        } else if (w < 6) {
+#pragma unroll
+            for (int n = 0; n < PW / 16; ++n) f = mma(kfrag(sx, LP, 16 * si, 16 * n, l), kfrag(sdy, LP, 16 * ti, 16 * n, l), f);
+        } else if (w == 7) {
+            steps(st, l);
+        }
+        __syncthreads();
+        if (at_t.single < 0 && (flag || st.odd)) {
             at_t.split_back();
             load();
             continue;
@@ -650,18 +711,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         bool whole;
         more = at_t.next_back(whole);
         if (more) load();
-        // the tiles with s <= t of M (waves 0 .. 2) and F (3 .. 5): rows = s, columns = t
-        const int tile = w < 3 ? w : w - 3, si = tile >> 1, ti = tile > 0;
-        const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
-        f32x4 f{0.0f, 0.0f, 0.0f, 0.0f};
-        if (w < 6) {
-            if (w < 3) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) f = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), f);
-            } else {
-#pragma unroll
-                for (int n = 0; n < PW / 16; ++n) f = mma(kfrag(sx, LP, 16 * si, 16 * n, l), kfrag(sdy, LP, 16 * ti, 16 * n, l), f);
-            }
+        if (w < 6) {  // M and F
             const float gi_t = st.gi[tm], gf_t = st.gf[tm];
             const int et = st.ep[tm];
             const f32x4 gi = *(const f32x4*)(st.gi + q0), gf = *(const f32x4*)(st.gf + q0);
@@ -674,6 +724,27 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
             }
             *(f32x4*)((w < 3 ? sm : sf) + tm * LQ + q0) = g;
         }
+        // What the states around the chunk give dc and db (rows = state, columns =
+        // steps) and dx (rows = channels), meanwhile.
+        constexpr int JOBS = (2 * NT + 7) / 8;
+        f32x4 ja[JOBS], jq[JOBS], xa{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < JOBS; ++u) {
+            const int job = w + 8 * u, n = job >> 1, i = job & 1;
+            f32x4 a{0.0f, 0.0f, 0.0f, 0.0f}, q = a;
+            if (job < 2 * NT) {
+#pragma unroll
+                for (int k = 0; k < PW / 16; ++k) {
+                    a = mma(rfrag(ss, LN, 16 * k, 16 * n, l), kfrag(sdy, LP, 16 * i, 16 * k, l), a);
+                    q = mma(rfrag(sr, LN, 16 * k, 16 * n, l), kfrag(sx, LP, 16 * i, 16 * k, l), q);
+                }
+            }
+            ja[u] = masked(a, st.from[16 * i + lc]);
+            jq[u] = masked(q, st.to[16 * i + lc]);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) xa = mma(kfrag(sr, LN, 16 * wp, 16 * n, l), kfrag(sb, LN, 16 * half, 16 * n, l), xa);
+        xa = masked(xa, st.to[16 * half + lc]);
         __syncthreads();
         if (w >= 3 && w < 6) {  // what passes from s to t: M F d without F's decay, summed for every step between
             const f32x4 v = *(const f32x4*)(sm + tm * LQ + q0) * f * *(const f32x4*)(st.d + q0);
@@ -690,15 +761,13 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                 // step q0 + j + 1 of this half: sum over t from it on
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float u = tm > q0 + j ? pre[j] : 0.0f;
-                    for (int o = 8; o; o >>= 1) u += __shfl_xor(u, o, 64);
+                    const float u = sum16(tm > q0 + j ? pre[j] : 0.0f);
                     if (lc == 0 && (q0 + j + 1) % 16) pairs[2 * si][q0 + j + 1] = u;
                 }
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {  // every t is behind step q0 + j + 1
-                    float u = pre[j];
-                    for (int o = 8; o; o >>= 1) u += __shfl_xor(u, o, 64);
+                    const float u = sum16(pre[j]);
                     if (lc == 0) pairs[1][q0 + j + 1] = u;
                 }
                 float u = __shfl(pre[3], 48 + lc, 64);  // all s, and t from a step of the second half on
@@ -709,17 +778,11 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                 if (lg == 0 && lc > 0) pairs[1][tm] = u;
             }
         }
-        // dc and db: rows = state, columns = steps
-        for (int job = w; job < 2 * NT; job += 8) {
-            const int n = job >> 1, i = job & 1, t = 16 * i + lc, n0 = 16 * n + 4 * lg;
-            f32x4 a{0.0f, 0.0f, 0.0f, 0.0f}, q = a;
 #pragma unroll
-            for (int k = 0; k < PW / 16; ++k) {
-                a = mma(rfrag(ss, LN, 16 * k, 16 * n, l), kfrag(sdy, LP, 16 * i, 16 * k, l), a);
-                q = mma(rfrag(sr, LN, 16 * k, 16 * n, l), kfrag(sx, LP, 16 * i, 16 * k, l), q);
-            }
-            a = masked(a, st.from[t]);
-            q = masked(q, st.to[t]);
+        for (int u = 0; u < JOBS; ++u) {
+            const int job = w + 8 * u, n = job >> 1, i = job & 1, t = 16 * i + lc, n0 = 16 * n + 4 * lg;
+            if (job >= 2 * NT) break;
+            f32x4 a = ja[u], q = jq[u];
             const f32x4 cv = *(const f32x4*)(sc + t * LN + n0), bv = *(const f32x4*)(sb + t * LN + n0);
             float h = (a[0] * cv[0] + a[1] * cv[1]) + (a[2] * cv[2] + a[3] * cv[3]);
             float kv = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
@@ -747,16 +810,12 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                 row_store<VEC>(s.pdb + o, q * st.d[t], s.N - n0);
             }
         }
-        {  // dx: rows = channels, columns = steps
+        {  // dx
             const int t = 16 * half + lc, p = 16 * wp + 4 * lg;
-            f32x4 a{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int n = 0; n < NT; ++n) a = mma(kfrag(sr, LN, 16 * wp, 16 * n, l), kfrag(sb, LN, 16 * half, 16 * n, l), a);
-            a = masked(a, st.to[t]);
-            for (int k = half; k < Q / 16; ++k) a = mma(rfrag(sdy, LP, 16 * k, 16 * wp, l), rfrag(sm, LQ, 16 * k, 16 * half, l), a);
+            for (int k = half; k < Q / 16; ++k) xa = mma(rfrag(sdy, LP, 16 * k, 16 * wp, l), rfrag(sm, LQ, 16 * k, 16 * half, l), xa);
             const f32x4 yv = *(const f32x4*)(sdy + t * LP + p), xv = *(const f32x4*)(sx + t * LP + p);
             skip_sum += (yv[0] * xv[0] + yv[1] * xv[1]) + (yv[2] * xv[2] + yv[3] * xv[3]);
-            if (t < len && p < at.pw) row_store<VEC>(dx + (t0 + t) * yt + p, a * st.d[t] + skip * yv, at.pw - p);
+            if (t < len && p < at.pw) row_store<VEC>(dx + (t0 + t) * yt + p, xa * st.d[t] + skip * yv, at.pw - p);
         }
         float pass = 0.0f;  // <R, S>, from the state before to the one behind
         if (on) {
@@ -1052,7 +1111,7 @@ int gorila_scan(const gorila_scan_args* args, void* y, float* state_out, gorila_
         constexpr int NP = decltype(np)::value;
         constexpr bool VEC = decltype(al)::value;
         if (v.nseg > 1) {
-            state_kernel<T, NP, VEC, false><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
+            state_kernel<T, NP, VEC><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
             join_kernel<NP, VEC><<<dim3((unsigned)(v.B * v.vh * (PW * NP / 256)), 1), 256, 0, c.stream>>>(v);
         }
         scan_kernel<T, NP, VEC><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
@@ -1097,8 +1156,7 @@ int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t d
         constexpr bool VEC = decltype(al)::value;
         if (blocks > 0) {
             if (v.nseg > 1) {
-                state_kernel<T, NP, VEC, false><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
-                state_kernel<T, NP, VEC, true><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
+                state_kernel<T, NP, VEC><<<dim3((unsigned)blocks, 2), THREADS, 0, c.stream>>>(v);
                 join_kernel<NP, VEC><<<dim3((unsigned)(v.B * v.vh * (PW * NP / 256)), 2), 256, 0, c.stream>>>(v);
             }
             scan_backward_kernel<T, NP, VEC><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
