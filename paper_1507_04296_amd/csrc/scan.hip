@@ -93,6 +93,86 @@ __device__ __forceinline__ f32x4 rfrag(const float* s, int ld, int k0, int col0,
     return f32x4{p[0], p[ld], p[2 * ld], p[3 * ld]};
 }
 
+// bf16 rows: their values are operands of the bf16 instruction as they are, 16 times
+// as fast as the fp32 one.  What is formed from them (states, decayed products) enters
+// as three bf16 terms, which hold an fp32 value; where only bf16 outputs come of it, as
+// two in one LDS word (16 bits, 2^-17 relative, against the outputs' 2^-9).  Two terms
+// throughout took the backward of 4 x 1999 steps, 128 states, from 244 to 229 us, and
+// the parameters' gradients from 2e-7 to 3e-6.  fp32 rows take the fp32 instruction:
+// three terms of both operands would cost the vector unit what the matrix unit saves.
+enum Operand { ROWS, WORDS, FP32 };  // rows' values; words of two terms; fp32 values
+template <class T> __device__ __forceinline__ float word(float v) { return v; }
+template <> __device__ __forceinline__ float word<uint16_t>(float v) {
+    const uint32_t hi = row_round<uint16_t>(v);
+    return __uint_as_float(hi << 16 | row_round<uint16_t>(v - __uint_as_float(hi << 16)));
+}
+template <class T> __device__ __forceinline__ f32x4 words(f32x4 v) { return f32x4{word<T>(v[0]), word<T>(v[1]), word<T>(v[2]), word<T>(v[3])}; }
+// Halves of eight words.
+__device__ __forceinline__ bf16x8 halves(f32x4 a, f32x4 b, uint32_t sel) {
+    uint4 o;
+    o.x = __builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), sel);
+    o.y = __builtin_amdgcn_perm(__float_as_uint(a[3]), __float_as_uint(a[2]), sel);
+    o.z = __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), sel);
+    o.w = __builtin_amdgcn_perm(__float_as_uint(b[3]), __float_as_uint(b[2]), sel);
+    return __builtin_bit_cast(bf16x8, o);
+}
+template <int KIND> struct Terms {
+    static constexpr int N = KIND == ROWS ? 1 : KIND == WORDS ? 2 : 3;
+    bf16x8 t[N];
+    __device__ __forceinline__ Terms(f32x4 a, f32x4 b) {
+        if constexpr (KIND == FP32) {
+            bf16x4 p[N], q[N];
+            split4<N>(a, p);
+            split4<N>(b, q);
+#pragma unroll
+            for (int i = 0; i < N; ++i) t[i] = __builtin_shufflevector(p[i], q[i], 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            t[0] = halves(a, b, 0x07060302u);
+            if constexpr (KIND == WORDS) t[1] = halves(a, b, 0x05040100u);
+        }
+    }
+};
+// c + two blocks of 16 reduction indices of a (rows' values) and b, and one block.
+template <class T, int KIND>
+__device__ __forceinline__ f32x4 mul2(f32x4 a0, f32x4 a1, f32x4 b0, f32x4 b1, f32x4 c) {
+    if constexpr (std::is_same<T, float>::value) return mma(a1, b1, mma(a0, b0, c));
+    else {
+        const Terms<ROWS> a(a0, a1);
+        const Terms<KIND> b(b0, b1);
+#pragma unroll
+        for (int i = Terms<KIND>::N - 1; i >= 0; --i) c = mfma16(a.t[0], b.t[i], c);
+        return c;
+    }
+}
+template <class T, int KIND>
+__device__ __forceinline__ f32x4 mul2_swapped(f32x4 a0, f32x4 a1, f32x4 b0, f32x4 b1, f32x4 c) {  // b holds the rows' values
+    if constexpr (std::is_same<T, float>::value) return mma(a1, b1, mma(a0, b0, c));
+    else {
+        const Terms<KIND> a(a0, a1);
+        const Terms<ROWS> b(b0, b1);
+#pragma unroll
+        for (int i = Terms<KIND>::N - 1; i >= 0; --i) c = mfma16(a.t[i], b.t[0], c);
+        return c;
+    }
+}
+template <class T, int KIND>
+__device__ __forceinline__ f32x4 mul1(f32x4 a, f32x4 b, f32x4 c) {
+    if constexpr (std::is_same<T, float>::value) return mma(a, b, c);
+    else return mul2<T, KIND>(a, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, b, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, c);
+}
+// Products over N blocks of 16, fa(i) and fb(i) the operands' blocks.
+template <class T, int KIND, int N, bool SWAPPED = false, class A, class B>
+__device__ __forceinline__ f32x4 product(A&& fa, B&& fb, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (N == 1 && std::is_same<T, float>::value) c = mma(fa(i), fb(i), c);
+        else if constexpr (SWAPPED) c = mul2_swapped<T, KIND>(fa(i), N > 1 ? fa(i + 1) : zero, fb(i), N > 1 ? fb(i + 1) : zero, c);
+        else c = mul2<T, KIND>(fa(i), N > 1 ? fa(i + 1) : zero, fb(i), N > 1 ? fb(i + 1) : zero, c);
+    }
+    return c;
+}
+
 // Q rows of COLS columns on their way from memory to LDS, as they are in memory; rows
 // past len and columns past cols are zeros.
 template <class T, bool VEC> struct Quad {
@@ -239,20 +319,22 @@ template <int NT> struct Half {
 // over steps of weight * m[step][state] * ch[step][channel].  AFTER: the state after
 // the chunk from the one before (weights w_s d_s); else the gradient before it from
 // the one after (weights e^G).
-template <int TILES, bool AFTER>
+template <class T, int TILES, bool AFTER>
 __device__ __forceinline__ void walk(f32x4 (&acc)[TILES], const float* m, int ldm, const float* ch, const Steps& st, int l) {
     const float all = st.all;
 #pragma unroll
     for (int n = 0; n < TILES; ++n) acc[n] = masked(acc[n], all);
     if (!AFTER && st.ep[0] != 0) return;  // an episode starts with the chunk
+    f32x4 v[Q / 16];
 #pragma unroll
     for (int kb = 0; kb < Q / 16; ++kb) {
         const int k0 = 16 * kb + 4 * (l >> 4);
-        f32x4 v = rfrag(ch, LP, 16 * kb, 0, l);
-        v *= AFTER ? *(const f32x4*)(st.to + k0) * *(const f32x4*)(st.d + k0) : *(const f32x4*)(st.from + k0);
-#pragma unroll
-        for (int n = 0; n < TILES; ++n) acc[n] = mma(rfrag(m, ldm, 16 * kb, 16 * n, l), v, acc[n]);
+        v[kb] = rfrag(ch, LP, 16 * kb, 0, l);
+        v[kb] *= AFTER ? *(const f32x4*)(st.to + k0) * *(const f32x4*)(st.d + k0) : *(const f32x4*)(st.from + k0);
     }
+#pragma unroll
+    for (int n = 0; n < TILES; ++n)
+        acc[n] = mul2<T, FP32>(rfrag(m, ldm, 0, 16 * n, l), rfrag(m, ldm, 16, 16 * n, l), v[0], v[1], acc[n]);
 }
 
 // Registers <-> state arrays [channel][state] of `ld` states a channel in memory, the
@@ -277,10 +359,10 @@ __device__ __forceinline__ void store_state(const f32x4 (&acc)[TILES], float* s,
     }
 }
 // To LDS [channel][state].
-template <int TILES>
+template <class T, int TILES>
 __device__ __forceinline__ void stage_state(const f32x4 (&acc)[TILES], float* s, int ld, int p0, int n0, int l) {
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) *(f32x4*)(s + (p0 + (l & 15)) * ld + n0 + 16 * i + 4 * (l >> 4)) = acc[i];
+    for (int i = 0; i < TILES; ++i) *(f32x4*)(s + (p0 + (l & 15)) * ld + n0 + 16 * i + 4 * (l >> 4)) = words<T>(acc[i]);
 }
 
 template <class T>
@@ -384,7 +466,7 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
         rx.store(sx, LP, bad);
         rb.store(sb, LN, bad);
         rc.store(sc, LN, bad);
-        if (on) stage_state<TILES>(S, ss, LN, 16 * wp, n_own, l);
+        if (on) stage_state<T, TILES>(S, ss, LN, 16 * wp, n_own, l);
         if (bad != bad) flag = 1;
         __syncthreads();
         // What needs no decays, beside the decays (a long chain of a few lanes): what the
@@ -393,12 +475,11 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
         const int t = 16 * half + lc, si = w >> 1, ti = w > 0;
         f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f}, m = acc;
         if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc = mma(kfrag(ss, LN, 16 * wp, 16 * n, l), kfrag(sc, LN, 16 * half, 16 * n, l), acc);
-        if (w < 3) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) m = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), m);
-        }
+        acc = product<T, WORDS, NT, true>([&](int n) { return kfrag(ss, LN, 16 * wp, 16 * n, l); },
+                                          [&](int n) { return kfrag(sc, LN, 16 * half, 16 * n, l); }, acc);
+        if (w < 3)
+            m = product<T, ROWS, NT>([&](int n) { return kfrag(sb, LN, 16 * si, 16 * n, l); },
+                                     [&](int n) { return kfrag(sc, LN, 16 * ti, 16 * n, l); }, m);
         __syncthreads();
         if (at_t.single < 0 && (flag || st.odd)) {
             at_t.split();
@@ -421,11 +502,14 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
                 const bool same = tm == q0 + j, behind = tm > q0 + j && ep[j] == et;
                 m[j] = same ? m[j] * d[j] : behind ? m[j] * (pow2((gi_t - gi[j]) + (gf_t - gf[j])) * d[j]) : 0.0f;
             }
-            *(f32x4*)(sm + tm * LQ + q0) = m;
+            *(f32x4*)(sm + tm * LQ + q0) = words<T>(m);
         }
-        if (on) walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, l);
+        if (on) walk<T, TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, l);
         __syncthreads();
-        for (int k = 0; k <= half; ++k) acc = mma(rfrag(sx, LP, 16 * k, 16 * wp, l), kfrag(sm, LQ, 16 * half, 16 * k, l), acc);
+        if (half)
+            acc = mul2<T, WORDS>(rfrag(sx, LP, 0, 16 * wp, l), rfrag(sx, LP, 16, 16 * wp, l), kfrag(sm, LQ, 16, 0, l), kfrag(sm, LQ, 16, 16, l), acc);
+        else
+            acc = mul1<T, WORDS>(rfrag(sx, LP, 0, 16 * wp, l), kfrag(sm, LQ, 0, 0, l), acc);
         const int p = 16 * wp + 4 * lg;
         if (t < len && p < at.pw) row_store<VEC>(y + t0 * yt, acc + skip * *(const f32x4*)(sx + t * LP + p), at.pw - p);
         if (whole && tid == 0) flag = 0;  // nobody reads it before the next chunk is staged
@@ -487,7 +571,7 @@ __device__ __forceinline__ void segment_state(const ScanView& s, float* sb, floa
         if (more) load();
         decay *= st[turn].all;
         starts |= st[turn].starts != 0;
-        if (on) walk<TILES, !REV>(S, sb + n_own, LN, sx + 16 * wp, st[turn], l);
+        if (on) walk<T, TILES, !REV>(S, sb + n_own, LN, sx + 16 * wp, st[turn], l);
         if (more && w == 7) steps(turn ^ 1);
         turn ^= 1;
         if (whole) {
@@ -639,7 +723,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                     __syncthreads();
                     if (tid == 0) flag = 0;
                 } else if (on) {
-                    walk<TILES, true>(S, sb + n_own, LN, sx + 16 * wp, *now, opaque(lane));
+                    walk<T, TILES, true>(S, sb + n_own, LN, sx + 16 * wp, *now, opaque(lane));
                 }
                 if (w == 7 && at_t.len < at_t.end - at_t.t) steps(*next, opaque(lane));
                 GradSteps* const other = now;
@@ -682,8 +766,8 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         ry.store(sdy, LP, bad);
         rc.store(sc, LN, bad);
         if (on) {
-            stage_state<TILES>(R, sr, LN, 16 * wp, n_own, l);
-            stage_state<TILES>(S, ss, LN, 16 * wp, n_own, l);
+            stage_state<float, TILES>(R, sr, LN, 16 * wp, n_own, l);
+            stage_state<float, TILES>(S, ss, LN, 16 * wp, n_own, l);
         }
         if (bad != bad) flag = 1;
         __syncthreads();
@@ -693,11 +777,11 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
         f32x4 f{0.0f, 0.0f, 0.0f, 0.0f};
         if (w < 3) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) f = mma(kfrag(sb, LN, 16 * si, 16 * n, l), kfrag(sc, LN, 16 * ti, 16 * n, l), f);
+            f = product<T, ROWS, NT>([&](int n) { return kfrag(sb, LN, 16 * si, 16 * n, l); },
+                                     [&](int n) { return kfrag(sc, LN, 16 * ti, 16 * n, l); }, f);
         } else if (w < 6) {
-#pragma unroll
-            for (int n = 0; n < PW / 16; ++n) f = mma(kfrag(sx, LP, 16 * si, 16 * n, l), kfrag(sdy, LP, 16 * ti, 16 * n, l), f);
+            f = product<T, ROWS, PW / 16>([&](int n) { return kfrag(sx, LP, 16 * si, 16 * n, l); },
+                                          [&](int n) { return kfrag(sdy, LP, 16 * ti, 16 * n, l); }, f);
         } else if (w == 7) {
             steps(st, l);
         }
@@ -733,17 +817,16 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
             const int job = w + 8 * u, n = job >> 1, i = job & 1;
             f32x4 a{0.0f, 0.0f, 0.0f, 0.0f}, q = a;
             if (job < 2 * NT) {
-#pragma unroll
-                for (int k = 0; k < PW / 16; ++k) {
-                    a = mma(rfrag(ss, LN, 16 * k, 16 * n, l), kfrag(sdy, LP, 16 * i, 16 * k, l), a);
-                    q = mma(rfrag(sr, LN, 16 * k, 16 * n, l), kfrag(sx, LP, 16 * i, 16 * k, l), q);
-                }
+                a = product<T, FP32, PW / 16, true>([&](int k) { return rfrag(ss, LN, 16 * k, 16 * n, l); },
+                                                     [&](int k) { return kfrag(sdy, LP, 16 * i, 16 * k, l); }, a);
+                q = product<T, FP32, PW / 16, true>([&](int k) { return rfrag(sr, LN, 16 * k, 16 * n, l); },
+                                                     [&](int k) { return kfrag(sx, LP, 16 * i, 16 * k, l); }, q);
             }
             ja[u] = masked(a, st.from[16 * i + lc]);
             jq[u] = masked(q, st.to[16 * i + lc]);
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) xa = mma(kfrag(sr, LN, 16 * wp, 16 * n, l), kfrag(sb, LN, 16 * half, 16 * n, l), xa);
+        xa = product<T, FP32, NT, true>([&](int n) { return kfrag(sr, LN, 16 * wp, 16 * n, l); },
+                                         [&](int n) { return kfrag(sb, LN, 16 * half, 16 * n, l); }, xa);
         xa = masked(xa, st.to[16 * half + lc]);
         __syncthreads();
         if (w >= 3 && w < 6) {  // what passes from s to t: M F d without F's decay, summed for every step between
@@ -786,12 +869,15 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
             const f32x4 cv = *(const f32x4*)(sc + t * LN + n0), bv = *(const f32x4*)(sb + t * LN + n0);
             float h = (a[0] * cv[0] + a[1] * cv[1]) + (a[2] * cv[2] + a[3] * cv[3]);
             float kv = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
-            for (int k = 0; k <= i; ++k) {  // steps up to this one
-                const f32x4 fd = kfrag(sf, LQ, 16 * i, 16 * k, l) * *(const f32x4*)(st.d + 16 * k + 4 * lg);
-                a = mma(rfrag(sb, LN, 16 * k, 16 * n, l), fd, a);
+            auto fd = [&](int k) { return kfrag(sf, LQ, 16 * i, 16 * k, l) * *(const f32x4*)(st.d + 16 * k + 4 * lg); };
+            // dc takes the steps up to this one, db those from this one on
+            if (i) {
+                a = mul2<T, FP32>(rfrag(sb, LN, 0, 16 * n, l), rfrag(sb, LN, 16, 16 * n, l), fd(0), fd(1), a);
+                q = mul1<T, FP32>(rfrag(sc, LN, 16, 16 * n, l), rfrag(sf, LQ, 16, 16, l), q);
+            } else {
+                a = mul1<T, FP32>(rfrag(sb, LN, 0, 16 * n, l), fd(0), a);
+                q = mul2<T, FP32>(rfrag(sc, LN, 0, 16 * n, l), rfrag(sc, LN, 16, 16 * n, l), rfrag(sf, LQ, 0, 0, l), rfrag(sf, LQ, 16, 0, l), q);
             }
-            for (int k = i; k < Q / 16; ++k)  // steps from this one on
-                q = mma(rfrag(sc, LN, 16 * k, 16 * n, l), rfrag(sf, LQ, 16 * k, 16 * i, l), q);
             float bq = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
 #pragma unroll
             for (int o = 16; o < 64; o <<= 1) {
@@ -812,7 +898,10 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         }
         {  // dx
             const int t = 16 * half + lc, p = 16 * wp + 4 * lg;
-            for (int k = half; k < Q / 16; ++k) xa = mma(rfrag(sdy, LP, 16 * k, 16 * wp, l), rfrag(sm, LQ, 16 * k, 16 * half, l), xa);
+            if (half)
+                xa = mul1<T, FP32>(rfrag(sdy, LP, 16, 16 * wp, l), rfrag(sm, LQ, 16, 16, l), xa);
+            else
+                xa = mul2<T, FP32>(rfrag(sdy, LP, 0, 16 * wp, l), rfrag(sdy, LP, 16, 16 * wp, l), rfrag(sm, LQ, 0, 0, l), rfrag(sm, LQ, 16, 0, l), xa);
             const f32x4 yv = *(const f32x4*)(sdy + t * LP + p), xv = *(const f32x4*)(sx + t * LP + p);
             skip_sum += (yv[0] * xv[0] + yv[1] * xv[1]) + (yv[2] * xv[2] + yv[3] * xv[3]);
             if (t < len && p < at.pw) row_store<VEC>(dx + (t0 + t) * yt + p, xa * st.d[t] + skip * yv, at.pw - p);
@@ -827,7 +916,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         }
         for (int o = 32; o; o >>= 1) pass += __shfl_xor(pass, o, 64);
         if (l == 0) inner[w] = pass;
-        if (on) walk<TILES, false>(R, sc + n_own, LN, sdy + 16 * wp, st, l);
+        if (on) walk<T, TILES, false>(R, sc + n_own, LN, sdy + 16 * wp, st, l);
         __syncthreads();
         if (w == 7) {  // the gradients of the steps' decays and sizes, lane = step
             const int t = l & (Q - 1);
