@@ -232,7 +232,7 @@ __global__ __launch_bounds__(LANES == 64 ? 512 : LANES) void norm_backward_kerne
 // lane has few loads to wait for, and their sums are added in LDS.  2048 parts of 512
 // columns, four waves of 64 columns each: 95 us; 512 parts, this way: 3 us.
 constexpr int SUM_COLS = 16, SUM_TEAMS = 64;
-__global__ __launch_bounds__(SUM_COLS * SUM_TEAMS) void sum_parts_kernel(const float* __restrict__ parts, int n_parts, int64_t n, int64_t first,
+__global__ __launch_bounds__(SUM_COLS * SUM_TEAMS) void sum_parts_kernel(const float* __restrict__ parts, int n_parts, int64_t n, int64_t first, int taps,
                                                                         float* __restrict__ out, float* __restrict__ out2) {
     __shared__ float sm[SUM_TEAMS][SUM_COLS + 1];
     const int c = threadIdx.x % SUM_COLS, team = threadIdx.x / SUM_COLS;
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(SUM_COLS * SUM_TEAMS) void sum_parts_kernel(const f
     v += __shfl_xor(v, 16, 64);
     v += __shfl_xor(v, 32, 64);
     if (team != 0 || i >= n) return;
-    if (i < first) out[i] = v;
+    if (i < first) out[i % (first / taps) * taps + i / (first / taps)] = v;
     else if (out2) out2[i - first] = v;
 }
 
@@ -315,8 +315,8 @@ int norm_forward(NormArgs a, int dtype, gorila_ctx* ctx, bool codes) {
 
 }  // namespace
 
-void launch_sum_parts(const float* parts, int n_parts, int64_t n, int64_t first, float* out, float* out2, hipStream_t st) {
-    sum_parts_kernel<<<(unsigned)((n + SUM_COLS - 1) / SUM_COLS), SUM_COLS * SUM_TEAMS, 0, st>>>(parts, n_parts, n, first, out, out2);
+void launch_sum_parts(const float* parts, int n_parts, int64_t n, int64_t first, int taps, float* out, float* out2, hipStream_t st) {
+    sum_parts_kernel<<<(unsigned)((n + SUM_COLS - 1) / SUM_COLS), SUM_COLS * SUM_TEAMS, 0, st>>>(parts, n_parts, n, first, taps, out, out2);
 }
 
 }  // namespace gorila
@@ -376,7 +376,7 @@ int gorila_add_rmsnorm_backward(const void* dy, int64_t dy_stride, const void* d
             norm_backward_kernel<decltype(t), L, QD, decltype(wide)::value><<<parts, THREADS, 0, c.stream>>>(a);
         });
     });
-    launch_sum_parts(a.parts, parts, width, width, dweight, nullptr, c.stream);
+    launch_sum_parts(a.parts, parts, width, width, 1, dweight, nullptr, c.stream);
     return launched();
 }
 

@@ -71,9 +71,10 @@ inline bool row_dtype(int dtype) { return dtype == GORILA_F32 || dtype == GORILA
 // Whether an address is one of an element of `bytes`, or of four of them.
 inline bool at_element(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 inline bool at_four(const void* p, int bytes) { return at_element(p, 4 * bytes); }
-// Sums of parts[0 .. n_parts-1][i] in a fixed order, to out[i] for i < first, else
-// to out2[i - first] (which may be null) (norm.hip).
-void launch_sum_parts(const float* parts, int n_parts, int64_t n, int64_t first, float* out, float* out2, hipStream_t st);
+// Sums of parts[0 .. n_parts-1][i] in a fixed order (norm.hip): column i < first, read
+// as [taps][first / taps], to out as [first / taps][taps]; the others to out2 (which may
+// be null).
+void launch_sum_parts(const float* parts, int n_parts, int64_t n, int64_t first, int taps, float* out, float* out2, hipStream_t st);
 inline int launched() { return hipGetLastError() == hipSuccess ? GORILA_OK : GORILA_EHIP; }
 
 }  // namespace gorila
