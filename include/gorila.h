@@ -46,7 +46,7 @@ extern "C" {
 enum {
     GORILA_OK = 0,
     GORILA_EINVAL = -1,        /* bad pointer, size, dtype or action count      */
-    GORILA_ERANGE = -2,        /* device saw an index or action out of range    */
+    GORILA_ERANGE = -2,        /* device saw an index, action or slot out of range */
     GORILA_EWORKSPACE = -3,    /* workspace too small for this call             */
     GORILA_EHIP = -4,          /* HIP runtime or launch error                   */
     GORILA_EUNSUPPORTED = -5   /* valid request the library does not implement */
@@ -141,7 +141,7 @@ int gorila_ctx_destroy(gorila_ctx* ctx);
 /* Point the context at another stream (subsequent calls enqueue there). */
 int gorila_ctx_set_stream(gorila_ctx* ctx, void* hip_stream);
 /* Synchronise the context's stream and report (then clear) the sticky device
- * error: GORILA_ERANGE if an index or action was out of range. */
+ * error: GORILA_ERANGE if an index, action or slot was out of range. */
 int gorila_ctx_check(gorila_ctx* ctx);
 const char* gorila_strerror(int code);
 
@@ -484,8 +484,8 @@ int gorila_quantize_weights(const void* weights, int64_t weights_stride, int32_t
 /* y[i][o] = sum_k x[i][k] w[o][k] for `rows` rows (row i of x at x + i *
  * x_stride elements).  x_dtype GORILA_F32 or GORILA_BF16 (y of the same type), or
  * GORILA_CODES: int8 rows with x_scale [rows] (as gorila_add_rmsnorm_codes makes
- * them), y fp32.  Made for the few rows of actors; any number of rows is
- * accepted. */
+ * them), y fp32.  Made for the few rows of actors; up to 65535 rows (else
+ * GORILA_EUNSUPPORTED). */
 enum { GORILA_CODES = 2 };
 int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_t x_dtype,
                    int64_t rows, const uint8_t* codes, const float* scales, int32_t outputs,

@@ -451,7 +451,7 @@ const char* gorila_strerror(int code) {
     switch (code) {
         case GORILA_OK: return "success";
         case GORILA_EINVAL: return "invalid argument";
-        case GORILA_ERANGE: return "minibatch index or action out of range (seen on the device)";
+        case GORILA_ERANGE: return "minibatch index, action or slot out of range (seen on the device)";
         case GORILA_EWORKSPACE: return "workspace too small";
         case GORILA_EHIP: return "HIP runtime error";
         case GORILA_EUNSUPPORTED: return "not supported by this library";
