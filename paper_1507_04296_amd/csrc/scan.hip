@@ -40,6 +40,8 @@ constexpr int THREADS = 512;
 constexpr int LP = PW + 4, LQ = Q + 4;  // LDS row lengths: 16 lanes' quads on all banks
 constexpr float LOG2E = 1.44269504088896341f;
 
+__host__ __device__ inline int padded_state(int n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
+
 struct ScanView {
     const void *x, *dt, *b, *c, *dy;
     int64_t xb, xt, dtb, dtt, bb, bt, cb, ct, dyb, dyt;
@@ -55,8 +57,8 @@ struct ScanView {
     float *seg_s, *seg_r, *seg_a;
     // backward
     const float* dstate_out;
-    float *chunk_s;             // states before the chunks [B][nch][vh][PW][NP]
-    float *pdb, *pdc;           // [B][T][vh][N]
+    float *chunk_s;             // states before the chunks [B][nch][vh][PW * NP], in the lanes' order
+    float *pdb, *pdc;           // [B][nch][vh][Q / 16][NP / 16][64][4], in the lanes' order
     float *pdt;                 // [B][T][vh]
     float *ppar;                // [B][nseg][vh][3]
     void* dx;
@@ -173,6 +175,31 @@ __device__ __forceinline__ f32x4 product(A&& fa, B&& fb, f32x4 c) {
     return c;
 }
 
+// The same with one a (FP32 values) and two b (rows' values).
+template <class T, int N, class A, class B>
+__device__ __forceinline__ void product_pair(A&& fa, B&& fb, f32x4 (&c)[2]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        const f32x4 zero{0.0f, 0.0f, 0.0f, 0.0f};
+        const f32x4 a0 = fa(i), a1 = N > 1 ? fa(i + 1) : zero;
+        if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                c[u] = mma(a0, fb(u, i), c[u]);
+                if constexpr (N > 1) c[u] = mma(a1, fb(u, i + 1), c[u]);
+            }
+        } else {
+            const Terms<FP32> a(a0, a1);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const Terms<ROWS> b(fb(u, i), N > 1 ? fb(u, i + 1) : zero);
+#pragma unroll
+                for (int k = Terms<FP32>::N - 1; k >= 0; --k) c[u] = mfma16(a.t[k], b.t[0], c[u]);
+            }
+        }
+    }
+}
+
 // Q rows of COLS columns on their way from memory to LDS, as they are in memory; rows
 // past len and columns past cols are zeros.
 template <class T, bool VEC> struct Quad {
@@ -221,6 +248,30 @@ struct Rows {
     }
 };
 
+// Moves between lanes without LDS.  move<C>: within rows of 16, 0 where there is no
+// such lane.
+constexpr int DOWN = 0x100, UP = 0x110;  // + n: from the lane n above, n below
+template <int C> __device__ __forceinline__ int move(int v) { return __builtin_amdgcn_update_dpp(0, v, C, 0xf, 0xf, true); }
+template <int C> __device__ __forceinline__ float move(float v) { return __int_as_float(move<C>(__float_as_int(v))); }
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ float lane_value(float v, int lane) { return __int_as_float(lane_value(__float_as_int(v), lane)); }
+// Sum over the row's 16 lanes; over the same lane of the four rows; over the wave (all get it).
+__device__ __forceinline__ float sum16(float v) {
+    v += move<0xb1>(v);   // lanes swapped in pairs
+    v += move<0x4e>(v);   // pairs in fours
+    v += move<0x141>(v);  // eight mirrored
+    v += move<0x140>(v);  // sixteen mirrored
+    return v;
+}
+__device__ __forceinline__ float sum_rows(float v) {
+    const uint32_t u = __float_as_uint(v);
+    const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t q = __float_as_uint(__uint_as_float(p[0]) + __uint_as_float(p[1]));
+    const auto r = __builtin_amdgcn_permlane32_swap(q, q, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float sum64(float v) { return sum_rows(sum16(v)); }
+
 // Step sizes, running log2-decays and episode numbers of a chunk.  A running sum is
 // kept as a whole number and a rest within +-1/2, so that the difference of two of
 // them is exact to 2^-23 however large both have grown: one sum in fp32 would lose
@@ -234,9 +285,6 @@ struct Steps {
     int starts;            // an episode starts in it
     int odd;               // a step size is not finite
 };
-struct GradSteps : Steps {
-    float sig[Q], dec[Q];  // d step size / d dt, own log2-decay
-};
 __device__ __forceinline__ float pow2(float v) { return __builtin_amdgcn_exp2f(v); }
 constexpr float LEAST_LOG2 = -65536.0f;  // 2^this is zero, and sums of Q of it are whole numbers below 2^24
 struct StepRegs {
@@ -249,8 +297,7 @@ struct StepRegs {
         reset = in && rs ? rs[t0 + l] != 0 : 0;
     }
     // By the lanes of one wave (lanes past Q take part and store nothing).
-    template <class S>
-    __device__ __forceinline__ void store(S& s, float bias, float rate2, int len, int l) const {
+    __device__ __forceinline__ void store(Steps& s, float bias, float rate2, int len, int l) const {
         const float v = dt + bias;
         const float e = expf(-fabsf(v));
         float d = fmaxf(v, 0.0f) + log1pf(e);
@@ -260,20 +307,23 @@ struct StepRegs {
         if (dec < LEAST_LOG2) dec = LEAST_LOG2;
         float gi = rintf(dec), gf = dec - gi;
         int ep = reset;
-#pragma unroll
-        for (int o = 1; o < Q; o <<= 1) {
-            const float iu = __shfl_up(gi, o, 64), fu = __shfl_up(gf, o, 64);
-            const int eu = __shfl_up(ep, o, 64);
-            if (l >= o) {
-                gf += fu;
-                const float r = rintf(gf);
-                gi += iu + r;
-                gf -= r;
-                ep += eu;
-            }
-        }
-        const float end_gi = __shfl(gi, Q - 1, 64), end_gf = __shfl(gf, Q - 1, 64);
-        const int end_ep = __shfl(ep, Q - 1, 64);
+        static_assert(Q == 32, "two rows of lanes");
+        auto add = [&](float iu, float fu, int eu) {
+            gf += fu;
+            const float r = rintf(gf);
+            gi += iu + r;
+            gf -= r;
+            ep += eu;
+        };
+        add(move<UP + 1>(gi), move<UP + 1>(gf), move<UP + 1>(ep));
+        add(move<UP + 2>(gi), move<UP + 2>(gf), move<UP + 2>(ep));
+        add(move<UP + 4>(gi), move<UP + 4>(gf), move<UP + 4>(ep));
+        add(move<UP + 8>(gi), move<UP + 8>(gf), move<UP + 8>(ep));
+        const float row_gi = lane_value(gi, 15), row_gf = lane_value(gf, 15);
+        const int row_ep = lane_value(ep, 15);
+        if (l >= 16) add(row_gi, row_gf, row_ep);
+        const float end_gi = lane_value(gi, Q - 1), end_gf = lane_value(gf, Q - 1);
+        const int end_ep = lane_value(ep, Q - 1);
         if (l < Q) {
             const bool in = l < len;
             s.d[l] = d;
@@ -282,10 +332,6 @@ struct StepRegs {
             s.ep[l] = in ? ep : -1;
             s.from[l] = in && ep == 0 ? pow2(gi + gf) : 0.0f;
             s.to[l] = in && ep == end_ep ? pow2((end_gi - gi) + (end_gf - gf)) : 0.0f;
-            if constexpr (std::is_same<S, GradSteps>::value) {
-                s.dec[l] = dec;
-                s.sig[l] = in ? (v >= 0.0f ? 1.0f : e) / (1.0f + e) : 0.0f;
-            }
         }
         const bool odd = __any(l < Q && d * 0.0f != 0.0f);
         if (l == 0) {
@@ -295,15 +341,6 @@ struct StepRegs {
         }
     }
 };
-// Sum over 16 lanes (all of them get it).
-__device__ __forceinline__ float sum16(float v) {
-    auto with = [&](auto ctrl) { v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
-    with(std::integral_constant<int, 0xb1>{});   // lanes swapped in pairs
-    with(std::integral_constant<int, 0x4e>{});   // pairs in fours
-    with(std::integral_constant<int, 0x141>{});  // eight mirrored
-    with(std::integral_constant<int, 0x140>{});  // sixteen mirrored
-    return v;
-}
 
 // v times a factor of a Steps, where a zero one is a mask whatever v is.
 __device__ __forceinline__ f32x4 masked(f32x4 v, float f) { return f != 0.0f ? v * f : f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
@@ -357,6 +394,20 @@ __device__ __forceinline__ void store_state(const f32x4 (&acc)[TILES], float* s,
         const int n = n0 + 16 * i + 4 * (l >> 4);
         if (p < pw && n < n_in) row_store<VEC>(s + (int64_t)p * ld + n, acc[i], n_in - n);
     }
+}
+// The same of the workspace's states, in the order of the lanes that hold them:
+// [state tile][channel tile][lane][4].  In rows of states, a wave's 16 bytes a lane lie
+// on 16 lines, which a load or store takes one after the other.
+__device__ __forceinline__ f32x4* own_state(float* s, int p0, int n0, int l) { return (f32x4*)s + ((n0 / 16) * (PW / 16) + p0 / 16) * 64 + l; }
+template <int TILES>
+__device__ __forceinline__ void load_own(f32x4 (&acc)[TILES], float* s, int p0, int n0, int l) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) acc[i] = own_state(s, p0, n0, l)[i * (PW / 16) * 64];
+}
+template <int TILES>
+__device__ __forceinline__ void store_own(const f32x4 (&acc)[TILES], float* s, int p0, int n0, int l) {
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) own_state(s, p0, n0, l)[i * (PW / 16) * 64] = acc[i];
 }
 // To LDS [channel][state].
 template <class T, int TILES>
@@ -443,7 +494,7 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
 
     f32x4 S[TILES];
     if (s.nseg > 1)
-        load_state<TILES, true>(S, s.seg_s + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * PW * NP, NP, PW, NP, 16 * wp, n_own, l);
+        load_own(S, s.seg_s + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * PW * NP, 16 * wp, on ? n_own : 0, l);
     else
         load_state<TILES, VEC>(S, s.state ? s.state + in.state : nullptr, s.N, at.pw, s.N, 16 * wp, n_own, l);
     if (tid == 0) flag = 0;
@@ -580,7 +631,7 @@ __device__ __forceinline__ void segment_state(const ScanView& s, float* sb, floa
         }
     }
     const int64_t o = ((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v;
-    if (on) store_state<TILES, true>(S, (REV ? s.seg_r : s.seg_s) + o * PW * NP, NP, PW, NP, 16 * wp, n_own, l);
+    if (on) store_own(S, (REV ? s.seg_r : s.seg_s) + o * PW * NP, 16 * wp, n_own, l);
     if (!REV && tid == 0) s.seg_a[o] = starts ? -1.0f : decay;
 }
 
@@ -598,7 +649,9 @@ __global__ __launch_bounds__(THREADS, 4) void state_kernel(ScanView s) {
 template <int NP, bool VEC>
 __global__ __launch_bounds__(256) void join_kernel(ScanView s) {
     const int e = (blockIdx.x % (PW * NP / 256)) * 256 + threadIdx.x, o = blockIdx.x / (PW * NP / 256);
-    const int v = o % s.vh, b = o / s.vh, h = v / s.ptiles, p = (v % s.ptiles) * PW + e / NP, n = e % NP;
+    const int v = o % s.vh, b = o / s.vh, h = v / s.ptiles;
+    // its place in the lanes' order
+    const int lane = e / 4 % 64, p = (v % s.ptiles) * PW + e / 256 % (PW / 16) * 16 + lane % 16, n = e / (PW * 16) * 16 + lane / 16 * 4 + e % 4;
     const bool rev = blockIdx.y != 0;
     const float* from = rev ? s.dstate_out : s.state;
     float* seg = (rev ? s.seg_r : s.seg_s) + ((int64_t)b * s.nseg * s.vh + v) * PW * NP + e;
@@ -652,7 +705,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
     constexpr int NT = NP / 16, LN = NP + 4, TILES = Half<NT>::TILES;
     __shared__ __align__(16) float sc[Q * LN], sb[Q * LN], sx[Q * LP], sdy[Q * LP], ss[PW * LN], sr[PW * LN];
     __shared__ __align__(16) float sm[Q * LQ], sf[Q * LQ];
-    __shared__ __align__(16) GradSteps st;
+    __shared__ __align__(16) Steps st;
     __shared__ float hc[NT][Q], qb[NT][Q], kb[NT][Q], pairs[3][Q], inner[8];
     __shared__ int flag;
     const Place at(s, blockIdx.x);
@@ -683,7 +736,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         rb.store(sb, LN, bad);
         if (bad != bad) flag = 1;
     };
-    auto steps = [&](GradSteps& to, int l) { rd.store(to, in.bias, in.rate2, at_t.len, l); };
+    auto steps = [&](Steps& to, int l) { rd.store(to, in.bias, in.rate2, at_t.len, l); };
     auto plain_walk = [&](f32x4 (&S)[TILES], int t0, int t1) {
         const int lc = lane & 15, lg = lane >> 4;
         Tiles<TILES> v;
@@ -697,19 +750,19 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
     {
         f32x4 S[TILES];
         if (s.nseg > 1)
-            load_state<TILES, true>(S, s.seg_s + seg0, NP, PW, NP, 16 * wp, n_own, lane);
+            load_own(S, s.seg_s + seg0, 16 * wp, on ? n_own : 0, lane);
         else
             load_state<TILES, VEC>(S, s.state ? s.state + in.state : nullptr, s.N, at.pw, s.N, 16 * wp, n_own, lane);
         // Wave 7 forms the decays of the next chunk beside the walk of this one; every
         // other chunk's stand in sf, which is not in use yet.
-        static_assert(sizeof(GradSteps) <= sizeof sf, "a place for the steps");
+        static_assert(sizeof(Steps) <= sizeof sf, "a place for the steps");
         if (at_t.start()) {
             load_in();
             if (w == 7 && at_t.len < at_t.end - at_t.t) steps(st, opaque(lane));
-            GradSteps *now = &st, *next = (GradSteps*)sf;
+            Steps *now = &st, *next = (Steps*)sf;
             for (;;) {
                 const int t0 = at_t.t, len = at_t.len;
-                if (on) store_state<TILES, true>(S, chunk_s + t0 / Q * chunk_step, NP, PW, NP, 16 * wp, n_own, lane);
+                if (on) store_own(S, chunk_s + t0 / Q * chunk_step, 16 * wp, n_own, lane);
                 bool whole;
                 if (t0 + len >= at_t.end) break;  // nobody asks for the state behind the last
                 __syncthreads();
@@ -726,13 +779,13 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                     walk<T, TILES, true>(S, sb + n_own, LN, sx + 16 * wp, *now, opaque(lane));
                 }
                 if (w == 7 && at_t.len < at_t.end - at_t.t) steps(*next, opaque(lane));
-                GradSteps* const other = now;
+                Steps* const other = now;
                 now = next;
                 next = other;
             }
         }
         if (s.nseg > 1)
-            load_state<TILES, true>(R, s.seg_r + seg0, NP, PW, NP, 16 * wp, n_own, lane);
+            load_own(R, s.seg_r + seg0, 16 * wp, on ? n_own : 0, lane);
         else
             load_state<TILES, VEC>(R, s.dstate_out ? s.dstate_out + in.state : nullptr, s.N, at.pw, s.N, 16 * wp, n_own, lane);
     }
@@ -743,15 +796,55 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
     auto load_out = [&]() {
         ry.load(at_t.t * s.dyt, at_t.len);
         rc.load(at_t.t * s.ct, at_t.len);
-        load_state<TILES, true>(S, chunk_s + at_t.chunk() / Q * chunk_step, NP, PW, NP, 16 * wp, n_own, opaque(lane));
+        load_own(S, chunk_s + at_t.chunk() / Q * chunk_step, 16 * wp, on ? n_own : 0, opaque(lane));
     };
     const float skip = s.skip[at.h];
     T* dx = (T*)s.dx + ((int64_t)at.b * s.T * s.H + at.h) * s.P + at.p0;
-    const int64_t part_t = (int64_t)s.vh * s.N;
-    const int64_t part0 = ((int64_t)at.b * s.T * s.vh + at.v) * s.N;
+    const int64_t part0 = ((int64_t)at.b * s.nch * s.vh + at.v) * Q * NP, part_step = (int64_t)s.vh * Q * NP;
     auto load = [&]() {
         load_in();
         load_out();
+    };
+    // The gradients of a chunk's step sizes and decays, lane = step: by wave 6, beside the
+    // next chunk's first products (a long chain of a few lanes).
+    float past_d = 0.0f, past_all = 0.0f;
+    int past_t = 0, past_len = 0;
+    auto finish = [&](int l) {
+        const int t = l & (Q - 1);
+        float h = 0.0f, k = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            h += hc[n][t];
+            k += kb[n][t];
+            q += qb[n][t];
+        }
+        k *= past_d;
+        h += move<DOWN + 1>(h);  // steps from t on
+        h += move<DOWN + 2>(h);
+        h += move<DOWN + 4>(h);
+        h += move<DOWN + 8>(h);
+        const float h16 = lane_value(h, 16);
+        if (t < 16) h += h16;
+        k += move<UP + 1>(k);  // steps up to t
+        k += move<UP + 2>(k);
+        k += move<UP + 4>(k);
+        k += move<UP + 8>(k);
+        const float k15 = lane_value(k, 15), below = move<UP + 1>(k);
+        float g = h + (t > 16 ? k15 + below : t == 16 ? k15 : below);
+        if (t > 0) g += pairs[1][t];
+        if (t > 0 && t < 16) g += pairs[0][t];
+        if (t > 16) g += pairs[2][t];
+        // without a start in the chunk, the state before it to the one behind it
+        if (!(past_all < 0.0f)) g += (((inner[0] + inner[1]) + (inner[2] + inner[3])) + ((inner[4] + inner[5]) + (inner[6] + inner[7]))) * past_all;
+        if (l < past_len) {
+            // log a = -exp(a_log) d, and d's derivative by dt is 1 - e^-d
+            const float rate = in.rate2 / LOG2E, dd = (q + g * rate) * -expm1f(-past_d);
+            const float log_a = rate * past_d;
+            decay_sum += g * (log_a < LEAST_LOG2 / LOG2E ? LEAST_LOG2 / LOG2E : log_a);
+            bias_sum += dd;
+            s.pdt[((int64_t)at.b * s.T + past_t + l) * s.vh + at.v] = dd;
+        }
+        past_len = 0;
     };
     bool more = at_t.start_back();
     if (more) load_out();  // the last chunk's inputs are here
@@ -765,9 +858,12 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         float bad = 0.0f;
         ry.store(sdy, LP, bad);
         rc.store(sc, LN, bad);
+        float pass = 0.0f;  // <R, S>, from the state before to the one behind
         if (on) {
             stage_state<float, TILES>(R, sr, LN, 16 * wp, n_own, l);
             stage_state<float, TILES>(S, ss, LN, 16 * wp, n_own, l);
+#pragma unroll
+            for (int n = 0; n < TILES; ++n) pass += (R[n][0] * S[n][0] + R[n][1] * S[n][1]) + (R[n][2] * S[n][2] + R[n][3] * S[n][3]);
         }
         if (bad != bad) flag = 1;
         __syncthreads();
@@ -784,6 +880,8 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                                           [&](int n) { return kfrag(sdy, LP, 16 * ti, 16 * n, l); }, f);
         } else if (w == 7) {
             steps(st, l);
+        } else if (past_len) {
+            finish(l);
         }
         __syncthreads();
         if (at_t.single < 0 && (flag || st.odd)) {
@@ -808,26 +906,30 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
             }
             *(f32x4*)((w < 3 ? sm : sf) + tm * LQ + q0) = g;
         }
-        // What the states around the chunk give dc and db (rows = state, columns =
-        // steps) and dx (rows = channels), meanwhile.
-        constexpr int JOBS = (2 * NT + 7) / 8;
-        f32x4 ja[JOBS], jq[JOBS], xa{0.0f, 0.0f, 0.0f, 0.0f};
+        // What the states around the chunk give dc (of S) and db (of R; rows = state,
+        // columns = steps) and dx (of R; rows = channels), meanwhile.  A wave has a tile
+        // of one of the two for both halves of the steps, and its own tiles of R for dx:
+        // no state is read and split twice.
+        constexpr int JOBS = NT == 8 ? 2 : 1;
+        f32x4 ja[JOBS][2], xa[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) xa[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < JOBS; ++u) {
-            const int job = w + 8 * u, n = job >> 1, i = job & 1;
-            f32x4 a{0.0f, 0.0f, 0.0f, 0.0f}, q = a;
-            if (job < 2 * NT) {
-                a = product<T, FP32, PW / 16, true>([&](int k) { return rfrag(ss, LN, 16 * k, 16 * n, l); },
-                                                     [&](int k) { return kfrag(sdy, LP, 16 * i, 16 * k, l); }, a);
-                q = product<T, FP32, PW / 16, true>([&](int k) { return rfrag(sr, LN, 16 * k, 16 * n, l); },
-                                                     [&](int k) { return kfrag(sx, LP, 16 * i, 16 * k, l); }, q);
-            }
-            ja[u] = masked(a, st.from[16 * i + lc]);
-            jq[u] = masked(q, st.to[16 * i + lc]);
+            const bool of_r = NT == 8 ? u : w >= NT;
+            const int n = NT == 8 ? w : w % NT;
+            const float *m = of_r ? sr : ss, *rows = of_r ? sx : sdy, *by = of_r ? st.to : st.from;
+            ja[u][0] = ja[u][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (w < 2 * NT)
+                product_pair<T, PW / 16>([&](int k) { return rfrag(m, LN, 16 * k, 16 * n, l); },
+                                         [&](int i, int k) { return kfrag(rows, LP, 16 * i, 16 * k, l); }, ja[u]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) ja[u][i] = masked(ja[u][i], by[16 * i + lc]);
         }
-        xa = product<T, FP32, NT, true>([&](int n) { return kfrag(sr, LN, 16 * wp, 16 * n, l); },
-                                         [&](int n) { return kfrag(sb, LN, 16 * half, 16 * n, l); }, xa);
-        xa = masked(xa, st.to[16 * half + lc]);
+        if (on)
+            product_pair<T, TILES>([&](int n) { return R[n]; }, [&](int i, int n) { return kfrag(sb, LN, 16 * i, n_own + 16 * n, l); }, xa);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) xa[i] = masked(xa[i], st.to[16 * i + lc]);
         __syncthreads();
         if (w >= 3 && w < 6) {  // what passes from s to t: M F d without F's decay, summed for every step between
             const f32x4 v = *(const f32x4*)(sm + tm * LQ + q0) * f * *(const f32x4*)(st.d + q0);
@@ -861,109 +963,80 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
                 if (lg == 0 && lc > 0) pairs[1][tm] = u;
             }
         }
+        // dx's part for the steps of the wave with the other half of the states
+        f32x4* const swap = (f32x4*)sr;
+        if (on) swap[w * 64 + l] = half ? xa[0] : xa[1];
+        f32x4 xo = half ? xa[1] : xa[0];
 #pragma unroll
         for (int u = 0; u < JOBS; ++u) {
-            const int job = w + 8 * u, n = job >> 1, i = job & 1, t = 16 * i + lc, n0 = 16 * n + 4 * lg;
-            if (job >= 2 * NT) break;
-            f32x4 a = ja[u], q = jq[u];
-            const f32x4 cv = *(const f32x4*)(sc + t * LN + n0), bv = *(const f32x4*)(sb + t * LN + n0);
-            float h = (a[0] * cv[0] + a[1] * cv[1]) + (a[2] * cv[2] + a[3] * cv[3]);
-            float kv = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
-            auto fd = [&](int k) { return kfrag(sf, LQ, 16 * i, 16 * k, l) * *(const f32x4*)(st.d + 16 * k + 4 * lg); };
-            // dc takes the steps up to this one, db those from this one on
-            if (i) {
-                a = mul2<T, FP32>(rfrag(sb, LN, 0, 16 * n, l), rfrag(sb, LN, 16, 16 * n, l), fd(0), fd(1), a);
-                q = mul1<T, FP32>(rfrag(sc, LN, 16, 16 * n, l), rfrag(sf, LQ, 16, 16, l), q);
-            } else {
-                a = mul1<T, FP32>(rfrag(sb, LN, 0, 16 * n, l), fd(0), a);
-                q = mul2<T, FP32>(rfrag(sc, LN, 0, 16 * n, l), rfrag(sc, LN, 16, 16 * n, l), rfrag(sf, LQ, 0, 0, l), rfrag(sf, LQ, 16, 0, l), q);
-            }
-            float bq = (q[0] * bv[0] + q[1] * bv[1]) + (q[2] * bv[2] + q[3] * bv[3]);
+            if (w >= 2 * NT) break;
+            const bool of_r = NT == 8 ? u : w >= NT;
+            const int n = NT == 8 ? w : w % NT, n0 = 16 * n + 4 * lg;
+            const float* own = of_r ? sc : sb;
+            const f32x4 low = rfrag(own, LN, 0, 16 * n, l), high = rfrag(own, LN, 16, 16 * n, l);
 #pragma unroll
-            for (int o = 16; o < 64; o <<= 1) {
-                h += __shfl_xor(h, o, 64);
-                kv += __shfl_xor(kv, o, 64);
-                bq += __shfl_xor(bq, o, 64);
-            }
-            if (lg == 0) {
-                hc[n][t] = h;
-                kb[n][t] = kv;
-                qb[n][t] = bq;
-            }
-            if (t < len && n0 < s.N) {
-                const int64_t o = part0 + (t0 + t) * part_t + n0;
-                row_store<VEC>(s.pdc + o, a, s.N - n0);
-                row_store<VEC>(s.pdb + o, q * st.d[t], s.N - n0);
-            }
-        }
-        {  // dx
-            const int t = 16 * half + lc, p = 16 * wp + 4 * lg;
-            if (half)
-                xa = mul1<T, FP32>(rfrag(sdy, LP, 16, 16 * wp, l), rfrag(sm, LQ, 16, 16, l), xa);
-            else
-                xa = mul2<T, FP32>(rfrag(sdy, LP, 0, 16 * wp, l), rfrag(sdy, LP, 16, 16 * wp, l), rfrag(sm, LQ, 0, 0, l), rfrag(sm, LQ, 16, 0, l), xa);
-            const f32x4 yv = *(const f32x4*)(sdy + t * LP + p), xv = *(const f32x4*)(sx + t * LP + p);
-            skip_sum += (yv[0] * xv[0] + yv[1] * xv[1]) + (yv[2] * xv[2] + yv[3] * xv[3]);
-            if (t < len && p < at.pw) row_store<VEC>(dx + (t0 + t) * yt + p, xa * st.d[t] + skip * yv, at.pw - p);
-        }
-        float pass = 0.0f;  // <R, S>, from the state before to the one behind
-        if (on) {
-#pragma unroll
-            for (int n = 0; n < TILES; ++n) {
-                const f32x4 v = *(const f32x4*)(ss + (16 * wp + lc) * LN + n_own + 16 * n + 4 * lg);
-                pass += (R[n][0] * v[0] + R[n][1] * v[1]) + (R[n][2] * v[2] + R[n][3] * v[3]);
+            for (int i = 0; i < 2; ++i) {
+                const int t = 16 * i + lc;
+                f32x4 a = ja[u][i];
+                const f32x4 v = *(const f32x4*)((of_r ? sb : sc) + t * LN + n0);
+                float h = (a[0] * v[0] + a[1] * v[1]) + (a[2] * v[2] + a[3] * v[3]), bq = 0.0f;
+                if (of_r) {  // the steps from this one on
+                    if (i) a = mul1<T, FP32>(high, rfrag(sf, LQ, 16, 16, l), a);
+                    else a = mul2<T, FP32>(low, high, rfrag(sf, LQ, 0, 0, l), rfrag(sf, LQ, 16, 0, l), a);
+                    bq = (a[0] * v[0] + a[1] * v[1]) + (a[2] * v[2] + a[3] * v[3]);
+                } else {  // the steps up to this one
+                    auto fd = [&](int k) { return kfrag(sf, LQ, 16 * i, 16 * k, l) * *(const f32x4*)(st.d + 16 * k + 4 * lg); };
+                    if (i) a = mul2<T, FP32>(low, high, fd(0), fd(1), a);
+                    else a = mul1<T, FP32>(low, fd(0), a);
+                }
+                h = sum_rows(h);
+                if (of_r) bq = sum_rows(bq);
+                if (lg == 0) {
+                    (of_r ? kb : hc)[n][t] = h;
+                    if (of_r) qb[n][t] = bq;
+                }
+                if (t < len && n0 < s.N) {
+                    const int at_q = t0 % Q + t;  // in its chunk
+                    float* o = (of_r ? s.pdb : s.pdc) + part0 + t0 / Q * part_step;
+                    *((f32x4*)o + ((at_q / 16 * NT + n) * 64 + 16 * lg + at_q % 16)) = of_r ? a * st.d[t] : a;
+                }
             }
         }
-        for (int o = 32; o; o >>= 1) pass += __shfl_xor(pass, o, 64);
+        if (half)
+            xo = mul1<T, FP32>(rfrag(sdy, LP, 16, 16 * wp, l), rfrag(sm, LQ, 16, 16, l), xo);
+        else
+            xo = mul2<T, FP32>(rfrag(sdy, LP, 0, 16 * wp, l), rfrag(sdy, LP, 16, 16 * wp, l), rfrag(sm, LQ, 0, 0, l), rfrag(sm, LQ, 16, 0, l), xo);
+        pass = sum64(pass);
         if (l == 0) inner[w] = pass;
         if (on) walk<T, TILES, false>(R, sc + n_own, LN, sdy + 16 * wp, st, l);
         __syncthreads();
-        if (w == 7) {  // the gradients of the steps' decays and sizes, lane = step
-            const int t = l & (Q - 1);
-            float h = 0.0f, k = 0.0f, q = 0.0f;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                h += hc[n][t];
-                k += kb[n][t];
-                q += qb[n][t];
-            }
-            const float d = st.d[t];
-            k *= d;
-#pragma unroll
-            for (int o = 1; o < Q; o <<= 1) {  // steps from t on; steps up to t
-                const float hu = __shfl_down(h, o, Q), ku = __shfl_up(k, o, Q);
-                if (t + o < Q) h += hu;
-                if (t >= o) k += ku;
-            }
-            const float before = __shfl_up(k, 1, Q);
-            float g = h + (t > 0 ? before : 0.0f);
-            if (t > 0) g += pairs[1][t];
-            if (t > 0 && t < 16) g += pairs[0][t];
-            if (t > 16) g += pairs[2][t];
-            if (!st.starts) g += (((inner[0] + inner[1]) + (inner[2] + inner[3])) + ((inner[4] + inner[5]) + (inner[6] + inner[7]))) * st.all;
-            if (l < len) {
-                // log a = dec / LOG2E = -exp(a_log) d
-                const float dd = (q + g * (in.rate2 / LOG2E)) * st.sig[t];
-                decay_sum += g * (st.dec[t] / LOG2E);
-                bias_sum += dd;
-                s.pdt[((int64_t)at.b * s.T + t0 + t) * s.vh + at.v] = dd;
-            }
+        {  // dx
+            const int t = 16 * half + lc, p = 16 * wp + 4 * lg;
+            if (Half<NT>::on(1 - half)) xo += swap[(w ^ 4) * 64 + l];
+            const f32x4 yv = *(const f32x4*)(sdy + t * LP + p), xv = *(const f32x4*)(sx + t * LP + p);
+            skip_sum += (yv[0] * xv[0] + yv[1] * xv[1]) + (yv[2] * xv[2] + yv[3] * xv[3]);
+            if (t < len && p < at.pw) row_store<VEC>(dx + (t0 + t) * yt + p, xo * st.d[t] + skip * yv, at.pw - p);
+        }
+        if (w == 6) {
+            past_d = st.d[l & (Q - 1)];
+            past_all = st.starts ? -1.0f : st.all;
+            past_t = t0;
+            past_len = len;
         }
         if (whole) {
             __syncthreads();
             if (tid == 0) flag = 0;
         }
     }
+    if (w == 6 && past_len) finish(lane);
     if (on && s.dstate && at.seg == 0) store_state<TILES, VEC>(R, s.dstate + in.state, s.N, at.pw, s.N, 16 * wp, n_own, lane);
-    for (int o = 32; o; o >>= 1) {
-        skip_sum += __shfl_xor(skip_sum, o, 64);
-        decay_sum += __shfl_xor(decay_sum, o, 64);
-        bias_sum += __shfl_xor(bias_sum, o, 64);
-    }
+    skip_sum = sum64(skip_sum);
+    decay_sum = sum64(decay_sum);
+    bias_sum = sum64(bias_sum);
     __syncthreads();
     if (lane == 0) inner[w] = skip_sum;
     __syncthreads();
-    if (tid == THREADS - 64) {
+    if (tid == THREADS - 128) {  // of wave 6
         float* o = s.ppar + (((int64_t)at.b * s.nseg + at.seg) * s.vh + at.v) * 3;
         o[0] = decay_sum;
         o[1] = bias_sum;
@@ -974,7 +1047,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
 // Sums the workgroups' parts, in order: of db and dc over the heads of a group,
 // of ddt over a head's tiles (blockIdx.y = 0), and of the parameters over sequences
 // and segments (blockIdx.y = 1: a wave a head).
-template <class T>
+template <class T, bool VEC>
 __global__ __launch_bounds__(256) void scan_reduce_kernel(ScanView s, T* db, T* dc, T* ddt, float* da_log, float* ddt_bias,
                                                           float* dskip) {
     if (blockIdx.y == 1) {
@@ -997,19 +1070,23 @@ __global__ __launch_bounds__(256) void scan_reduce_kernel(ScanView s, T* db, T* 
         }
         return;
     }
-    const int64_t rows = (int64_t)s.B * s.T, per = (int64_t)s.G * s.N, total = rows * per;
-    const int heads = s.vh / s.G;
+    const int heads = s.vh / s.G, tiles = (s.N + 15) / 16, nt = padded_state(s.N) / 16;
+    const int64_t rows = (int64_t)s.B * s.T, total = (int64_t)s.B * s.nch * s.G * (Q / 16) * tiles * 64, part = Q * nt * 4;
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
-        const int64_t row = e / per;
-        const int g = (int)(e % per) / s.N, n = (int)(e % per) % s.N;
-        const int64_t o = (row * s.vh + (int64_t)g * heads) * s.N + n;
-        float b = 0.0f, c = 0.0f;
-        for (int i = 0; i < heads; ++i) {
-            b += s.pdb[o + (int64_t)i * s.N];
-            c += s.pdc[o + (int64_t)i * s.N];
+        const int l = (int)(e & 63), i = (int)(e / 64 / tiles % (Q / 16)), n = (int)(e / 64 % tiles);
+        const int64_t r = e / 64 / tiles / (Q / 16), bk = r / s.G;  // (sequence, chunk)
+        const int g = (int)(r % s.G), n0 = 16 * n + 4 * (l >> 4);
+        const int64_t t = bk % s.nch * Q + 16 * i + (l & 15);
+        if (t >= s.T || n0 >= s.N) continue;
+        const int64_t o = (bk * s.vh + (int64_t)g * heads) * part + (i * nt + n) * 64 + l;
+        f32x4 b{0.0f, 0.0f, 0.0f, 0.0f}, c = b;
+        for (int k = 0; k < heads; ++k) {
+            b += ((const f32x4*)s.pdb)[o + k * part];
+            c += ((const f32x4*)s.pdc)[o + k * part];
         }
-        db[e] = row_round<T>(b);
-        dc[e] = row_round<T>(c);
+        const int64_t to = ((bk / s.nch * s.T + t) * s.G + g) * s.N + n0;
+        row_store<VEC>(db + to, b, s.N - n0);
+        row_store<VEC>(dc + to, c, s.N - n0);
     }
     for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * s.H; e += (int64_t)gridDim.x * 256) {
         float d = 0.0f;
@@ -1075,7 +1152,6 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanView s, float* pool,
 
 // ---- host ----
 
-int padded_state(int n) { return n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : 128; }
 
 // Segments a sequence is cut into: none where the (sequence, head, channels) fill
 // the chip, else enough for two workgroups a compute unit, of one chunk at least.
@@ -1103,8 +1179,9 @@ struct ScanPlan {
         seg_a = take(k.nseg > 1 ? segs : 0);
         seg_r = take(backward && k.nseg > 1 ? segs * state : 0);
         chunk_s = take(backward ? (size_t)B * k.nch * k.vh * state : 0);
-        pdb = take(backward ? rows * N : 0);
-        pdc = take(backward ? rows * N : 0);
+        const size_t parts = backward ? (size_t)B * k.nch * k.vh * Q * padded_state(N) : 0;
+        pdb = take(parts);
+        pdc = take(parts);
         pdt = take(backward ? rows : 0);
         ppar = take(backward ? segs * 3 : 0);
         total = o;
@@ -1229,7 +1306,7 @@ int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t d
     const int64_t blocks = (int64_t)v.B * v.nseg * v.vh;
     if (!grid_fits(blocks * (PW * MAX_STATE / 256))) return GORILA_EUNSUPPORTED;
     if ((rc = ctx_view(ctx, p.total, c))) return rc;
-    vec = vec && !((dy_batch_stride | dy_step_stride) & 3) && at_four(dy, e) && at_four(dx, e) && at_four(dstate_out, 4) && at_four(dstate, 4);
+    vec = vec && !((dy_batch_stride | dy_step_stride) & 3) && at_four(dy, e) && at_four(dx, e) && at_four(db, e) && at_four(dc, e) && at_four(dstate_out, 4) && at_four(dstate, 4);
     v.dy = dy;
     v.dyb = dy_batch_stride;
     v.dyt = dy_step_stride;
@@ -1250,10 +1327,11 @@ int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t d
             }
             scan_backward_kernel<T, NP, VEC><<<(unsigned)blocks, THREADS, 0, c.stream>>>(v);
         }
-        const int64_t per = ((int64_t)v.B * v.T * v.G * v.N + 255) / 256, heads = (v.H + 3) / 4;
+        const int64_t quads = (int64_t)v.B * v.nch * v.G * (Q / 16) * ((v.N + 15) / 16) * 64;
+        const int64_t least = (int64_t)v.B * v.T * v.H, per = ((quads > least ? quads : least) + 255) / 256, heads = (v.H + 3) / 4;
         const unsigned gx = (unsigned)(per > 8192 ? 8192 : per);
-        scan_reduce_kernel<T><<<dim3(gx > heads ? gx : (unsigned)heads, 2), 256, 0, c.stream>>>(v, (T*)db, (T*)dc, (T*)ddt, da_log,
-                                                                                              ddt_bias, dskip);
+        scan_reduce_kernel<T, VEC><<<dim3(gx > heads ? gx : (unsigned)heads, 2), 256, 0, c.stream>>>(v, (T*)db, (T*)dc, (T*)ddt, da_log,
+                                                                                                   ddt_bias, dskip);
     });
     return launched();
 }
