@@ -221,20 +221,23 @@ template <int COLS, bool VEC, class T>
 struct Rows {
     static constexpr int QUADS = COLS * Q / 4, R = (QUADS + THREADS - 1) / THREADS;
     Quad<T, VEC> v[R];
-    const T* p[R];
+    const T* base;
+    int64_t stride;
     int cols;
-    static __device__ __forceinline__ int row(int i) { return (threadIdx.x + THREADS * i) / (COLS / 4); }
-    static __device__ __forceinline__ int col(int i) { return (threadIdx.x + THREADS * i) % (COLS / 4) * 4; }
-    __device__ __forceinline__ Rows(const T* base, int64_t stride, int n) : cols(n) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) p[i] = base + (col(i) < n ? row(i) * stride + col(i) : 0);
-    }
-    // off: elements from step 0 to the first step
-    __device__ __forceinline__ void load(int64_t off, int len) {
+    static __device__ __forceinline__ int row(int i, int tid) { return (tid + THREADS * i) / (COLS / 4); }
+    static __device__ __forceinline__ int col(int i, int tid) { return (tid + THREADS * i) % (COLS / 4) * 4; }
+    __device__ __forceinline__ Rows(const T* b, int64_t st, int n) : base(b), stride(st), cols(n) {}
+    // The len steps from t on.  The lanes' addresses are formed again each time: kept
+    // over the loop they went to scratch memory, and reading them back waited for the
+    // loads before.
+    __device__ __forceinline__ void load(int t, int len) {
+        const T* from = base + t * stride;
+        const int tid = opaque((int)threadIdx.x);
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            const bool in = row(i) < len && col(i) < cols;
-            v[i].load(in ? p[i] + off : p[i], in ? cols - col(i) : 0);
+            const int r = row(i, tid), c = col(i, tid);
+            const bool in = r < len && c < cols;
+            v[i].load(from + (in ? r * stride + c : 0), in ? cols - c : 0);
         }
     }
     // Adds 0 to bad, or NaN where a value is not finite.
@@ -242,7 +245,7 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const f32x4 f = v[i].get();
-            if (QUADS % THREADS == 0 || (int)threadIdx.x + THREADS * i < QUADS) *(f32x4*)(lds + row(i) * ld + col(i)) = f;
+            if (QUADS % THREADS == 0 || (int)threadIdx.x + THREADS * i < QUADS) *(f32x4*)(lds + row(i, (int)threadIdx.x) * ld + col(i, (int)threadIdx.x)) = f;
             bad += (f[0] * 0.0f + f[1] * 0.0f) + (f[2] * 0.0f + f[3] * 0.0f);
         }
     }
@@ -287,18 +290,20 @@ struct Steps {
 };
 __device__ __forceinline__ float pow2(float v) { return __builtin_amdgcn_exp2f(v); }
 constexpr float LEAST_LOG2 = -65536.0f;  // 2^this is zero, and sums of Q of it are whole numbers below 2^24
-struct StepRegs {
-    float dt;
-    int reset;
-    template <class T>
+template <class T> struct StepRegs {  // as they are in memory: a value that is changed here is waited for here
+    T raw;
+    uint8_t raw_reset;
     __device__ __forceinline__ void load(const T* dt_base, int64_t stride, const uint8_t* rs, int t0, int len, int l) {
-        const bool in = l < len;
-        dt = in ? row_value(dt_base[(int64_t)(t0 + l) * stride]) : 0.0f;
-        reset = in && rs ? rs[t0 + l] != 0 : 0;
+        raw = T{0};
+        raw_reset = 0;
+        if (l < len) {
+            raw = dt_base[(int64_t)(t0 + l) * stride];
+            if (rs) raw_reset = rs[t0 + l];
+        }
     }
     // By the lanes of one wave (lanes past Q take part and store nothing).
     __device__ __forceinline__ void store(Steps& s, float bias, float rate2, int len, int l) const {
-        const float v = dt + bias;
+        const float v = row_value(raw) + bias;
         const float e = expf(-fabsf(v));
         float d = fmaxf(v, 0.0f) + log1pf(e);
         if (v != v) d = v;
@@ -306,7 +311,7 @@ struct StepRegs {
         float dec = rate2 * d;
         if (dec < LEAST_LOG2) dec = LEAST_LOG2;
         float gi = rintf(dec), gf = dec - gi;
-        int ep = reset;
+        int ep = raw_reset != 0;
         static_assert(Q == 32, "two rows of lanes");
         auto add = [&](float iu, float fu, int eu) {
             gf += fu;
@@ -501,12 +506,12 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
 
     Rows<PW, VEC, T> rx(in.x, s.xt, at.pw);
     Rows<NP, VEC, T> rb(in.b, s.bt, s.N), rc(in.c, s.ct, s.N);
-    StepRegs rd;
+    StepRegs<T> rd;
     Walk at_t(s, at.seg);
     auto load = [&]() {
-        rx.load(at_t.t * s.xt, at_t.len);
-        rb.load(at_t.t * s.bt, at_t.len);
-        rc.load(at_t.t * s.ct, at_t.len);
+        rx.load(at_t.t, at_t.len);
+        rb.load(at_t.t, at_t.len);
+        rc.load(at_t.t, at_t.len);
         if (w == 7) rd.load(in.dt, s.dtt, in.reset, at_t.t, at_t.len, l);
     };
     bool more = at_t.start();
@@ -587,11 +592,11 @@ __device__ __forceinline__ void segment_state(const ScanView& s, float* sb, floa
     const int64_t xt = REV ? s.dyt : s.xt, bt = REV ? s.ct : s.bt;
     Rows<PW, VEC, T> rx(REV ? in.dy : in.x, xt, at.pw);
     Rows<NP, VEC, T> rb(REV ? in.c : in.b, bt, s.N);
-    StepRegs rd;
+    StepRegs<T> rd;
     Walk at_t(s, at.seg);
     auto load = [&]() {
-        rx.load(at_t.t * xt, at_t.len);
-        rb.load(at_t.t * bt, at_t.len);
+        rx.load(at_t.t, at_t.len);
+        rb.load(at_t.t, at_t.len);
         if (w == 7) rd.load(in.dt, s.dtt, in.reset, at_t.t, at_t.len, l);
     };
     // Where nothing stops it, wave 7 forms the decays of the next chunk beside the walk
@@ -720,14 +725,14 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
 
     Rows<PW, VEC, T> rx(in.x, s.xt, at.pw);
     Rows<NP, VEC, T> rb(in.b, s.bt, s.N);
-    StepRegs rd;
+    StepRegs<T> rd;
     f32x4 R[TILES];
     float decay_sum = 0.0f, bias_sum = 0.0f, skip_sum = 0.0f;  // of the three parameters' gradients
     if (tid == 0) flag = 0;
     Walk at_t(s, at.seg);
     auto load_in = [&]() {
-        rx.load(at_t.t * s.xt, at_t.len);
-        rb.load(at_t.t * s.bt, at_t.len);
+        rx.load(at_t.t, at_t.len);
+        rb.load(at_t.t, at_t.len);
         if (w == 7) rd.load(in.dt, s.dtt, in.reset, at_t.t, at_t.len, opaque(lane));
     };
     auto stage_in = [&](int l) {
@@ -794,8 +799,10 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
     Rows<NP, VEC, T> rc(in.c, s.ct, s.N);
     f32x4 S[TILES];
     auto load_out = [&]() {
-        ry.load(at_t.t * s.dyt, at_t.len);
-        rc.load(at_t.t * s.ct, at_t.len);
+        ry.load(at_t.t, at_t.len);
+        rc.load(at_t.t, at_t.len);
+    };
+    auto load_s = [&]() {
         load_own(S, chunk_s + at_t.chunk() / Q * chunk_step, 16 * wp, on ? n_own : 0, opaque(lane));
     };
     const float skip = s.skip[at.h];
@@ -847,7 +854,10 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         past_len = 0;
     };
     bool more = at_t.start_back();
-    if (more) load_out();  // the last chunk's inputs are here
+    if (more) {
+        load_out();
+        load_s();
+    }  // the last chunk's inputs are here
     while (more) {
         // what the lane number decides is decided again for every chunk: kept over the
         // loop it took more scalar registers than there are
@@ -887,12 +897,14 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         if (at_t.single < 0 && (flag || st.odd)) {
             at_t.split_back();
             load();
+            load_s();
             continue;
         }
         const int t0 = at_t.t, len = at_t.len;
         bool whole;
         more = at_t.next_back(whole);
         if (more) load();
+        load_s();  // after the last chunk too: loaded in a branch, it would be copied, and waited for, at its end
         if (w < 6) {  // M and F
             const float gi_t = st.gi[tm], gf_t = st.gf[tm];
             const int et = st.ep[tm];
