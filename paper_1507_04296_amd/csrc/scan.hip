@@ -517,30 +517,31 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
     bool more = at_t.start();
     if (more) load();
     while (more) {
-        __syncthreads();
-        float bad = 0.0f;
-        rx.store(sx, LP, bad);
-        rb.store(sb, LN, bad);
-        rc.store(sc, LN, bad);
-        if (on) stage_state<T, TILES>(S, ss, LN, 16 * wp, n_own, l);
-        if (bad != bad) flag = 1;
-        __syncthreads();
         // What needs no decays, beside the decays (a long chain of a few lanes): what the
         // state gives 16 steps (rows = channels, columns = steps), c_t . b_s of the three
         // tiles with s <= t.
         const int t = 16 * half + lc, si = w >> 1, ti = w > 0;
-        f32x4 acc{0.0f, 0.0f, 0.0f, 0.0f}, m = acc;
-        if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l);
-        acc = product<T, WORDS, NT, true>([&](int n) { return kfrag(ss, LN, 16 * wp, 16 * n, l); },
-                                          [&](int n) { return kfrag(sc, LN, 16 * half, 16 * n, l); }, acc);
-        if (w < 3)
-            m = product<T, ROWS, NT>([&](int n) { return kfrag(sb, LN, 16 * si, 16 * n, l); },
-                                     [&](int n) { return kfrag(sc, LN, 16 * ti, 16 * n, l); }, m);
-        __syncthreads();
-        if (at_t.single < 0 && (flag || st.odd)) {
+        f32x4 acc, m;
+        for (;;) {  // again where the chunk is to be walked step by step
+            __syncthreads();
+            float bad = 0.0f;
+            rx.store(sx, LP, bad);
+            rb.store(sb, LN, bad);
+            rc.store(sc, LN, bad);
+            if (on) stage_state<T, TILES>(S, ss, LN, 16 * wp, n_own, l);
+            if (bad != bad) flag = 1;
+            __syncthreads();
+            acc = m = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l);
+            acc = product<T, WORDS, NT, true>([&](int n) { return kfrag(ss, LN, 16 * wp, 16 * n, l); },
+                                              [&](int n) { return kfrag(sc, LN, 16 * half, 16 * n, l); }, acc);
+            if (w < 3)
+                m = product<T, ROWS, NT>([&](int n) { return kfrag(sb, LN, 16 * si, 16 * n, l); },
+                                         [&](int n) { return kfrag(sc, LN, 16 * ti, 16 * n, l); }, m);
+            __syncthreads();
+            if (at_t.single >= 0 || !(flag || st.odd)) break;
             at_t.split();
             load();
-            continue;
         }
         const int t0 = at_t.t, len = at_t.len;
         bool whole;
@@ -609,18 +610,18 @@ __device__ __forceinline__ void segment_state(const ScanView& s, float* sb, floa
         if (w == 7) steps(0);
     }
     while (more) {
-        __syncthreads();
-        float bad = 0.0f;
-        rx.store(sx, LP, bad);
-        rb.store(sb, LN, bad);
-        if (bad != bad) flag = 1;
-        __syncthreads();
-        if (at_t.single < 0 && (flag || st[turn].odd)) {
+        for (;;) {  // again where the chunk is to be walked step by step
+            __syncthreads();
+            float bad = 0.0f;
+            rx.store(sx, LP, bad);
+            rb.store(sb, LN, bad);
+            if (bad != bad) flag = 1;
+            __syncthreads();
+            if (at_t.single >= 0 || !(flag || st[turn].odd)) break;
             REV ? at_t.split_back() : at_t.split();
             load();
             __syncthreads();  // everyone has read st[turn]
             if (w == 7) steps(turn);
-            continue;
         }
         bool whole;
         more = REV ? at_t.next_back(whole) : at_t.next(whole);
@@ -862,43 +863,47 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         // what the lane number decides is decided again for every chunk: kept over the
         // loop it took more scalar registers than there are
         const int l = opaque(lane), lg = l >> 4, lc = l & 15;
-        if (at_t.single >= 0 && on) plain_walk(S, at_t.chunk(), at_t.t);
-        __syncthreads();
-        stage_in(l);
-        float bad = 0.0f;
-        ry.store(sdy, LP, bad);
-        rc.store(sc, LN, bad);
-        float pass = 0.0f;  // <R, S>, from the state before to the one behind
-        if (on) {
-            stage_state<float, TILES>(R, sr, LN, 16 * wp, n_own, l);
-            stage_state<float, TILES>(S, ss, LN, 16 * wp, n_own, l);
-#pragma unroll
-            for (int n = 0; n < TILES; ++n) pass += (R[n][0] * S[n][0] + R[n][1] * S[n][1]) + (R[n][2] * S[n][2] + R[n][3] * S[n][3]);
-        }
-        if (bad != bad) flag = 1;
-        __syncthreads();
         // What needs no decays, beside the decays: the tiles with s <= t of c_t . b_s
         // (waves 0 .. 2) and dy_t . x_s (3 .. 5); rows = s, columns = t.
         const int tile = w < 3 ? w : w - 3, si = tile >> 1, ti = tile > 0;
         const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
-        f32x4 f{0.0f, 0.0f, 0.0f, 0.0f};
-        if (w < 3) {
-            f = product<T, ROWS, NT>([&](int n) { return kfrag(sb, LN, 16 * si, 16 * n, l); },
-                                     [&](int n) { return kfrag(sc, LN, 16 * ti, 16 * n, l); }, f);
-        } else if (w < 6) {
-            f = product<T, ROWS, PW / 16>([&](int n) { return kfrag(sx, LP, 16 * si, 16 * n, l); },
-                                          [&](int n) { return kfrag(sdy, LP, 16 * ti, 16 * n, l); }, f);
-        } else if (w == 7) {
-            steps(st, l);
-        } else if (past_len) {
-            finish(l);
-        }
-        __syncthreads();
-        if (at_t.single < 0 && (flag || st.odd)) {
+        f32x4 f;
+        float pass;
+        // (Again with a chunk's last step where it is to be walked step by step: in this
+        // small loop, or the other loop's registers would be copied at its end, and waited for.)
+        for (;;) {
+            if (at_t.single >= 0 && on) plain_walk(S, at_t.chunk(), at_t.t);
+            __syncthreads();
+            stage_in(l);
+            float bad = 0.0f;
+            ry.store(sdy, LP, bad);
+            rc.store(sc, LN, bad);
+            pass = 0.0f;  // <R, S>, from the state before to the one behind
+            if (on) {
+                stage_state<float, TILES>(R, sr, LN, 16 * wp, n_own, l);
+                stage_state<float, TILES>(S, ss, LN, 16 * wp, n_own, l);
+#pragma unroll
+                for (int n = 0; n < TILES; ++n) pass += (R[n][0] * S[n][0] + R[n][1] * S[n][1]) + (R[n][2] * S[n][2] + R[n][3] * S[n][3]);
+            }
+            if (bad != bad) flag = 1;
+            __syncthreads();
+            f = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (w < 3) {
+                f = product<T, ROWS, NT>([&](int n) { return kfrag(sb, LN, 16 * si, 16 * n, l); },
+                                         [&](int n) { return kfrag(sc, LN, 16 * ti, 16 * n, l); }, f);
+            } else if (w < 6) {
+                f = product<T, ROWS, PW / 16>([&](int n) { return kfrag(sx, LP, 16 * si, 16 * n, l); },
+                                              [&](int n) { return kfrag(sdy, LP, 16 * ti, 16 * n, l); }, f);
+            } else if (w == 7) {
+                steps(st, l);
+            } else if (past_len) {
+                finish(l);
+            }
+            __syncthreads();
+            if (at_t.single >= 0 || !(flag || st.odd)) break;
             at_t.split_back();
             load();
             load_s();
-            continue;
         }
         const int t0 = at_t.t, len = at_t.len;
         bool whole;
