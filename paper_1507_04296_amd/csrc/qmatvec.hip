@@ -15,9 +15,10 @@
 // their codes, so that each instruction reduces over one run of 32, in one group.
 //
 // Code c as bf16 is 1 + c / 16 = 0x3f80 | c << 3: the weight is 16 (that - 1.5), and
-// the sum of 1.5 x comes from the same instruction with a constant operand.  (128 + c needs no shifts, but its sums cancel 30 times their
-// rounding instead of 5.)  fp32 rows are three exact bf16 terms, bf16 rows one; 8-bit
-// rows take the integer instruction, whose sums are exact, with c and 8.
+// the sum of 1.5 x comes from the same instruction with a constant operand.  (128 + c
+// needs no shifts, but its sums cancel 30 times their rounding instead of 5.)  fp32
+// rows are three exact bf16 terms, bf16 rows one; 8-bit rows take the integer
+// instruction, whose sums are exact, with c and 8.
 //
 // The waves of a workgroup share the outputs and split the inputs; their sums are
 // added in LDS, in order.
