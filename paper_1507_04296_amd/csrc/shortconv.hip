@@ -1,17 +1,18 @@
 // The short causal convolution (gorila_causal_conv, _backward, _step).
 //
-// Memory bound.  A lane takes four channels (one, where quads are not aligned) and
-// walks a run of steps with the last taps in a ring of registers, the loads of the next
-// four steps ahead of it, so a value is read once (and once more by the next run's
-// lane, from the cache).  A wave has one run, so that its steps, episode starts and
+// Memory bound.  A lane takes four channels (backward two; one, where quads are not
+// aligned) and walks a run of steps with the last taps in a ring of registers, the
+// loads of the next four steps ahead of it, so a value is read once (and once more by
+// the next run's lane, from the cache).  A wave has one run, so that its steps, episode starts and
 // addresses are scalars: with runs that differ in a wave, the address arithmetic and
 // the masks were twice the convolution, and a wait for every step's reset cost 0.5 us a
 // step.  An episode start empties the ring: nothing before it is multiplied, whatever
 // it holds.
 //
-// 32 sequences of 128 steps, 1152 channels, fp32: 10.7 us forward (3.5 TB/s), 24.7 us
-// backward with the sums of the workgroups' gradients of the taps (2.3 TB/s; two waves
-// a SIMD, by its registers).  1 x 8192 steps: 18.3 and 46.2 us.
+// 32 sequences of 128 steps, 1152 channels, fp32: 10.6 us forward (3.6 TB/s), 23.2 us
+// backward with the sums of the workgroups' gradients of the taps (2.4 TB/s).  1 x 8192
+// steps: 18.3 and 42.7 us.  Backward, 4 x 2000 steps, 2304 channels, bf16: 56.6 us with
+// two channels a lane, 70.9 with four (half the waves, 192 registers), 64.3 with one.
 #include "seq.h"
 
 namespace gorila {
@@ -19,6 +20,7 @@ namespace {
 
 constexpr int RUN = 8;          // steps a lane, forward
 constexpr int BACK_RUN = 16;    // and backward, which walks K - 1 more
+constexpr int BACK_W = 2;      // channels a lane, backward
 constexpr int MAX_TAPS = 4;
 constexpr int MAX_PARTS = 512;  // of the weight gradient's sums
 
@@ -33,28 +35,40 @@ struct ConvView {
     float* sums;
 };
 
-// W channels from p (a quad, or one value in element 0).
-template <bool VEC, class T>
-__device__ __forceinline__ f32x4 get(const T* p) {
-    return VEC ? row_load4(p) : f32x4{row_value(p[0]), 0.0f, 0.0f, 0.0f};
+// W channels (1, 2 or 4) from p.
+template <int W> using Vec = float __attribute__((ext_vector_type(W)));
+template <int W, class T>
+__device__ __forceinline__ Vec<W> get(const T* p) {
+    constexpr bool F = std::is_same<T, float>::value;
+    if constexpr (W == 4) return row_load4(p);
+    else if constexpr (W == 2 && F) return *(const Vec<2>*)p;
+    else if constexpr (W == 2) {
+        const uint32_t v = *(const uint32_t*)p;
+        return Vec<2>{__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)};
+    } else {
+        Vec<1> v;
+        v[0] = row_value(p[0]);
+        return v;
+    }
 }
-template <bool VEC, class T>
-__device__ __forceinline__ void put(T* p, f32x4 v) {
-    if (VEC) row_store4(p, v);
+template <int W, class T>
+__device__ __forceinline__ void put(T* p, Vec<W> v) {
+    constexpr bool F = std::is_same<T, float>::value;
+    if constexpr (W == 4) row_store4(p, v);
+    else if constexpr (W == 2 && F) *(Vec<2>*)p = v;
+    else if constexpr (W == 2) *(uint32_t*)p = (uint32_t)row_round<uint16_t>(v[0]) | (uint32_t)row_round<uint16_t>(v[1]) << 16;
     else p[0] = row_round<T>(v[0]);
 }
-constexpr f32x4 ZERO4{0.0f, 0.0f, 0.0f, 0.0f};
 
-template <int K, bool VEC>
-__device__ __forceinline__ void load_taps(const ConvView& s, int c, f32x4 (&w)[K], f32x4& bias) {
-    constexpr int W = VEC ? 4 : 1;
+template <int K, int W>
+__device__ __forceinline__ void load_taps(const ConvView& s, int c, Vec<W> (&w)[K], Vec<W>& bias) {
 #pragma unroll
     for (int j = 0; j < K; ++j) {
-        w[j] = ZERO4;
+        w[j] = Vec<W>(0.0f);
 #pragma unroll
         for (int i = 0; i < W; ++i) w[j][i] = s.weight[(int64_t)(c + i) * K + j];
     }
-    bias = s.bias ? get<VEC>(s.bias + c) : ZERO4;
+    bias = s.bias ? get<W>(s.bias + c) : Vec<W>(0.0f);
 }
 
 // The steps that a walk loads ahead: whole turns of the ring of K.
@@ -69,17 +83,17 @@ __device__ __forceinline__ uint64_t starts_from(const uint8_t* rs, int t, int T)
 
 // Ring places of the K - 1 steps before t0 (step t at place (t - t0) mod K): their
 // values, or zeros where an episode starts behind them.  starts: from t0 - (K - 1) on.
-template <class T, int K, bool VEC>
-__device__ __forceinline__ void load_past(const ConvView& s, int b, int c, int t0, const T* x, uint64_t starts, f32x4 (&e)[K]) {
-    e[0] = ZERO4;
+template <class T, int K, int W>
+__device__ __forceinline__ void load_past(const ConvView& s, int b, int c, int t0, const T* x, uint64_t starts, Vec<W> (&e)[K]) {
+    e[0] = Vec<W>(0.0f);
 #pragma unroll
     for (int j = 1; j < K; ++j) {  // step t0 - j
         const int t = t0 - j;
-        f32x4 v = ZERO4;
+        Vec<W> v = Vec<W>(0.0f);
         const uint64_t behind = (starts >> (K - j)) & ((1ull << (j - 1)) - 1);  // steps t + 1 .. t0 - 1
         if (!behind) {
-            if (t >= 0) v = get<VEC>(x + (int64_t)t * s.xt);
-            else if (s.window) v = get<VEC>((const T*)s.window + ((int64_t)b * (K - 1) + K - 1 + t) * s.C + c);
+            if (t >= 0) v = get<W>(x + (int64_t)t * s.xt);
+            else if (s.window) v = get<W>((const T*)s.window + ((int64_t)b * (K - 1) + K - 1 + t) * s.C + c);
         }
         e[K - j] = v;
     }
@@ -91,9 +105,9 @@ __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f));
 }
 
-template <class T, int K, bool VEC>
+template <class T, int K, int W>
 __global__ __launch_bounds__(256) void conv_kernel(ConvView s) {
-    constexpr int W = VEC ? 4 : 1, A = ahead<K>();
+    constexpr int A = ahead<K>();
     const int unit = (int)(blockIdx.x / (unsigned)s.blocks), run = unit % s.runs, b = unit / s.runs;
     const int quad = (int)(blockIdx.x % (unsigned)s.blocks) * (int)blockDim.x + (int)threadIdx.x;
     const int t0 = run * RUN, t1 = t0 + RUN < s.T ? t0 + RUN : s.T;
@@ -102,12 +116,12 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvView s) {
     const int c = quad * W;
     const T* x = (const T*)s.x + b * s.xb + c;
     T* y = (T*)s.y + (int64_t)b * s.T * s.C + c;
-    f32x4 w[K], bias, e[K], now[A], next[A];
-    load_taps<K, VEC>(s, c, w, bias);
-    load_past<T, K, VEC>(s, b, c, t0, x, starts, e);
-    auto load = [&](int t, f32x4 (&v)[A]) {  // steps past the run's take its last one's place
+    Vec<W> w[K], bias, e[K], now[A], next[A];
+    load_taps<K, W>(s, c, w, bias);
+    load_past<T, K, W>(s, b, c, t0, x, starts, e);
+    auto load = [&](int t, Vec<W> (&v)[A]) {  // steps past the run's take its last one's place
 #pragma unroll
-        for (int u = 0; u < A; ++u) v[u] = get<VEC>(x + (int64_t)(t + u < t1 ? t + u : t1 - 1) * s.xt);
+        for (int u = 0; u < A; ++u) v[u] = get<W>(x + (int64_t)(t + u < t1 ? t + u : t1 - 1) * s.xt);
     };
     if (t0 < t1) load(t0, now);
     for (int tb = t0; tb < t1; tb += A) {
@@ -118,17 +132,17 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvView s) {
             if (t < t1) {
                 if (starts >> (t - t0 + K - 1) & 1u) {
 #pragma unroll
-                    for (int j = 0; j < K; ++j) e[j] = ZERO4;
+                    for (int j = 0; j < K; ++j) e[j] = Vec<W>(0.0f);
                 }
                 e[u % K] = now[u];
-                f32x4 v = bias;
+                Vec<W> v = bias;
 #pragma unroll
                 for (int j = 0; j < K; ++j) v += w[j] * e[(u + 1 + j) % K];
                 if (s.silu) {
 #pragma unroll
                     for (int i = 0; i < W; ++i) v[i] *= sigmoid(v[i]);
                 }
-                put<VEC>(y + (int64_t)t * s.C, v);
+                put<W>(y + (int64_t)t * s.C, v);
             }
             now[u] = next[u];
         }
@@ -137,11 +151,11 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvView s) {
         const int n = t1 - t0;
 #pragma unroll
         for (int j = 0; j < K - 1; ++j) {
-            f32x4 v = ZERO4;
+            Vec<W> v = Vec<W>(0.0f);
 #pragma unroll
             for (int i = 0; i < K; ++i)
                 if ((n - (K - 1) + j + K) % K == i) v = e[i];
-            put<VEC>((T*)s.window_out + ((int64_t)b * (K - 1) + j) * s.C + c, v);
+            put<W>((T*)s.window_out + ((int64_t)b * (K - 1) + j) * s.C + c, v);
         }
     }
 }
@@ -150,17 +164,17 @@ __global__ __launch_bounds__(256) void conv_kernel(ConvView s) {
 // forms the gradient of v for its steps and the K - 1 after them, and keeps the sums of
 // dx of the last K steps in a ring.  A step's is written when its last tap has passed,
 // or an episode starts.
-template <class T, int K, bool VEC>
+template <class T, int K, int W>
 __global__ __launch_bounds__(256) void conv_backward_kernel(ConvView s) {
-    constexpr int W = VEC ? 4 : 1, A = ahead<K>();
+    constexpr int A = ahead<K>();
     static_assert(BACK_RUN + 2 * (K - 1) <= 64, "a bit a step");
     const int part = (int)(blockIdx.x / (unsigned)s.blocks);
     const int quad = (int)(blockIdx.x % (unsigned)s.blocks) * (int)blockDim.x + (int)threadIdx.x;
     const int c = (quad < s.quads ? quad : 0) * W;
-    f32x4 w[K], bias, dw[K], db = ZERO4;
-    load_taps<K, VEC>(s, c, w, bias);
+    Vec<W> w[K], bias, dw[K], db = Vec<W>(0.0f);
+    load_taps<K, W>(s, c, w, bias);
 #pragma unroll
-    for (int j = 0; j < K; ++j) dw[j] = ZERO4;
+    for (int j = 0; j < K; ++j) dw[j] = Vec<W>(0.0f);
     for (int unit = part; unit < s.B * s.runs; unit += s.parts) {
         const int run = unit % s.runs, b = unit / s.runs;
         const int t0 = run * BACK_RUN, t1 = t0 + BACK_RUN < s.T ? t0 + BACK_RUN : s.T;
@@ -172,29 +186,29 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvView s) {
         T* dx = (T*)s.dx + (int64_t)b * s.T * s.C + c;
         const T* dwo = s.dwindow_out ? (const T*)s.dwindow_out + (int64_t)b * (K - 1) * s.C + c : nullptr;
         T* dwi = s.dwindow ? (T*)s.dwindow + (int64_t)b * (K - 1) * s.C + c : nullptr;
-        f32x4 e[K], d[K], xs[A], gs[A], nx[A], ng[A];  // rings: step t at place (t - t0) mod K
-        load_past<T, K, VEC>(s, b, c, t0, x, starts, e);
+        Vec<W> e[K], d[K], xs[A], gs[A], nx[A], ng[A];  // rings: step t at place (t - t0) mod K
+        load_past<T, K, W>(s, b, c, t0, x, starts, e);
 #pragma unroll
-        for (int j = 0; j < K; ++j) d[j] = ZERO4;
+        for (int j = 0; j < K; ++j) d[j] = Vec<W>(0.0f);
         const int end = t1 + K - 1, most = (end < s.T ? end : s.T) - 1;
-        auto load = [&](int t, f32x4 (&vx)[A], f32x4 (&vg)[A]) {
+        auto load = [&](int t, Vec<W> (&vx)[A], Vec<W> (&vg)[A]) {
 #pragma unroll
             for (int u = 0; u < A; ++u) {
                 const int at = t + u < most ? t + u : most;
-                vx[u] = get<VEC>(x + (int64_t)at * s.xt);
-                vg[u] = get<VEC>(dy + (int64_t)at * s.dyt);
+                vx[u] = get<W>(x + (int64_t)at * s.xt);
+                vg[u] = get<W>(dy + (int64_t)at * s.dyt);
             }
         };
         int done = run == 0 ? -(K - 1) : t0;  // the next step to write; of the first run, the window's before
         // Writes step `at` if it is this run's; the window behind the sequence adds its
         // gradient where no episode starts after it.
-        auto write = [&](int at, f32x4 v) {
+        auto write = [&](int at, Vec<W> v) {
             if (at < done || at >= t1) return;
             done = at + 1;
             const int k = at - (s.T - (K - 1));  // its place in the window behind
-            if (dwo && k >= 0 && !(tail >> (k + 1))) v += get<VEC>(dwo + (int64_t)k * s.C);
-            if (at >= 0) put<VEC>(dx + (int64_t)at * s.C, v);
-            else if (dwi) put<VEC>(dwi + (int64_t)(at + K - 1) * s.C, v);
+            if (dwo && k >= 0 && !(tail >> (k + 1))) v += get<W>(dwo + (int64_t)k * s.C);
+            if (at >= 0) put<W>(dx + (int64_t)at * s.C, v);
+            else if (dwi) put<W>(dwi + (int64_t)(at + K - 1) * s.C, v);
         };
         if (s.T > 0) load(t0, xs, gs);
         for (int tb = t0; tb < end; tb += A) {
@@ -208,12 +222,12 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvView s) {
 #pragma unroll
                             for (int j = K - 1; j >= 1; --j) write(t - j, d[(u + K - j) % K]);
 #pragma unroll
-                            for (int j = 0; j < K; ++j) e[j] = ZERO4;
+                            for (int j = 0; j < K; ++j) e[j] = Vec<W>(0.0f);
                         }
                         e[u % K] = xs[u];
-                        f32x4 dv = gs[u];
+                        Vec<W> dv = gs[u];
                         if (s.silu) {
-                            f32x4 v = bias;
+                            Vec<W> v = bias;
 #pragma unroll
                             for (int j = 0; j < K; ++j) v += w[j] * e[(u + 1 + j) % K];
 #pragma unroll
@@ -227,11 +241,11 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvView s) {
 #pragma unroll
                             for (int j = 0; j < K; ++j) dw[j] += dv * e[(u + 1 + j) % K];
                         }
-                        d[u % K] = ZERO4;
+                        d[u % K] = Vec<W>(0.0f);
 #pragma unroll
                         for (int j = 0; j < K; ++j) d[(u + 1 + j) % K] += w[j] * dv;
                     } else {
-                        d[u % K] = ZERO4;
+                        d[u % K] = Vec<W>(0.0f);
                     }
                     write(t - (K - 1), d[(u + 1) % K]);  // its last tap has passed
                 }
@@ -243,13 +257,12 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvView s) {
     if (quad >= s.quads) return;
     float* o = s.sums + part * (int64_t)s.C * (K + 1);
 #pragma unroll
-    for (int j = 0; j < K; ++j) put<VEC>(o + (int64_t)j * s.C + c, dw[j]);  // [taps][channels]
-    put<VEC>(o + (int64_t)K * s.C + c, db);
+    for (int j = 0; j < K; ++j) put<W>(o + (int64_t)j * s.C + c, dw[j]);  // [taps][channels]
+    put<W>(o + (int64_t)K * s.C + c, db);
 }
 
-template <class T, int K, bool VEC>
+template <class T, int K, int W>
 __global__ __launch_bounds__(256) void conv_step_kernel(ConvView s, T* pool, int64_t slots, const int32_t* slot, unsigned* err) {
-    constexpr int W = VEC ? 4 : 1;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int c = (int)(id % s.quads) * W;
     const int64_t row = id / s.quads;
@@ -262,22 +275,22 @@ __global__ __launch_bounds__(256) void conv_step_kernel(ConvView s, T* pool, int
     }
     const bool empty = out || (s.reset && s.reset[row]);
     T* p = pool + at * (K - 1) * s.C + c;
-    f32x4 w[K], bias, e[K];
-    load_taps<K, VEC>(s, c, w, bias);
+    Vec<W> w[K], bias, e[K];
+    load_taps<K, W>(s, c, w, bias);
 #pragma unroll
-    for (int j = 0; j < K - 1; ++j) e[j] = empty ? ZERO4 : get<VEC>(p + (int64_t)j * s.C);
-    e[K - 1] = get<VEC>((const T*)s.x + row * s.xb + c);
-    f32x4 v = bias;
+    for (int j = 0; j < K - 1; ++j) e[j] = empty ? Vec<W>(0.0f) : get<W>(p + (int64_t)j * s.C);
+    e[K - 1] = get<W>((const T*)s.x + row * s.xb + c);
+    Vec<W> v = bias;
 #pragma unroll
     for (int j = 0; j < K; ++j) v += w[j] * e[j];
     if (s.silu) {
 #pragma unroll
         for (int i = 0; i < W; ++i) v[i] *= sigmoid(v[i]);
     }
-    put<VEC>((T*)s.y + row * s.C + c, v);
+    put<W>((T*)s.y + row * s.C + c, v);
     if (!out) {
 #pragma unroll
-        for (int j = 0; j < K - 1; ++j) put<VEC>(p + (int64_t)j * s.C, e[j + 1]);
+        for (int j = 0; j < K - 1; ++j) put<W>(p + (int64_t)j * s.C, e[j + 1]);
     }
 }
 
@@ -341,7 +354,7 @@ int gorila_causal_conv(const gorila_causal_conv_args* args, void* y, void* windo
     v.quads = vec ? v.C / 4 : v.C;
     const int threads = run_threads(v);
     by_taps(args->taps, args->dtype, vec, [&](auto t, auto k, auto al) {
-        conv_kernel<decltype(t), decltype(k)::value, decltype(al)::value>
+        conv_kernel<decltype(t), decltype(k)::value, decltype(al)::value ? 4 : 1>
             <<<(unsigned)(v.B * v.runs * v.blocks), threads, 0, c.stream>>>(v);
     });
     return launched();
@@ -372,7 +385,7 @@ int gorila_causal_conv_backward(const gorila_causal_conv_args* args, const void*
           at_four(dwindow, e);
     v.dy = dy, v.dyb = dy_batch_stride, v.dyt = dy_step_stride;
     v.dwindow_out = dwindow_out, v.dx = dx, v.dwindow = dwindow;
-    v.quads = vec ? v.C / 4 : v.C;
+    v.quads = vec ? v.C / BACK_W : v.C;
     const int threads = run_threads(v);
     v.sums = (float*)c.ws;
     v.runs = v.T > 0 ? (v.T + BACK_RUN - 1) / BACK_RUN : 1;
@@ -380,7 +393,7 @@ int gorila_causal_conv_backward(const gorila_causal_conv_args* args, const void*
     v.parts = (int)(units < MAX_PARTS ? units : MAX_PARTS);
     if (v.parts > 0)
         by_taps(args->taps, args->dtype, vec, [&](auto t, auto k, auto al) {
-            conv_backward_kernel<decltype(t), decltype(k)::value, decltype(al)::value>
+            conv_backward_kernel<decltype(t), decltype(k)::value, decltype(al)::value ? BACK_W : 1>
                 <<<(unsigned)(v.parts * v.blocks), threads, 0, c.stream>>>(v);
         });
     launch_sum_parts(v.sums, v.parts, (int64_t)cols, (int64_t)v.C * args->taps, args->taps, dweight, dbias, c.stream);
@@ -404,7 +417,7 @@ int gorila_causal_conv_step(const gorila_causal_conv_args* args, void* window_po
     v.quads = vec ? v.C / 4 : v.C;
     by_taps(args->taps, args->dtype, vec, [&](auto t, auto k, auto al) {
         using T = decltype(t);
-        conv_step_kernel<T, decltype(k)::value, decltype(al)::value>
+        conv_step_kernel<T, decltype(k)::value, decltype(al)::value ? 4 : 1>
             <<<lanes_grid((int64_t)v.B * v.quads), 256, 0, c.stream>>>(v, (T*)window_pool, slots, slot, c.err);
     });
     return launched();
