@@ -32,8 +32,9 @@
 // forward, seven backward with the states before the chunks walked again), not the
 // matrix unit or memory: fp32, 32 x 128 steps, 16 heads of 64, state 64: forward 28 us,
 // backward 71 us + 8 us for the sums over heads, the matrix unit busy a third of the
-// time.  bf16, 4 x 1999 steps, state 128: states 21 us, joins 9 us, forward 50 us;
-// backward 194 us (one workgroup a compute unit, by its LDS), sums 26 us (131 MB).
+// time.  bf16, 4 x 1999 steps, state 128: states 28 us (47 of both directions),
+// joins 9 us (14), forward 50 us; backward 194 us (one workgroup a compute unit, by its
+// LDS), sums 26 us (131 MB).
 // Chunks of 32 steps: with 64, the products inside the chunk double and LDS holds one
 // workgroup a compute unit at every state size.
 //
