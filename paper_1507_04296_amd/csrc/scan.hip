@@ -35,8 +35,8 @@
 // time.  bf16, 4 x 1999 steps, state 128: states 28 us (47 of both directions),
 // joins 9 us (14), forward 50 us; backward 194 us (one workgroup a compute unit, by its
 // LDS), sums 26 us (131 MB).
-// Chunks of 32 steps: with 64, the products inside the chunk double and LDS holds one
-// workgroup a compute unit at every state size.
+// Chunks of 32 steps: with 64, the products inside a chunk double a step, and the
+// backward's LDS holds one workgroup a compute unit at state 64 too.
 //
 // Masked products multiply by zero, which is no mask for infinities and NaN, so a
 // chunk that holds any is walked one step at a time.
