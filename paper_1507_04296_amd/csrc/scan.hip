@@ -297,7 +297,7 @@ struct Steps {
     float from[Q], to[Q];  // e^G_t from the state before, e^(G_end - G_t) to the one behind; 0 in another episode
     int ep[Q];             // -1: past the end
     float all;             // from the state before to the one behind
-    int starts;            // an episode starts in it
+    int last;              // episode of its end; not 0: one starts in it
     int odd;               // a step size is not finite
 };
 __device__ __forceinline__ float pow2(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -354,13 +354,15 @@ template <class T> struct StepRegs {  // as they are in memory: a value that is 
         if (l == 0) {
             s.odd = odd;
             s.all = end_ep == 0 ? pow2(end_gi + end_gf) : 0.0f;
-            s.starts = end_ep != 0;
+            s.last = end_ep;
         }
     }
 };
 
-// v times a factor of a Steps, where a zero one is a mask whatever v is.
-__device__ __forceinline__ f32x4 masked(f32x4 v, float f) { return f != 0.0f ? v * f : f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
+// v times a factor of a Steps where both are of one episode, else 0 whatever v is.  The
+// factor itself is no mask: it is also zero where a decay is too small for it, and there
+// a v that is not finite stays so.
+__device__ __forceinline__ f32x4 masked(f32x4 v, float f, bool one_episode) { return one_episode ? v * f : f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 
 // State tiles of a wave: the half h of NT (all of one).
 template <int NT> struct Half {
@@ -376,8 +378,9 @@ template <int NT> struct Half {
 template <class T, int TILES, bool AFTER>
 __device__ __forceinline__ void walk(f32x4 (&acc)[TILES], const float* m, int ldm, const float* ch, const Steps& st, int l) {
     const float all = st.all;
+    const bool starts = st.last != 0;
 #pragma unroll
-    for (int n = 0; n < TILES; ++n) acc[n] = masked(acc[n], all);
+    for (int n = 0; n < TILES; ++n) acc[n] = masked(acc[n], all, !starts);
     if (!AFTER && st.ep[0] != 0) return;  // an episode starts with the chunk
     f32x4 v[Q / 16];
 #pragma unroll
@@ -559,7 +562,7 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
         bool whole;
         more = at_t.next(whole);
         if (more) load();
-        acc = masked(acc, st.from[t]);
+        acc = masked(acc, st.from[t], st.ep[t] == 0);
         if (w < 3) {  // decay * (c_t . b_s) * d_s
             const int tm = 16 * ti + lc, q0 = 16 * si + 4 * lg;
             const float gi_t = st.gi[tm], gf_t = st.gf[tm];
@@ -639,7 +642,7 @@ __device__ __forceinline__ void segment_state(const ScanView& s, float* sb, floa
         more = REV ? at_t.next_back(whole) : at_t.next(whole);
         if (more) load();
         decay *= st[turn].all;
-        starts |= st[turn].starts != 0;
+        starts |= st[turn].last != 0;
         if (on) walk<T, TILES, !REV>(S, sb + n_own, LN, sx + 16 * wp, st[turn], l);
         if (more && w == 7) steps(turn ^ 1);
         turn ^= 1;
@@ -948,17 +951,18 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
             const bool of_r = NT == 8 ? u : w >= NT;
             const int n = NT == 8 ? w : w % NT;
             const float *m = of_r ? sr : ss, *rows = of_r ? sx : sdy, *by = of_r ? st.to : st.from;
+            const int ep = of_r ? st.last : 0;
             ja[u][0] = ja[u][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if (w < 2 * NT)
                 product_pair<T, PW / 16>([&](int k) { return rfrag(m, LN, 16 * k, 16 * n, l); },
                                          [&](int i, int k) { return kfrag(rows, LP, 16 * i, 16 * k, l); }, ja[u]);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) ja[u][i] = masked(ja[u][i], by[16 * i + lc]);
+            for (int i = 0; i < 2; ++i) ja[u][i] = masked(ja[u][i], by[16 * i + lc], st.ep[16 * i + lc] == ep);
         }
         if (on)
             product_pair<T, TILES>([&](int n) { return R[n]; }, [&](int i, int n) { return kfrag(sb, LN, 16 * i, n_own + 16 * n, l); }, xa);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) xa[i] = masked(xa[i], st.to[16 * i + lc]);
+        for (int i = 0; i < 2; ++i) xa[i] = masked(xa[i], st.to[16 * i + lc], st.ep[16 * i + lc] == st.last);
         __syncthreads();
         if (w >= 3 && w < 6) {  // what passes from s to t: M F d without F's decay, summed for every step between
             const f32x4 v = *(const f32x4*)(sm + tm * LQ + q0) * f * *(const f32x4*)(st.d + q0);
@@ -1048,7 +1052,7 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
         }
         if (w == 6) {
             past_d = st.d[l & (Q - 1)];
-            past_all = st.starts ? -1.0f : st.all;
+            past_all = st.last ? -1.0f : st.all;
             past_t = t0;
             past_len = len;
         }

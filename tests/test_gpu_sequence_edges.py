@@ -1,0 +1,43 @@
+"""The sequence operators at the ends of their ranges.  Tolerances are those of
+test_gpu_sequence.py where nothing else is said."""
+import pytest
+import torch
+
+import sequence_ref as ref
+from test_gpu_sequence import BF16, F32, ctx, g, rand, scan_inputs  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+def same_finite(got, want, what):
+    assert torch.equal(torch.isfinite(got.cpu()), torch.isfinite(want.cpu())), f"{what}: other values are finite"
+
+
+@pytest.mark.parametrize("value", [NAN, INF])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,H,N", [(1, 100, 2, 20), (32, 100, 16, 20), (2, 90, 3, 100)])
+def test_scan_decay_of_zero_is_no_episode_start(g, ctx, B, T, H, N, dtype, value):  # noqa: F811
+    """Steps so large that a chunk's decay is zero in 32 bits: what is not finite stays in its episode all the same,
+    however the sequence is cut, as in single steps."""
+    P = 4
+    i = scan_inputs(B, T, H, P, 1, N, dtype)
+    i["dt"] += 3
+    i["a_log"][:] = 1.5
+    state, ds = rand(B, H, P, N, seed=20), rand(B, H, P, N, seed=22)
+    state[0, 0, 1, 2] = value
+    y, end = g.scan(ctx, **i, state=state)
+    wy, wend = ref.scan(**i, state=state)
+    same_finite(y, wy, "y")
+    same_finite(end, wend, "state")
+    pool = state.clone()
+    for t in range(T):
+        one = {k: v[:, t] if v.dim() > 2 else v for k, v in i.items()}
+        same_finite(g.scan_step(ctx, **one, state_pool=pool), y[:, t], "step")
+    same_finite(pool, end, "steps")
+    dy = rand(B, T, H, P, dtype=dtype, seed=21)
+    names = ("dx", "ddt", "db", "dc", "da_log", "ddt_bias", "dskip", "dstate")
+    for s, d in ((state, ds), (ds, state)):
+        got, want = g.scan_backward(ctx, dy, **i, state=s, dstate_out=d), ref.scan_backward(dy, **i, state=s, dstate=d)
+        for n, p in zip(names, got):
+            same_finite(p, want[n], n)
