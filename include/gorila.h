@@ -436,7 +436,10 @@ int gorila_causal_conv_step(const gorila_causal_conv_args* args, void* window_po
  * [batch][length][groups][state_dim], y as x; state and state_out
  * [batch][heads][head_dim][state_dim] (NULL: zeros / not wanted; state_out may be
  * state).  head_dim and state_dim 1 .. 128 (else GORILA_EUNSUPPORTED).  Uses
- * gorila_scan_workspace_bytes(..., backward) of the workspace (0: none). */
+ * gorila_scan_workspace_bytes(..., backward) of the workspace (0: none), which is
+ * enough for every smaller batch and length too (few sequences are cut into segments,
+ * many are not).  A forward call of up to 128 steps never needs any: it is not cut
+ * where the workspace has no place for the segments' states. */
 typedef struct {
     int32_t dtype, batch, length, heads, head_dim, groups, state_dim, reserved;
     const void* x;

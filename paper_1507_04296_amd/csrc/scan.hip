@@ -1186,9 +1186,12 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanView s, float* pool,
 
 // ---- host ----
 
-
 // Segments a sequence is cut into: none where the (sequence, head, channels) fill
 // the chip, else enough for two workgroups a compute unit, of one chunk at least.
+constexpr int FULL = 512;  // workgroups that fill it
+// Chunks of sequences that a forward call walks in one segment where the workspace has
+// no place for more: the contexts of uncut calls have none, and take smaller ones too.
+constexpr int SHORT = 4;
 struct Cut {
     int ptiles, vh, nch, cps, nseg;
     Cut(int B, int T, int H, int P) {
@@ -1196,30 +1199,42 @@ struct Cut {
         vh = H * ptiles;
         nch = (T + Q - 1) / Q;
         const int64_t groups = (int64_t)B * vh;
-        const int want = groups > 0 && groups < 512 ? (int)((512 + groups - 1) / groups) : 1;
+        const int want = groups > 0 && groups < FULL ? (int)((FULL + groups - 1) / groups) : 1;
         nseg = want < nch ? want : nch;
         if (nseg < 1) nseg = 1;
         cps = nch > 0 ? (nch + nseg - 1) / nseg : 1;
         nseg = nch > 0 ? (nch + cps - 1) / cps : 1;
     }
+    void whole() { nseg = 1, cps = nch > 0 ? nch : 1; }
+    // Segments of B sequences that have states in the workspace.
+    size_t joined(int B) const { return nseg > 1 ? (size_t)B * nseg * vh : 0; }
+    // The most of them in any call of up to B sequences of up to nch chunks: calls of
+    // g < FULL workgroups are cut, into less than FULL + g segments in all.
+    size_t most_joined(int B) const {
+        const size_t groups = (size_t)B * vh, cut = groups < FULL ? groups : FULL - 1, all = cut * nch;
+        return nch <= 1 ? 0 : all < 2 * FULL ? all : 2 * FULL;
+    }
 };
 struct ScanPlan {
     size_t seg_s, seg_r, seg_a, chunk_s, pdb, pdc, pdt, ppar, total;
-    ScanPlan(const Cut& k, int B, int T, int N, bool backward) {
+    // joined: states of segments; walks: workgroups that walk one.
+    ScanPlan(const Cut& k, size_t joined, size_t walks, int B, int T, int N, bool backward) {
         size_t o = 0;
         auto take = [&](size_t floats) { size_t at = o; o += (floats * 4 + 255) / 256 * 256; return at; };
-        const size_t state = (size_t)PW * padded_state(N), segs = (size_t)B * k.nseg * k.vh, rows = (size_t)B * T * k.vh;
-        seg_s = take(k.nseg > 1 ? segs * state : 0);
-        seg_a = take(k.nseg > 1 ? segs : 0);
-        seg_r = take(backward && k.nseg > 1 ? segs * state : 0);
+        const size_t state = (size_t)PW * padded_state(N), rows = (size_t)B * T * k.vh;
+        seg_s = take(joined * state);
+        seg_a = take(joined);
+        seg_r = take(backward ? joined * state : 0);
         chunk_s = take(backward ? (size_t)B * k.nch * k.vh * state : 0);
         const size_t parts = backward ? (size_t)B * k.nch * k.vh * Q * padded_state(N) : 0;
         pdb = take(parts);
         pdc = take(parts);
         pdt = take(backward ? rows : 0);
-        ppar = take(backward ? segs * 3 : 0);
+        ppar = take(backward ? walks * 3 : 0);
         total = o;
     }
+    ScanPlan(const Cut& k, int B, int T, int N, bool backward)
+        : ScanPlan(k, k.joined(B), (size_t)B * k.nseg * k.vh, B, T, N, backward) {}
 };
 
 constexpr int MAX_WIDTH = 128, MAX_STATE = 128;
@@ -1283,7 +1298,11 @@ size_t gorila_scan_workspace_bytes(int32_t batch, int32_t length, int32_t heads,
                                    int32_t state_dim, int32_t backward) {
     if (batch < 0 || length < 0 || heads < 1 || heads > 65536 || groups < 1 || heads % groups) return 0;
     if (head_dim < 1 || head_dim > MAX_WIDTH || state_dim < 1 || state_dim > MAX_STATE) return 0;
-    const size_t own = ScanPlan(Cut(batch, length, heads, head_dim), batch, length, state_dim, backward != 0).total;
+    const Cut k(batch, length, heads, head_dim);
+    // enough for every smaller batch and length too, which may be cut where this is not
+    const bool exact = !backward && k.nch <= SHORT;
+    const size_t joined = exact ? k.joined(batch) : k.most_joined(batch), all = (size_t)batch * k.vh;
+    const size_t own = ScanPlan(k, joined, joined > all ? joined : all, batch, length, state_dim, backward != 0).total;
     return own ? WS_FIXED_BYTES + own : 0;
 }
 
@@ -1295,7 +1314,8 @@ int gorila_scan(const gorila_scan_args* args, void* y, float* state_out, gorila_
     if (rc || (rc = scan_view(args, false, v, vec))) return rc;
     if (v.B == 0 || (v.T == 0 && !state_out)) return GORILA_OK;
     if ((v.T > 0 && !y) || !at_element(y, dtype_bytes(args->dtype)) || !at_element(state_out, 4)) return GORILA_EINVAL;
-    const Cut k(v.B, v.T, v.H, v.P);
+    Cut k(v.B, v.T, v.H, v.P);
+    if (k.nch <= SHORT && ctx_view(ctx, ScanPlan(k, v.B, v.T, v.N, false).total, c) == GORILA_EWORKSPACE) k.whole();
     const ScanPlan p(k, v.B, v.T, v.N, false);
     cut_view(v, k);
     const int64_t blocks = (int64_t)v.B * v.nseg * v.vh;

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import sequence_ref as ref
-from test_gpu_sequence import BF16, F32, ctx, g, rand, scan_inputs  # noqa: F401
+from test_gpu_sequence import BF16, BWD, F32, FWD, close, ctx, g, rand, scan_inputs  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -41,3 +41,35 @@ def test_scan_decay_of_zero_is_no_episode_start(g, ctx, B, T, H, N, dtype, value
         got, want = g.scan_backward(ctx, dy, **i, state=s, dstate_out=d), ref.scan_backward(dy, **i, state=s, dstate=d)
         for n, p in zip(names, got):
             same_finite(p, want[n], n)
+
+
+@pytest.mark.parametrize("B,T,smaller", [(32, 128, [(31, 128), (1, 128), (7, 97), (32, 33), (3, 1)]),
+                                         (40, 300, [(32, 300), (31, 299), (1, 300), (40, 128), (9, 130)])])
+def test_scan_context_of_the_largest_takes_all_smaller(g, ctx, B, T, smaller):  # noqa: F811
+    """Fewer sequences are cut into segments that more are not."""
+    H, P, N = 16, 4, 128
+    for backward in (False, True):
+        own = g.Context(1, 1, min_bytes=g.scan_workspace_bytes(B, T, H, P, 1, N, backward))
+        for b, t in smaller:
+            i = scan_inputs(b, t, H, P, 1, N, F32)
+            if backward:
+                dy = rand(b, t, H, P, seed=21)
+                got, want = g.scan_backward(own, dy, **i)[:7], g.scan_backward(ctx, dy, **i)[:7]
+            else:
+                got, want = g.scan(own, **i), g.scan(ctx, **i)
+            for p, q in zip(got, want):
+                close(p, q, BWD if backward else FWD, (b, t))
+        own.close()
+
+
+def test_scan_short_sequences_need_no_workspace(g, ctx):  # noqa: F811
+    """A forward call of up to 128 steps takes one segment where the workspace has no place for more."""
+    none = g.Context(0, 1)
+    for b, t in ((31, 128), (1, 128), (2, 40)):
+        i = scan_inputs(b, t, 16, 4, 1, 20, F32)
+        for p, q in zip(g.scan(none, **i), g.scan(ctx, **i)):
+            close(p, q, FWD, (b, t))
+    with pytest.raises(g.GorilaError) as e:
+        g.scan(none, **scan_inputs(1, 129, 16, 4, 1, 20, F32))
+    assert e.value.code == -3
+    none.close()
