@@ -379,8 +379,9 @@ int gorila_add_rmsnorm(const void* x, int64_t x_stride, const void* residual,
 /* The same with 8-bit rows out: u = total * weight, m = max |u| of the row,
  * codes = round to nearest even of u * (127 / m) (int8; each operation one fp32
  * operation rounded once), scale [rows] = rho * (m / 127), so codes * scale
- * stands for y.  A row of zeros has codes and scale 0; a row that is not finite
- * has codes 0 and a NaN scale. */
+ * stands for y.  Rows with m < 2^-100 are taken 2^64 times as large for it (127 / m
+ * could be past fp32's range), and their scale 2^-64 times.  A row of zeros has codes
+ * and scale 0; a row that is not finite has codes 0 and a NaN scale. */
 int gorila_add_rmsnorm_codes(const void* x, int64_t x_stride, const void* residual,
                              int64_t residual_stride, const float* weight, int64_t rows,
                              int32_t width, int32_t dtype, float eps, int8_t* codes, float* scale,

@@ -154,9 +154,14 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
         }
     }
     most = row_max<LANES>(bad == bad ? most : INFINITY, sm);
-    const bool fine = most < INFINITY;
+    const bool fine = most < INFINITY, tiny = most < TINY;
+    if (tiny) {
+#pragma unroll
+        for (int i = 0; i < QUADS; ++i) v[i] *= TINY_UP;
+        most *= TINY_UP;
+    }
     const float inv = most > 0.0f && fine ? 127.0f / most : 0.0f;
-    if (l == 0) a.scale[row] = fine ? rho * (most / 127.0f) : NAN;
+    if (l == 0) a.scale[row] = fine ? rho * (most / 127.0f) * (tiny ? 1.0f / TINY_UP : 1.0f) : NAN;
     int8_t* q = a.codes + row * a.width;
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) {

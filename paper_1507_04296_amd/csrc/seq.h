@@ -65,6 +65,10 @@ __device__ __forceinline__ void row_store(T* p, f32x4 v, int n) {
     }
 }
 
+// A quotient of 127 or 7 by a value below TINY may be past the range of fp32: such values
+// are taken TINY_UP times as large before (a power of two, so no bit changes).
+constexpr float TINY = 0x1p-100f, TINY_UP = 0x1p64f;
+
 inline int dtype_bytes(int dtype) { return dtype == GORILA_BF16 ? 2 : 4; }
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool row_dtype(int dtype) { return dtype == GORILA_F32 || dtype == GORILA_BF16; }

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import sequence_ref as ref
-from test_gpu_sequence import BF16, BWD, F32, FWD, close, ctx, g, rand, scan_inputs  # noqa: F401
+from test_gpu_sequence import BF16, BWD, EPS, F32, FWD, close, ctx, g, rand, scan_inputs  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -73,3 +73,23 @@ def test_scan_short_sequences_need_no_workspace(g, ctx):  # noqa: F811
         g.scan(none, **scan_inputs(1, 129, 16, 4, 1, 20, F32))
     assert e.value.code == -3
     none.close()
+
+
+TINY = [1e-36, 3e-37, 1e-38, 1e-40]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("top", TINY)
+@pytest.mark.parametrize("width", [64, 130, 2500])
+def test_norm_codes_of_tiny_rows(g, ctx, width, top, dtype):  # noqa: F811
+    """127 over the largest is past fp32's range: codes and scale stand for the row all the same."""
+    x = (top * torch.linspace(-1, 1, width, dtype=torch.float64)).flip(0).repeat(3, 1).to(dtype)
+    x[1] = -x[1]
+    x[2, width // 2:] = 0
+    codes, scale, total = g.add_rmsnorm_codes(ctx, x.cuda(), torch.ones(width, device="cuda"), None, EPS)
+    u = x.double()
+    m = u.abs().amax(1, keepdim=True)
+    # half a step, and the quotient's rounding
+    assert ((codes.cpu().double() - 127 * u / m).abs() <= 0.5 + 1e-4).all()
+    want = m[:, 0] / 127 / torch.sqrt(u.square().mean(1) + EPS)
+    assert ((scale.cpu().double() - want).abs() <= 1e-6 * want + 2.0 ** -149).all()
