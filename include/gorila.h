@@ -480,8 +480,8 @@ int gorila_scan_step(const gorila_scan_args* args, float* state_pool, int64_t sl
  *
  * gorila_quantize_weights makes them from weights [outputs][inputs] (dtype): m =
  * max |w| of the group, scale = m / 7, code = 8 + round to nearest even of w *
- * (7 / m) (a group of zeros: scale 0, codes 8; a group that is not finite: NaN
- * scale, codes 8). */
+ * (7 / m), w and m 2^64 times as large where m < 2^-100 (a group of zeros: scale 0,
+ * codes 8; a group that is not finite: NaN scale, codes 8). */
 int gorila_quantize_weights(const void* weights, int64_t weights_stride, int32_t outputs,
                             int32_t inputs, int32_t dtype, int32_t group, uint8_t* codes,
                             float* scales, gorila_ctx* ctx);

@@ -479,7 +479,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* w, int64_t ws, i
     const int64_t row = id / per;
     const int k = (int)(id % per) * 4, lanes = group / 4;
     const bool on = row < outputs;
-    const f32x4 v = row_load<VEC>(w + (on && k < inputs ? row * ws + k : 0), on ? inputs - k : 0);
+    f32x4 v = row_load<VEC>(w + (on && k < inputs ? row * ws + k : 0), on ? inputs - k : 0);
     float most = 0.0f, bad = 0.0f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -490,9 +490,10 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* w, int64_t ws, i
     for (int m = lanes >> 1; m; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
     if (!on) return;
     const bool fine = most < INFINITY;
-    const float inv = most > 0.0f && fine ? 7.0f / most : 0.0f;
     if (k % group == 0) scales[row * groups + k / group] = fine ? most / 7.0f : NAN;
     if (k >= chunks * 32) return;  // past the row's codes
+    if (most < TINY) v *= TINY_UP, most *= TINY_UP;
+    const float inv = most > 0.0f && fine ? 7.0f / most : 0.0f;
     uint32_t q = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) q |= (uint32_t)(8 + (fine ? (int)rintf(v[j] * inv) : 0)) << (4 * j);

@@ -93,3 +93,19 @@ def test_norm_codes_of_tiny_rows(g, ctx, width, top, dtype):  # noqa: F811
     assert ((codes.cpu().double() - 127 * u / m).abs() <= 0.5 + 1e-4).all()
     want = m[:, 0] / 127 / torch.sqrt(u.square().mean(1) + EPS)
     assert ((scale.cpu().double() - want).abs() <= 1e-6 * want + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("top", [1e-37, 2e-38, 1e-38, 1e-40])
+def test_quantizer_of_tiny_groups(g, ctx, top, group, dtype):  # noqa: F811
+    """7 over the largest is past fp32's range: codes stand for the weights all the same, and neighbours keep theirs."""
+    w = (top * torch.linspace(-1, 1, 2 * group, dtype=torch.float64)).to(dtype).repeat(3, 1)
+    w[1] = -w[1]
+    w[2, group:] = 1.0
+    codes, scales = g.quantize_weights(ctx, w.cuda(), group)
+    u = w.double().unflatten(1, (2, group))
+    m = u.abs().amax(2, keepdim=True)
+    q = torch.stack((codes.cpu() % 16, codes.cpu() // 16), 2).flatten(1).double().unflatten(1, (2, group)) - 8
+    assert ((q - 7 * u / m).abs() <= 0.5 + 1e-4).all()
+    assert ((scales.cpu().double() - m[..., 0] / 7).abs() <= 1e-7 * m[..., 0] + 2.0 ** -149).all()
