@@ -161,7 +161,8 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void norm_kernel(NormArg
         most *= TINY_UP;
     }
     const float inv = most > 0.0f && fine ? 127.0f / most : 0.0f;
-    if (l == 0) a.scale[row] = fine ? rho * (most / 127.0f) * (tiny ? 1.0f / TINY_UP : 1.0f) : NAN;
+    if (l == 0)  // (rho of a row of zeros is infinite where eps is 0)
+        a.scale[row] = !fine ? NAN : most > 0.0f ? rho * (most / 127.0f) * (tiny ? 1.0f / TINY_UP : 1.0f) : 0.0f;
     int8_t* q = a.codes + row * a.width;
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) {

@@ -109,3 +109,12 @@ def test_quantizer_of_tiny_groups(g, ctx, top, group, dtype):  # noqa: F811
     q = torch.stack((codes.cpu() % 16, codes.cpu() // 16), 2).flatten(1).double().unflatten(1, (2, group)) - 8
     assert ((q - 7 * u / m).abs() <= 0.5 + 1e-4).all()
     assert ((scales.cpu().double() - m[..., 0] / 7).abs() <= 1e-7 * m[..., 0] + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("width", [130, 2500])
+def test_norm_codes_of_zeros_without_eps(g, ctx, width):  # noqa: F811
+    x = rand(3, width, seed=1)
+    x[1] = 0
+    codes, scale, _ = g.add_rmsnorm_codes(ctx, x, torch.ones(width, device="cuda"), None, 0.0)
+    assert int(codes[1].abs().max()) == 0 and float(scale[1]) == 0
+    close(scale[[0, 2]], (x.double().abs().amax(1) / 127 / x.double().square().mean(1).sqrt())[[0, 2]], FWD)
