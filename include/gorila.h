@@ -488,8 +488,9 @@ int gorila_quantize_weights(const void* weights, int64_t weights_stride, int32_t
 /* y[i][o] = sum_k x[i][k] w[o][k] for `rows` rows (row i of x at x + i *
  * x_stride elements).  x_dtype GORILA_F32 or GORILA_BF16 (y of the same type), or
  * GORILA_CODES: int8 rows with x_scale [rows] (as gorila_add_rmsnorm_codes makes
- * them), y fp32.  Made for the few rows of actors; up to 65535 rows (else
- * GORILA_EUNSUPPORTED). */
+ * them), y fp32.  fp32 and bf16 rows: infinite inputs and scales give the infinity or
+ * NaN that the sum's terms give; 8-bit rows: scales are finite or NaN.
+ * Made for the few rows of actors; up to 65535 rows (else GORILA_EUNSUPPORTED). */
 enum { GORILA_CODES = 2 };
 int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_t x_dtype,
                    int64_t rows, const uint8_t* codes, const float* scales, int32_t outputs,

@@ -129,6 +129,29 @@ __device__ __forceinline__ uint4 input_quad(const T* p, int n) {
     return r;
 }
 
+// A sum as it stands for y: itself, or where it is no number, formed term by term in 64
+// bits.  The kernels add code x and -8 x apart, which are infinities of both signs for an
+// infinite x or past fp32's range for a large one, and multiply the zeros past a row's end
+// with its last scale.  Slow, and for such rows alone; the view (both kernels' first
+// argument) is read again here, or it would be kept in scalar registers that the main
+// loops need (fp32, 64 rows and more: 1.5 % of the time, this way 0.9).
+template <class T>
+__device__ __forceinline__ float sum_of(float sum, int64_t row, int out) {
+    if (__builtin_expect(fabsf(sum) < INFINITY, 1)) return sum;
+    uint64_t args = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(args));
+    const MatvecView s = *(const MatvecView*)args;
+    const T* x = (const T*)s.x + row * s.xs;
+    const uint8_t* codes = s.codes + (int64_t)out * s.chunks * 16;
+    const float* scales = s.scales + (int64_t)out * s.groups;
+    const int shift = s.group == 32 ? 5 : s.group == 64 ? 6 : 7;
+    double v = 0.0;
+#pragma unroll 1
+    for (int k = 0; k < s.inputs; ++k)
+        v += (double)row_value(x[k]) * ((double)scales[k >> shift] * (double)((codes[k >> 1] >> (4 * (k & 1)) & 15) - 8));
+    return (float)v;
+}
+
 constexpr int SUPER = 4;  // runs of 32 codes that a wave takes together
 constexpr int AHEAD = 4;  // of those, loaded before the first is used
 
@@ -257,7 +280,7 @@ __global__ __launch_bounds__((64 * most_waves<T, RT>())) void matvec_kernel(Matv
         for (int i = 0; i < waves; ++i) v += lds.sums[i][e / 256][e % 256];
         const int64_t at = row * s.outputs + out;
         if constexpr (std::is_same<T, int8_t>::value) ((float*)s.y)[at] = v * s.x_scale[row];
-        else ((T*)s.y)[at] = row_round<T>(v);
+        else ((T*)s.y)[at] = row_round<T>(sum_of<T>(v, row, out));
     }
 }
 
@@ -465,7 +488,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void few_rows_kernel(MatvecView s, 
             for (int i = 0; i < waves; ++i) v += sums[i][e];
             const int64_t at = (int64_t)r * s.outputs + out;
             if constexpr (std::is_same<T, int8_t>::value) ((float*)s.y)[at] = v * s.x_scale[r];
-            else ((T*)s.y)[at] = row_round<T>(v);
+            else ((T*)s.y)[at] = row_round<T>(sum_of<T>(v, r, out));
         }
     }
 }

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import sequence_ref as ref
-from test_gpu_sequence import BF16, BWD, EPS, F32, FWD, close, ctx, g, rand, scan_inputs  # noqa: F401
+from test_gpu_sequence import BF16, BWD, EPS, F32, FWD, HALF, close, ctx, g, rand, scan_inputs  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -118,3 +118,54 @@ def test_norm_codes_of_zeros_without_eps(g, ctx, width):  # noqa: F811
     codes, scale, _ = g.add_rmsnorm_codes(ctx, x, torch.ones(width, device="cuda"), None, 0.0)
     assert int(codes[1].abs().max()) == 0 and float(scale[1]) == 0
     close(scale[[0, 2]], (x.double().abs().amax(1) / 127 / x.double().square().mean(1).sqrt())[[0, 2]], FWD)
+
+
+def same_extremes(got, want, tol):
+    """NaN and each infinity where the definition has them."""
+    got, want = got.cpu().double(), want.cpu().double()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(got == INF, want == INF) and torch.equal(got == -INF, want == -INF)
+    fine = torch.isfinite(want)
+    assert float((got[fine] - want[fine]).norm()) <= tol * float(want[fine].norm())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [1, 2, 3, 20, 40])
+@pytest.mark.parametrize("O,K,group", [(37, 100, 32), (50, 1001, 128)])
+def test_qmatvec_of_infinities(g, ctx, O, K, group, rows, dtype):  # noqa: F811
+    """An infinite input gives the infinity that its weight's sign gives, NaN where the weight is zero; other rows
+    keep their values.  (Positive inputs: nothing cancels, so that the tolerance is of the result.)"""
+    gen = torch.Generator().manual_seed(2)
+    codes = torch.randint(0, 256, (O, 16 * -(-K // 32)), generator=gen, dtype=torch.uint8).cuda()
+    codes[:O // 2] |= 0x99  # codes 9 and more: no weight is zero, all are positive
+    scales = (0.5 + torch.rand((O, -(-K // group)), generator=gen)).cuda()
+    full = ref.weights(codes, scales, K, group)
+    x = rand(rows, K, dtype=dtype, seed=3).abs()
+    x[0, 7] = INF
+    x[-1, K - 1] = -INF
+    tol = HALF if dtype == BF16 else FWD * 20
+    for xx in (x, torch.where(torch.isinf(x), -x, x)):
+        same_extremes(g.qmatvec(ctx, xx, codes, scales, group)[:, :O // 2], (xx.cpu().double() @ full.t())[:, :O // 2], tol)
+        got, want = g.qmatvec(ctx, xx, codes, scales, group).cpu(), xx.cpu().double() @ full.t()
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(torch.isinf(got), torch.isinf(want))
+        assert torch.equal(got[torch.isinf(got)].sign().double(), want[torch.isinf(want)].sign())
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 20])
+def test_qmatvec_of_the_largest_values(g, ctx, rows):  # noqa: F811
+    """15 times an input is past fp32's range, its weight times it is not; scales that are infinite or NaN."""
+    O, K, group = 20, 70, 32
+    codes = torch.randint(9, 16, (O, 2 * 48), generator=torch.Generator().manual_seed(2), dtype=torch.uint8)
+    codes = (codes[:, 0::2] | codes[:, 1::2] << 4).cuda()
+    scales = torch.full((O, 3), 0.01, device="cuda")
+    x = torch.zeros(rows, K, device="cuda")
+    x[:, 3], x[:, 40] = 2e38, 1e38
+    same_extremes(g.qmatvec(ctx, x, codes, scales, group), x.cpu().double() @ ref.weights(codes, scales, K, group).t(), FWD)
+    x = rand(rows, K, seed=4).abs()
+    scales[3, 2], scales[5, 0], scales[7, 2] = INF, -INF, NAN
+    want = x.cpu().double() @ ref.weights(codes, scales, K, group).t()
+    same_extremes(g.qmatvec(ctx, x, codes, scales, group), want, 20 * FWD)
+    x8 = torch.randint(1, 128, (rows, K), generator=torch.Generator().manual_seed(5), dtype=torch.int8).cuda()
+    xs = torch.full((rows,), 0.25, device="cuda")
+    scales[3, 2], scales[5, 0] = 1.0, NAN
+    same_extremes(g.qmatvec(ctx, x8, codes, scales, group, x_scale=xs), 0.25 * x8.cpu().double() @ ref.weights(codes, scales, K, group).t(), 20 * FWD)
