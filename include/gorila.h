@@ -363,6 +363,9 @@ int gorila_ps_apply(float* theta_plus, float* accum, int64_t n, const float* gra
  *    (GORILA_EWORKSPACE).
  *  - Calls that use the workspace say so; after them the values behind
  *    gorila_learner_td are gone.
+ *  - Sizes that a launch cannot hold (2^32 lanes; a norm's row has 64 or more, a
+ *    scan's (sequence, head, 64 channels) 512, a step's four channels one) and
+ *    lengths above 2^30: GORILA_EUNSUPPORTED.
  *  - Zero rows, sequences or steps are a no-op that still writes the outputs that
  *    have elements (a carried state, zero parameter gradients). */
 

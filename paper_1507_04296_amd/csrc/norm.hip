@@ -311,8 +311,11 @@ int norm_forward(NormArgs a, int dtype, gorila_ctx* ctx, bool codes) {
     const bool vec = !(strides & 3) && at_four(a.x, e) && at_four(a.residual, e) && at_four(a.y, e) && at_four(a.total, e) &&
                      at_four(a.weight, 4) && at_four(a.codes, 1);
     const bool pairs = vec && !(strides & 7) && aligned16(a.x) && aligned16(a.residual) && aligned16(a.y) && aligned16(a.total);
+    bool fits = true;
     by_width(a.width, [&](auto lanes, auto quads) {
         constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, PER = L < 256 ? 256 / L : 1;
+        fits = launch_fits((double)((a.rows + PER - 1) / PER), L < 256 ? 256 : L);
+        if (!fits) return;
         by_load(dtype, vec, pairs, [&](auto t, auto wide) {
             auto go = [&](auto co) {
                 norm_kernel<decltype(t), L, QD, decltype(wide)::value, decltype(co)::value>
@@ -321,7 +324,7 @@ int norm_forward(NormArgs a, int dtype, gorila_ctx* ctx, bool codes) {
             codes ? go(std::true_type{}) : go(std::false_type{});
         });
     });
-    return launched();
+    return fits ? launched() : GORILA_EUNSUPPORTED;
 }
 
 }  // namespace

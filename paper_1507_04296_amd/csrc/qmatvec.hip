@@ -523,6 +523,9 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* w, int64_t ws, i
     *(uint16_t*)(codes + row * chunks * 16 + k / 2) = (uint16_t)q;
 }
 
+// Inputs and outputs whose sums with a workgroup's are 32 bits: the lanes of eight waves
+// take a run of 32 inputs each at a time, a team 8 batches of 64 outputs.
+constexpr int MAX_INPUTS = INT32_MAX - 32 * (64 * FEW_WAVES + 1), MAX_OUTPUTS = INT32_MAX - 512;
 bool group_size(int g) { return g == 32 || g == 64 || g == 128; }
 
 }  // namespace
@@ -538,13 +541,13 @@ int gorila_quantize_weights(const void* weights, int64_t weights_stride, int32_t
     const int rc = ctx_view(ctx, 0, c);
     if (rc) return rc;
     if (!row_dtype(dtype) || outputs < 0 || inputs < 1 || !group_size(group)) return GORILA_EINVAL;
-    if (inputs > INT32_MAX - 128) return GORILA_EUNSUPPORTED;
+    if (inputs > MAX_INPUTS) return GORILA_EUNSUPPORTED;
     if (outputs == 0) return GORILA_OK;
     const int e = dtype_bytes(dtype);
     if (!weights || !codes || !scales || !at_element(weights, e) || !aligned16(codes) || !at_element(scales, 4)) return GORILA_EINVAL;
     const int chunks = (inputs + 31) / 32, groups = (inputs + group - 1) / group;
     const int64_t lanes = (int64_t)outputs * groups * (group / 4);
-    if ((lanes + 255) / 256 > INT32_MAX) return GORILA_EUNSUPPORTED;
+    if (!launch_fits((double)lanes + 255, 1)) return GORILA_EUNSUPPORTED;
     const bool vec = !((weights_stride | inputs) & 3) && at_four(weights, e);
     const unsigned grid = (unsigned)((lanes + 255) / 256);
     auto go = [&](auto t, auto al) {
@@ -570,17 +573,19 @@ int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_
     if (!at_element(x, e) || !aligned16(codes) || !at_element(scales, 4) || !at_element(x_scale, 4) ||
         !at_element(y, x_dtype == GORILA_BF16 ? 2 : 4))
         return GORILA_EINVAL;
-    if (inputs > INT32_MAX - 128 || rows > 65535) return GORILA_EUNSUPPORTED;
+    if (inputs > MAX_INPUTS || outputs > MAX_OUTPUTS || rows > 65535) return GORILA_EUNSUPPORTED;
     MatvecView v{x, x_stride, rows, x_scale, codes, scales, outputs, inputs, group, (inputs + 31) / 32, (inputs + group - 1) / group, y};
     const int supers = (v.chunks + SUPER - 1) / SUPER, tiles = (outputs + 15) / 16;
     using std::integral_constant;
+    bool fits = true;
     auto go = [&](auto t, auto rt, auto al) {
         using T = decltype(t);
         constexpr int RT = decltype(rt)::value;
         int waves = 1;
         while (waves < most_waves<T, RT>() && waves < supers) waves <<= 1;
-        matvec_kernel<T, RT, decltype(al)::value>
-            <<<dim3((unsigned)tiles, (unsigned)((rows + 16 * RT - 1) / (16 * RT))), 64 * waves, 0, c.stream>>>(v);
+        fits = launch_fits(tiles, 64 * waves);
+        const dim3 grid((unsigned)tiles, (unsigned)((rows + 16 * RT - 1) / (16 * RT)));
+        if (fits) matvec_kernel<T, RT, decltype(al)::value><<<grid, 64 * waves, 0, c.stream>>>(v);
     };
     // Rows in as few passes over the codes as the registers allow: 64 8-bit rows at
     // once 38 us for 8192 x 8192, two times 32 54; bf16 82 and 70.
@@ -599,8 +604,9 @@ int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_
         const int teams = 64 / lk, per = teams * OUT;
         int batches = 1;
         while (batches < 8 && (int64_t)(outputs + per - 1) / per * waves > 16 * batches * c.cus) batches <<= 1;
-        few_rows_kernel<decltype(t), R, decltype(al)::value>
-            <<<(outputs + per * batches - 1) / (per * batches), 64 * waves, 0, c.stream>>>(v, lk, batches);
+        const int blocks = (outputs + per * batches - 1) / (per * batches);
+        fits = launch_fits(blocks, 64 * waves);
+        if (fits) few_rows_kernel<decltype(t), R, decltype(al)::value><<<blocks, 64 * waves, 0, c.stream>>>(v, lk, batches);
     };
     auto by_few = [&](auto t, auto al) {
         if (rows == 1) few(t, integral_constant<int, 1>{}, al);
@@ -612,13 +618,13 @@ int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_
         if (x_dtype == GORILA_F32) four ? by_few(float{}, std::true_type{}) : by_few(float{}, std::false_type{});
         else if (x_dtype == GORILA_BF16) four ? by_few(uint16_t{}, std::true_type{}) : by_few(uint16_t{}, std::false_type{});
         else four ? by_few(int8_t{}, std::true_type{}) : by_few(int8_t{}, std::false_type{});
-        return launched();
+        return fits ? launched() : GORILA_EUNSUPPORTED;
     }
     const bool vec = aligned16(x) && ((x_stride * e) & 15) == 0;
     if (x_dtype == GORILA_F32) vec ? by(float{}, std::true_type{}) : by(float{}, std::false_type{});
     else if (x_dtype == GORILA_BF16) vec ? by(uint16_t{}, std::true_type{}) : by(uint16_t{}, std::false_type{});
     else vec ? by(int8_t{}, std::true_type{}) : by(int8_t{}, std::false_type{});
-    return launched();
+    return fits ? launched() : GORILA_EUNSUPPORTED;
 }
 
 }  // extern "C"

@@ -1238,13 +1238,15 @@ struct ScanPlan {
 };
 
 constexpr int MAX_WIDTH = 128, MAX_STATE = 128;
+// Sequences and steps whose sums with a segment's are 32 bits.
+bool sizes_fit(int batch, int length) { return length <= 1 << 30 && (int64_t)batch * length <= INT32_MAX; }
 
 // The view of valid arguments; `step`: strides along the steps are not used.
 int scan_view(const gorila_scan_args* a, bool step, ScanView& v, bool& vec) {
     if (!a || !row_dtype(a->dtype) || a->batch < 0 || a->length < 0 || a->heads < 1 || a->groups < 1) return GORILA_EINVAL;
     if (a->heads % a->groups || a->head_dim < 1 || a->state_dim < 1) return GORILA_EINVAL;
     if (a->head_dim > MAX_WIDTH || a->state_dim > MAX_STATE || a->heads > 65536) return GORILA_EUNSUPPORTED;
-    if ((int64_t)a->batch * a->length > INT32_MAX) return GORILA_EUNSUPPORTED;
+    if (!sizes_fit(a->batch, a->length)) return GORILA_EUNSUPPORTED;
     if (!a->a_log || !a->dt_bias || !a->skip) return GORILA_EINVAL;
     if (a->batch > 0 && a->length > 0 && (!a->x || !a->dt || !a->b || !a->c)) return GORILA_EINVAL;
     const int e = dtype_bytes(a->dtype);
@@ -1285,8 +1287,6 @@ void by_kind(int dtype, int n, bool vec, F&& f) {
     });
 }
 
-bool grid_fits(int64_t blocks) { return blocks <= INT32_MAX; }
-
 }  // namespace
 }  // namespace gorila
 
@@ -1297,7 +1297,7 @@ extern "C" {
 size_t gorila_scan_workspace_bytes(int32_t batch, int32_t length, int32_t heads, int32_t head_dim, int32_t groups,
                                    int32_t state_dim, int32_t backward) {
     if (batch < 0 || length < 0 || heads < 1 || heads > 65536 || groups < 1 || heads % groups) return 0;
-    if (head_dim < 1 || head_dim > MAX_WIDTH || state_dim < 1 || state_dim > MAX_STATE) return 0;
+    if (head_dim < 1 || head_dim > MAX_WIDTH || state_dim < 1 || state_dim > MAX_STATE || !sizes_fit(batch, length)) return 0;
     const Cut k(batch, length, heads, head_dim);
     // enough for every smaller batch and length too, which may be cut where this is not
     const bool exact = !backward && k.nch <= SHORT;
@@ -1319,7 +1319,7 @@ int gorila_scan(const gorila_scan_args* args, void* y, float* state_out, gorila_
     const ScanPlan p(k, v.B, v.T, v.N, false);
     cut_view(v, k);
     const int64_t blocks = (int64_t)v.B * v.nseg * v.vh;
-    if (!grid_fits(blocks * (PW * MAX_STATE / 256))) return GORILA_EUNSUPPORTED;
+    if (!launch_fits((double)blocks, THREADS)) return GORILA_EUNSUPPORTED;
     if ((rc = ctx_view(ctx, p.total, c))) return rc;
     vec = vec && at_four(y, dtype_bytes(args->dtype)) && at_four(state_out, 4);
     v.y = y;
@@ -1358,7 +1358,7 @@ int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t d
     const ScanPlan p(k, v.B, v.T, v.N, true);
     cut_view(v, k);
     const int64_t blocks = (int64_t)v.B * v.nseg * v.vh;
-    if (!grid_fits(blocks * (PW * MAX_STATE / 256))) return GORILA_EUNSUPPORTED;
+    if (!launch_fits((double)blocks, THREADS)) return GORILA_EUNSUPPORTED;
     if ((rc = ctx_view(ctx, p.total, c))) return rc;
     vec = vec && !((dy_batch_stride | dy_step_stride) & 3) && at_four(dy, e) && at_four(dx, e) && at_four(db, e) && at_four(dc, e) && at_four(dstate_out, 4) && at_four(dstate, 4);
     v.dy = dy;
@@ -1413,7 +1413,7 @@ int gorila_scan_step(const gorila_scan_args* args, float* state_pool, int64_t sl
     while (pblocks < most && (int64_t)v.B * v.H * pblocks < 2 * c.cus) pblocks <<= 1;
     if (pblocks > most) pblocks = most;
     const int64_t blocks = (int64_t)v.B * v.H * pblocks;
-    if (!grid_fits(blocks)) return GORILA_EUNSUPPORTED;
+    if (!launch_fits((double)blocks, 256)) return GORILA_EUNSUPPORTED;
     auto go = [&](auto t, auto al) {
         scan_step_kernel<decltype(t), decltype(al)::value><<<(unsigned)blocks, 256, 0, c.stream>>>(v, state_pool, slots, slot, lanes, pblocks, c.err);
     };

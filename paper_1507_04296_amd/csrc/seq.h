@@ -79,6 +79,9 @@ inline bool at_four(const void* p, int bytes) { return at_element(p, 4 * bytes);
 // as [taps][first / taps], to out as [first / taps][taps]; the others to out2 (which may
 // be null).
 void launch_sum_parts(const float* parts, int n_parts, int64_t n, int64_t first, int taps, float* out, float* out2, hipStream_t st);
+// HIP refuses a launch of 2^32 lanes or more in one dimension: such calls are unsupported.
+// (In floating point: products of sizes may be past 64 bits.)
+inline bool launch_fits(double blocks, int threads) { return blocks * threads < 4294967296.0; }
 inline int launched() { return hipGetLastError() == hipSuccess ? GORILA_OK : GORILA_EHIP; }
 
 }  // namespace gorila

@@ -23,6 +23,7 @@ constexpr int BACK_RUN = 16;    // and backward, which walks K - 1 more
 constexpr int BACK_W = 2;      // channels a lane, backward
 constexpr int MAX_TAPS = 4;
 constexpr int MAX_PARTS = 512;  // of the weight gradient's sums
+constexpr int MAX_SIZE = 1 << 30;  // steps, channels, runs: sums of them and of a workgroup's are 32 bits
 
 struct ConvView {
     const void *x, *window, *dy, *dwindow_out;
@@ -304,11 +305,10 @@ int conv_view(const gorila_causal_conv_args* a, bool step, ConvView& v, bool& ve
     v.x = a->x, v.xb = a->x_batch_stride, v.xt = a->x_step_stride, v.weight = a->weight, v.bias = a->bias;
     v.reset = a->reset, v.window = step ? nullptr : a->window;
     v.B = a->batch, v.T = a->length, v.C = a->channels, v.silu = a->silu;
+    if (v.T > MAX_SIZE || v.C > MAX_SIZE) return GORILA_EUNSUPPORTED;
     v.runs = v.T > 0 ? (v.T + RUN - 1) / RUN : 1;  // the backward takes fewer
     vec = !((v.C | v.xb | (step ? 0 : v.xt)) & 3) && at_four(a->x, e) && at_four(v.window, e) && at_four(a->bias, 4);
-    // a wave or more a run, in a 32-bit grid
-    if ((int64_t)v.B * v.runs * ((v.C + 63) / 64) > INT32_MAX / 2) return GORILA_EUNSUPPORTED;
-    return GORILA_OK;
+    return (int64_t)v.B * v.runs > MAX_SIZE ? GORILA_EUNSUPPORTED : GORILA_OK;
 }
 
 template <class F>
@@ -353,6 +353,7 @@ int gorila_causal_conv(const gorila_causal_conv_args* args, void* y, void* windo
     v.window_out = window_out;
     v.quads = vec ? v.C / 4 : v.C;
     const int threads = run_threads(v);
+    if (!launch_fits((double)v.B * v.runs * v.blocks, threads)) return GORILA_EUNSUPPORTED;
     by_taps(args->taps, args->dtype, vec, [&](auto t, auto k, auto al) {
         conv_kernel<decltype(t), decltype(k)::value, decltype(al)::value ? 4 : 1>
             <<<(unsigned)(v.B * v.runs * v.blocks), threads, 0, c.stream>>>(v);
@@ -391,6 +392,8 @@ int gorila_causal_conv_backward(const gorila_causal_conv_args* args, const void*
     v.runs = v.T > 0 ? (v.T + BACK_RUN - 1) / BACK_RUN : 1;
     const int64_t units = (int64_t)v.B * v.runs;
     v.parts = (int)(units < MAX_PARTS ? units : MAX_PARTS);
+    // the sums take 64 lanes a column
+    if (!launch_fits((double)v.parts * v.blocks, threads) || !launch_fits((double)cols, 64)) return GORILA_EUNSUPPORTED;
     if (v.parts > 0)
         by_taps(args->taps, args->dtype, vec, [&](auto t, auto k, auto al) {
             conv_backward_kernel<decltype(t), decltype(k)::value, decltype(al)::value ? BACK_W : 1>
@@ -415,6 +418,7 @@ int gorila_causal_conv_step(const gorila_causal_conv_args* args, void* window_po
     vec = vec && at_four(window_pool, e) && at_four(y, e);
     v.y = y;
     v.quads = vec ? v.C / 4 : v.C;
+    if (!launch_fits((double)v.B * v.quads + 255, 1)) return GORILA_EUNSUPPORTED;
     by_taps(args->taps, args->dtype, vec, [&](auto t, auto k, auto al) {
         using T = decltype(t);
         conv_step_kernel<T, decltype(k)::value, decltype(al)::value ? 4 : 1>

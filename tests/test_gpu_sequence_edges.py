@@ -1,5 +1,7 @@
 """The sequence operators at the ends of their ranges.  Tolerances are those of
 test_gpu_sequence.py where nothing else is said."""
+import ctypes
+
 import pytest
 import torch
 
@@ -169,3 +171,41 @@ def test_qmatvec_of_the_largest_values(g, ctx, rows):  # noqa: F811
     xs = torch.full((rows,), 0.25, device="cuda")
     scales[3, 2], scales[5, 0] = 1.0, NAN
     same_extremes(g.qmatvec(ctx, x8, codes, scales, group, x_scale=xs), 0.25 * x8.cpu().double() @ ref.weights(codes, scales, K, group).t(), 20 * FWD)
+
+
+def test_sizes_past_a_launch(g, ctx):  # noqa: F811
+    """Refused by the library's own checks, before anything is launched (the pointers are of one small buffer)."""
+    from paper_1507_04296_amd import sequence as sq
+    L, p, at = g.lib(), torch.zeros(1 << 12, device="cuda").data_ptr(), ctx.bind_stream()
+    top = 2 ** 31 - 1
+
+    def scan(batch, length, heads=1):
+        return ctypes.byref(sq._ScanArgs(0, batch, length, heads, 4, 1, 4, 0, *([p, 0, 0] * 4), p, p, p, None, None))
+
+    def conv(batch, length, channels):
+        return ctypes.byref(sq._ConvArgs(0, batch, length, channels, 4, 1, p, 0, 0, p, None, None, None))
+
+    calls = dict(
+        norm=lambda: L.gorila_add_rmsnorm(p, 0, None, 0, p, 1 << 26, 8, 0, 1e-6, p, None, None, at),
+        norm_wide=lambda: L.gorila_add_rmsnorm(p, 0, None, 0, p, 1 << 24, 4000, 1, 1e-6, p, None, None, at),
+        codes=lambda: L.gorila_add_rmsnorm_codes(p, 0, None, 0, p, top, 8, 0, 1e-6, p, p, None, at),
+        conv_runs=lambda: L.gorila_causal_conv(conv(1 << 26, 8, 4), p, None, at),
+        conv_length=lambda: L.gorila_causal_conv(conv(1, top, 4), p, None, at),
+        conv_channels=lambda: L.gorila_causal_conv(conv(1, 4, top), p, None, at),
+        conv_backward=lambda: L.gorila_causal_conv_backward(conv(1, top, 4), p, 0, 0, None, p, p, None, None, at),
+        conv_step=lambda: L.gorila_causal_conv_step(conv(1 << 28, 1, 64), p, top, None, p, at),
+        scan=lambda: L.gorila_scan(scan(1 << 23, 1), p, p, at),
+        scan_heads=lambda: L.gorila_scan(scan(1 << 9, 1, 1 << 14), p, p, at),
+        scan_length=lambda: L.gorila_scan(scan(1, top), p, p, at),
+        scan_steps=lambda: L.gorila_scan(scan(top, 2), p, p, at),
+        scan_step=lambda: L.gorila_scan_step(scan(1 << 24, 1), p, top, None, p, at),
+        outputs=lambda: L.gorila_qmatvec(p, 0, None, 0, 1, p, p, top, 32, 32, p, at),
+        inputs=lambda: L.gorila_qmatvec(p, 0, None, 0, 1, p, p, 1, top - 200, 32, p, at),
+        tiles=lambda: L.gorila_qmatvec(p, 0, None, 0, 16, p, p, 1 << 30, 512, 32, p, at),
+        quantiser=lambda: L.gorila_quantize_weights(p, 0, 1 << 30, 32, 0, 32, p, p, at),
+    )
+    for name, call in calls.items():
+        assert call() == -5, name
+    torch.cuda.synchronize()
+    for length in (top, 1 << 30):
+        assert g.scan_workspace_bytes(4, length, 1, 4, 1, 4) == 0
