@@ -60,7 +60,6 @@ def build(verbose: bool = False) -> str:
     with ThreadPoolExecutor(max_workers=min(len(SOURCES), 8)) as ex:
         binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, SOURCES))
-        binding.result()
     tmp = OUT + ".tmp%d" % os.getpid()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -69,6 +68,9 @@ def build(verbose: bool = False) -> str:
     os.replace(tmp, OUT)
     if verbose:
         print("built", OUT)
+    # the library is there whatever the binding needs (g++, torch's headers); only the
+    # sequence operators are called through it
+    binding.result()
     return OUT
 
 
