@@ -109,29 +109,19 @@ __device__ __forceinline__ f32x4 rfrag(const float* s, int ld, int k0, int col0,
 
 // bf16 rows: their values are operands of the bf16 instruction as they are, 16 times
 // as fast as the fp32 one.  What is formed from them (states, decayed products) enters
-// as three bf16 terms, which hold an fp32 value; where only bf16 outputs come of it, as
-// two in one LDS word (16 bits, 2^-17 relative, against the outputs' 2^-9).  Two terms
-// throughout took the backward of 4 x 1999 steps, 128 states, from 244 to 229 us, and
-// the parameters' gradients from 2e-7 to 3e-6.  fp32 rows take the fp32 instruction:
-// three terms of both operands would cost the vector unit what the matrix unit saves.
-enum Operand { ROWS, WORDS, FP32 };  // rows' values; words of two terms; fp32 values
-template <class T> __device__ __forceinline__ float word(float v) { return v; }
-template <> __device__ __forceinline__ float word<uint16_t>(float v) {
-    const uint32_t hi = row_round<uint16_t>(v);
-    return __uint_as_float(hi << 16 | row_round<uint16_t>(v - __uint_as_float(hi << 16)));
-}
-template <class T> __device__ __forceinline__ f32x4 words(f32x4 v) { return f32x4{word<T>(v[0]), word<T>(v[1]), word<T>(v[2]), word<T>(v[3])}; }
-// Halves of eight words.
-__device__ __forceinline__ bf16x8 halves(f32x4 a, f32x4 b, uint32_t sel) {
-    uint4 o;
-    o.x = __builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), sel);
-    o.y = __builtin_amdgcn_perm(__float_as_uint(a[3]), __float_as_uint(a[2]), sel);
-    o.z = __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), sel);
-    o.w = __builtin_amdgcn_perm(__float_as_uint(b[3]), __float_as_uint(b[2]), sel);
+// as three bf16 terms, which hold an fp32 value.  (Two terms, 16 bits: 2^-17 of every
+// term, which products that cancel show.)  fp32 rows take the fp32 instruction: three
+// terms of both operands would cost the vector unit what the matrix unit saves.
+enum Operand { ROWS, FP32 };  // rows' values; fp32 values
+// Upper halves of eight values that are bf16.
+__device__ __forceinline__ bf16x8 rows_of(f32x4 a, f32x4 b) {
+    constexpr uint32_t HIGH = 0x07060302u;
+    const uint4 o{__builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), HIGH), __builtin_amdgcn_perm(__float_as_uint(a[3]), __float_as_uint(a[2]), HIGH),
+                  __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), HIGH), __builtin_amdgcn_perm(__float_as_uint(b[3]), __float_as_uint(b[2]), HIGH)};
     return __builtin_bit_cast(bf16x8, o);
 }
 template <int KIND> struct Terms {
-    static constexpr int N = KIND == ROWS ? 1 : KIND == WORDS ? 2 : 3;
+    static constexpr int N = KIND == ROWS ? 1 : 3;
     bf16x8 t[N];
     __device__ __forceinline__ Terms(f32x4 a, f32x4 b) {
         if constexpr (KIND == FP32) {
@@ -141,8 +131,7 @@ template <int KIND> struct Terms {
 #pragma unroll
             for (int i = 0; i < N; ++i) t[i] = __builtin_shufflevector(p[i], q[i], 0, 1, 2, 3, 4, 5, 6, 7);
         } else {
-            t[0] = halves(a, b, 0x07060302u);
-            if constexpr (KIND == WORDS) t[1] = halves(a, b, 0x05040100u);
+            t[0] = rows_of(a, b);
         }
     }
 };
@@ -430,10 +419,10 @@ __device__ __forceinline__ void store_own(const f32x4 (&acc)[TILES], float* s, i
     for (int i = 0; i < TILES; ++i) own_state(s, p0, n0, l)[i * (PW / 16) * 64] = acc[i];
 }
 // To LDS [channel][state].
-template <class T, int TILES>
+template <int TILES>
 __device__ __forceinline__ void stage_state(const f32x4 (&acc)[TILES], float* s, int ld, int p0, int n0, int l) {
 #pragma unroll
-    for (int i = 0; i < TILES; ++i) *(f32x4*)(s + (p0 + (l & 15)) * ld + n0 + 16 * i + 4 * (l >> 4)) = words<T>(acc[i]);
+    for (int i = 0; i < TILES; ++i) *(f32x4*)(s + (p0 + (l & 15)) * ld + n0 + 16 * i + 4 * (l >> 4)) = acc[i];
 }
 
 template <class T>
@@ -543,12 +532,12 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
             rx.store(sx, LP, bad);
             rb.store(sb, LN, bad);
             rc.store(sc, LN, bad);
-            if (on) stage_state<T, TILES>(S, ss, LN, 16 * wp, n_own, l);
+            if (on) stage_state<TILES>(S, ss, LN, 16 * wp, n_own, l);
             if (bad != bad) flag = 1;
             __syncthreads();
             acc = m = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if (w == 7) rd.store(st, in.bias, in.rate2, at_t.len, l);
-            acc = product<T, WORDS, NT, true>([&](int n) { return kfrag(ss, LN, 16 * wp, 16 * n, l); },
+            acc = product<T, FP32, NT, true>([&](int n) { return kfrag(ss, LN, 16 * wp, 16 * n, l); },
                                               [&](int n) { return kfrag(sc, LN, 16 * half, 16 * n, l); }, acc);
             if (w < 3)
                 m = product<T, ROWS, NT>([&](int n) { return kfrag(sb, LN, 16 * si, 16 * n, l); },
@@ -574,14 +563,14 @@ __global__ __launch_bounds__(THREADS, 4) void scan_kernel(ScanView s) {
                 const bool same = tm == q0 + j, behind = tm > q0 + j && ep[j] == et;
                 m[j] = same ? m[j] * d[j] : behind ? m[j] * (pow2((gi_t - gi[j]) + (gf_t - gf[j])) * d[j]) : 0.0f;
             }
-            *(f32x4*)(sm + tm * LQ + q0) = words<T>(m);
+            *(f32x4*)(sm + tm * LQ + q0) = m;
         }
         if (on) walk<T, TILES, true>(S, sb + n_own, LN, sx + 16 * wp, st, l);
         __syncthreads();
         if (half)
-            acc = mul2<T, WORDS>(rfrag(sx, LP, 0, 16 * wp, l), rfrag(sx, LP, 16, 16 * wp, l), kfrag(sm, LQ, 16, 0, l), kfrag(sm, LQ, 16, 16, l), acc);
+            acc = mul2<T, FP32>(rfrag(sx, LP, 0, 16 * wp, l), rfrag(sx, LP, 16, 16 * wp, l), kfrag(sm, LQ, 16, 0, l), kfrag(sm, LQ, 16, 16, l), acc);
         else
-            acc = mul1<T, WORDS>(rfrag(sx, LP, 0, 16 * wp, l), kfrag(sm, LQ, 0, 0, l), acc);
+            acc = mul1<T, FP32>(rfrag(sx, LP, 0, 16 * wp, l), kfrag(sm, LQ, 0, 0, l), acc);
         const int p = 16 * wp + 4 * lg;
         if (t < len && p < at.pw) row_store<VEC>(y + t0 * yt, acc + skip * *(const f32x4*)(sx + t * LP + p), at.pw - p);
         if (whole && tid == 0) flag = 0;  // nobody reads it before the next chunk is staged
@@ -895,8 +884,8 @@ __global__ __launch_bounds__(THREADS, NP > 64 ? 2 : 4) void scan_backward_kernel
             rc.store(sc, LN, bad);
             pass = 0.0f;  // <R, S>, from the state before to the one behind
             if (on) {
-                stage_state<float, TILES>(R, sr, LN, 16 * wp, n_own, l);
-                stage_state<float, TILES>(S, ss, LN, 16 * wp, n_own, l);
+                stage_state<TILES>(R, sr, LN, 16 * wp, n_own, l);
+                stage_state<TILES>(S, ss, LN, 16 * wp, n_own, l);
 #pragma unroll
                 for (int n = 0; n < TILES; ++n) pass += (R[n][0] * S[n][0] + R[n][1] * S[n][1]) + (R[n][2] * S[n][2] + R[n][3] * S[n][3]);
             }

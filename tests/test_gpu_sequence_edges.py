@@ -209,3 +209,42 @@ def test_sizes_past_a_launch(g, ctx):  # noqa: F811
     torch.cuda.synchronize()
     for length in (top, 1 << 30):
         assert g.scan_workspace_bytes(4, length, 1, 4, 1, 4) == 0
+
+
+def cancelled(got, want, size):
+    """bf16 values that are small differences of terms of `size`: one rounding of the value to 8 bits, and 2^-21 of the
+    terms (fp32 holds each to 2^-24; three or four roundings a term, an exponential of one unit)."""
+    got, want = got.cpu().double(), want.cpu().double()
+    off = float((got - want).norm())
+    assert off <= HALF * float(want.norm()) + 2.0 ** -21 * float(size.norm()), f"{off / float(size.norm()):.2e} of the terms"
+
+
+@pytest.mark.parametrize("N", [16, 32, 64, 128])
+def test_scan_of_bf16_rows_holds_states_in_32_bits(g, ctx, N):  # noqa: F811
+    """Outputs that are small differences of the carried state's products."""
+    B, T, H, P = 3, 20, 2, 64
+    i = scan_inputs(B, T, H, P, 1, N, BF16)
+    i["x"].zero_()
+    i["dt_bias"] -= 4
+    i["c"][..., 1::2] = -i["c"][..., 0::2]
+    state = rand(B, H, P, N, seed=20)
+    state[..., 1::2] = state[..., 0::2] * (1 + 1e-4 * rand(B, H, P, N // 2, seed=21))
+    y = g.scan(ctx, **i, state=state)[0]
+    size = ref.scan(**dict(i, c=i["c"].abs()), state=state.abs())[0]
+    cancelled(y, ref.scan(**i, state=state)[0], size)
+
+
+def test_scan_of_bf16_rows_holds_decayed_products_in_32_bits(g, ctx):  # noqa: F811
+    """Two steps whose inputs differ in sign and whose weights differ by one step's decay, of 5e-5."""
+    B, H, P, N = 64, 16, 4, 16
+    i = scan_inputs(B, 2, H, P, 1, N, BF16)
+    for k in ("x", "dt", "b"):
+        i[k][:, 1] = i[k][:, 0]
+    i["x"][:, 1] *= -1
+    i["skip"].zero_()
+    i["dt"] *= 0.25
+    i["dt_bias"][:] = -7
+    i["a_log"][:] = -3
+    y = g.scan(ctx, **i)[0]
+    size = ref.scan(**dict(i, x=i["x"].abs()))[0].abs()
+    cancelled(y[:, 1], ref.scan(**i)[0][:, 1], size[:, 1])
