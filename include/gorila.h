@@ -341,7 +341,10 @@ int gorila_ps_apply(float* theta_plus, float* accum, int64_t n, const float* gra
                     const uint8_t* keep, const int64_t* grad_version, int64_t* ps_version,
                     int64_t max_delay, float lr, float eps, uint8_t* applied_out, gorila_ctx* ctx);
 
-/* ---- A recurrent core on the network's features (partially observed games) ----
+/* ---- A recurrent core on features (partially observed games) ----
+ *
+ * The rows are the caller's: no call of this library returns the network's 512
+ * features or takes their gradient.
  *
  * Operators for sequences of feature rows: learners train on replayed sequences
  * that hold episode starts, actors take one step at a time with a state kept for
@@ -361,6 +364,8 @@ int gorila_ps_apply(float* theta_plus, float* accum, int64_t n, const float* gra
  *    of range reads a zero state, writes none and sets the sticky device error
  *    (GORILA_ERANGE from gorila_ctx_check); it needs a context with a workspace
  *    (GORILA_EWORKSPACE).
+ *  - An infinite or NaN value makes what its definition lets it reach infinite or
+ *    NaN, and nothing else.  Which of the two is kept only where a call says so.
  *  - Calls that use the workspace say so; after them the values behind
  *    gorila_learner_td are gone.
  *  - Sizes that a launch cannot hold (2^32 lanes; a norm's row has 64 or more, a
@@ -374,7 +379,9 @@ int gorila_ps_apply(float* theta_plus, float* accum, int64_t n, const float* gra
  *   rho = 1 / sqrt(mean(total^2) + eps),   y = total * rho * weight.
  * Row i of x is at x + i * x_stride elements, of residual at residual + i *
  * residual_stride.  total, y [rows, width], rstd [rows] = rho fp32; total may be
- * NULL, and so may rstd.  EINVAL for eps < 0. */
+ * NULL, and so may rstd.  EINVAL for eps < 0.  Squares are fp32: values from about
+ * 2^63 on give rho 0, and with eps 0 a row of values below 2^-75 (or of zeros) rho
+ * infinite. */
 int gorila_add_rmsnorm(const void* x, int64_t x_stride, const void* residual,
                        int64_t residual_stride, const float* weight, int64_t rows, int32_t width,
                        int32_t dtype, float eps, void* y, void* total, float* rstd,
@@ -406,7 +413,8 @@ int gorila_add_rmsnorm_backward(const void* dy, int64_t dy_stride, const void* d
  * with e the steps before the sequence (window [batch][taps-1][channels] of
  * dtype, oldest first; NULL: zeros), then x; a tap with an episode start after
  * it, up to t, counts as zero.  window_out (may be NULL, may not be window) is
- * the window for the steps that follow.  bias may be NULL. */
+ * the window for the steps that follow.  bias may be NULL.  The sigmoid's relative
+ * error is about (2 + |v|) 2^-23. */
 typedef struct {
     int32_t dtype, batch, length, channels, taps, silu;
     const void* x;
@@ -436,6 +444,8 @@ int gorila_causal_conv_step(const gorila_causal_conv_args* args, void* window_po
  *   d = softplus(dt + dt_bias[h]),   a = exp(-exp(a_log[h]) * d), 0 at a reset,
  *   S_t = a_t S_{t-1} + d_t x_t b_t^T   (head_dim x state_dim, from `state`),
  *   y_t = S_t c_t + skip[h] x_t.
+ * (Sequences form c_t . b_s, and backward dy_t . x_s, before the other factors: these
+ * products have to be in fp32's range too.)
  * x [batch][length][heads][head_dim], dt [batch][length][heads], b and c
  * [batch][length][groups][state_dim], y as x; state and state_out
  * [batch][heads][head_dim][state_dim] (NULL: zeros / not wanted; state_out may be

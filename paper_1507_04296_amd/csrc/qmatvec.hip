@@ -153,7 +153,10 @@ __device__ __forceinline__ float sum_of(float sum, int64_t row, int out) {
 }
 
 constexpr int SUPER = 4;  // runs of 32 codes that a wave takes together
-constexpr int AHEAD = 4;  // of those, loaded before the first is used
+// Of those, loaded together.  (All of them are waited for before the first product: `raw`
+// is indexed in a loop that breaks off, so the compiler keeps it in scratch memory, 80
+// bytes a lane.)
+constexpr int AHEAD = 4;
 
 // What a wave has in LDS, and how many waves a workgroup has at most (one of 150 KB
 // of LDS takes 1.5 us longer to start than one of 40).
@@ -291,9 +294,10 @@ __global__ __launch_bounds__((64 * most_waves<T, RT>())) void matvec_kernel(Matv
 // kilobyte in one piece a wave) is all that an output costs beside the products.  fp32:
 // a code costs its conversion and one multiply-add a row, counts as 0 .. 15, and 8
 // times the sum of the inputs comes off; bf16: pairs as above in dot products of two;
-// 8-bit rows: integer dot products of four.  8192 x 8192, one row: fp32 17.6 us, bf16
-// 14.9, 8-bit 10.2 (the matrix unit's kernel 38, 30 and 22: its operands cost the
-// vector unit more than these products); four rows bf16 37.7, and 23.8 there.
+// 8-bit rows: integer dot products of four.  8192 x 8192, one row: fp32 15.2 us, bf16
+// 13.6, 8-bit 9.4 (the matrix unit's kernel 38, 30 and 22: its operands cost the
+// vector unit more than these products; what the three differ by is the work of a
+// code); four rows bf16 37.7, and 20.7 there.
 
 // Inputs of a lane's run, as the products take them, and the sum that the offset costs.
 template <class T> struct Run {

@@ -25,21 +25,25 @@
 // head, 64 channels), the state in registers: wave w holds 16 channels (w % 4) and
 // half of their states (w / 4).  Where there are few of those, sequences are cut into
 // segments whose states are formed first (state_kernel), joined (join_kernel), and
-// walked again side by side: a prompt of 8192 steps takes 63 us, where one workgroup a
+// walked again side by side: a prompt of 8192 steps takes 65 us, where one workgroup a
 // head would walk 256 chunks one after the other.
 //
-// What bounds it is the chain of a chunk (stage, decays, products, walk; four barriers
-// forward, seven backward with the states before the chunks walked again), not the
-// matrix unit or memory: fp32, 32 x 128 steps, 16 heads of 64, state 64: forward 28 us,
-// backward 71 us + 8 us for the sums over heads, the matrix unit busy a third of the
-// time.  bf16, 4 x 1999 steps, state 128: states 28 us (47 of both directions),
-// joins 9 us (14), forward 50 us; backward 194 us (one workgroup a compute unit, by its
-// LDS), sums 26 us (131 MB).
+// What bounds it is mostly the chain of a chunk (stage, decays, products, walk; four
+// barriers forward, seven backward with the states before the chunks walked again).
+// fp32, 32 x 128 steps, 16 heads of 64, state 64: forward 28 us, backward 71 us + 8 us
+// for the sums over heads, the matrix unit busy 30 % of the time.  bf16, 4 x 1999 steps,
+// state 128: states 29 us (46 of both directions), joins 9 us (14), forward 54 us;
+// backward 196 us, sums 26 us (131 MB), the matrix unit busy 10 % and less.  There the
+// backward also moves 395 MB of workspace (the chunks' states out and in, the parts of
+// db and dc), 82 us at the rate of a copy, with one workgroup a compute unit (132 KB of
+// LDS, 185 registers and more).
 // Chunks of 32 steps: with 64, the products inside a chunk double a step, and the
 // backward's LDS holds one workgroup a compute unit at state 64 too.
 //
 // Masked products multiply by zero, which is no mask for infinities and NaN, so a
-// chunk that holds any is walked one step at a time.
+// chunk that holds any is walked one step at a time.  Its products still have zeros
+// beside them (padded states and channels, the lower terms of bf16 rows' partners), so
+// that an infinity may come out as NaN; finite it never becomes within its episode.
 #include "planes.h"
 #include "seq.h"
 

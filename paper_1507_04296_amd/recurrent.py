@@ -1,6 +1,7 @@
-"""A recurrent Q-head on features, made of the sequence operators: the learner's pass
+"""A recurrent Q-head on feature rows, made of the sequence operators: the learner's pass
 over replayed sequences with its gradients, and the actors' single steps on a replica
-with 4-bit weights.
+with 4-bit weights.  The rows are the caller's, and so is what `backward` returns for
+them: the library's forward calls give Q values and actions, not the network's features.
 
     y = norm(f);  (x, B, C, dt) = W_in y;  (x, B, C) = conv(x, B, C)
     s = scan(x, dt, B, C);  u = W_out s;  h = norm(f + u);  Q = W_q h
@@ -58,7 +59,7 @@ class RecurrentCore:
         return out
 
     def workspace_bytes(self, batch: int, length: int, backward: bool = True) -> int:
-        """What a Context needs for forward (and backward) of [batch, length] steps."""
+        """What a Context needs for forward (and backward) of up to [batch, length] steps."""
         return max(scan_workspace_bytes(batch, length, self.heads, self.head_dim, self.groups, self.state_dim, backward),
                    causal_conv_workspace_bytes(self.channels, self.taps), add_rmsnorm_workspace_bytes(self.features))
 

@@ -2,10 +2,12 @@
 
 Every function checks its tensors, allocates its outputs and makes one call of the
 library on the current stream, in native code (csrc/binding.cpp): the host's time is
-what a single step costs.  include/gorila.h has the definitions, layouts and errors.  Rows (x, y, their gradients, windows) are float32 or bfloat16,
-parameters, parameter gradients, states and scales float32, resets uint8, slots
-int32.  Inputs may be strided in their leading dimensions.  `ctx` needs a workspace
-where a `*_workspace_bytes` function exists: ``Context(..., min_bytes=...)``.
+what a single step costs.  include/gorila.h has the definitions, layouts and errors.
+Rows (x, y, their gradients, windows) are float32 or bfloat16, parameters, parameter
+gradients, states and scales float32, resets uint8, slots int32.  Inputs may be strided
+in their leading dimensions.  `ctx` needs a workspace where a `*_workspace_bytes`
+function exists: ``Context(..., min_bytes=...)`` of the largest batch and length takes
+the smaller ones too.
 """
 from __future__ import annotations
 
