@@ -1,4 +1,4 @@
-"""Binding of the sequence operators: a recurrent core on the network's features.
+"""Binding of the sequence operators: a recurrent core on feature rows.
 
 Every function checks its tensors, allocates its outputs and makes one call of the
 library on the current stream, in native code (csrc/binding.cpp): the host's time is
