@@ -407,6 +407,32 @@ int gorila_add_rmsnorm_backward(const void* dy, int64_t dy_stride, const void* d
                                 const float* weight, int64_t rows, int32_t width, int32_t dtype,
                                 void* dx, float* dweight, gorila_ctx* ctx);
 
+/* Layer norm with the residual's addition, rows, strides and sizes as above:
+ *   total = x + residual, rounded to dtype (residual NULL: total = x),
+ *   mu = mean(total), rho = 1 / sqrt(mean((total - mu)^2) + eps),
+ *   y = (total - mu) * rho * weight + bias (bias NULL: none).
+ * The mean is taken out of the values before they are squared, with what its rounding
+ * leaves, so that a row's common offset costs no more than its own values' rounding.
+ * mean, rstd [rows] = mu, rho fp32; total, mean and rstd may be NULL.  EINVAL for
+ * eps < 0.  Sums and squares are fp32: values whose sum is past its range make the
+ * row NaN, deviations from about 2^63 on give rho 0.  A row of equal values is bias
+ * (NaN where eps is 0). */
+int gorila_add_layernorm(const void* x, int64_t x_stride, const void* residual,
+                         int64_t residual_stride, const float* weight, const float* bias,
+                         int64_t rows, int32_t width, int32_t dtype, float eps, void* y,
+                         void* total, float* mean, float* rstd, gorila_ctx* ctx);
+/* Gradients: with g = weight * dy and xh = (total - mu) * rho,
+ *   dx = dtotal + rho * (g - mean(g) - xh * mean(g * xh))
+ * [rows, width] (of x and of residual alike), dweight [width] = sum over rows of
+ * dy * xh, dbias [width] = sum of dy (may be NULL).  Uses
+ * gorila_add_layernorm_workspace_bytes(width) of the workspace. */
+size_t gorila_add_layernorm_workspace_bytes(int32_t width);
+int gorila_add_layernorm_backward(const void* dy, int64_t dy_stride, const void* dtotal,
+                                  int64_t dtotal_stride, const void* total, const float* mean,
+                                  const float* rstd, const float* weight, int64_t rows,
+                                  int32_t width, int32_t dtype, void* dx, float* dweight,
+                                  float* dbias, gorila_ctx* ctx);
+
 /* Short causal convolution of every channel with its own `taps` (2 .. 4) weights:
  *   v[t][c] = bias[c] + sum_j weight[c][j] * e[t - taps + 1 + j][c],
  *   y = v * sigmoid(v) (silu = 1) or v (silu = 0),
@@ -485,6 +511,49 @@ int gorila_scan_backward(const gorila_scan_args* args, const void* dy, int64_t d
 int gorila_scan_step(const gorila_scan_args* args, float* state_pool, int64_t slots,
                      const int32_t* slot, void* y, gorila_ctx* ctx);
 
+/* Gated scan: a recurrence with a state and two gates for every channel (the selective
+ * scan's state is head_dim x state_dim a head).
+ *   L = -exp(a_log[c]) * sigmoid(gate_a),   a = exp(L), 0 at a reset,
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) * sigmoid(gate_x) * x_t   (from `state`),   y = h.
+ * (At a reset the root is 1.)  1 - a^2 is formed from L, without cancellation.
+ * exp(a_log) past fp32's range counts as its largest value.
+ * x, gate_a, gate_x, y [batch][length][channels]; state and state_out
+ * [batch][channels] (NULL: zeros / not wanted; state_out may be state).  marks
+ * [batch][ceil(length / GORILA_GATED_MARK)][channels] fp32 (NULL: not wanted): the
+ * state before every GORILA_GATED_MARK-th step (`state` itself first), which the
+ * backward takes.  Uses gorila_gated_scan_workspace_bytes(..., backward) of the
+ * workspace (0: none), which is enough for every smaller batch and length too (few
+ * sequences are cut into segments, many are not).  A call of up to 256 steps never
+ * needs any forward. */
+enum { GORILA_GATED_MARK = 64 };
+typedef struct {
+    int32_t dtype, batch, length, channels;
+    const void* x;
+    int64_t x_batch_stride, x_step_stride;
+    const void* gate_a;
+    int64_t gate_a_batch_stride, gate_a_step_stride;
+    const void* gate_x;
+    int64_t gate_x_batch_stride, gate_x_step_stride;
+    const float* a_log;       /* [channels] */
+    const uint8_t* reset;     /* [batch][length] */
+    const float* state;
+} gorila_gated_scan_args;
+size_t gorila_gated_scan_workspace_bytes(int32_t batch, int32_t length, int32_t channels,
+                                         int32_t backward);
+int gorila_gated_scan(const gorila_gated_scan_args* args, void* y, float* state_out, float* marks,
+                      gorila_ctx* ctx);
+/* Gradients for dy and dstate_out (NULL: none) of every input: dx, dgate_a, dgate_x
+ * (contiguous), da_log [channels], dstate [batch][channels] (may be NULL).  marks as
+ * the forward call wrote them; args->state is unused (it is their first). */
+int gorila_gated_scan_backward(const gorila_gated_scan_args* args, const float* marks,
+                               const void* dy, int64_t dy_batch_stride, int64_t dy_step_stride,
+                               const float* dstate_out, void* dx, void* dgate_a, void* dgate_x,
+                               float* da_log, float* dstate, gorila_ctx* ctx);
+/* One step of `batch` rows (length 1): row i's state is state_pool[slot[i]]
+ * ([slots][channels]), updated in place; args->state is unused. */
+int gorila_gated_scan_step(const gorila_gated_scan_args* args, float* state_pool, int64_t slots,
+                           const int32_t* slot, void* y, gorila_ctx* ctx);
+
 /* 4-bit weights with group scales: w[o][k] stands for scales[o][k / group] *
  * (code - 8), code 0 .. 15.  codes [outputs][16 * ceil(inputs / 32)] bytes (whole
  * runs of 32 codes, what lies past `inputs` is never read as a weight): code k in
@@ -508,6 +577,87 @@ enum { GORILA_CODES = 2 };
 int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_t x_dtype,
                    int64_t rows, const uint8_t* codes, const float* scales, int32_t outputs,
                    int32_t inputs, int32_t group, void* y, gorila_ctx* ctx);
+
+/* ---- The update of many tensors, and actions sampled from values ---- */
+
+/* AdamW (decoupled weight decay) over `count` tensors in one call, with
+ * t = clock[0] + 1, g the gradient and every product, sum, root and quotient below one
+ * fp32 operation rounded once unless it says otherwise:
+ *   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + (1 - beta2) (g g)
+ *   (beta1, beta2 and their complements rounded to fp32 once),
+ *   theta' = theta - lr (decay theta + (m' / (1 - beta1^t)) / (sqrt(v' / (1 - beta2^t)) + eps))
+ *   (to fp32's precision).
+ * `tensors` is a HOST array, read before the call returns; what its members point to is
+ * on the device.  Elements are contiguous; grad is of grad_dtype (GORILA_F32 or
+ * GORILA_BF16).  No two tensors of a call may overlap.  Any alignment of the element
+ * types is accepted, 16 bytes (bf16 gradients: 8, codes: 4) is faster.
+ *
+ * state_bits 32: m and v are fp32 [n].  state_bits 8: m and v are codes u8 [n], and
+ * m_scale, v_scale fp32 [ceil(n / 256)] the largest |m'| and v' of each 256 consecutive
+ * elements; theta' is formed from m' and v' before they are held.  A code c > 0 of v
+ * stands for v_scale * f(c + 761), one of m (its low 7 bits; bit 7 is the sign) for
+ * m_scale * f(c + 889), rounded to fp32; f(k) is the fp32 value with the bits k << 20
+ * (three bits of mantissa; the last code is 1), code 0 is zero.  So v reaches down to
+ * 2^-31.75 of the block's largest, m to 2^-15.75 (smaller ones are held as zero; but
+ * v > 0 keeps code 1, so that no m is divided by eps alone).  A value q = size / scale
+ * is rounded to a neighbour by chance, so that slow averages keep moving: its code is
+ * ((bits(q) + 16 R) >> 20) - 761 (- 889), R 16 random bits.  Those of element e are in
+ *   z = mix(mix(seed + t G) + (p + 1) G),   p = sum over the tensors before of
+ *   ceil(n / 256) * 128, + floor(e / 2),
+ * mix the SplitMix64 output function, G = 0x9E3779B97F4A7C15: for even e bits 0 .. 15
+ * (m) and 16 .. 31 (v), for odd e 32 .. 47 and 48 .. 63.  A block with a value that is not
+ * finite gets NaN scales (of m, v or both) and codes 0.
+ *
+ * clock [3] fp64 (device, 8-byte aligned, zero before the first call): the number of
+ * steps taken, 1 - beta1^t and 1 - beta2^t; the call advances it, so that a captured
+ * call can be replayed.  keep (u8 device scalar, NULL = 1; e.g. of gorila_loss_filter):
+ * 0 leaves everything as it was, the clock included.
+ * EINVAL for beta outside [0, 1), eps < 0, lr < 0, n < 0.  n of 2^35 and more, and
+ * more than GORILA_ADAMW_MAX_TENSORS: GORILA_EUNSUPPORTED.  Uses no workspace. */
+#define GORILA_ADAMW_MAX_TENSORS 65536
+typedef struct {
+    float* theta;
+    const void* grad;
+    void* m;
+    void* v;
+    float* m_scale;           /* state_bits 8 */
+    float* v_scale;
+    int64_t n;
+    float decay;
+    int32_t reserved;
+} gorila_adamw_tensor;
+int gorila_adamw(const gorila_adamw_tensor* tensors, int32_t count, int32_t grad_dtype,
+                 int32_t state_bits, double* clock, const uint8_t* keep, float lr, double beta1,
+                 double beta2, float eps, uint64_t seed, gorila_ctx* ctx);
+/* What 8-bit states stand for: for each tensor (its m, v, m_scale, v_scale and n; the
+ * others are unused) m_out[i], v_out[i] fp32 [n].  m_out and v_out are HOST arrays of
+ * `count` device pointers. */
+int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float* const* m_out,
+                        float* const* v_out, gorila_ctx* ctx);
+
+/* Actions drawn from values (Q or logits) with given random numbers.  Row i of values
+ * ([rows] of `actions` (1 .. 2^20), dtype) is at values + i * stride elements; u [rows]
+ * fp32 in [0, 1).  temperature, top_p, min_p [rows] fp32 and top_k [rows] int32 may be
+ * NULL: 1, 1, 0 and all.  NaN counts as -infinity; with `most` the row's largest value,
+ *   w = round to nearest even of 2^40 exp((value - most) / temperature),
+ * formed in fp64 (2^40 where value = most, also if that is infinite; 0 for
+ * -infinity and beside an infinite `most`).  In the order of values, the lowest action
+ * first among equal ones:
+ *   top_k: the first k stay (k outside 1 .. actions: all; temperature not above 0:
+ *     one, the greedy action);
+ *   top_p < 1: an action stays if the sum of the w before it is less than
+ *     max(1, ceil(top_p * the sum of all that stayed)), the product in fp64;
+ *   min_p: an action stays if w >= ceil(min_p * 2^40) (min_p above 1 counts as 1).
+ * With S the sum of the w that stayed, the action is the first whose running sum, in
+ * the order of actions, is above min(floor(u S), S - 1), the product in fp64 (u not
+ * above 0, or NaN: 0; 1 and more: the last).  All sums are of whole numbers, so no order of
+ * addition shows.  probability_out (may be NULL) [rows] fp32: w / S.  A row without a value
+ * above -infinity has action -1 and probability 0.
+ * More than 2^20 actions: GORILA_EUNSUPPORTED.  Uses no workspace. */
+int gorila_sample_actions(const void* values, int64_t stride, int64_t rows, int32_t actions,
+                          int32_t dtype, const float* u, const float* temperature,
+                          const int32_t* top_k, const float* top_p, const float* min_p,
+                          int32_t* action_out, float* probability_out, gorila_ctx* ctx);
 
 #ifdef __cplusplus
 }

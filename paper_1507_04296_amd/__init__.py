@@ -37,7 +37,10 @@ EXPORTS = (
     "gorila_add_rmsnorm_backward", "gorila_causal_conv", "gorila_causal_conv_workspace_bytes",
     "gorila_causal_conv_backward", "gorila_causal_conv_step", "gorila_scan_workspace_bytes",
     "gorila_scan", "gorila_scan_backward", "gorila_scan_step", "gorila_quantize_weights",
-    "gorila_qmatvec",
+    "gorila_qmatvec", "gorila_add_layernorm", "gorila_add_layernorm_workspace_bytes",
+    "gorila_add_layernorm_backward", "gorila_gated_scan_workspace_bytes", "gorila_gated_scan",
+    "gorila_gated_scan_backward", "gorila_gated_scan_step", "gorila_adamw", "gorila_adamw_values",
+    "gorila_sample_actions",
 )
 NOALLOC_MAX_STATES = 256  # GORILA_NOALLOC_MAX_STATES
 
@@ -472,7 +475,10 @@ INF = math.inf
 
 _SEQUENCE = ("add_rmsnorm", "add_rmsnorm_codes", "add_rmsnorm_workspace_bytes", "add_rmsnorm_backward",
              "causal_conv", "causal_conv_workspace_bytes", "causal_conv_backward", "causal_conv_step",
-             "scan", "scan_workspace_bytes", "scan_backward", "scan_step", "quantize_weights", "qmatvec")
+             "scan", "scan_workspace_bytes", "scan_backward", "scan_step", "quantize_weights", "qmatvec",
+             "add_layernorm", "add_layernorm_workspace_bytes", "add_layernorm_backward",
+             "gated_scan", "gated_scan_workspace_bytes", "gated_scan_backward", "gated_scan_step",
+             "adamw", "adamw_clock", "adamw_state", "adamw_values", "sample_actions")
 
 
 def __getattr__(name: str):

@@ -1,0 +1,329 @@
+// AdamW over many tensors (gorila_adamw, gorila_adamw_values).
+//
+// Memory bound: fp32 states move 28 bytes an element (fp32 gradients), 8-bit ones 16,
+// for 20 and 60 operations.  A wave takes 256 consecutive elements, four a lane, so that
+// a block of 8-bit states has its largest value after six shuffles, and a workgroup's
+// chunk of elements is found by its number among those of all tensors, which
+// travel in the kernel's arguments: a launch for 48 tensors, and nothing to copy.
+#include "seq.h"
+
+namespace gorila {
+namespace {
+
+constexpr int MOST = 48;      // tensors a launch (its arguments hold 4 KB)
+constexpr int GROUP = 256;    // elements that share a scale
+constexpr int CHUNK = 2048;   // elements a workgroup: 256 lanes of four, twice
+constexpr uint64_t GOLDEN = 0x9E3779B97F4A7C15ull;
+
+struct Tensor {
+    float* theta;
+    const void* grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t n;
+    uint64_t place;  // of its first pair of elements among the random numbers
+    uint32_t chunk;  // its first among the launch's
+    float decay;
+};
+struct Tensors {
+    Tensor t[MOST];
+    int count;
+    uint64_t wide;  // bit i: tensor i is aligned for four elements a load
+};
+static_assert(sizeof(Tensors) <= 4032, "the arguments fit a launch's");
+
+struct Rule {
+    double* clock;
+    const uint8_t* keep;
+    float lr, eps, beta1, beta2, rest1, rest2;
+    uint64_t seed;
+};
+
+__device__ __forceinline__ uint64_t mix(uint64_t z) {  // SplitMix64's output function (Steele, Lea and Flood 2014)
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
+
+__global__ void clock_kernel(double* clock, const uint8_t* keep, double beta1, double beta2) {
+    if (keep && !*keep) return;
+    const double t = clock[0] + 1.0;
+    clock[0] = t;
+    clock[1] = 1.0 - pow(beta1, t);
+    clock[2] = 1.0 - pow(beta2, t);
+}
+
+// The tensor that holds the workgroup's chunk: the last one that starts at it or before.
+__device__ __forceinline__ int tensor_of(const Tensors& s, uint32_t chunk) {
+    int lo = 0, hi = s.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (s.t[mid].chunk <= chunk) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ f32x4 load4(const float* p, int n, bool wide) { return wide ? row_load<true>(p, n) : row_load<false>(p, n); }
+__device__ __forceinline__ f32x4 load4(const uint16_t* p, int n, bool wide) { return wide ? row_load<true>(p, n) : row_load<false>(p, n); }
+__device__ __forceinline__ void store4(float* p, f32x4 v, int n, bool wide) {
+    if (wide) row_store<true>(p, v, n);
+    else row_store<false>(p, v, n);
+}
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n, bool wide) {
+    if (wide) return n > 0 ? *(const uint32_t*)p : 0u;
+    uint32_t v = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < n) v |= (uint32_t)p[j] << (8 * j);
+    return v;
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t v, int n, bool wide) {
+    if (wide) {
+        if (n > 0) *(uint32_t*)p = v;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < n) p[j] = (uint8_t)(v >> (8 * j));
+}
+
+// Codes are the upper bits of an fp32 value of 2^-31.75 (m: 2^-15.75) to 1: three bits
+// of mantissa, so that a value is off by at most 1/16 of itself before chance
+// decides, where linear codes would lose all small ones.
+constexpr int LEAST_M = 889, LEAST_V = 761;
+__device__ __forceinline__ float value_of(uint32_t code, int least, float scale) {
+    const float unit = code ? __uint_as_float((code + least) << 20) : 0.0f;
+    return unit * scale;
+}
+__device__ __forceinline__ int code_of(float size, float most, uint32_t chance, int least) {
+    const float unit = most > 0.0f ? size / most : 0.0f;
+    const int c = (int)((__float_as_uint(unit) + (chance << 4)) >> 20) - least;
+    return c < 0 ? 0 : c;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+
+// G: the gradients' type; BITS: the states'.
+template <class G, int BITS>
+__global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
+// m' and v' are held to the bit as the header says: products and sums are rounded apart
+#pragma clang fp contract(off)
+    if (r.keep && !*r.keep) return;
+    const int which = tensor_of(s, blockIdx.x);
+    const Tensor& t = s.t[which];
+    const bool aligned = s.wide >> which & 1u;
+    const int64_t first = (int64_t)(blockIdx.x - t.chunk) * CHUNK;
+    const float c1 = 1.0f / (float)r.clock[1], c2 = 1.0f / (float)r.clock[2];
+    const uint64_t key = BITS == 8 ? mix(r.seed + (uint64_t)(int64_t)r.clock[0] * GOLDEN) : 0;
+#pragma unroll
+    for (int k = 0; k < CHUNK / 1024; ++k) {
+        const int64_t at = first + k * 1024 + threadIdx.x * 4, left = t.n - at;
+        const int n = left > 4 ? 4 : left > 0 ? (int)left : 0;
+        const bool wide = aligned && n == 4;
+        if (__ballot(n > 0) == 0) break;
+        const int64_t p = n > 0 ? at : 0;
+        f32x4 theta = load4(t.theta + p, n, wide);
+        const f32x4 g = load4((const G*)t.grad + p, n, wide);
+        f32x4 m, v;
+        uint32_t cm = 0, cv = 0;
+        const int64_t block = p / GROUP;
+        if (BITS == 32) {
+            m = load4((const float*)t.m + p, n, wide);
+            v = load4((const float*)t.v + p, n, wide);
+        } else {
+            cm = load_codes((const uint8_t*)t.m + p, n, wide);
+            cv = load_codes((const uint8_t*)t.v + p, n, wide);
+            const float sm = n > 0 ? t.m_scale[block] : 0.0f, sv = n > 0 ? t.v_scale[block] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t c = cm >> (8 * j) & 255u;
+                const float size = value_of(c & 127u, LEAST_M, sm);
+                m[j] = c & 128u ? -size : size;
+                v[j] = value_of(cv >> (8 * j) & 255u, LEAST_V, sv);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            m[j] = r.beta1 * m[j] + r.rest1 * g[j];
+            v[j] = r.beta2 * v[j] + r.rest2 * (g[j] * g[j]);
+            const float step = m[j] * c1 / (sqrtf(v[j] * c2) + r.eps);
+            theta[j] = theta[j] - r.lr * (t.decay * theta[j] + step);
+        }
+        if (n > 0) store4(t.theta + p, theta, n, wide);
+        if (BITS == 32) {
+            if (n > 0) {
+                store4((float*)t.m + p, m, n, wide);
+                store4((float*)t.v + p, v, n, wide);
+            }
+            continue;
+        }
+        float mm = 0.0f, mv = 0.0f, bad_m = 0.0f, bad_v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j >= n) m[j] = v[j] = 0.0f;
+            mm = fmaxf(mm, fabsf(m[j])), mv = fmaxf(mv, v[j]);
+            bad_m += m[j] * 0.0f, bad_v += v[j] * 0.0f;
+        }
+        mm = wave_max(bad_m == bad_m ? mm : INFINITY);
+        mv = wave_max(bad_v == bad_v ? mv : INFINITY);
+        cm = cv = 0;
+        const uint64_t pair = t.place + (uint64_t)p / 2;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint64_t z = mix(key + (pair + h + 1) * GOLDEN);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int j = 2 * h + i;
+                const uint32_t chance = (uint32_t)(z >> (32 * i));
+                uint32_t a = code_of(fabsf(m[j]), mm, chance & 0xffffu, LEAST_M), b = code_of(v[j], mv, chance >> 16, LEAST_V);
+                if (v[j] > 0.0f && b == 0) b = 1;
+                if (m[j] < 0.0f) a |= 128u;
+                if (mm == INFINITY) a = 0;
+                if (mv == INFINITY) b = 0;
+                cm |= a << (8 * j), cv |= b << (8 * j);
+            }
+        }
+        if (n > 0) {
+            store_codes((uint8_t*)t.m + p, cm, n, wide);
+            store_codes((uint8_t*)t.v + p, cv, n, wide);
+            if ((threadIdx.x & 63) == 0) {
+                t.m_scale[block] = mm == INFINITY ? NAN : mm;
+                t.v_scale[block] = mv == INFINITY ? NAN : mv;
+            }
+        }
+    }
+}
+
+// theta and grad: where m's and v's values go.
+__global__ __launch_bounds__(256) void values_kernel(Tensors s) {
+    const int which = tensor_of(s, blockIdx.x);
+    const Tensor& t = s.t[which];
+    const bool aligned = s.wide >> which & 1u;
+    const int64_t first = (int64_t)(blockIdx.x - t.chunk) * CHUNK;
+#pragma unroll
+    for (int k = 0; k < CHUNK / 1024; ++k) {
+        const int64_t p = first + k * 1024 + threadIdx.x * 4, left = t.n - p;
+        if (left <= 0) return;
+        const int n = left > 4 ? 4 : (int)left;
+        const bool wide = aligned && n == 4;
+        const uint32_t cm = load_codes((const uint8_t*)t.m + p, n, wide), cv = load_codes((const uint8_t*)t.v + p, n, wide);
+        const float sm = t.m_scale[p / GROUP], sv = t.v_scale[p / GROUP];
+        f32x4 m, v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t c = cm >> (8 * j) & 255u;
+            const float size = value_of(c & 127u, LEAST_M, sm);
+            m[j] = c & 128u ? -size : size;
+            v[j] = value_of(cv >> (8 * j) & 255u, LEAST_V, sv);
+        }
+        store4(t.theta + p, m, n, wide);
+        store4((float*)t.grad + p, v, n, wide);
+    }
+}
+
+// ---- host ----
+
+// Calls launch(tensors, chunks) for the tensors that have elements, MOST or as many chunks
+// as a launch holds at a time; fill(i, t) sets the addresses and says whether all are aligned.
+template <class F, class L>
+void by_launch(const gorila_adamw_tensor* tensors, int count, F&& fill, L&& launch) {
+    Tensors s{};
+    uint64_t chunks = 0, place = 0;
+    auto flush = [&] {
+        if (s.count) launch(s, (unsigned)chunks);
+        s.count = 0, s.wide = 0, chunks = 0;
+    };
+    for (int i = 0; i < count; ++i) {
+        const int64_t n = tensors[i].n;
+        const uint64_t need = (uint64_t)(n + CHUNK - 1) / CHUNK;
+        if (need > 0) {
+            if (s.count == MOST || !launch_fits((double)(chunks + need), 256)) flush();
+            Tensor& t = s.t[s.count];
+            t.n = n, t.place = place, t.chunk = (uint32_t)chunks, t.decay = tensors[i].decay;
+            if (fill(tensors[i], i, t)) s.wide |= 1ull << s.count;
+            ++s.count;
+            chunks += need;
+        }
+        place += (uint64_t)(n + GROUP - 1) / GROUP * (GROUP / 2);
+    }
+    flush();
+}
+
+int check_count(const gorila_adamw_tensor* tensors, int count) {
+    if (count < 0 || (count > 0 && !tensors)) return GORILA_EINVAL;
+    for (int i = 0; i < count; ++i)
+        if (tensors[i].n < 0) return GORILA_EINVAL;
+    if (count > GORILA_ADAMW_MAX_TENSORS) return GORILA_EUNSUPPORTED;
+    for (int i = 0; i < count; ++i)
+        if (!launch_fits((double)((tensors[i].n + CHUNK - 1) / CHUNK), 256)) return GORILA_EUNSUPPORTED;
+    return GORILA_OK;
+}
+// What 8-bit states need of a tensor with elements.
+bool held8(const gorila_adamw_tensor& t) { return t.m && t.v && t.m_scale && t.v_scale && at_element(t.m_scale, 4) && at_element(t.v_scale, 4); }
+
+}  // namespace
+}  // namespace gorila
+
+using namespace gorila;
+
+extern "C" {
+
+int gorila_adamw(const gorila_adamw_tensor* tensors, int32_t count, int32_t grad_dtype, int32_t state_bits, double* clock,
+                 const uint8_t* keep, float lr, double beta1, double beta2, float eps, uint64_t seed, gorila_ctx* ctx) {
+    CtxView c;
+    int rc = ctx_view(ctx, 0, c);
+    if (rc || (rc = check_count(tensors, count))) return rc;
+    if (!row_dtype(grad_dtype) || (state_bits != 8 && state_bits != 32) || !clock || !at_element(clock, 8)) return GORILA_EINVAL;
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0f && eps < INFINITY) || !(lr >= 0.0f && lr < INFINITY))
+        return GORILA_EINVAL;
+    const int e = dtype_bytes(grad_dtype);
+    for (int i = 0; i < count; ++i) {
+        const gorila_adamw_tensor& t = tensors[i];
+        if (t.n == 0) continue;
+        if (!t.theta || !t.grad || !t.m || !t.v || !at_element(t.theta, 4) || !at_element(t.grad, e)) return GORILA_EINVAL;
+        if (state_bits == 8 ? !held8(t) : !at_element(t.m, 4) || !at_element(t.v, 4)) return GORILA_EINVAL;
+    }
+    Rule r{clock, keep, lr, eps, (float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), seed};
+    clock_kernel<<<1, 1, 0, c.stream>>>(clock, keep, beta1, beta2);
+    by_launch(
+        tensors, count,
+        [&](const gorila_adamw_tensor& from, int, Tensor& t) {
+            t.theta = from.theta, t.grad = from.grad, t.m = from.m, t.v = from.v, t.m_scale = from.m_scale, t.v_scale = from.v_scale;
+            const int bytes = state_bits == 8 ? 1 : 4;
+            return aligned16(t.theta) && at_four(t.grad, e) && at_four(t.m, bytes) && at_four(t.v, bytes);
+        },
+        [&](const Tensors& s, unsigned chunks) {
+            if (grad_dtype == GORILA_F32) {
+                if (state_bits == 32) adamw_kernel<float, 32><<<chunks, 256, 0, c.stream>>>(s, r);
+                else adamw_kernel<float, 8><<<chunks, 256, 0, c.stream>>>(s, r);
+            } else {
+                if (state_bits == 32) adamw_kernel<uint16_t, 32><<<chunks, 256, 0, c.stream>>>(s, r);
+                else adamw_kernel<uint16_t, 8><<<chunks, 256, 0, c.stream>>>(s, r);
+            }
+        });
+    return launched();
+}
+
+int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float* const* m_out, float* const* v_out, gorila_ctx* ctx) {
+    CtxView c;
+    int rc = ctx_view(ctx, 0, c);
+    if (rc || (rc = check_count(tensors, count))) return rc;
+    if (count > 0 && (!m_out || !v_out)) return GORILA_EINVAL;
+    for (int i = 0; i < count; ++i)
+        if (tensors[i].n > 0 && (!held8(tensors[i]) || !m_out[i] || !v_out[i] || !at_element(m_out[i], 4) || !at_element(v_out[i], 4)))
+            return GORILA_EINVAL;
+    by_launch(
+        tensors, count,
+        [&](const gorila_adamw_tensor& from, int i, Tensor& t) {
+            t.m = from.m, t.v = from.v, t.m_scale = from.m_scale, t.v_scale = from.v_scale, t.theta = m_out[i], t.grad = v_out[i];
+            return aligned16(t.theta) && aligned16(t.grad) && at_four(t.m, 1) && at_four(t.v, 1);
+        },
+        [&](const Tensors& s, unsigned chunks) { values_kernel<<<chunks, 256, 0, c.stream>>>(s); });
+    return launched();
+}
+
+}  // extern "C"

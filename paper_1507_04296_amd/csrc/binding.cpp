@@ -11,7 +11,10 @@
 #include <ATen/ATen.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <array>
 #include <string>
+#include <vector>
 
 #include "../../include/gorila.h"
 
@@ -35,6 +38,14 @@ struct Api {
     decltype(&gorila_scan_step) scan_step;
     decltype(&gorila_quantize_weights) quantize_weights;
     decltype(&gorila_qmatvec) qmatvec;
+    decltype(&gorila_add_layernorm) add_layernorm;
+    decltype(&gorila_add_layernorm_backward) add_layernorm_backward;
+    decltype(&gorila_gated_scan) gated_scan;
+    decltype(&gorila_gated_scan_backward) gated_scan_backward;
+    decltype(&gorila_gated_scan_step) gated_scan_step;
+    decltype(&gorila_adamw) adamw;
+    decltype(&gorila_adamw_values) adamw_values;
+    decltype(&gorila_sample_actions) sample_actions;
 };
 Api api{};
 PyObject* raise_code = nullptr;  // of a return code and a call's name
@@ -76,10 +87,16 @@ struct Call {
         if (v == -1 && PyErr_Occurred()) throw Refused{nullptr, ""};
         return v;
     }
-    float number(int i) const {
+    double real(int i) const {
         const double v = PyFloat_AsDouble(a[i]);
         if (v == -1.0 && PyErr_Occurred()) throw Refused{nullptr, ""};
-        return (float)v;
+        return v;
+    }
+    float number(int i) const { return (float)real(i); }
+    uint64_t bits(int i) const {
+        const uint64_t v = PyLong_AsUnsignedLongLong(a[i]);
+        if (PyErr_Occurred()) throw Refused{nullptr, ""};
+        return v;
     }
     const Tensor* maybe(int i, const char* name) const {
         if (a[i] == Py_None) return nullptr;
@@ -388,6 +405,242 @@ PyObject* qmatvec(PyObject* const* args, Py_ssize_t n) {
     return one(y);
 }
 
+// ---- layer norm ----
+
+// x, weight, bias, residual, eps
+PyObject* add_layernorm(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 8);
+    const Tensor &x = c.tensor(3, "x"), &w = c.tensor(4, "weight");
+    const Tensor *b = c.maybe(5, "bias"), *r = c.maybe(6, "residual");
+    want(x.dim() == 2, "x must be [rows, width]");
+    const int64_t rows = x.size(0), width = x.size(1);
+    const int32_t dtype = row_type(x);
+    const void *px = c.at(x, "x", x.sizes(), x.scalar_type(), 1), *pr = c.at(r, "residual", x.sizes(), x.scalar_type(), 1);
+    const float *pw = (const float*)c.at(w, "weight", {width}, F32), *pb = (const float*)c.at(b, "bias", {width}, F32);
+    const Tensor y = same(x), total = r || !x.is_contiguous() ? same(x) : Tensor(), mean = make({rows}, x, F32), rstd = make({rows}, x, F32);
+    c.check(api.add_layernorm(px, x.stride(0), pr, r ? r->stride(0) : 0, pw, pb, rows, size32(width), dtype, c.number(7), ptr(y), ptr(total),
+                              (float*)ptr(mean), (float*)ptr(rstd), c.ctx), "gorila_add_layernorm");
+    return tuple({&y, total.defined() ? &total : &x, &mean, &rstd});
+}
+
+// dy, total, mean, rstd, weight, dtotal
+PyObject* add_layernorm_backward(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 9);
+    const Tensor &dy = c.tensor(3, "dy"), &total = c.tensor(4, "total");
+    const Tensor* dtotal = c.maybe(8, "dtotal");
+    want(total.dim() == 2, "total must be [rows, width]");
+    const int64_t rows = total.size(0), width = total.size(1);
+    const int32_t dtype = row_type(total);
+    const auto typ = total.scalar_type();
+    const void *pdy = c.at(dy, "dy", total.sizes(), typ, 1), *pdt = c.at(dtotal, "dtotal", total.sizes(), typ, 1);
+    const void* pt = c.at(total, "total", total.sizes(), typ);
+    const float *mean = (const float*)c.at(c.tensor(5, "mean"), "mean", {rows}, F32),
+                *rstd = (const float*)c.at(c.tensor(6, "rstd"), "rstd", {rows}, F32),
+                *weight = (const float*)c.at(c.tensor(7, "weight"), "weight", {width}, F32);
+    const Tensor dx = same(total), dweight = make({width}, total, F32), dbias = make({width}, total, F32);
+    c.check(api.add_layernorm_backward(pdy, dy.stride(0), pdt, dtotal ? dtotal->stride(0) : 0, pt, mean, rstd, weight, rows, size32(width),
+                                       dtype, ptr(dx), (float*)ptr(dweight), (float*)ptr(dbias), c.ctx), "gorila_add_layernorm_backward");
+    return tuple({&dx, &dweight, &dbias});
+}
+
+// ---- gated scan ----
+
+// x, gate_a, gate_x, a_log from argument `i` on, reset at `reset`.
+struct Gated {
+    const Tensor &x, &ga, &gx;
+    gorila_gated_scan_args a{};
+    Gated(const Call& k, int i, int reset, bool step) : x(k.tensor(i, "x")), ga(k.tensor(i + 1, "gate_a")), gx(k.tensor(i + 2, "gate_x")) {
+        const int64_t lead = step ? 1 : 2;
+        want(x.dim() == lead + 1, step ? "x must be [rows, channels]" : "x must be [batch, length, channels]");
+        a.dtype = row_type(x);
+        const auto typ = x.scalar_type();
+        a.batch = size32(x.size(0)), a.length = step ? 1 : size32(x.size(1)), a.channels = size32(x.size(lead));
+        a.x = k.at(x, "x", x.sizes(), typ, lead);
+        a.gate_a = k.at(ga, "gate_a", x.sizes(), typ, lead);
+        a.gate_x = k.at(gx, "gate_x", x.sizes(), typ, lead);
+        a.x_batch_stride = x.stride(0), a.gate_a_batch_stride = ga.stride(0), a.gate_x_batch_stride = gx.stride(0);
+        if (!step) a.x_step_stride = x.stride(1), a.gate_a_step_stride = ga.stride(1), a.gate_x_step_stride = gx.stride(1);
+        a.a_log = (const float*)k.at(k.tensor(i + 3, "a_log"), "a_log", {(int64_t)a.channels}, F32);
+        a.reset = (const uint8_t*)k.at(k.maybe(reset, "reset"), "reset", x.sizes().slice(0, (size_t)lead), at::kByte);
+    }
+    std::array<int64_t, 2> state() const { return {a.batch, a.channels}; }
+    std::array<int64_t, 3> marks() const { return {a.batch, ((int64_t)a.length + GORILA_GATED_MARK - 1) / GORILA_GATED_MARK, a.channels}; }
+};
+
+// x, gate_a, gate_x, a_log, reset, state, marks
+PyObject* gated_scan(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 10);
+    Gated v(c, 3, 7, false);
+    v.a.state = (const float*)c.at(c.maybe(8, "state"), "state", v.state(), F32);
+    const Tensor y = same(v.x), out = make(v.state(), v.x, F32), marks = c.integer(9) ? make(v.marks(), v.x, F32) : Tensor();
+    c.check(api.gated_scan(&v.a, ptr(y), (float*)ptr(out), (float*)ptr(marks), c.ctx), "gorila_gated_scan");
+    return tuple({&y, &out, &marks});
+}
+
+// dy, x, gate_a, gate_x, a_log, marks, reset, dstate_out
+PyObject* gated_scan_backward(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 11);
+    const Gated v(c, 4, 9, false);
+    const Tensor& dy = c.tensor(3, "dy");
+    const void* pdy = c.at(dy, "dy", v.x.sizes(), v.x.scalar_type(), 2);
+    const float* marks = (const float*)c.at(c.tensor(8, "marks"), "marks", v.marks(), F32);
+    const float* pds = (const float*)c.at(c.maybe(10, "dstate_out"), "dstate_out", v.state(), F32);
+    const Tensor dx = same(v.x), dga = same(v.x), dgx = same(v.x), da = make({(int64_t)v.a.channels}, v.x, F32), ds = make(v.state(), v.x, F32);
+    c.check(api.gated_scan_backward(&v.a, marks, pdy, dy.stride(0), dy.stride(1), pds, ptr(dx), ptr(dga), ptr(dgx), (float*)ptr(da),
+                                    (float*)ptr(ds), c.ctx), "gorila_gated_scan_backward");
+    return tuple({&dx, &dga, &dgx, &da, &ds});
+}
+
+// x, gate_a, gate_x, a_log, state_pool, slot, reset
+PyObject* gated_scan_step(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 10);
+    const Gated v(c, 3, 9, true);
+    const Tensor& pool = c.tensor(7, "state_pool");
+    want(pool.dim() == 2, "state_pool must be [slots, channels]");
+    const int64_t slots = pool.size(0);
+    float* p = (float*)c.at(pool, "state_pool", {slots, (int64_t)v.a.channels}, F32);
+    const int32_t* slot = (const int32_t*)c.at(c.maybe(8, "slot"), "slot", {(int64_t)v.a.batch}, at::kInt);
+    const Tensor y = same(v.x);
+    c.check(api.gated_scan_step(&v.a, p, slots, slot, ptr(y), c.ctx), "gorila_gated_scan_step");
+    return one(y);
+}
+
+// ---- AdamW ----
+
+struct Listed {  // a list or tuple; it must outlive what is taken from it
+    PyObject* o;
+    Py_ssize_t n;
+    Listed(PyObject* from, const char* name) {
+        if (!PyList_Check(from) && !PyTuple_Check(from)) type(std::string(name) + " must be a list or a tuple");
+        o = from, n = PySequence_Fast_GET_SIZE(from);
+    }
+    PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(o, i); }
+    const Tensor& tensor(Py_ssize_t i, const char* name) const {
+        if (!THPVariable_Check((*this)[i])) type(std::string(name) + " must hold tensors");
+        return THPVariable_Unpack((*this)[i]);
+    }
+};
+struct Written {  // bytes that a call writes
+    std::vector<std::pair<const char*, const char*>> spans;
+    void add(const void* p, int64_t bytes) {
+        if (bytes > 0) spans.emplace_back((const char*)p, (const char*)p + bytes);
+    }
+    void check() {
+        std::sort(spans.begin(), spans.end());
+        for (size_t i = 1; i < spans.size(); ++i) want(spans[i].first >= spans[i - 1].second, "tensors and states must not overlap");
+    }
+};
+// m and v of a state, and its scales where it has four members (8 bits).
+int state_of(const Call& c, PyObject* state, c10::IntArrayRef shape, int64_t n, gorila_adamw_tensor& t, Written& w) {
+    const Listed s(state, "a state");
+    want(s.n == 2 || s.n == 4, "a state is (m, v), or (m, v, m_scale, v_scale) in 8 bits");
+    const auto typ = s.n == 2 ? F32 : at::kByte;
+    const int64_t bytes = s.n == 2 ? 4 : 1, groups = (n + 255) / 256;
+    t.m = c.at(s.tensor(0, "a state"), "m", shape, typ);
+    t.v = c.at(s.tensor(1, "a state"), "v", shape, typ);
+    w.add(t.m, n * bytes), w.add(t.v, n * bytes);
+    if (s.n == 4) {
+        t.m_scale = (float*)c.at(s.tensor(2, "a state"), "m_scale", {groups}, F32);
+        t.v_scale = (float*)c.at(s.tensor(3, "a state"), "v_scale", {groups}, F32);
+        w.add(t.m_scale, groups * 4), w.add(t.v_scale, groups * 4);
+    }
+    return s.n == 2 ? 32 : 8;
+}
+
+// thetas, grads, states, clock, lr, beta1, beta2, eps, decay, seed, keep
+PyObject* adamw(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 14);
+    const Listed thetas(args[3], "thetas"), grads(args[4], "grads"), states(args[5], "states");
+    want(grads.n == thetas.n && states.n == thetas.n, "thetas, grads and states must be as many");
+    const bool each = PyList_Check(args[11]) || PyTuple_Check(args[11]);
+    if (each) want(PySequence_Fast_GET_SIZE(args[11]) == thetas.n, "decay must be a number, or one for each tensor");
+    const float all = each ? 0.0f : c.number(11);
+    std::vector<gorila_adamw_tensor> ts((size_t)thetas.n);
+    Written w;
+    int bits = 32;
+    int32_t dtype = GORILA_F32;
+    for (Py_ssize_t i = 0; i < thetas.n; ++i) {
+        gorila_adamw_tensor& t = ts[(size_t)i];
+        const Tensor &theta = thetas.tensor(i, "thetas"), &grad = grads.tensor(i, "grads");
+        t = gorila_adamw_tensor{};
+        t.n = theta.numel();
+        t.theta = (float*)c.at(theta, "theta", theta.sizes(), F32);
+        const int32_t d = row_type(grad);
+        t.grad = c.at(grad, "grad", theta.sizes(), grad.scalar_type());
+        w.add(t.theta, t.n * 4);
+        const int b = state_of(c, states[i], theta.sizes(), t.n, t, w);
+        if (i == 0) bits = b, dtype = d;
+        want(b == bits && d == dtype, "all states have the same bits and all gradients the same type");
+        t.decay = all;
+        if (each) {
+            const double v = PyFloat_AsDouble(PySequence_Fast_GET_ITEM(args[11], i));
+            if (v == -1.0 && PyErr_Occurred()) throw Refused{nullptr, ""};
+            t.decay = (float)v;
+        }
+    }
+    double* clock = (double*)c.at(c.tensor(6, "clock"), "clock", {3}, at::kDouble);
+    w.add(clock, 24);
+    w.check();
+    const Tensor* keep = c.maybe(13, "keep");
+    const uint8_t* pk = keep ? (const uint8_t*)c.at(keep, "keep", {1}, at::kByte) : nullptr;
+    c.check(api.adamw(ts.data(), size32(thetas.n), dtype, bits, clock, pk, c.number(7), c.real(8), c.real(9), c.number(10), c.bits(12), c.ctx),
+            "gorila_adamw");
+    Py_RETURN_NONE;
+}
+
+// states
+PyObject* adamw_values(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 4);
+    const Listed states(args[3], "states");
+    std::vector<gorila_adamw_tensor> ts((size_t)states.n);
+    std::vector<Tensor> m, v;
+    std::vector<float*> pm, pv;
+    Written w;
+    for (Py_ssize_t i = 0; i < states.n; ++i) {
+        const Tensor& first = Listed(states[i], "a state").n > 0 ? Listed(states[i], "a state").tensor(0, "a state") : Tensor();
+        ts[(size_t)i] = gorila_adamw_tensor{};
+        ts[(size_t)i].n = first.defined() ? first.numel() : 0;
+        want(state_of(c, states[i], first.sizes(), ts[(size_t)i].n, ts[(size_t)i], w) == 8, "the states must be held in 8 bits");
+        m.push_back(make(first.sizes(), first, F32)), v.push_back(make(first.sizes(), first, F32));
+        pm.push_back((float*)ptr(m.back())), pv.push_back((float*)ptr(v.back()));
+    }
+    c.check(api.adamw_values(ts.data(), size32(states.n), pm.data(), pv.data(), c.ctx), "gorila_adamw_values");
+    PyObject* o = PyList_New(states.n);
+    if (!o) throw Refused{nullptr, ""};
+    for (Py_ssize_t i = 0; i < states.n; ++i) {
+        PyObject* pair = nullptr;
+        try {
+            pair = tuple({&m[(size_t)i], &v[(size_t)i]});
+        } catch (...) {
+            Py_DECREF(o);
+            throw;
+        }
+        PyList_SET_ITEM(o, i, pair);
+    }
+    return o;
+}
+
+// ---- sampled actions ----
+
+// values, u, temperature, top_k, top_p, min_p
+PyObject* sample_actions(PyObject* const* args, Py_ssize_t n) {
+    const Call c(args, n, 9);
+    const Tensor& values = c.tensor(3, "values");
+    want(values.dim() == 2, "values must be [rows, actions]");
+    const int32_t dtype = row_type(values);
+    const int64_t rows = values.size(0), actions = values.size(1);
+    const void* p = c.at(values, "values", values.sizes(), values.scalar_type(), 1);
+    const float* u = (const float*)c.at(c.tensor(4, "u"), "u", {rows}, F32);
+    const float* t = (const float*)c.at(c.maybe(5, "temperature"), "temperature", {rows}, F32);
+    const int32_t* k = (const int32_t*)c.at(c.maybe(6, "top_k"), "top_k", {rows}, at::kInt);
+    const float* tp = (const float*)c.at(c.maybe(7, "top_p"), "top_p", {rows}, F32);
+    const float* mp = (const float*)c.at(c.maybe(8, "min_p"), "min_p", {rows}, F32);
+    const Tensor action = make({rows}, values, at::kInt), probability = make({rows}, values, F32);
+    c.check(api.sample_actions(p, values.stride(0), rows, size32(actions), dtype, u, t, k, tp, mp, (int32_t*)ptr(action), (float*)ptr(probability),
+                               c.ctx), "gorila_sample_actions");
+    return tuple({&action, &probability});
+}
+
 // The Python entry: what is thrown below becomes a Python exception.
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -428,6 +681,14 @@ PyObject* init(PyObject* const* args, Py_ssize_t n) {
     take(p.scan_step, d, "gorila_scan_step");
     take(p.quantize_weights, d, "gorila_quantize_weights");
     take(p.qmatvec, d, "gorila_qmatvec");
+    take(p.add_layernorm, d, "gorila_add_layernorm");
+    take(p.add_layernorm_backward, d, "gorila_add_layernorm_backward");
+    take(p.gated_scan, d, "gorila_gated_scan");
+    take(p.gated_scan_backward, d, "gorila_gated_scan_backward");
+    take(p.gated_scan_step, d, "gorila_gated_scan_step");
+    take(p.adamw, d, "gorila_adamw");
+    take(p.adamw_values, d, "gorila_adamw_values");
+    take(p.sample_actions, d, "gorila_sample_actions");
     Py_INCREF(args[1]);
     Py_XDECREF(raise_code);
     raise_code = args[1];
@@ -438,7 +699,9 @@ PyObject* init(PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(init), ENTRY(add_rmsnorm), ENTRY(add_rmsnorm_codes), ENTRY(add_rmsnorm_backward), ENTRY(causal_conv),
                          ENTRY(causal_conv_backward), ENTRY(causal_conv_step), ENTRY(scan), ENTRY(scan_backward), ENTRY(scan_step),
-                         ENTRY(quantize_weights), ENTRY(qmatvec), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(quantize_weights), ENTRY(qmatvec), ENTRY(add_layernorm), ENTRY(add_layernorm_backward),
+                         ENTRY(gated_scan), ENTRY(gated_scan_backward), ENTRY(gated_scan_step), ENTRY(adamw), ENTRY(adamw_values),
+                         ENTRY(sample_actions), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Native half of the sequence operators' binding.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

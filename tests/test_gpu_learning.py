@@ -1,0 +1,732 @@
+"""The layer norm, the gated scan, AdamW and sampled actions on the GPU against their
+definitions in 64 bits (learning_ref.py), at the sizes, strides, resets, masks and
+values where they can go wrong.
+
+Tolerances, relative L2.  fp32 results are sums of at most a few hundred rounded products
+(each 2^-24 relative, adding as a random walk) on both sides of one or two
+exponentials (2 units of the last place): 2e-6 forward; a gradient passes three such
+stages: 1e-5.  bf16 results are those rounded once, to 8 bits: at most 2^-8.  An AdamW
+step is ten operations of 2^-24 each at most on a change that is a part of theta: 1e-6 of
+the change and half a unit of theta.  Codes, scales, averages and actions are equal; a
+probability is rounded once from 64 bits: 2^-24 and what a weight's last unit (2^-40) is.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import learning_ref as ref
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+FWD, BWD, HALF = 2e-6, 1e-5, 2.0 ** -8
+EPS = 1e-5
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(scope="module")
+def g():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm device")
+    import paper_1507_04296_amd as gmod
+    gmod.lib()
+    return gmod
+
+
+@pytest.fixture(scope="module")
+def ctx(g):
+    c = g.Context(1, 1, min_bytes=1 << 28)
+    yield c
+    c.check()
+    c.close()
+
+
+def spoil(ctx):
+    """What a call has not written itself is NaN."""
+    ctx.workspace[8192:].fill_(255)
+
+
+def rand(*shape, dtype=F32, scale=1.0, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    return (scale * torch.randn(shape, generator=gen)).to(dtype).cuda()
+
+
+def uniform(*shape, seed=0):
+    return torch.rand(shape, generator=torch.Generator().manual_seed(seed)).cuda()
+
+
+def close(got, want, tol, what="", size=None):
+    got, want = got.detach().cpu().double(), want.detach().cpu().double()
+    assert got.shape == want.shape, what
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(got), fine), f"{what}: other values are finite"
+    size = float(want[fine].norm()) if size is None else size
+    off = float((got[fine] - want[fine]).norm())
+    assert off <= tol * size + 1e-30, f"{what}: {off / max(size, 1e-300):.2e} over {tol:.1e}"
+
+
+def tol_of(dtype, exact):
+    return exact if dtype == F32 else HALF
+
+
+def strided(t, lead, extra=3, off=0):
+    """The same values as a view into wider rows, `off` elements past their start."""
+    inner = math.prod(t.shape[lead:])
+    wide = torch.full((*t.shape[:lead], inner + extra + off), 7.0, dtype=t.dtype, device=t.device)
+    wide[..., off:off + inner] = t.reshape(*t.shape[:lead], inner)
+    return wide[..., off:off + inner].unflatten(-1, t.shape[lead:])
+
+
+def replayed(call, outputs, eager):
+    """Captures call() and compares `outputs` with the eager ones after each of several replays."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for _ in range(3):
+        for o in outputs(got):
+            o.fill_(3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outputs(got), eager):
+            assert torch.equal(a, b)
+
+
+# ---- layer norm ----
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width", [(1, 1), (3, 5), (5, 64), (1, 512), (257, 512), (7, 1000), (2, 2047), (3, 3136), (2, 5000),
+                                        (2, 8190), (2, 16384), (1, 40003), (5000, 36)])
+def test_layernorm(g, ctx, rows, width, dtype):
+    x, r = rand(rows, width, dtype=dtype, seed=1), rand(rows, width, dtype=dtype, scale=2.0, seed=2)
+    w, b = 1 + rand(width, scale=0.1, seed=3), rand(width, scale=0.1, seed=6)
+    dy, dt = rand(rows, width, dtype=dtype, seed=4), rand(rows, width, dtype=dtype, seed=5)
+    y, total, mean, rstd = g.add_layernorm(ctx, x, w, b, r, EPS)
+    assert torch.equal(total, (x.float() + r.float()).to(dtype))
+    want, wmean, rho = ref.layernorm(total, w, b, EPS)
+    close(y, want, tol_of(dtype, FWD), "y")
+    if width > 1:  # (a single value's mean is itself, and its deviation nothing)
+        close(mean, wmean, FWD, "mean", size=float(total.double().norm()) / math.sqrt(width))
+    close(rstd, rho, FWD, "rstd")
+    spoil(ctx)
+    dx, dw, db = g.add_layernorm_backward(ctx, dy, total, mean, rstd, w, dt)
+    wdx, wdw, wdb = ref.layernorm_backward(dy, total, w, EPS, dt)
+    # what cancels in dx is as large as rho * w * dy
+    size = float((rho[:, None] * (w.cpu().double() * dy.cpu().double()).abs()).norm()) + float(wdx.norm())
+    close(dx, wdx, tol_of(dtype, BWD), "dx", size=size)
+    xh = (total.cpu().double() - wmean[:, None]) * rho[:, None]
+    close(dw, wdw, BWD, "dweight", size=float((dy.cpu().double() * xh).norm()))
+    close(db, wdb, BWD, "dbias", size=float(dy.double().norm()))
+    again = g.add_layernorm_backward(ctx, dy, total, mean, rstd, w, dt)
+    assert all(torch.equal(p, q) for p, q in zip((dx, dw, db), again))
+    y2, t2, _, _ = g.add_layernorm(ctx, x, w)
+    assert t2 is x
+    close(y2, ref.layernorm(x, w, None, EPS)[0], tol_of(dtype, FWD), "no bias, no residual")
+
+
+@pytest.mark.parametrize("width", [64, 512, 2000, 9000])
+@pytest.mark.parametrize("offset", [1e3, -3e5])
+def test_layernorm_of_rows_with_a_large_offset(g, ctx, width, offset):
+    """The deviations are a thousandth (a millionth) of the values, which hold them to the bit."""
+    x = rand(5, width, seed=1, scale=1.0) + offset
+    w, b, dy = 1 + rand(width, scale=0.1, seed=3), rand(width, scale=0.1, seed=6), rand(5, width, seed=4)
+    y, total, mean, rstd = g.add_layernorm(ctx, x, w, b)
+    want, _, rho = ref.layernorm(x, w, b, EPS)
+    close(y, want, FWD, "y")
+    close(rstd, rho, FWD, "rstd")
+    dx, dw, db = g.add_layernorm_backward(ctx, dy, total, mean, rstd, w)
+    wdx, wdw, _ = ref.layernorm_backward(dy, x, w, EPS)
+    close(dx, wdx, BWD, "dx")
+    close(dw, wdw, BWD, "dweight")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [130, 1300])
+def test_layernorm_odd_rows(g, ctx, dtype, width):
+    """Strides, alignment of one element, broadcast gradients, rows of one value, rows that are not finite."""
+    x, r = rand(9, width, dtype=dtype, seed=1), rand(9, width, dtype=dtype, seed=2)
+    w, b = 1 + rand(width, scale=0.1, seed=3), rand(width, seed=4)
+    want = g.add_layernorm(ctx, x, w, b, r)
+    got = g.add_layernorm(ctx, strided(x, 1, 5, 1), w, b, strided(r, 1, 2, 3))
+    close(got[0], want[0], tol_of(dtype, FWD))
+    assert torch.equal(got[1], want[1])
+    one = rand(9, width, dtype=dtype, seed=4)[:1].expand(9, width)
+    close(g.add_layernorm_backward(ctx, one, *want[1:], w)[0], ref.layernorm_backward(one, want[1], w, EPS)[0], tol_of(dtype, BWD))
+    x[2], r[2], x[3, 7], x[4, 0] = 3, 0, INF, NAN
+    y, total, mean, rstd = g.add_layernorm(ctx, x, w, b, r)
+    assert torch.equal(y[2], b.to(dtype)) and bool(y[3:5].isnan().all())
+    rest = [0, 1, 5, 6, 7, 8]
+    close(y[rest], ref.layernorm(total[rest], w, b, EPS)[0], tol_of(dtype, FWD))
+    dx, dw, _ = g.add_layernorm_backward(ctx, rand(9, width, dtype=dtype, seed=5), total, mean, rstd, w)
+    assert bool(torch.isfinite(dx[rest]).all()) and bool(dx[3:5].isnan().all()) and bool(dw.isnan().all())
+    y, total, mean, rstd = g.add_layernorm(ctx, x[:0], w, b, r[:0])
+    dx, dw, db = g.add_layernorm_backward(ctx, y, total, mean, rstd, w)
+    assert dx.shape == (0, width) and float(dw.abs().max()) == 0 == float(db.abs().max())
+
+
+def test_layernorm_refusals(g, ctx):
+    x, w = rand(3, 8), rand(8)
+    y, total, mean, rstd = g.add_layernorm(ctx, x, w)
+    with pytest.raises(g.GorilaError, match="EINVAL"):
+        g.add_layernorm(ctx, x, w, eps=-1.0)
+    with pytest.raises(g.GorilaError, match="EINVAL"):
+        g.add_layernorm(ctx, rand(1, 65537), rand(65537))
+    with pytest.raises(ValueError, match="bias"):
+        g.add_layernorm(ctx, x, w, rand(7))
+    with pytest.raises(TypeError, match="rows must be"):
+        g.add_layernorm(ctx, x.double(), w)
+    with pytest.raises(ValueError, match="contiguous"):
+        g.add_layernorm(ctx, rand(8, 3).t(), w)
+    with pytest.raises(ValueError, match="device"):
+        g.add_layernorm(ctx, x, w.cpu())
+    bare = g.Context(0, 1)
+    close(g.add_layernorm(bare, x, w)[0], y.cpu(), 0.0)
+    with pytest.raises(g.GorilaError, match="EWORKSPACE"):
+        g.add_layernorm_backward(bare, x, total, mean, rstd, w)
+    bare.close()
+
+
+# ---- gated scan ----
+
+def gated_inputs(B, T, C, dtype=F32, seed=0, resets=0.03, span=700.0):
+    a_log = math.log(1e-3) + math.log(span) * uniform(C, seed=seed + 1)
+    args = [rand(B, T, C, dtype=dtype, seed=seed + k) for k in (2, 3, 4)] + [a_log]
+    reset = (uniform(B, T, seed=seed + 5) < resets).to(torch.uint8)
+    return args, reset, rand(B, C, seed=seed + 6), rand(B, T, C, dtype=dtype, seed=seed + 7), rand(B, C, seed=seed + 8)
+
+
+def check_gated(g, ctx, args, reset, state, dy, dstate, dtype):
+    y, out, marks = g.gated_scan(ctx, *args, reset, state)
+    wy, wh, before = ref.gated(*args, reset, state)
+    close(y, wy, tol_of(dtype, FWD), "y")
+    close(out, wh, FWD, "state")
+    if y.shape[1]:
+        close(marks, torch.stack(before[::64], 1), FWD, "marks")
+    spoil(ctx)
+    got = g.gated_scan_backward(ctx, dy, *args, marks, reset, dstate)
+    want = ref.gated_backward(dy, *args, reset, state, dstate)
+    names = ("dx", "dgate_a", "dgate_x", "da_log", "dstate")
+    for name, a, b in zip(names, got, want):
+        close(a, b, tol_of(dtype, BWD) if name in names[:3] else BWD, name)
+    again = g.gated_scan_backward(ctx, dy, *args, marks, reset, dstate)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,C", [(1, 1, 1), (2, 5, 3), (1, 64, 64), (3, 65, 130), (2, 130, 36), (1, 300, 64), (1, 1100, 20), (5, 200, 68),
+                                   (40, 7, 256), (2100, 3, 4), (1, 4200, 68)])
+def test_gated_scan(g, ctx, B, T, C, dtype):
+    args, reset, state, dy, dstate = gated_inputs(B, T, C, dtype)
+    check_gated(g, ctx, args, reset, state, dy, dstate, dtype)
+
+
+@pytest.mark.parametrize("resets", [0.0, 0.3, 1.0])
+@pytest.mark.parametrize("T", [63, 700])
+def test_gated_scan_starts(g, ctx, T, resets):
+    args, reset, state, dy, dstate = gated_inputs(2, T, 12, seed=20, resets=resets)
+    reset[0, 0], reset[1, -1] = 1, 1
+    check_gated(g, ctx, args, reset, state, dy, dstate, F32)
+
+
+@pytest.mark.parametrize("T", [50, 600])
+def test_gated_scan_without_options(g, ctx, T):
+    args, _, _, dy, _ = gated_inputs(2, T, 16, seed=30)
+    y, out, marks = g.gated_scan(ctx, *args)
+    wy, wh, _ = ref.gated(*args)
+    close(y, wy, FWD)
+    close(out, wh, FWD)
+    for a, b in zip(g.gated_scan_backward(ctx, dy, *args, marks), ref.gated_backward(dy, *args)):
+        close(a, b, BWD)
+    y2, out2, none = g.gated_scan(ctx, *args, marks=False)
+    assert none is None and torch.equal(y, y2) and torch.equal(out, out2)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [70, 520])
+def test_gated_scan_strides(g, ctx, T, dtype):
+    """Slices of one projection, steps of a longer sequence, one element's alignment, broadcast rows."""
+    B, C = 2, 36
+    args, reset, state, dy, dstate = gated_inputs(B, T, C, dtype, seed=40)
+    both = torch.cat([a for a in args[:3]], 2)
+    views = [both[..., k * C:(k + 1) * C] for k in range(3)]
+    want = g.gated_scan(ctx, *args, reset, state)
+    for x, ga, gx in (views, [strided(a, 2, 1, 1) for a in args[:3]], [a.transpose(0, 1).contiguous().transpose(0, 1) for a in args[:3]]):
+        got = g.gated_scan(ctx, x, ga, gx, args[3], reset, state)
+        for a, b in zip(got, want):
+            close(a, b, FWD if dtype == F32 or a.dtype == F32 else HALF)
+        for a, b in zip(g.gated_scan_backward(ctx, strided(dy, 2, 5, 1), x, ga, gx, args[3], got[2], reset, dstate),
+                        ref.gated_backward(dy, *args, reset, state, dstate)):
+            close(a, b, tol_of(a.dtype, BWD))
+    one = dy[:1, :1].expand(B, T, C)
+    for a, b in zip(g.gated_scan_backward(ctx, one, *args, want[2], reset), ref.gated_backward(one, *args, reset, state)):
+        close(a, b, tol_of(a.dtype, BWD))
+
+
+def test_gated_scan_goes_on(g, ctx):
+    args, reset, state, _, _ = gated_inputs(2, 900, 24, seed=50)
+    whole = g.gated_scan(ctx, *args, reset, state)
+    parts, carried = [], state
+    for t0, t1 in ((0, 1), (1, 64), (64, 400), (400, 900)):
+        y, carried, _ = g.gated_scan(ctx, *[a[:, t0:t1] for a in args[:3]], args[3], reset[:, t0:t1].contiguous(), carried)
+        parts.append(y)
+    close(torch.cat(parts, 1), whole[0].cpu(), FWD)
+    close(carried, whole[1].cpu(), FWD)
+
+
+@pytest.mark.parametrize("T,start", [(40, 23), (64, 63), (700, 401), (700, 64)])
+def test_gated_scan_nothing_passes_a_start(g, ctx, T, start):
+    """Infinities and NaN before an episode's start, in values, gates and the carried state, and behind it in the gradients."""
+    args, reset, state, dy, dstate = gated_inputs(1, T, 8, seed=60, resets=0.0)
+    reset[:, start] = 1
+    clean = g.gated_scan(ctx, *args, reset, state)
+    clean_back = g.gated_scan_backward(ctx, dy, *args, clean[2], reset, dstate)
+    bad = [a.clone() for a in args]
+    bad[0][:, start - 3], bad[0][:, 0], bad[2][:, 1] = INF, NAN, NAN
+    y, out, marks = g.gated_scan(ctx, *bad, reset, torch.full_like(state, INF))
+    assert torch.equal(y[:, start:], clean[0][:, start:]) and torch.equal(out, clean[1])
+    assert not bool(torch.isfinite(y[:, :start]).any())
+    worse = dy.clone()
+    worse[:, start:] = NAN
+    got = g.gated_scan_backward(ctx, worse, *args, clean[2], reset, torch.full_like(dstate, INF))
+    for k in range(3):
+        assert torch.equal(got[k][:, :start], clean_back[k][:, :start])
+    assert torch.equal(got[4], clean_back[4])
+
+
+def test_gated_scan_extreme_gates_and_decays(g, ctx):
+    """Gates that are shut or wide open, decays of zero and of one: finite values, and gradients."""
+    args, reset, state, dy, dstate = gated_inputs(2, 200, 8, seed=70)
+    x, ga, gx, al = args
+    ga[:, ::5], ga[:, 1::5], gx[:, ::7], gx[:, 1::7] = -200.0, 200.0, -200.0, 200.0
+    al[0], al[1], al[2], al[3] = -100.0, 80.0, 5.0, 200.0
+    y, out, marks = g.gated_scan(ctx, x, ga, gx, al, reset, state)
+    got = g.gated_scan_backward(ctx, dy, x, ga, gx, al, marks, reset, dstate)
+    assert all(bool(torch.isfinite(v).all()) for v in (y, out, *got))
+    wy, wh, _ = ref.gated(x, ga, gx, al, reset, state)
+    close(y, wy, FWD)
+    close(out, wh, FWD)
+    # the formula's own gradient has 0 / 0 where a gate is shut to the last bit: the others
+    want = ref.gated_backward(dy, x, ga, gx, al, reset, state, dstate)
+    for k in (0, 2, 4):
+        close(got[k], want[k], BWD)
+    fine = torch.isfinite(want[1])
+    assert fine.float().mean() > 0.7
+    close(torch.where(fine.cuda(), got[1], torch.zeros_like(got[1])), torch.where(fine, want[1], torch.zeros_like(want[1])), BWD)
+
+
+def test_gated_scan_empty_calls(g, ctx):
+    args, reset, state, dy, dstate = gated_inputs(2, 0, 8, seed=80)
+    y, out, marks = g.gated_scan(ctx, *args, reset, state)
+    assert y.shape == (2, 0, 8) and torch.equal(out, state) and marks.shape == (2, 0, 8)
+    dx, dga, dgx, da, ds = g.gated_scan_backward(ctx, dy, *args, marks, reset, dstate)
+    assert float(da.abs().max()) == 0 and torch.equal(ds, dstate)
+    assert float(g.gated_scan(ctx, *args)[1].abs().max()) == 0
+    args, reset, state, dy, dstate = gated_inputs(0, 5, 8, seed=80)
+    y, out, marks = g.gated_scan(ctx, *args, reset, state)
+    assert y.shape == (0, 5, 8)
+    assert float(g.gated_scan_backward(ctx, dy, *args, marks, reset, dstate)[3].abs().max()) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("C", [1, 30, 64, 1000])
+def test_gated_scan_step(g, ctx, C, dtype):
+    """Steps of rows whose states lie anywhere in a pool are the sequence's steps; other states stay."""
+    n, T, slots = 5, 9, 8
+    args, reset, _, _, _ = gated_inputs(n, T, C, dtype, seed=90, resets=0.2)
+    pool = rand(slots, C, seed=91)
+    slot = torch.tensor([6, 0, 3, 7, 2], dtype=torch.int32, device="cuda")
+    start = pool[slot.long()].clone()
+    kept = pool[[1, 4, 5]].clone()
+    wy, wh, _ = ref.gated(*args, reset, start)
+    ys = [g.gated_scan_step(ctx, *[a[:, t] for a in args[:3]], args[3], pool, slot, reset[:, t].contiguous()) for t in range(T)]
+    close(torch.stack(ys, 1), wy, tol_of(dtype, FWD))
+    close(pool[slot.long()], wh, FWD)
+    assert torch.equal(pool[[1, 4, 5]], kept)
+    a = [strided(v[:, 0].contiguous(), 1, 3, 1) for v in args[:3]]
+    one, two = pool.clone(), pool.clone()
+    close(g.gated_scan_step(ctx, *a, args[3], one), g.gated_scan_step(ctx, *[v[:, 0] for v in args[:3]], args[3], two).cpu(), tol_of(dtype, FWD))
+    assert torch.equal(one[5:], pool[5:]) and g.gated_scan_step(ctx, *[v[:0, 0] for v in args[:3]], args[3], pool).shape == (0, C)
+
+
+def test_gated_scan_step_slots_out_of_range(g, ctx):
+    args, _, _, _, _ = gated_inputs(3, 1, 16, seed=95)
+    pool = rand(4, 16, seed=96)
+    before = pool.clone()
+    slot = torch.tensor([-1, 2, 4], dtype=torch.int32, device="cuda")
+    y = g.gated_scan_step(ctx, *[a[:, 0] for a in args[:3]], args[3], pool, slot)
+    with pytest.raises(g.GorilaError, match="ERANGE"):
+        ctx.check()
+    assert torch.equal(pool[[0, 1, 3]], before[[0, 1, 3]]) and not torch.equal(pool[2], before[2])
+    zero, _, _ = ref.gated(*args)
+    close(y[[0, 2]], zero[[0, 2], 0], FWD)
+    ctx.check()
+
+
+def test_gated_scan_refusals(g, ctx):
+    (x, ga, gx, al), reset, state, dy, _ = gated_inputs(2, 300, 8, seed=97)
+    with pytest.raises(ValueError, match="gate_a"):
+        g.gated_scan(ctx, x, ga[:, :299], gx, al)
+    with pytest.raises(TypeError, match="gate_x"):
+        g.gated_scan(ctx, x, ga, gx.bfloat16(), al)
+    with pytest.raises(ValueError, match="a_log"):
+        g.gated_scan(ctx, x, ga, gx, al[:7])
+    with pytest.raises(TypeError, match="reset"):
+        g.gated_scan(ctx, x, ga, gx, al, reset.int())
+    with pytest.raises(ValueError, match="marks"):
+        g.gated_scan_backward(ctx, dy, x, ga, gx, al, torch.zeros(2, 4, 8, device="cuda"))
+    with pytest.raises(g.GorilaError, match="EINVAL"):
+        g.gated_scan_step(ctx, x[:, 0], ga[:, 0], gx[:, 0], al, state[:1].contiguous())
+    bare = g.Context(0, 1)
+    short = [v[:, :256].contiguous() for v in (x, ga, gx)]
+    y, _, marks = g.gated_scan(bare, *short, al)
+    close(y, ref.gated(*short, al)[0], FWD)
+    for call in (lambda: g.gated_scan(bare, x, ga, gx, al), lambda: g.gated_scan_backward(bare, short[0], *short, al, marks),
+                 lambda: g.gated_scan_step(bare, x[:, 0], ga[:, 0], gx[:, 0], al, state, torch.zeros(2, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(g.GorilaError, match="EWORKSPACE"):
+            call()
+    bare.close()
+
+
+def test_gated_scan_in_a_graph(g, ctx):
+    args, reset, state, dy, dstate = gated_inputs(2, 600, 64, seed=98)
+    def call():
+        y, out, marks = g.gated_scan(ctx, *args, reset, state)
+        return (y, out, *g.gated_scan_backward(ctx, dy, *args, marks, reset, dstate))
+    replayed(call, lambda o: o, [v.clone() for v in call()])
+
+
+def test_gated_scan_state_in_place(g, ctx):
+    """The C entry takes the carried state's place for the new one, in segments too."""
+    import ctypes
+    from paper_1507_04296_amd import sequence
+    for T in (30, 700):
+        (x, ga, gx, al), reset, state, _, _ = gated_inputs(2, T, 8, seed=99)
+        y, out, _ = g.gated_scan(ctx, x, ga, gx, al, reset, state)
+        held, got = state.clone(), torch.empty_like(x)
+        a = sequence._GatedArgs(0, 2, T, 8)
+        for n, v in (("x", x), ("gate_a", ga), ("gate_x", gx)):
+            setattr(a, n, v.data_ptr())
+            setattr(a, n + "_batch_stride", v.stride(0))
+            setattr(a, n + "_step_stride", v.stride(1))
+        a.a_log, a.reset, a.state = al.data_ptr(), reset.data_ptr(), held.data_ptr()
+        assert g.lib().gorila_gated_scan(ctypes.byref(a), got.data_ptr(), held.data_ptr(), None, ctx.bind_stream()) == 0
+        assert torch.equal(got, y) and torch.equal(held, out)
+
+
+# ---- AdamW ----
+
+RULE = dict(lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8)
+
+
+def adamw_inputs(sizes, bits, dtype=F32, seed=0):
+    thetas = [rand(*(s if isinstance(s, tuple) else (s,)), scale=0.05, seed=seed + 3 * i) for i, s in enumerate(sizes)]
+    grads = [rand(*t.shape, scale=1e-3, dtype=dtype, seed=seed + 3 * i + 1) for i, t in enumerate(thetas)]
+    return thetas, grads
+
+
+def check_step(g, ctx, thetas, grads, states, clock, decay=0.0, seed=0, **more):
+    t = int(clock[0]) + 1
+    rule = {**RULE, **more}
+    place, want = 0, []
+    for i, theta in enumerate(thetas):
+        d = decay[i] if isinstance(decay, list) else decay
+        want.append(ref.adamw(theta, grads[i], states[i], t, place, decay=float(np.float32(d)), seed=seed, **{k: float(np.float32(v)) if k in ("lr", "eps") else v for k, v in rule.items()}))
+        place += -(-theta.numel() // 256) * 128
+    old = [v.clone() for v in thetas]
+    g.adamw(ctx, thetas, grads, states, clock, decay=decay, seed=seed, **rule)
+    assert int(clock[0]) == t
+    close(clock[1:], torch.tensor([1 - rule["beta1"] ** t, 1 - rule["beta2"] ** t], dtype=torch.float64), 1e-14)
+    for i, (new, held) in enumerate(want):
+        for got, w in zip(states[i], held):
+            assert np.array_equal(got.cpu().numpy().reshape(-1), w, equal_nan=got.dtype == F32), i
+        got, new = thetas[i].cpu().double().numpy().reshape(-1), new
+        fine = np.isfinite(new)
+        assert np.array_equal(fine, np.isfinite(got))
+        was = old[i].cpu().double().numpy().reshape(-1)
+        most = 1e-6 * np.abs(new - was) + 2.0 ** -24 * np.maximum(np.abs(was), np.abs(new)) + 1e-37
+        assert (np.abs(got - new) <= most)[fine].all(), i
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("sizes", [[1], [255, 256, 257], [0, 5, (3, 700)], [4097, 100003], [7] * 100 + [300] * 5])
+def test_adamw(g, ctx, sizes, bits, dtype):
+    thetas, grads = adamw_inputs(sizes, bits, dtype)
+    states, clock = g.adamw_state(thetas, bits), g.adamw_clock()
+    decay = [0.1 if t.dim() > 1 or t.numel() > 256 else 0.0 for t in thetas]
+    for step in range(3):
+        check_step(g, ctx, thetas, grads, states, clock, decay, seed=11)
+        grads = [v * 0.7 + 1e-4 for v in grads]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_of_views(g, ctx, bits):
+    """Views of one flat vector at any element, what lies between them as it was."""
+    flat, grad = rand(5000, seed=1), rand(5000, seed=2, scale=1e-3)
+    spans = [(0, 300), (301, 302), (305, 1700), (1704, 1704), (1705, 4999)]
+    thetas, grads = [flat[a:b] for a, b in spans], [grad[a:b] for a, b in spans]
+    states, clock = g.adamw_state(thetas, bits), g.adamw_clock()
+    if bits == 32:
+        m, v = torch.zeros(5000, device="cuda"), torch.zeros(5000, device="cuda")
+        states = [(m[a:b], v[a:b]) for a, b in spans]
+    between = [300, 302, 303, 304, 1700, 1703, 1704, 4999]
+    was = flat[between].clone()
+    for _ in range(2):
+        check_step(g, ctx, thetas, grads, states, clock, 0.01, seed=3)
+    assert torch.equal(flat[between], was)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_extreme_gradients(g, ctx, bits):
+    """Zeros, tiny, large and infinite gradients, each in a block of its own and mixed in one."""
+    n = 256 * 6
+    theta, grad = rand(n, seed=1), rand(n, seed=2)
+    grad[:256], grad[256:512], grad[512:768] = 0, grad[256:512] * 1e-19, grad[512:768] * 1e17
+    grad[768:1024] *= 10.0 ** (-12 * uniform(256, seed=3))
+    grad[1030] = 1e-30
+    thetas, states, clock = [theta], g.adamw_state([theta], bits), g.adamw_clock()
+    for _ in range(3):
+        check_step(g, ctx, thetas, [grad], states, clock, 0.0, seed=5)
+    assert torch.equal(theta[:256], rand(n, seed=1)[:256])
+    grad[1300], grad[1301] = INF, NAN
+    check_step(g, ctx, thetas, [grad], states, clock, 0.0, seed=5)
+    assert bool(torch.isfinite(theta[:1280]).all())
+    if bits == 8:  # the block that was hit, and it alone, is lost
+        assert states[0][2].isnan().tolist() == [False] * 5 + [True] == states[0][3].isnan().tolist()
+
+
+def test_adamw_keep_and_no_tensors(g, ctx):
+    thetas, grads = adamw_inputs([700], 8)
+    states, clock = g.adamw_state(thetas, 8), g.adamw_clock()
+    keep = torch.ones(1, dtype=torch.uint8, device="cuda")
+    g.adamw(ctx, thetas, grads, states, clock, 0.1, keep=keep)
+    assert int(clock[0]) == 1
+    was = [v.clone() for v in (thetas[0], *states[0], clock)]
+    keep.zero_()
+    g.adamw(ctx, thetas, grads, states, clock, 0.1, keep=keep)
+    assert all(torch.equal(a, b) for a, b in zip(was, (thetas[0], *states[0], clock)))
+    g.adamw(ctx, [], [], [], clock, 0.1)
+    assert int(clock[0]) == 2 and g.adamw_values(ctx, []) == []
+
+
+@pytest.mark.parametrize("sizes", [[1], [0, 257, (3, 100)], [5000, 4096] + [3] * 60])
+def test_adamw_values(g, ctx, sizes):
+    thetas, grads = adamw_inputs(sizes, 8)
+    states, clock = g.adamw_state(thetas, 8), g.adamw_clock()
+    g.adamw(ctx, thetas, grads, states, clock, 0.1)
+    for (m, v), s, t in zip(g.adamw_values(ctx, states), states, thetas):
+        n, (cm, cv, sm, sv) = t.numel(), [x.cpu().numpy().reshape(-1) for x in s]
+        assert m.shape == v.shape == t.shape
+        want = ref.held(cm & 127, 889, sm.repeat(256)[:n]) * np.where(cm >= 128, np.float32(-1), np.float32(1))
+        assert np.array_equal(m.cpu().numpy().reshape(-1), want)
+        assert np.array_equal(v.cpu().numpy().reshape(-1), ref.held(cv, 761, sv.repeat(256)[:n]))
+
+
+def test_adamw_averages_keep_moving_in_8_bits(g, ctx):
+    """v's average over many equal elements follows the exact one through steps that change it by a thousandth, where
+    nearest rounding of 3 bits would stand still: a code is off by 2^-4 of its value at most, independently each
+    step; the mean of 2^16 elements over 400 steps by less than 1 %."""
+    n = 1 << 16
+    theta, grad = torch.zeros(n, device="cuda"), 0.5 + 0.5 * uniform(n, seed=1)
+    grad[::256] = 4.0  # every block's largest, so that the others' codes have room on both sides
+    states, clock = g.adamw_state([theta], 8), g.adamw_clock()
+    for step in range(400):
+        g.adamw(ctx, [theta], [grad], states, clock, 0.0, seed=13)
+    m, v = g.adamw_values(ctx, states)[0]
+    want = grad.double().square() * (1 - 0.999 ** 400)
+    assert abs(float(v.double().sum() / want.sum()) - 1) < 0.01
+    assert abs(float(m.double().sum() / grad.double().sum()) - 1) < 0.01
+
+
+def test_adamw_in_a_graph(g, ctx):
+    """A captured step replayed is the next step each time: the clock and the chances move on."""
+    for bits in (32, 8):
+        thetas, grads = adamw_inputs([1000, 300], bits, seed=7)
+        a, b = [t.clone() for t in thetas], [t.clone() for t in thetas]
+        sa, sb, ca, cb = g.adamw_state(a, bits), g.adamw_state(b, bits), g.adamw_clock(), g.adamw_clock()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            g.adamw(ctx, a, grads, sa, ca, 0.01, seed=3)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            g.adamw(ctx, a, grads, sa, ca, 0.01, seed=3)
+        g.adamw(ctx, b, grads, sb, cb, 0.01, seed=3)
+        for _ in range(3):
+            graph.replay()
+            torch.cuda.synchronize()
+            g.adamw(ctx, b, grads, sb, cb, 0.01, seed=3)
+            assert torch.equal(ca, cb)
+            for x, y in zip([*a, *(v for s in sa for v in s)], [*b, *(v for s in sb for v in s)]):
+                assert torch.equal(x, y)
+
+
+def test_adamw_refusals(g, ctx):
+    thetas, grads = adamw_inputs([300, 40], 32)
+    states, clock = g.adamw_state(thetas), g.adamw_clock()
+
+    def bad(exc, match, *a, **k):
+        with pytest.raises(exc, match=match):
+            g.adamw(ctx, *a, **k)
+
+    bad(ValueError, "as many", thetas, grads[:1], states, clock, 0.1)
+    bad(TypeError, "list", thetas[0], grads, states, clock, 0.1)
+    bad(ValueError, "overlap", [thetas[0], thetas[0]], [grads[0]] * 2, [states[0], g.adamw_state(thetas)[0]], clock, 0.1)
+    bad(ValueError, "overlap", [thetas[0], thetas[0].clone()], [grads[0]] * 2, [states[0], states[0]], clock, 0.1)
+    bad(ValueError, "same bits", thetas, grads, [states[0], g.adamw_state(thetas, 8)[1]], clock, 0.1)
+    bad(ValueError, "same type", thetas, [grads[0], grads[1].bfloat16()], states, clock, 0.1)
+    bad(ValueError, "grad must have shape", thetas, [grads[0], grads[0]], states, clock, 0.1)
+    bad(ValueError, "decay", thetas, grads, states, clock, 0.1, decay=[0.1])
+    bad(TypeError, "clock", thetas, grads, states, clock.float(), 0.1)
+    bad(ValueError, "m_scale", thetas, grads, [(*s[:2], s[2][:0], s[3]) for s in g.adamw_state(thetas, 8)], clock, 0.1)
+    for k in (dict(beta1=1.0), dict(beta2=-0.1), dict(eps=-1.0), dict(eps=NAN)):
+        bad(g.GorilaError, "EINVAL", thetas, grads, states, clock, 0.1, **k)
+    bad(g.GorilaError, "EINVAL", thetas, grads, states, clock, -0.1)
+    with pytest.raises(ValueError, match="8 bits"):
+        g.adamw_values(ctx, states)
+    assert clock.tolist() == [0.0] * 3 and not bool(states[0][0].any())
+
+
+# ---- sampled actions ----
+
+def sample_inputs(rows, actions, filters, dtype=F32, seed=0, scale=2.0):
+    values, u = rand(rows, actions, dtype=dtype, scale=scale, seed=seed), uniform(rows, seed=seed + 1)
+    options = {}
+    if "t" in filters:
+        t = 0.1 + 2 * uniform(rows, seed=seed + 2)
+        options["temperature"] = torch.where(uniform(rows, seed=seed + 3) < 0.15, torch.zeros_like(t), t)
+    if "k" in filters:
+        options["top_k"] = torch.randint(-1, actions + 3, (rows,), generator=torch.Generator().manual_seed(seed + 4), dtype=torch.int32).cuda()
+    if "p" in filters:
+        options["top_p"] = 0.05 + uniform(rows, seed=seed + 5)
+    if "m" in filters:
+        options["min_p"] = 0.2 * uniform(rows, seed=seed + 6)
+    return values, u, options
+
+
+def check_sample(g, ctx, values, u, options):
+    action, probability = g.sample_actions(ctx, values, u, **options)
+    want, p = ref.sample(values, u, **options)
+    assert action.dtype == torch.int32 and torch.equal(action.cpu(), want)
+    assert ((probability.cpu().double() - p).abs() <= 2.0 ** -24 * p + 2.0 ** -39).all()
+    again = g.sample_actions(ctx, values, u, **options)
+    assert torch.equal(action, again[0]) and torch.equal(probability, again[1])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("filters", ["", "t", "k", "p", "m", "tkpm"])
+@pytest.mark.parametrize("rows,actions", [(5, 1), (9, 2), (300, 18), (33, 63), (33, 64), (33, 65), (20, 300), (10, 2048), (10, 2049), (4, 9001)])
+def test_sample(g, ctx, rows, actions, filters, dtype):
+    check_sample(g, ctx, *sample_inputs(rows, actions, filters, dtype))
+
+
+@pytest.mark.parametrize("actions", [7, 64, 100, 3000])
+@pytest.mark.parametrize("filters", ["", "k", "p", "kp", "tkpm"])
+def test_sample_of_equal_values(g, ctx, actions, filters):
+    """Values of a few kinds, so that the borders of the filters lie between equal ones; rows of one value alone."""
+    values, u, options = sample_inputs(40, actions, filters, seed=20)
+    values = (values / 3).round()
+    values[:10] = -1.5
+    values[10:14] = torch.where(values[10:14] > 0, 0.0, -0.0)
+    if "p" in filters:
+        options["top_p"][::3] = torch.tensor([0.25, 0.5, 0.125] * 5)[:14].cuda()
+    check_sample(g, ctx, values, u, options)
+
+
+@pytest.mark.parametrize("actions", [18, 64, 65, 700])
+@pytest.mark.parametrize("filters", ["", "tkpm"])
+def test_sample_masks_and_extremes(g, ctx, actions, filters):
+    """-infinity, NaN and +infinity among the values; rows that leave nothing; the ends of u; odd settings."""
+    rows = 24
+    values, u, options = sample_inputs(rows, actions, filters, seed=30)
+    values[0] = -INF
+    values[1] = NAN
+    values[2, 1:] = -INF
+    values[3, ::2] = -INF
+    values[4, ::3] = NAN
+    values[5, actions // 2] = INF
+    values[6, 1], values[6, actions - 1] = INF, INF
+    values[7] = torch.finfo(F32).min
+    values[8, 3] = torch.finfo(F32).max
+    values[9] *= 1e-30
+    values[10] *= 1e30
+    values[11, :-1] = -INF
+    u[12], u[13], u[14], u[15], u[16] = 0.0, 1.0 - 2.0 ** -24, 1.0, 5.0, -1.0
+    u[17] = NAN
+    check_sample(g, ctx, values, u, options)
+    odd = torch.tensor([0.0, -1.0, NAN, INF, 1e-30, 1e30, 1.0, 0.5] * 3, device="cuda")
+    check_sample(g, ctx, values, u, dict(temperature=odd))
+    check_sample(g, ctx, values, u, dict(top_p=odd))
+    check_sample(g, ctx, values, u, dict(min_p=odd))
+    check_sample(g, ctx, values, u, dict(top_k=torch.tensor([0, -5, 1, 2, actions, actions + 1, 3, 2 ** 31 - 1] * 3, dtype=torch.int32, device="cuda")))
+
+
+def test_sample_many_actions(g, ctx):
+    values, u, options = sample_inputs(2, 150001, "tkpm", seed=40)
+    check_sample(g, ctx, values, u, {"temperature": options["temperature"], "top_p": options["top_p"]})
+    options["top_k"] = torch.tensor([50, 149990], dtype=torch.int32, device="cuda")
+    check_sample(g, ctx, values, u, options)
+    big = torch.zeros(1, 1 << 20, device="cuda")
+    for x in (0.0, 0.25, 0.9999999):
+        action, p = g.sample_actions(ctx, big, torch.tensor([x], device="cuda"))
+        assert int(action) == int(np.float32(x) * np.float64(1 << 20)) and float(p) == 2.0 ** -20
+
+
+@pytest.mark.parametrize("actions", [5, 300])
+def test_sample_strides(g, ctx, actions):
+    for dtype in (F32, BF16):
+        values, u, options = sample_inputs(30, actions, "tkpm", dtype, seed=50)
+        check_sample(g, ctx, strided(values, 1, 3, 1), u, options)
+        check_sample(g, ctx, values[:1].expand(30, actions), u, options)
+    action, p = g.sample_actions(ctx, values[:0], u[:0])
+    assert action.shape == (0,) == p.shape
+
+
+@pytest.mark.parametrize("actions", [6, 500])
+def test_sample_follows_the_distribution(g, ctx, actions):
+    """u over a fine grid gives each action as often as its probability says, to a grid step on either side."""
+    n = 4096
+    values = rand(1, actions, seed=60).expand(n, actions)
+    u = (torch.arange(n, device="cuda") + 0.5) / n
+    action, p = g.sample_actions(ctx, values, u)
+    want = torch.softmax(values[0].double(), 0)
+    count = torch.bincount(action.long(), minlength=actions).double() / n
+    assert bool(((count - want).abs() <= 1.01 / n).all())
+    close(p, want[action.long()], 1e-6)
+
+
+def test_sample_refusals(g, ctx):
+    values, u, _ = sample_inputs(4, 10, "")
+    with pytest.raises(ValueError, match="u must"):
+        g.sample_actions(ctx, values, u[:3])
+    with pytest.raises(TypeError, match="top_k"):
+        g.sample_actions(ctx, values, u, top_k=u)
+    with pytest.raises(TypeError, match="rows must be"):
+        g.sample_actions(ctx, values.double(), u)
+    with pytest.raises(g.GorilaError, match="EINVAL"):
+        g.sample_actions(ctx, values[:, :0], u)
+    with pytest.raises(g.GorilaError, match="EUNSUPPORTED"):
+        g.sample_actions(ctx, torch.zeros(1, (1 << 20) + 1, device="cuda"), u[:1])
+
+
+def test_calls_on_another_stream(g, ctx):
+    """Each call runs on torch's current stream, after what was queued there."""
+    args, reset, state, _, _ = gated_inputs(2, 300, 32, seed=70)
+    values, u, options = sample_inputs(20, 200, "tkpm", seed=71)
+    want = g.gated_scan(ctx, *args, reset, state)[0], g.sample_actions(ctx, values, u, **options)[0]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        late = torch.zeros_like(args[0])
+        torch.cuda._sleep(20_000_000)
+        late.copy_(args[0])
+        got = g.gated_scan(ctx, late, *args[1:], reset, state)[0], g.sample_actions(ctx, values, u, **options)[0]
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
