@@ -516,7 +516,7 @@ int gorila_scan_step(const gorila_scan_args* args, float* state_pool, int64_t sl
  *   L = -exp(a_log[c]) * sigmoid(gate_a),   a = exp(L), 0 at a reset,
  *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) * sigmoid(gate_x) * x_t   (from `state`),   y = h.
  * (At a reset the root is 1.)  1 - a^2 is formed from L, without cancellation.
- * exp(a_log) past fp32's range counts as its largest value.
+ * exp(a_log) above 2^127 counts as 2^127.
  * x, gate_a, gate_x, y [batch][length][channels]; state and state_out
  * [batch][channels] (NULL: zeros / not wanted; state_out may be state).  marks
  * [batch][ceil(length / GORILA_GATED_MARK)][channels] fp32 (NULL: not wanted): the

@@ -1,23 +1,27 @@
 // Gated scan (gorila_gated_scan, _backward, _step): h_t = a_t h_{t-1} + b_t i_t x_t in every
 // channel, with a = exp(-exp(a_log) sigmoid(gate_a)), b = sqrt(1 - a^2), i = sigmoid(gate_x).
 //
-// Memory bound where it can be: a step of a channel is 40 operations forward and 100
-// backward on 4 and 7 values.  So a value is read once: the steps of a chunk lie in the
-// lanes' registers (4 steps of 4 channels a lane, 16 lanes a step, 4 runs of steps a
-// wave), each lane runs through its own steps from zero, and what enters a lane's run is
-// joined from the products of decays and the ends of the runs before it: over the lanes
-// of a wave by shuffles, over the waves in LDS, over the chunks in registers.  An episode
-// start is a flag beside the product of decays, not a factor of zero: what is before
-// it may be infinite.
+// Bound by memory and by the vector unit alike: a step of a channel has 3 values in and 1
+// out for 25 operations and 6 of the slow kind (exponentials, reciprocals, a root: four
+// slots each), so a value is read once and its decay formed once.  The steps of a chunk
+// lie in the lanes' registers: 8 steps of 2 channels a lane, 32 lanes a step, 2 runs of
+// steps a wave.  Each lane runs through its own steps from zero, and what enters a
+// lane's run is joined from the products of decays and the ends of the runs before it:
+// between the halves of a wave by a shuffle, over the waves in LDS, over the chunks in
+// registers.  (4 steps of 4 channels make twice the joins: 10 % of all operations.)
+// The next chunk's loads are under way while this one's runs are joined.
+//
+// An episode start is a flag beside the product of decays, not a factor of zero:
+// what is before it may be infinite.  Chunks without one, and inside the sequence,
+// have a copy of the code without the flags (a fifth of all operations).
 #include "seq.h"
 
 namespace gorila {
 namespace {
 
-constexpr int STEPS = 4, RUNS = 4, TILE = 64;  // steps a lane, runs a wave, channels a workgroup
-constexpr int WAVES = 4, BLOCK = 64 * WAVES, CHUNK = STEPS * RUNS * WAVES;
-static_assert(CHUNK == GORILA_GATED_MARK, "a chunk of the backward starts at a mark");
-constexpr float LOG2E = 1.44269504088896341f;
+constexpr int TILE = 64;  // channels of a workgroup
+constexpr int MARK = GORILA_GATED_MARK;
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
 struct Rows {
     const void* p;
@@ -39,351 +43,508 @@ struct GatedView {
 __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -LOG2E));
 }
-__device__ __forceinline__ float rate_of(float a_log) {
+// exp(a_log) for a base of two: log2 a = -rate2 sigmoid(gate_a).
+__device__ __forceinline__ float rate2_of(float a_log) {
     const float e = expf(a_log);
-    return e > 3.40282347e38f ? 3.40282347e38f : e;  // (NaN stays)
+    return (e > 0x1p127f ? 0x1p127f : e) * LOG2E;  // (NaN stays)
 }
-// a = exp(l) and b = sqrt(1 - a^2) for l <= 0: 1 - exp(u), u = 2 l, is its series where
-// u > -1/2 (the next term is 2^-27 of the sum).
 struct Decay {
     float a, b;
 };
+// a = 2^l and b = sqrt(1 - a^2) for l <= 0: 1 - exp(u), u = 2 l ln 2, is its series where
+// u > -1/4 (the next term is 2^-24 of the sum); below, 1 - a^2 loses two bits at most.
 __device__ __forceinline__ Decay decay(float l) {
-    const float a = __builtin_amdgcn_exp2f(l * LOG2E);
-    const float u = 2.0f * l;
-    float s = fmaf(u, 1.0f / 40320.0f, 1.0f / 5040.0f);
-    s = fmaf(u, s, 1.0f / 720.0f);
-    s = fmaf(u, s, 1.0f / 120.0f);
-    s = fmaf(u, s, 1.0f / 24.0f);
-    s = fmaf(u, s, 1.0f / 6.0f);
-    s = fmaf(u, s, 0.5f);
-    s = fmaf(u, s, 1.0f);
-    const float q = u > -0.5f ? -u * s : fmaf(-a, a, 1.0f);
+    constexpr float K = 2.0f * LN2, K2 = K * K;
+    const float a = __builtin_amdgcn_exp2f(l);
+    float s = fmaf(l, K2 * K2 * K2 / 720.0f, K2 * K2 * K / 120.0f);
+    s = fmaf(l, s, K2 * K2 / 24.0f);
+    s = fmaf(l, s, K2 * K / 6.0f);
+    s = fmaf(l, s, K2 / 2.0f);
+    s = fmaf(l, s, K);
+    const float q = l > -0.25f / K ? -l * s : fmaf(-a, a, 1.0f);
     return {a, __builtin_amdgcn_sqrtf(q)};
 }
 
-// A run of steps as a map of the state before it: h -> cut ? end : a h + end.
-struct Map {
-    f32x4 a, h;
-    bool cut;
+// Two channels of a lane: `n` (0, 1 or 2) exist; a lane without any reads channel 0, the second of
+// a lone one is the first again, and neither is stored.  PAIR: all rows' addresses are even.
+struct Two {
+    float v[2];
+    __device__ __forceinline__ float& operator[](int j) { return v[j]; }
+    __device__ __forceinline__ float operator[](int j) const { return v[j]; }
 };
-__device__ __forceinline__ f32x4 through(const Map& m, f32x4 h) {
-    f32x4 o;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = m.cut ? m.h[j] : fmaf(m.a[j], h[j], m.h[j]);
-    return o;
+template <class T, bool PAIR> struct Raw;  // as it is read
+template <> struct Raw<float, true> {
+    float2 u;
+    __device__ __forceinline__ void load(const float* p, int) { u = *(const float2*)p; }
+    __device__ __forceinline__ Two get() const { return {{u.x, u.y}}; }
+};
+template <> struct Raw<float, false> {
+    float a, b;
+    __device__ __forceinline__ void load(const float* p, int second) { a = p[0], b = p[second]; }
+    __device__ __forceinline__ Two get() const { return {{a, b}}; }
+};
+template <> struct Raw<uint16_t, true> {
+    uint32_t u;
+    __device__ __forceinline__ void load(const uint16_t* p, int) { u = *(const uint32_t*)p; }
+    __device__ __forceinline__ Two get() const { return {{__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)}}; }
+};
+template <> struct Raw<uint16_t, false> {
+    uint16_t a, b;
+    __device__ __forceinline__ void load(const uint16_t* p, int second) { a = p[0], b = p[second]; }
+    __device__ __forceinline__ Two get() const { return {{row_value(a), row_value(b)}}; }
+};
+template <bool PAIR, class T>
+__device__ __forceinline__ Two get2(const T* p, int second) {
+    Raw<T, PAIR> r;
+    r.load(p, second);
+    return r.get();
 }
-// `later` after `first`.
-__device__ __forceinline__ Map join(const Map& first, const Map& later) {
-    Map o;
-    o.a = first.a * later.a;
-    o.h = through(later, first.h);
-    o.cut = first.cut || later.cut;
-    return o;
+template <bool PAIR>
+__device__ __forceinline__ void put2(float* p, Two v, int n) {
+    if (PAIR) {
+        if (n > 0) *(float2*)p = float2{v[0], v[1]};
+    } else {
+        if (n > 0) p[0] = v[0];
+        if (n > 1) p[1] = v[1];
+    }
 }
-__device__ __forceinline__ Map none() { return Map{f32x4{1.0f, 1.0f, 1.0f, 1.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, false}; }
-__device__ __forceinline__ Map moved(const Map& m, int by) {  // of the lane `by` further
-    Map o;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o.a[j] = __shfl(m.a[j], (threadIdx.x + by) & 63, 64), o.h[j] = __shfl(m.h[j], (threadIdx.x + by) & 63, 64);
-    o.cut = __shfl((int)m.cut, (threadIdx.x + by) & 63, 64);
-    return o;
-}
-// The map of the runs before this lane's in its wave (BACK: behind it); `all` that of the wave's last (first)
-// run and all others.
-template <bool BACK>
-__device__ __forceinline__ Map before(const Map& own, Map& all) {
-    const int g = BACK ? RUNS - 1 - (threadIdx.x & 63) / 16 : (threadIdx.x & 63) / 16;
-    const int dir = BACK ? 1 : -1;
-    Map m = own, p = moved(m, dir * 16);
-    if (g >= 1) m = join(p, m);
-    p = moved(m, dir * 32);
-    if (g >= 2) m = join(p, m);
-    all = m;  // in the lanes of the last run
-    p = moved(m, dir * 16);
-    return g >= 1 ? p : none();
+template <bool PAIR>
+__device__ __forceinline__ void put2(uint16_t* p, Two v, int n) {
+    if (PAIR) {
+        typedef __bf16 Pair __attribute__((ext_vector_type(2)));
+        typedef float Wide __attribute__((ext_vector_type(2)));
+        if (n > 0) *(uint32_t*)p = __builtin_bit_cast(uint32_t, __builtin_convertvector(Wide{v[0], v[1]}, Pair));  // nearest even
+    } else {
+        if (n > 0) p[0] = row_round<uint16_t>(v[0]);
+        if (n > 1) p[1] = row_round<uint16_t>(v[1]);
+    }
 }
 
-// One wave's map in LDS.
-struct Shared {
-    f32x4 a[WAVES][16], h[WAVES][16];
-    int cut[WAVES];
-};
-// What enters this lane's run, and what leaves the chunk, of what enters the chunk
-// (`carry`, replaced).  The caller uses two Shared in turn: one barrier a chunk.
-template <bool BACK>
-__device__ __forceinline__ f32x4 enter(const Map& own, f32x4& carry, Shared& sh) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15;
-    Map all;
-    const Map inside = before<BACK>(own, all);
-    if (lane / 16 == (BACK ? 0 : RUNS - 1)) {
-        sh.a[wave][c] = all.a;
-        sh.h[wave][c] = all.h;
-        if (c == 0) sh.cut[wave] = all.cut;
+// Where a lane is.
+struct Place {
+    int lane, wave, half, c, n, second;
+    __device__ __forceinline__ Place(const GatedView& v, int tile) {
+        lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+        c = tile * TILE + 2 * (lane & 31);
+        n = v.C - c < 0 ? 0 : v.C - c > 2 ? 2 : v.C - c;
+        if (n == 0) c = 0;
+        second = n > 1;
     }
-    __syncthreads();
-    f32x4 mine = carry;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-        const int w = BACK ? WAVES - 1 - i : i;
-        if (w == wave) mine = carry;
-        carry = through(Map{sh.a[w][c], sh.h[w][c], sh.cut[w] != 0}, carry);
+    template <bool PAIR> __device__ __forceinline__ Two rate2(const GatedView& v) const {
+        Two r = get2<PAIR>(v.a_log + c, second);
+        return {{rate2_of(r[0]), rate2_of(r[1])}};
     }
-    return through(inside, mine);
-}
-
-// The steps of a lane's run: x and the gates as they are read.
-struct Steps {
-    f32x4 x[STEPS], ga[STEPS], gx[STEPS];
-    bool start[STEPS], in[STEPS];
 };
-template <bool VEC, class T>
-__device__ __forceinline__ f32x4 load(const Rows& r, int64_t b, int64_t t, int c, int n) {
-    return row_load<VEC>((const T*)r.p + b * r.b + t * r.t + c, n);
-}
-// Time t0 and on, channels c and on (n of them, 0: none); what is past the end moves nothing.
-template <bool VEC, class T, bool X>
-__device__ __forceinline__ void load_steps(Steps& s, const GatedView& v, int64_t b, int t0, int end, int c, int n) {
+// Steps of one tensor: `p` is the lane's first step of the chunk at hand; the pointer moves
+// on by whole chunks, so that a load costs one addition.
+template <class T, bool PAIR, int S>
+struct Stream {
+    const T* p;
+    int64_t step;
+    Raw<T, PAIR> r[S];
+    __device__ __forceinline__ Stream(const Rows& rows, int64_t b, int t, const Place& at) {
+        p = (const T*)rows.p + b * rows.b + (int64_t)(t + (at.wave * 2 + at.half) * S) * rows.t + at.c;
+        step = rows.t;
+    }
+    __device__ __forceinline__ void move(int steps) { p += steps * step; }
+    // `left`: steps from the first on that exist (1 or more of the wave's chunk); others read the last.
+    template <bool FULL>
+    __device__ __forceinline__ void fetch(int left, int second) {
+        if (FULL) {
+            const T* q = p;
 #pragma unroll
-    for (int k = 0; k < STEPS; ++k) {
-        const int t = t0 + k;
-        s.in[k] = t < end;
-        const int m = s.in[k] ? n : 0, at = s.in[k] ? t : 0, ch = m > 0 ? c : 0;
-        s.ga[k] = load<VEC, T>(v.ga, b, at, ch, m);
-        if (X) {
-            s.x[k] = load<VEC, T>(v.x, b, at, ch, m);
-            s.gx[k] = load<VEC, T>(v.gx, b, at, ch, m);
+            for (int k = 0; k < S; ++k, q += step) r[k].load(q, second);
+        } else {
+#pragma unroll
+            for (int k = 0; k < S; ++k) r[k].load(p + (int64_t)(k < left ? k : left - 1) * step, second);
         }
-        s.start[k] = s.in[k] && v.reset && v.reset[b * v.T + t];
     }
+};
+// Episode starts among the 2 S steps of a wave, a lane each.
+template <int S>
+__device__ __forceinline__ int start_of(const GatedView& v, int64_t b, int t, int end, int lane) {
+    return v.reset && lane < 2 * S && t + lane < end ? v.reset[b * v.T + t + lane] : 0;
+}
+__device__ __forceinline__ uint32_t starts(int own) { return (uint32_t)__ballot(own != 0); }
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32, 64); }
+__device__ __forceinline__ Two other_half(Two v) { return {{other_half(v[0]), other_half(v[1])}}; }
+// What leaves a run that h enters; `cut`: an episode starts in it.
+__device__ __forceinline__ Two through(Two a, Two end, bool cut, Two h) {
+    return {{cut ? end[0] : fmaf(a[0], h[0], end[0]), cut ? end[1] : fmaf(a[1], h[1], end[1])}};
 }
 
-// Forward.  A workgroup walks the chunks of one segment of 64 channels.
+// The waves' maps in LDS: products of decays, ends forward and (B) back.
+template <int W, int DIRECTIONS>
+struct Shared {
+    float2 a[W][32], end[DIRECTIONS][W][32];
+    int cut[W];
+};
+template <int W>
+__device__ __forceinline__ uint32_t cuts_of(const int (&cut)[W], int lane) {
+    return (uint32_t)__ballot(lane < W && cut[lane < W ? lane : 0] != 0);
+}
+__device__ __forceinline__ Two two(float2 v) { return {{v.x, v.y}}; }
+
+// What enters segment `seg` of the segments before it (behind it).
+template <bool PAIR>
+__device__ __forceinline__ void pass(Two& carry, const GatedView& v, int64_t b, int seg, const Place& at) {
+    const int64_t from = (b * v.nseg + seg) * v.C + at.c;
+    const Two a = get2<PAIR>(v.seg_a + from, at.second), h = get2<PAIR>(v.seg_h + from, at.second);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) carry[j] = a[j] < 0.0f ? h[j] : fmaf(a[j], carry[j], h[j]);
+}
+template <bool PAIR>
+__device__ __forceinline__ void put_segment(const GatedView& v, int64_t b, int seg, Two prod, bool cut, Two end, const Place& at) {
+    const int64_t to = (b * v.nseg + seg) * v.C + at.c;
+    if (cut) prod = {{-1.0f, -1.0f}};
+    put2<PAIR>(v.seg_a + to, prod, at.n);
+    put2<PAIR>(v.seg_h + to, end, at.n);
+}
+
+// Forward.  A workgroup of W waves walks the chunks of one segment of 64 channels.
 // AGG: the segment's map alone, for the workgroups of the segments behind it.
-template <class T, bool VEC, bool AGG>
-__global__ __launch_bounds__(BLOCK) void gated_kernel(GatedView v) {
-    __shared__ Shared sh[2];
+template <class T, bool PAIR, int W, int S, bool AGG>
+__global__ __launch_bounds__(64 * W) void gated_kernel(GatedView v) {
+    constexpr int CHUNK = 2 * S * W;
+    __shared__ Shared<W, 1> sh[2];
     const int tile = blockIdx.x % v.tiles, item = blockIdx.x / v.tiles, seg = item % v.nseg;
     const int64_t b = item / v.nseg;
-    const int lane = threadIdx.x & 63, q = threadIdx.x / 16, c = tile * TILE + (lane & 15) * 4, n = v.C - c > 0 ? v.C - c : 0;
     if (AGG && seg == v.nseg - 1) return;
+    const Place at(v, tile);
     const int begin = seg * v.seg, end = begin + v.seg < v.T ? begin + v.seg : v.T;
-    f32x4 rate = row_load<VEC>(v.a_log + (n > 0 ? c : 0), n);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) rate[j] = rate_of(rate[j]);
-    f32x4 carry{0.0f, 0.0f, 0.0f, 0.0f}, prod{1.0f, 1.0f, 1.0f, 1.0f};
-    bool cut = false;
+    const Two rate2 = at.rate2<PAIR>(v);
+    Two carry{{0.0f, 0.0f}}, prod{{1.0f, 1.0f}};
+    uint32_t cut = 0;
     if (AGG) {
-        if (seg == 0 && q == 0 && n > 0) row_store<VEC>(v.state_copy + b * v.C + c, v.state ? row_load<VEC>(v.state + b * v.C + c, n) : carry, n);
+        if (seg == 0 && threadIdx.x < 32) put2<PAIR>(v.state_copy + b * v.C + at.c, v.state ? get2<PAIR>(v.state + b * v.C + at.c, at.second) : carry, at.n);
     } else {
         const float* from = v.nseg > 1 ? v.state_copy : v.state;
-        if (from) carry = row_load<VEC>(from + b * v.C + (n > 0 ? c : 0), n);
-        for (int s = 0; s < seg; ++s) {
-            const int64_t at = (b * v.nseg + s) * v.C + (n > 0 ? c : 0);
-            const f32x4 a = row_load<VEC>(v.seg_a + at, n), h = row_load<VEC>(v.seg_h + at, n);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) carry[j] = a[j] < 0.0f ? h[j] : fmaf(a[j], carry[j], h[j]);
-        }
+        if (from) carry = get2<PAIR>(from + b * v.C + at.c, at.second);
+        for (int s = 0; s < seg; ++s) pass<PAIR>(carry, v, b, s, at);
     }
-    int turn = 0;
-    for (int t0 = begin; t0 < end; t0 += CHUNK, turn ^= 1) {
-        Steps s;
-        load_steps<VEC, T, true>(s, v, b, t0 + q * STEPS, end, c, n);
-        if (!AGG && v.marks && q == 0 && n > 0)
-            row_store<VEC>(v.marks + (b * ((v.T + CHUNK - 1) / CHUNK) + t0 / CHUNK) * v.C + c, carry, n);
-        f32x4 a[STEPS], u[STEPS];
-        Map own = none();
+    Stream<T, PAIR, S> x(v.x, b, begin, at), ga(v.ga, b, begin, at), gx(v.gx, b, begin, at);
+    int reset = 0;
+    auto fetch_all = [&](int t0) {
+        reset = start_of<S>(v, b, t0 + at.wave * 2 * S, end, at.lane);
+        auto all = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            const int left = end - t0 - (at.wave * 2 + at.half) * S;
+            ga.template fetch<FULL>(left, at.second);
+            gx.template fetch<FULL>(left, at.second);
+            x.template fetch<FULL>(left, at.second);
+        };
+        if (t0 + CHUNK <= end) all(std::true_type{});
+        else all(std::false_type{});
+        x.move(CHUNK), ga.move(CHUNK), gx.move(CHUNK);
+    };
+    if (begin < end) fetch_all(begin);
+    for (int t0 = begin, turn = 0; t0 < end; t0 += CHUNK, turn ^= 1) {
+        const uint32_t mask = starts(reset), own = at.half ? mask >> S : mask & ((1u << S) - 1);
+        const int t = t0 + (at.wave * 2 + at.half) * S;
+        const bool plain = mask == 0 && t0 + CHUNK <= end;
+        Two a[S], u[S], A{{1.0f, 1.0f}}, H{{0.0f, 0.0f}};
+        auto run = [&](auto simple) {
+            constexpr bool PLAIN = decltype(simple)::value;
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k) {
+            for (int k = 0; k < S; ++k) {
+                const Two xv = x.r[k].get(), gav = ga.r[k].get(), gxv = gx.r[k].get();
+                const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const Decay d = decay(-rate[j] * sigmoid(s.ga[k][j]));
-                a[k][j] = d.a;
-                u[k][j] = (s.start[k] ? 1.0f : d.b) * sigmoid(s.gx[k][j]) * s.x[k][j];
-                if (!s.in[k]) a[k][j] = 1.0f, u[k][j] = 0.0f;
-                own.h[j] = s.start[k] ? u[k][j] : fmaf(a[k][j], own.h[j], u[k][j]);
-                own.a[j] *= a[k][j];
+                for (int j = 0; j < 2; ++j) {
+                    const Decay d = decay(-rate2[j] * sigmoid(gav[j]));
+                    a[k][j] = in ? d.a : 1.0f;
+                    u[k][j] = in ? (start ? 1.0f : d.b) * sigmoid(gxv[j]) * xv[j] : 0.0f;
+                    H[j] = start ? u[k][j] : fmaf(a[k][j], H[j], u[k][j]);
+                    A[j] *= a[k][j];
+                }
             }
-            own.cut = own.cut || s.start[k];
-        }
-        if (AGG) {
-            enter<false>(own, carry, sh[turn]);
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) {
-                prod *= sh[turn].a[w][lane & 15];
-                cut = cut || sh[turn].cut[w] != 0;
+        };
+        if (plain) run(std::true_type{});
+        else run(std::false_type{});
+        if (t0 + CHUNK < end) fetch_all(t0 + CHUNK);
+        // the wave's two runs joined
+        const Two oa = other_half(A), oh = other_half(H);
+        const bool cut0 = mask & ((1u << S) - 1), cut1 = mask >> S;
+        Two all{{A[0] * oa[0], A[1] * oa[1]}}, enter;
+        if (W > 1) {
+            if (at.half) {
+                const Two h = through(A, H, cut1, oh);
+                sh[turn].a[at.wave][at.lane & 31] = float2{all[0], all[1]};
+                sh[turn].end[0][at.wave][at.lane & 31] = float2{h[0], h[1]};
+                if (at.lane == 63) sh[turn].cut[at.wave] = mask != 0;
             }
-            continue;
+            __syncthreads();
+            const uint32_t cuts = cuts_of(sh[turn].cut, at.lane);
+            if (AGG) cut |= cuts;
+            enter = carry;
+            auto over_waves = [&](uint32_t cuts) {
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    if (w == at.wave) enter = carry;
+                    const Two p = two(sh[turn].a[w][at.lane & 31]), e = two(sh[turn].end[0][w][at.lane & 31]);
+                    carry = through(p, e, cuts >> w & 1u, carry);
+                    if (AGG) prod[0] *= p[0], prod[1] *= p[1];
+                }
+            };
+            if (cuts == 0) over_waves(0);
+            else over_waves(cuts);
+        } else {
+            enter = carry;
+            const Two first = at.half ? through(oa, oh, cut0, carry) : through(A, H, cut0, carry);
+            carry = at.half ? through(A, H, cut1, first) : through(oa, oh, cut1, first);
         }
-        f32x4 h = enter<false>(own, carry, sh[turn]);
+        if (AGG) continue;
+        if (v.marks && at.wave % (MARK / (2 * S)) == 0 && at.half == 0 && t < end)
+            put2<PAIR>(v.marks + (b * ((v.T + MARK - 1) / MARK) + t / MARK) * v.C + at.c, enter, at.n);
+        Two h = at.half ? through(oa, oh, cut0, enter) : enter;
+        T* y = (T*)v.y + (b * v.T + t) * v.C + at.c;
+        if (plain) {
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k) {
+            for (int k = 0; k < S; ++k) {
+                h = through(a[k], u[k], false, h);
+                put2<PAIR>(y + (int64_t)k * v.C, h, at.n);
+            }
+        } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) h[j] = s.start[k] ? u[k][j] : fmaf(a[k][j], h[j], u[k][j]);
-            if (s.in[k] && n > 0) row_store<VEC>((T*)v.y + (b * v.T + t0 + q * STEPS + k) * v.C + c, h, n);
+            for (int k = 0; k < S; ++k) {
+                h = through(a[k], u[k], own >> k & 1u, h);
+                if (t + k < end) put2<PAIR>(y + (int64_t)k * v.C, h, at.n);
+            }
         }
     }
-    if (q != 0 || n <= 0) return;
-    if (AGG) {
-        const int64_t at = (b * v.nseg + seg) * v.C + c;
-        if (cut) prod = f32x4{-1.0f, -1.0f, -1.0f, -1.0f};
-        row_store<VEC>(v.seg_a + at, prod, n);
-        row_store<VEC>(v.seg_h + at, carry, n);
-    } else if (seg == v.nseg - 1 && v.state_out) {
-        row_store<VEC>(v.state_out + b * v.C + c, carry, n);
-    }
+    if (threadIdx.x >= 32) return;
+    if (AGG) put_segment<PAIR>(v, b, seg, prod, cut != 0, carry, at);
+    else if (seg == v.nseg - 1 && v.state_out) put2<PAIR>(v.state_out + b * v.C + at.c, carry, at.n);
 }
 
-// What passes back through a segment, for the segments before it: back -> a back + end.
-template <class T, bool VEC>
-__global__ __launch_bounds__(BLOCK) void gated_back_kernel(GatedView v) {
-    __shared__ Shared sh[2];
+// What passes back through a segment, for the segments before it.
+template <class T, bool PAIR, int W, int S>
+__global__ __launch_bounds__(64 * W) void gated_back_kernel(GatedView v) {
+    constexpr int CHUNK = 2 * S * W;
+    __shared__ Shared<W, 1> sh[2];
     const int tile = blockIdx.x % v.tiles, item = blockIdx.x / v.tiles, seg = item % v.nseg;
     const int64_t b = item / v.nseg;
-    const int lane = threadIdx.x & 63, q = threadIdx.x / 16, c = tile * TILE + (lane & 15) * 4, n = v.C - c > 0 ? v.C - c : 0;
     if (seg == 0) return;
+    const Place at(v, tile);
     const int begin = seg * v.seg, end = begin + v.seg < v.T ? begin + v.seg : v.T;
-    f32x4 rate = row_load<VEC>(v.a_log + (n > 0 ? c : 0), n);
+    const Two rate2 = at.rate2<PAIR>(v);
+    Two carry{{0.0f, 0.0f}}, prod{{1.0f, 1.0f}};
+    uint32_t cut = 0;
+    const int first = begin + (end - begin - 1) / CHUNK * CHUNK;
+    Stream<T, PAIR, S> ga(v.ga, b, first, at), dy(v.dy, b, first, at);
+    int reset = 0;
+    auto fetch_all = [&](int t0) {
+        reset = start_of<S>(v, b, t0 + at.wave * 2 * S, end, at.lane);
+        auto all = [&](auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            const int left = end - t0 - (at.wave * 2 + at.half) * S;
+            ga.template fetch<FULL>(left, at.second);
+            dy.template fetch<FULL>(left, at.second);
+        };
+        if (t0 + CHUNK <= end) all(std::true_type{});
+        else all(std::false_type{});
+        ga.move(-CHUNK), dy.move(-CHUNK);
+    };
+    fetch_all(first);
+    for (int t0 = first, turn = 0; t0 >= begin; t0 -= CHUNK, turn ^= 1) {
+        const uint32_t mask = starts(reset), own = at.half ? mask >> S : mask & ((1u << S) - 1);
+        const int t = t0 + (at.wave * 2 + at.half) * S;
+        Two A{{1.0f, 1.0f}}, H{{0.0f, 0.0f}};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) rate[j] = rate_of(rate[j]);
-    f32x4 carry{0.0f, 0.0f, 0.0f, 0.0f}, prod{1.0f, 1.0f, 1.0f, 1.0f};
-    bool cut = false;
-    int turn = 0;
-    for (int t0 = begin + (end - begin - 1) / CHUNK * CHUNK; t0 >= begin && t0 < end; t0 -= CHUNK, turn ^= 1) {
-        Steps s;
-        load_steps<VEC, T, false>(s, v, b, t0 + q * STEPS, end, c, n);
-        Map own = none();
+        for (int k = S - 1; k >= 0; --k) {
+            const Two gav = ga.r[k].get(), d = dy.r[k].get();
+            const bool start = own >> k & 1u, in = t + k < end;
 #pragma unroll
-        for (int k = STEPS - 1; k >= 0; --k) {
-            const int t = t0 + q * STEPS + k, m = s.in[k] ? n : 0;
-            const f32x4 dy = load<VEC, T>(v.dy, b, s.in[k] ? t : 0, m > 0 ? c : 0, m);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float a = s.in[k] ? __builtin_amdgcn_exp2f(-rate[j] * sigmoid(s.ga[k][j]) * LOG2E) : 1.0f;
-                own.h[j] = s.start[k] ? 0.0f : a * (own.h[j] + dy[j]);
-                own.a[j] *= a;
+            for (int j = 0; j < 2; ++j) {
+                const float a = in ? __builtin_amdgcn_exp2f(-rate2[j] * sigmoid(gav[j])) : 1.0f;
+                H[j] = start ? 0.0f : in ? a * (H[j] + d[j]) : H[j];
+                A[j] *= a;
             }
-            own.cut = own.cut || s.start[k];
         }
-        enter<true>(own, carry, sh[turn]);
+        if (t0 > begin) fetch_all(t0 - CHUNK);
+        const Two oa = other_half(A), oh = other_half(H);
+        if (!at.half) {
+            const Two h = through(A, H, mask & ((1u << S) - 1), oh);
+            sh[turn].a[at.wave][at.lane] = float2{A[0] * oa[0], A[1] * oa[1]};
+            sh[turn].end[0][at.wave][at.lane] = float2{h[0], h[1]};
+            if (at.lane == 0) sh[turn].cut[at.wave] = mask != 0;
+        }
+        __syncthreads();
+        const uint32_t cuts = cuts_of(sh[turn].cut, at.lane);
+        cut |= cuts;
+        auto over_waves = [&](uint32_t cuts) {
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            prod *= sh[turn].a[w][lane & 15];
-            cut = cut || sh[turn].cut[w] != 0;
-        }
+            for (int w = W - 1; w >= 0; --w) {
+                const Two p = two(sh[turn].a[w][at.lane & 31]), e = two(sh[turn].end[0][w][at.lane & 31]);
+                carry = through(p, e, cuts >> w & 1u, carry);
+                prod[0] *= p[0], prod[1] *= p[1];
+            }
+        };
+        if (cuts == 0) over_waves(0);
+        else over_waves(cuts);
     }
-    if (q != 0 || n <= 0) return;
-    const int64_t at = (b * v.nseg + seg) * v.C + c;
-    if (cut) prod = f32x4{-1.0f, -1.0f, -1.0f, -1.0f};
-    row_store<VEC>(v.seg_a + at, prod, n);
-    row_store<VEC>(v.seg_h + at, carry, n);
+    if (threadIdx.x < 32) put_segment<PAIR>(v, b, seg, prod, cut != 0, carry, at);
 }
 
 // Backward: with R_t = dy_t + a_{t+1} R_{t+1},
 //   dx = R b i,   dgate_x = R b i (1 - i) x,   G = log a (R a h_{t-1} - R i x a^2 / b),
 //   dgate_a = G (1 - r),   da_log = sum of G      (at a start G is zero).
-// Chunks are walked from the last on; the state before one is its mark, so that both
-// directions are in registers at once and every value is read once.
-template <class T, bool VEC>
-__global__ __launch_bounds__(BLOCK) void gated_backward_kernel(GatedView v) {
-    __shared__ Shared sh[2], shf[2];
-    __shared__ f32x4 sums[RUNS * WAVES][16];
+// Chunks are walked from the last on; the state before every fourth wave's steps is a
+// mark, so that both directions are in registers at once and every value is read once.
+template <class T, bool PAIR, int W, int S>
+__global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
+    constexpr int CHUNK = 2 * S * W, GROUP = MARK / (2 * S);  // steps, waves that share a mark
+    __shared__ Shared<W, 2> sh[2];
+    __shared__ float2 sums[2 * W][32];
     const int tile = blockIdx.x % v.tiles;
-    const int lane = threadIdx.x & 63, q = threadIdx.x / 16, c = tile * TILE + (lane & 15) * 4, n = v.C - c > 0 ? v.C - c : 0;
-    f32x4 rate = row_load<VEC>(v.a_log + (n > 0 ? c : 0), n), dal{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) rate[j] = rate_of(rate[j]);
+    const Place at(v, tile);
+    const Two rate2 = at.rate2<PAIR>(v);
+    Two dal{{0.0f, 0.0f}};
     int turn = 0;
     for (int64_t item = blockIdx.x / v.tiles; item < (int64_t)v.B * v.nseg; item += v.items) {
         const int seg = (int)(item % v.nseg);
         const int64_t b = item / v.nseg;
         const int begin = seg * v.seg, end = begin + v.seg < v.T ? begin + v.seg : v.T;
-        f32x4 carry{0.0f, 0.0f, 0.0f, 0.0f};
-        if (v.dstate_out) carry = row_load<VEC>(v.dstate_out + b * v.C + (n > 0 ? c : 0), n);
-        for (int s = v.nseg - 1; s > seg; --s) {
-            const int64_t at = (b * v.nseg + s) * v.C + (n > 0 ? c : 0);
-            const f32x4 a = row_load<VEC>(v.seg_a + at, n), h = row_load<VEC>(v.seg_h + at, n);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) carry[j] = a[j] < 0.0f ? h[j] : fmaf(a[j], carry[j], h[j]);
+        Two carry{{0.0f, 0.0f}};
+        if (v.dstate_out) carry = get2<PAIR>(v.dstate_out + b * v.C + at.c, at.second);
+        for (int s = v.nseg - 1; s > seg; --s) pass<PAIR>(carry, v, b, s, at);
+        if (end <= begin) {  // no steps: what comes in goes out
+            if (seg == 0 && v.dstate && threadIdx.x < 32) put2<PAIR>(v.dstate + b * v.C + at.c, carry, at.n);
+            continue;
         }
-        for (int t0 = begin + (end - begin - 1) / CHUNK * CHUNK; t0 >= begin && t0 < end; t0 -= CHUNK, turn ^= 1) {
-            Steps s;
-            f32x4 dy[STEPS];
-            load_steps<VEC, T, true>(s, v, b, t0 + q * STEPS, end, c, n);
+        const int first = begin + (end - begin - 1) / CHUNK * CHUNK;
+        Stream<T, PAIR, S> x(v.x, b, first, at), ga(v.ga, b, first, at), gx(v.gx, b, first, at), dy(v.dy, b, first, at);
+        for (int t0 = first; t0 >= begin; t0 -= CHUNK, turn ^= 1) {
+            const int t = t0 + (at.wave * 2 + at.half) * S;
+            const int reset = start_of<S>(v, b, t0 + at.wave * 2 * S, end, at.lane);
+            auto fetch_all = [&](auto full) {
+                constexpr bool FULL = decltype(full)::value;
+                ga.template fetch<FULL>(end - t, at.second);
+                gx.template fetch<FULL>(end - t, at.second);
+                x.template fetch<FULL>(end - t, at.second);
+                dy.template fetch<FULL>(end - t, at.second);
+            };
+            if (t0 + CHUNK <= end) fetch_all(std::true_type{});
+            else fetch_all(std::false_type{});
+            x.move(-CHUNK), ga.move(-CHUNK), gx.move(-CHUNK), dy.move(-CHUNK);
+            const int group = t0 + at.wave / GROUP * MARK;  // the mark's step, if it exists
+            Two now = get2<PAIR>(v.marks_in + (b * ((v.T + MARK - 1) / MARK) + (group < end ? group : t0) / MARK) * v.C + at.c, at.second);
+            const uint32_t mask = starts(reset), own = at.half ? mask >> S : mask & ((1u << S) - 1);
+            const bool plain = mask == 0 && t0 + CHUNK <= end;
+            const bool cut0 = mask & ((1u << S) - 1), cut1 = mask >> S;
+            Two r[S], i[S], a[S], bb[S], A{{1.0f, 1.0f}}, F{{0.0f, 0.0f}}, H{{0.0f, 0.0f}};
+            auto runs = [&](auto simple) {
+                constexpr bool PLAIN = decltype(simple)::value;
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) {
-                const int m = s.in[k] ? n : 0;
-                dy[k] = load<VEC, T>(v.dy, b, s.in[k] ? t0 + q * STEPS + k : 0, m > 0 ? c : 0, m);
-            }
-            f32x4 mark = row_load<VEC>(v.marks_in + (b * ((v.T + CHUNK - 1) / CHUNK) + t0 / CHUNK) * v.C + (n > 0 ? c : 0), n);
-            f32x4 a[STEPS], bb[STEPS], h[STEPS];  // h: the state before the step
-            Map fwd = none(), own = none();
+                for (int k = 0; k < S; ++k) {
+                    const Two xv = x.r[k].get(), gav = ga.r[k].get(), gxv = gx.r[k].get();
+                    const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s.ga[k][j] = sigmoid(s.ga[k][j]);
-                    s.gx[k][j] = sigmoid(s.gx[k][j]);
-                    const Decay d = decay(-rate[j] * s.ga[k][j]);
-                    a[k][j] = d.a, bb[k][j] = d.b;
-                    if (!s.in[k]) a[k][j] = 1.0f, bb[k][j] = 0.0f;
-                    if (s.start[k]) bb[k][j] = 1.0f;
-                    const float u = bb[k][j] * s.gx[k][j] * s.x[k][j];
-                    fwd.h[j] = s.start[k] ? u : fmaf(a[k][j], fwd.h[j], u);
-                    fwd.a[j] *= a[k][j];
+                    for (int j = 0; j < 2; ++j) {
+                        r[k][j] = sigmoid(gav[j]);
+                        i[k][j] = sigmoid(gxv[j]);
+                        const Decay d = decay(-rate2[j] * r[k][j]);
+                        a[k][j] = in ? d.a : 1.0f;
+                        bb[k][j] = !in ? 0.0f : start ? 1.0f : d.b;
+                        const float u = in ? bb[k][j] * i[k][j] * xv[j] : 0.0f;
+                        F[j] = start ? u : fmaf(a[k][j], F[j], u);
+                        A[j] *= a[k][j];
+                    }
                 }
-                fwd.cut = fwd.cut || s.start[k];
-            }
-            own.a = fwd.a;
-            own.cut = fwd.cut;
 #pragma unroll
-            for (int k = STEPS - 1; k >= 0; --k)
+                for (int k = S - 1; k >= 0; --k) {
+                    const Two d = dy.r[k].get();
+                    const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) own.h[j] = s.start[k] ? 0.0f : a[k][j] * (own.h[j] + dy[k][j]);
-            f32x4 now = enter<false>(fwd, mark, shf[turn]);
-            f32x4 back = enter<true>(own, carry, sh[turn]);
-#pragma unroll
-            for (int k = 0; k < STEPS; ++k) {
-                h[k] = now;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float u = bb[k][j] * s.gx[k][j] * s.x[k][j];
-                    now[j] = s.start[k] ? u : fmaf(a[k][j], now[j], u);
+                    for (int j = 0; j < 2; ++j) H[j] = start ? 0.0f : in ? a[k][j] * (H[j] + d[j]) : H[j];
                 }
-            }
-#pragma unroll
-            for (int k = STEPS - 1; k >= 0; --k) {
-                f32x4 dx, dga, dgx;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float r = s.ga[k][j], i = s.gx[k][j], x = s.x[k][j], l = a[k][j] * (-rate[j] * r);
-                    const float R = dy[k][j] + back[j], Ri = R * i;
-                    dx[j] = Ri * bb[k][j];
-                    dgx[j] = dx[j] * x * (1.0f - i);
-                    // log a times a, before any other factor: log a may be as large as fp32 goes where a is 0;
-                    // with log a, its quotient by b goes to zero as a root
-                    const float over = bb[k][j] > 0.0f ? l * a[k][j] * __builtin_amdgcn_rcpf(bb[k][j]) : 0.0f;
-                    const float G = s.start[k] ? 0.0f : R * (l * h[k][j]) - Ri * x * over;
-                    dga[j] = G * (1.0f - r);
-                    if (s.in[k]) dal[j] += G;
-                    back[j] = s.start[k] ? 0.0f : a[k][j] * R;
+            };
+            if (plain) runs(std::true_type{});
+            else runs(std::false_type{});
+            const Two oa = other_half(A), of = other_half(F), oh = other_half(H);
+            Two back = carry;
+            if (W > 1) {
+                if (at.half) {
+                    const Two f = through(A, F, cut1, of);
+                    sh[turn].end[0][at.wave][at.lane & 31] = float2{f[0], f[1]};
+                    sh[turn].a[at.wave][at.lane & 31] = float2{A[0] * oa[0], A[1] * oa[1]};
+                } else {
+                    const Two h = through(A, H, cut0, oh);
+                    sh[turn].end[1][at.wave][at.lane] = float2{h[0], h[1]};
+                    if (at.lane == 0) sh[turn].cut[at.wave] = mask != 0;
                 }
-                if (s.in[k] && n > 0) {
-                    const int64_t at = (b * v.T + t0 + q * STEPS + k) * v.C + c;
-                    row_store<VEC>((T*)v.dx + at, dx, n);
-                    row_store<VEC>((T*)v.dga + at, dga, n);
-                    row_store<VEC>((T*)v.dgx + at, dgx, n);
+                __syncthreads();
+                const uint32_t cuts = cuts_of(sh[turn].cut, at.lane);
+                for (int w = at.wave / GROUP * GROUP; w < at.wave; ++w)
+                    now = through(two(sh[turn].a[w][at.lane & 31]), two(sh[turn].end[0][w][at.lane & 31]), cuts >> w & 1u, now);
+#pragma unroll
+                for (int w = W - 1; w >= 0; --w) {
+                    if (w == at.wave) back = carry;
+                    carry = through(two(sh[turn].a[w][at.lane & 31]), two(sh[turn].end[1][w][at.lane & 31]), cuts >> w & 1u, carry);
                 }
+            } else {
+                const Two later = at.half ? through(A, H, cut1, carry) : through(oa, oh, cut1, carry);
+                carry = at.half ? through(oa, oh, cut0, later) : through(A, H, cut0, later);
             }
+            if (at.half) now = through(oa, of, cut0, now);
+            else back = through(oa, oh, cut1, back);
+            const int64_t to = (b * v.T + t) * v.C + at.c;
+            T *dxp = (T*)v.dx + to, *dgap = (T*)v.dga + to, *dgxp = (T*)v.dgx + to;
+            auto outputs = [&](auto simple) {
+                constexpr bool PLAIN = decltype(simple)::value;
+                Two h[S];  // the state before the step
+#pragma unroll
+                for (int k = 0; k < S; ++k) {
+                    const Two xv = x.r[k].get();
+                    const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
+                    h[k] = now;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float u = in ? bb[k][j] * i[k][j] * xv[j] : 0.0f;
+                        now[j] = start ? u : fmaf(a[k][j], now[j], u);
+                    }
+                }
+#pragma unroll
+                for (int k = S - 1; k >= 0; --k) {
+                    const Two xv = x.r[k].get(), d = dy.r[k].get();
+                    const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
+                    Two dx, dga, dgx;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float R = (in ? d[j] : 0.0f) + back[j], Ri = R * i[k][j];
+                        dx[j] = Ri * bb[k][j];
+                        dgx[j] = dx[j] * xv[j] * (1.0f - i[k][j]);
+                        // log a times a, before any other factor: log a may be as large as fp32 goes where a is 0;
+                        // with log a, its quotient by b goes to zero as a root
+                        const float l = a[k][j] * (-rate2[j] * LN2 * r[k][j]);
+                        const float over = bb[k][j] > 0.0f ? l * a[k][j] * __builtin_amdgcn_rcpf(bb[k][j]) : 0.0f;
+                        const float G = start ? 0.0f : R * (l * h[k][j]) - Ri * xv[j] * over;
+                        dga[j] = G * (1.0f - r[k][j]);
+                        if (in) dal[j] += G;
+                        back[j] = start ? 0.0f : a[k][j] * R;
+                    }
+                    if (in) {
+                        put2<PAIR>(dxp + (int64_t)k * v.C, dx, at.n);
+                        put2<PAIR>(dgap + (int64_t)k * v.C, dga, at.n);
+                        put2<PAIR>(dgxp + (int64_t)k * v.C, dgx, at.n);
+                    }
+                }
+            };
+            if (plain) outputs(std::true_type{});
+            else outputs(std::false_type{});
         }
-        if (seg == 0 && v.dstate && q == 0 && n > 0) row_store<VEC>(v.dstate + b * v.C + c, carry, n);
+        if (seg == 0 && v.dstate && threadIdx.x < 32) put2<PAIR>(v.dstate + b * v.C + at.c, carry, at.n);
     }
-    sums[q][lane & 15] = dal;
+    sums[2 * at.wave + at.half][at.lane & 31] = float2{dal[0], dal[1]};
     __syncthreads();
-    if (q != 0 || n <= 0) return;
+    if (threadIdx.x >= 32) return;
 #pragma unroll
-    for (int k = 1; k < RUNS * WAVES; ++k) dal += sums[k][lane & 15];
-    row_store<VEC>(v.parts + (int64_t)(blockIdx.x / v.tiles) * v.C + c, dal, n);
+    for (int k = 1; k < 2 * W; ++k) {
+        const float2 s = sums[k][at.lane];
+        dal[0] += s.x, dal[1] += s.y;
+    }
+    put2<PAIR>(v.parts + (int64_t)(blockIdx.x / v.tiles) * v.C + at.c, dal, at.n);
 }
 
 // One step of every row: four channels a lane.
@@ -400,14 +561,15 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedView v, float* poo
         at = 0;
     }
     const bool start = v.reset && v.reset[row];
-    const f32x4 ga = load<VEC, T>(v.ga, row, 0, c, n), gx = load<VEC, T>(v.gx, row, 0, c, n), x = load<VEC, T>(v.x, row, 0, c, n);
+    auto read = [&](const Rows& r) { return row_load<VEC>((const T*)r.p + row * r.b + c, n); };
+    const f32x4 ga = read(v.ga), gx = read(v.gx), x = read(v.x);
     const f32x4 al = row_load<VEC>(v.a_log + c, n);
     float* st = pool + at * v.C + c;
     f32x4 h{0.0f, 0.0f, 0.0f, 0.0f};
     if (!reset) h = row_load<VEC>(st, n);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const Decay d = decay(-rate_of(al[j]) * sigmoid(ga[j]));
+        const Decay d = decay(-rate2_of(al[j]) * sigmoid(ga[j]));
         const float u = (start ? 1.0f : d.b) * sigmoid(gx[j]) * x[j];
         h[j] = reset ? u : fmaf(d.a, h[j], u);
     }
@@ -417,36 +579,39 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedView v, float* poo
 
 // ---- host ----
 
-constexpr int FULL = 512;       // workgroups that fill the chip
+constexpr int CUT_BELOW = 128;  // workgroups (a sequence's tile each) below which forward calls are cut,
+constexpr int FULL = 256;       // and how many fill the chip
+constexpr int BACK_FULL = 512;  // the same backward, where the cut's own pass is cheap
 constexpr int LEAST_SEG = 256;  // steps of a segment at least
 constexpr int MAX_SEG = 64;     // segments of a sequence at most
 constexpr int WALKS = 2048;     // workgroups of the backward at most: each adds a part of da_log
 
 struct Cut {
     int tiles, nseg = 1, seg;
-    Cut(int64_t B, int T, int C) {
+    Cut(int64_t B, int T, int C, bool backward) {
         tiles = (C + TILE - 1) / TILE;
-        const int64_t have = B * tiles, want = have > 0 ? (FULL + have - 1) / have : 1, most = (T + LEAST_SEG - 1) / LEAST_SEG;
-        int64_t k = want < most ? want : most;
+        seg = T > 0 ? T : 1;
+        const int64_t have = B * tiles, full = backward ? BACK_FULL : FULL, most = (T + LEAST_SEG - 1) / LEAST_SEG;
+        if (have < 1 || have >= (backward ? BACK_FULL : CUT_BELOW)) return;
+        int64_t k = (full + have - 1) / have;
+        k = k < most ? k : most;
         k = k < MAX_SEG ? k : MAX_SEG;
-        whole(T);
         if (k < 2) return;
-        seg = (int)((T + k - 1) / k + CHUNK - 1) / CHUNK * CHUNK;
+        seg = (int)(((T + k - 1) / k + LEAST_SEG - 1) / LEAST_SEG * LEAST_SEG);
         nseg = (T + seg - 1) / seg;
     }
-    void whole(int T) { nseg = 1, seg = T > 0 ? T : 1; }
 };
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // Bytes of the workspace: the segments' maps and the states before the first (cut
-// calls have B * tiles < FULL, so B * nseg < 2 FULL / tiles), then the parts.
+// calls have B * tiles < BACK_FULL, so B * nseg < 2 BACK_FULL / tiles), then the parts.
 struct Plan {
     size_t maps, states, parts, total;
     Plan(int T, int C, bool backward) {
         const int tiles = (C + TILE - 1) / TILE;
         const size_t cut = T > LEAST_SEG ? 4 * (size_t)C : 0;
-        maps = up256(cut * (2 * FULL / tiles + 1));
-        states = up256(cut * (FULL / tiles + 1));
+        maps = up256(cut * (2 * BACK_FULL / tiles + 1));
+        states = up256(cut * (BACK_FULL / tiles + 1));
         parts = up256(backward ? 4 * (size_t)C * walks(tiles) : 0);
         total = 2 * maps + states + parts;
     }
@@ -470,9 +635,28 @@ int gated_view(const gorila_gated_scan_args* a, bool step, GatedView& v, bool& v
     v.gx = {a->gate_x, a->gate_x_batch_stride, a->gate_x_step_stride};
     v.a_log = a->a_log, v.reset = a->reset, v.state = a->state;
     const int64_t strides = v.x.b | v.ga.b | v.gx.b | (step ? 0 : v.x.t | v.ga.t | v.gx.t);
-    vec = !(v.C & 3) && !(strides & 3) && at_four(a->x, e) && at_four(a->gate_a, e) && at_four(a->gate_x, e) && at_four(a->a_log, 4) &&
-          at_four(a->state, 4);
+    const int w = step ? 4 : 2;  // values a load
+    vec = !((v.C | strides) & (w - 1));
+    for (const void* p : {a->x, a->gate_a, a->gate_x}) vec = vec && at_element(p, w * e);
+    for (const float* p : {a->a_log, a->state}) vec = vec && at_element(p, w * 4);
     return GORILA_OK;
+}
+
+// Waves a workgroup, of 16 steps each (a wave in which T ends, or a mark's four and more): forward two
+// chunks or more where there are as many steps, so that loads are under way while a
+// chunk is joined (32 x 128 x 1024 fp32: 14.6 us; one chunk of eight waves: 18.4).  Backward a lane
+// has 216 registers, and more waves than two a SIMD do not pay: 8 steps a lane and four
+// waves 22.7 us (5.2 TB/s), eight waves 27.6; 4 steps and eight waves, half of the registers, 26.2.
+constexpr int S = 8;
+int forward_waves(int T) { return T <= 16 ? 1 : T <= 128 ? 4 : T <= 256 ? 8 : 16; }
+int backward_waves(int T) { return T <= 16 ? 1 : 4; }
+template <class F>
+void by_waves(int waves, F&& f) {
+    using std::integral_constant;
+    if (waves == 1) f(integral_constant<int, 1>{});
+    else if (waves == 4) f(integral_constant<int, 4>{});
+    else if (waves == 8) f(integral_constant<int, 8>{});
+    else f(integral_constant<int, 16>{});
 }
 
 template <class F>
@@ -503,20 +687,24 @@ int gorila_gated_scan(const gorila_gated_scan_args* args, void* y, float* state_
     if (v.B == 0 || (v.T == 0 && !state_out)) return GORILA_OK;
     const int e = dtype_bytes(args->dtype);
     if ((v.T > 0 && !y) || !at_element(y, e) || !at_element(state_out, 4) || !at_element(marks, 4)) return GORILA_EINVAL;
-    const Cut k(v.B, v.T, v.C);
+    const Cut k(v.B, v.T, v.C, false);
     const Plan p(v.T, v.C, false);
     const double blocks = (double)v.B * k.nseg * k.tiles;
-    if (!launch_fits(blocks, BLOCK)) return GORILA_EUNSUPPORTED;
+    const int waves = forward_waves(v.T);
+    if (!launch_fits(blocks, 64 * waves)) return GORILA_EUNSUPPORTED;
     if ((rc = ctx_view(ctx, k.nseg > 1 ? p.total : 0, c))) return rc;
-    vec = vec && at_four(y, e) && at_four(state_out, 4) && at_four(marks, 4);
+    vec = vec && at_element(y, 2 * e) && at_element(state_out, 8) && at_element(marks, 8);
     v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg;
     v.y = y, v.state_out = state_out, v.marks = marks;
     if (k.nseg > 1) v.seg_a = (float*)c.ws, v.seg_h = (float*)(c.ws + p.maps), v.state_copy = (float*)(c.ws + 2 * p.maps);
     by_rows(args->dtype, vec, [&](auto t, auto al) {
         using T = decltype(t);
         constexpr bool VEC = decltype(al)::value;
-        if (k.nseg > 1) gated_kernel<T, VEC, true><<<(unsigned)blocks, BLOCK, 0, c.stream>>>(v);
-        gated_kernel<T, VEC, false><<<(unsigned)blocks, BLOCK, 0, c.stream>>>(v);
+        if (k.nseg > 1) gated_kernel<T, VEC, 16, S, true><<<(unsigned)blocks, 1024, 0, c.stream>>>(v);
+        by_waves(waves, [&](auto w) {
+            constexpr int W = decltype(w)::value;
+            gated_kernel<T, VEC, W, S, false><<<(unsigned)blocks, 64 * W, 0, c.stream>>>(v);
+        });
     });
     return launched();
 }
@@ -536,13 +724,15 @@ int gorila_gated_scan_backward(const gorila_gated_scan_args* args, const float* 
         if (!at_element(p, e)) return GORILA_EINVAL;
     for (const float* p : {marks, dstate_out, (const float*)da_log, (const float*)dstate})
         if (!at_element(p, 4)) return GORILA_EINVAL;
-    const Cut k(v.B, v.T, v.C);
+    const Cut k(v.B, v.T, v.C, true);
     const Plan p(v.T, v.C, true);
     const double all = (double)v.B * k.nseg * k.tiles;
-    if (!launch_fits(all, BLOCK)) return GORILA_EUNSUPPORTED;
+    const int waves = backward_waves(v.T);
+    if (!launch_fits(all, 64 * waves)) return GORILA_EUNSUPPORTED;
     if ((rc = ctx_view(ctx, p.total, c))) return rc;
-    vec = vec && !((dy_batch_stride | dy_step_stride) & 3) && at_four(dy, e) && at_four(dx, e) && at_four(dgate_a, e) && at_four(dgate_x, e) &&
-          at_four(marks, 4) && at_four(dstate_out, 4) && at_four(dstate, 4);
+    vec = vec && !((dy_batch_stride | dy_step_stride) & 1);
+    for (const void* p : {dy, (const void*)dx, (const void*)dgate_a, (const void*)dgate_x}) vec = vec && at_element(p, 2 * e);
+    for (const float* p : {marks, dstate_out, (const float*)dstate}) vec = vec && at_element(p, 8);
     v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg;
     const int64_t items = (int64_t)v.B * k.nseg;
     v.items = (int)(items < Plan::walks(k.tiles) ? items : Plan::walks(k.tiles));
@@ -553,8 +743,9 @@ int gorila_gated_scan_backward(const gorila_gated_scan_args* args, const float* 
         by_rows(args->dtype, vec, [&](auto t, auto al) {
             using T = decltype(t);
             constexpr bool VEC = decltype(al)::value;
-            if (k.nseg > 1) gated_back_kernel<T, VEC><<<(unsigned)all, BLOCK, 0, c.stream>>>(v);
-            gated_backward_kernel<T, VEC><<<(unsigned)(v.items * k.tiles), BLOCK, 0, c.stream>>>(v);
+            if (k.nseg > 1) gated_back_kernel<T, VEC, 8, S><<<(unsigned)all, 512, 0, c.stream>>>(v);
+            if (waves == 1) gated_backward_kernel<T, VEC, 1, S><<<(unsigned)(v.items * k.tiles), 64, 0, c.stream>>>(v);
+            else gated_backward_kernel<T, VEC, 4, S><<<(unsigned)(v.items * k.tiles), 256, 0, c.stream>>>(v);
         });
     launch_sum_parts(v.parts, v.items, v.C, v.C, 1, da_log, nullptr, c.stream);
     return launched();

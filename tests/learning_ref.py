@@ -34,7 +34,7 @@ def layernorm_leaves(total, weight, bias, eps):
 def gated_leaves(x, gate_a, gate_x, a_log, reset, state):
     """y and every step's state before it, in the type of the arguments."""
     h, y, before = state, [], []
-    log_a = -torch.exp(a_log).clamp(max=torch.finfo(torch.float32).max) * torch.sigmoid(gate_a)
+    log_a = -torch.exp(a_log).clamp(max=2.0 ** 127) * torch.sigmoid(gate_a)
     for t in range(x.shape[1]):
         before.append(h)
         u = torch.sigmoid(gate_x[:, t]) * x[:, t]
