@@ -640,7 +640,7 @@ int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float
  * fp32 in [0, 1).  temperature, top_p, min_p [rows] fp32 and top_k [rows] int32 may be
  * NULL: 1, 1, 0 and all.  NaN counts as -infinity; with `most` the row's largest value,
  *   w = round to nearest even of 2^40 exp((value - most) / temperature),
- * formed in fp64 (2^40 where value = most, also if that is infinite; 0 for
+ * formed in fp64, to about 2^-50 of itself (2^40 where value = most, also if that is infinite; 0 for
  * -infinity and beside an infinite `most`).  In the order of values, the lowest action
  * first among equal ones:
  *   top_k: the first k stay (k outside 1 .. actions: all; temperature not above 0:
@@ -653,7 +653,9 @@ int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float
  * above 0, or NaN: 0; 1 and more: the last).  All sums are of whole numbers, so no order of
  * addition shows.  probability_out (may be NULL) [rows] fp32: w / S.  A row without a value
  * above -infinity has action -1 and probability 0.
- * More than 2^20 actions: GORILA_EUNSUPPORTED.  Uses no workspace. */
+ * More than 2^20 actions: GORILA_EUNSUPPORTED.  Needs no workspace; few rows of more than
+ * 16384 actions are faster where the context has one (66 KB a row; the result is the
+ * same, and the call then counts as one that uses it). */
 int gorila_sample_actions(const void* values, int64_t stride, int64_t rows, int32_t actions,
                           int32_t dtype, const float* u, const float* temperature,
                           const int32_t* top_k, const float* top_p, const float* min_p,
