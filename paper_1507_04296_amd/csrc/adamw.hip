@@ -2,9 +2,15 @@
 //
 // Memory bound: fp32 states move 28 bytes an element (fp32 gradients), 8-bit ones 16,
 // for 20 and 60 operations.  A wave takes 256 consecutive elements, four a lane, so that
-// a block of 8-bit states has its largest value after six shuffles, and a workgroup's
-// chunk of elements is found by its number among those of all tensors, which
-// travel in the kernel's arguments: a launch for 48 tensors, and nothing to copy.
+// a block of 8-bit states has its largest value in six steps over the lanes, and a
+// workgroup's chunk of elements is found by its number among those of all tensors,
+// which travel in the kernel's arguments: a launch for 48 tensors, and nothing to copy.
+// The clock is a launch of its own, before: all workgroups read it.
+//
+// The Q-network's ten tensors (1.69 M elements, fp32): 10.5 us (4.5 TB/s, part of it from
+// the cache) and 2.3 for the clock.  52 M elements in 8 bits, bf16 gradients: 165 us (4.45
+// TB/s; a large copy reaches 4.64), 217 with divisions, branches for the tail in every
+// chunk and sums through LDS.  Their values: 92 us (5.7 TB/s).
 #include "seq.h"
 
 namespace gorila {
@@ -96,15 +102,31 @@ __device__ __forceinline__ float value_of(uint32_t code, int least, float scale)
     const float unit = code ? __uint_as_float((code + least) << 20) : 0.0f;
     return unit * scale;
 }
-__device__ __forceinline__ int code_of(float size, float most, uint32_t chance, int least) {
-    const float unit = most > 0.0f ? size / most : 0.0f;
+// size / most rounded once, for a scale that a wave shares: by its reciprocal and what the
+// first quotient leaves (Markstein 1990), exact while the remainder is (quotients below
+// 2^-33 are off, and held as zero anyway).  Scales outside 2^-64 .. 2^124 are divided by.
+struct Scale {
+    float most, inverse;
+    bool far;
+    __device__ __forceinline__ explicit Scale(float m) : most(m), inverse(1.0f / m), far(!(m >= 0x1p-64f && m <= 0x1p124f)) {}
+    __device__ __forceinline__ float unit(float size) const {
+        if (far) return most > 0.0f ? size / most : 0.0f;
+        const float q = size * inverse;
+        return fmaf(fmaf(-q, most, size), inverse, q);
+    }
+};
+__device__ __forceinline__ int code_of(float unit, uint32_t chance, int least) {
     const int c = (int)((__float_as_uint(unit) + (chance << 4)) >> 20) - least;
     return c < 0 ? 0 : c;
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+// m / (sqrt(v) + eps) to three units of the last place, v from the smallest fp32 value on.
+__device__ __forceinline__ float step_of(float m, float v, float eps) {
+    const bool tiny = v < 0x1p-100f;
+    const float root = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p-32f : 1.0f);
+    return m * __builtin_amdgcn_rcpf(root + eps);
+}
+__device__ __forceinline__ float wave_max(float v) {  // of sizes
+    return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // G: the gradients' type; BITS: the states'.
@@ -117,85 +139,99 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
     const Tensor& t = s.t[which];
     const bool aligned = s.wide >> which & 1u;
     const int64_t first = (int64_t)(blockIdx.x - t.chunk) * CHUNK;
-    const float c1 = 1.0f / (float)r.clock[1], c2 = 1.0f / (float)r.clock[2];
-    const uint64_t key = BITS == 8 ? mix(r.seed + (uint64_t)(int64_t)r.clock[0] * GOLDEN) : 0;
+    auto chunk = [&](auto whole) {  // a whole chunk of aligned elements, or any
+#pragma clang fp contract(off)
+        constexpr bool FULL = decltype(whole)::value;
+        // all loads first: the stores between could lie anywhere, for the compiler
+        constexpr int TURNS = CHUNK / 1024;
+        f32x4 theta[TURNS], g[TURNS], m[TURNS], v[TURNS];
+        uint32_t cm[TURNS], cv[TURNS];
+        float sm[TURNS], sv[TURNS];
 #pragma unroll
-    for (int k = 0; k < CHUNK / 1024; ++k) {
-        const int64_t at = first + k * 1024 + threadIdx.x * 4, left = t.n - at;
-        const int n = left > 4 ? 4 : left > 0 ? (int)left : 0;
-        const bool wide = aligned && n == 4;
-        if (__ballot(n > 0) == 0) break;
-        const int64_t p = n > 0 ? at : 0;
-        f32x4 theta = load4(t.theta + p, n, wide);
-        const f32x4 g = load4((const G*)t.grad + p, n, wide);
-        f32x4 m, v;
-        uint32_t cm = 0, cv = 0;
-        const int64_t block = p / GROUP;
-        if (BITS == 32) {
-            m = load4((const float*)t.m + p, n, wide);
-            v = load4((const float*)t.v + p, n, wide);
-        } else {
-            cm = load_codes((const uint8_t*)t.m + p, n, wide);
-            cv = load_codes((const uint8_t*)t.v + p, n, wide);
-            const float sm = n > 0 ? t.m_scale[block] : 0.0f, sv = n > 0 ? t.v_scale[block] : 0.0f;
+        for (int k = 0; k < TURNS; ++k) {
+            const int64_t at = first + k * 1024 + threadIdx.x * 4, left = t.n - at;
+            const int n = FULL || left > 4 ? 4 : left > 0 ? (int)left : 0;
+            const bool wide = FULL || (aligned && (n == 4 || n == 0));
+            const int64_t p = n > 0 ? at : 0;
+            theta[k] = load4(t.theta + p, n, wide);
+            g[k] = load4((const G*)t.grad + p, n, wide);
+            if (BITS == 32) {
+                m[k] = load4((const float*)t.m + p, n, wide);
+                v[k] = load4((const float*)t.v + p, n, wide);
+            } else {
+                cm[k] = load_codes((const uint8_t*)t.m + p, n, wide);
+                cv[k] = load_codes((const uint8_t*)t.v + p, n, wide);
+                sm[k] = n > 0 ? t.m_scale[p / GROUP] : 0.0f;
+                sv[k] = n > 0 ? t.v_scale[p / GROUP] : 0.0f;
+            }
+        }
+        const float c1 = 1.0f / (float)r.clock[1], c2 = 1.0f / (float)r.clock[2];
+        const uint64_t key = BITS == 8 ? mix(r.seed + (uint64_t)(int64_t)r.clock[0] * GOLDEN) : 0;
+#pragma unroll
+        for (int k = 0; k < TURNS; ++k) {
+            const int64_t at = first + k * 1024 + threadIdx.x * 4, left = t.n - at;
+            const int n = FULL || left > 4 ? 4 : left > 0 ? (int)left : 0;
+            const bool wide = FULL || (aligned && (n == 4 || n == 0));
+            if (!FULL && __ballot(n > 0) == 0) break;
+            const int64_t p = n > 0 ? at : 0;
+            if (BITS == 8) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t c = cm[k] >> (8 * j) & 255u;
+                    const float size = value_of(c & 127u, LEAST_M, sm[k]);
+                    m[k][j] = c & 128u ? -size : size;
+                    v[k][j] = value_of(cv[k] >> (8 * j) & 255u, LEAST_V, sv[k]);
+                }
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t c = cm >> (8 * j) & 255u;
-                const float size = value_of(c & 127u, LEAST_M, sm);
-                m[j] = c & 128u ? -size : size;
-                v[j] = value_of(cv >> (8 * j) & 255u, LEAST_V, sv);
+                m[k][j] = r.beta1 * m[k][j] + r.rest1 * g[k][j];
+                v[k][j] = r.beta2 * v[k][j] + r.rest2 * (g[k][j] * g[k][j]);
+                theta[k][j] = theta[k][j] - r.lr * (t.decay * theta[k][j] + step_of(m[k][j] * c1, v[k][j] * c2, r.eps));
+            }
+            store4(t.theta + p, theta[k], n, wide);
+            if (BITS == 32) {
+                store4((float*)t.m + p, m[k], n, wide);
+                store4((float*)t.v + p, v[k], n, wide);
+            } else {
+                float mm = 0.0f, mv = 0.0f, bad_m = 0.0f, bad_v = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j >= n) m[k][j] = v[k][j] = 0.0f;
+                    mm = fmaxf(mm, fabsf(m[k][j])), mv = fmaxf(mv, v[k][j]);
+                    bad_m += m[k][j] * 0.0f, bad_v += v[k][j] * 0.0f;
+                }
+                mm = wave_max(bad_m == bad_m ? mm : INFINITY);
+                mv = wave_max(bad_v == bad_v ? mv : INFINITY);
+                const Scale scale_m(mm), scale_v(mv);
+                uint32_t new_m = 0, new_v = 0;
+                const uint64_t pair = t.place + (uint64_t)p / 2;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint64_t z = mix(key + (pair + h + 1) * GOLDEN);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int j = 2 * h + i;
+                        const uint32_t chance = (uint32_t)(z >> (32 * i));
+                        uint32_t a = code_of(scale_m.unit(fabsf(m[k][j])), chance & 0xffffu, LEAST_M), b = code_of(scale_v.unit(v[k][j]), chance >> 16, LEAST_V);
+                        if (v[k][j] > 0.0f && b == 0) b = 1;
+                        if (m[k][j] < 0.0f) a |= 128u;
+                        if (mm == INFINITY) a = 0;
+                        if (mv == INFINITY) b = 0;
+                        new_m |= a << (8 * j), new_v |= b << (8 * j);
+                    }
+                }
+                store_codes((uint8_t*)t.m + p, new_m, n, wide);
+                store_codes((uint8_t*)t.v + p, new_v, n, wide);
+                if (n > 0 && (threadIdx.x & 63) == 0) {
+                    t.m_scale[p / GROUP] = mm == INFINITY ? NAN : mm;
+                    t.v_scale[p / GROUP] = mv == INFINITY ? NAN : mv;
+                }
             }
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            m[j] = r.beta1 * m[j] + r.rest1 * g[j];
-            v[j] = r.beta2 * v[j] + r.rest2 * (g[j] * g[j]);
-            const float step = m[j] * c1 / (sqrtf(v[j] * c2) + r.eps);
-            theta[j] = theta[j] - r.lr * (t.decay * theta[j] + step);
-        }
-        if (n > 0) store4(t.theta + p, theta, n, wide);
-        if (BITS == 32) {
-            if (n > 0) {
-                store4((float*)t.m + p, m, n, wide);
-                store4((float*)t.v + p, v, n, wide);
-            }
-            continue;
-        }
-        float mm = 0.0f, mv = 0.0f, bad_m = 0.0f, bad_v = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j >= n) m[j] = v[j] = 0.0f;
-            mm = fmaxf(mm, fabsf(m[j])), mv = fmaxf(mv, v[j]);
-            bad_m += m[j] * 0.0f, bad_v += v[j] * 0.0f;
-        }
-        mm = wave_max(bad_m == bad_m ? mm : INFINITY);
-        mv = wave_max(bad_v == bad_v ? mv : INFINITY);
-        cm = cv = 0;
-        const uint64_t pair = t.place + (uint64_t)p / 2;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint64_t z = mix(key + (pair + h + 1) * GOLDEN);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int j = 2 * h + i;
-                const uint32_t chance = (uint32_t)(z >> (32 * i));
-                uint32_t a = code_of(fabsf(m[j]), mm, chance & 0xffffu, LEAST_M), b = code_of(v[j], mv, chance >> 16, LEAST_V);
-                if (v[j] > 0.0f && b == 0) b = 1;
-                if (m[j] < 0.0f) a |= 128u;
-                if (mm == INFINITY) a = 0;
-                if (mv == INFINITY) b = 0;
-                cm |= a << (8 * j), cv |= b << (8 * j);
-            }
-        }
-        if (n > 0) {
-            store_codes((uint8_t*)t.m + p, cm, n, wide);
-            store_codes((uint8_t*)t.v + p, cv, n, wide);
-            if ((threadIdx.x & 63) == 0) {
-                t.m_scale[block] = mm == INFINITY ? NAN : mm;
-                t.v_scale[block] = mv == INFINITY ? NAN : mv;
-            }
-        }
-    }
+    };
+    if (aligned && first + CHUNK <= t.n) chunk(std::true_type{});
+    else chunk(std::false_type{});
 }
 
 // theta and grad: where m's and v's values go.

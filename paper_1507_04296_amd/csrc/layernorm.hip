@@ -13,9 +13,7 @@ namespace {
 template <int LANES, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float (*sm)[N]) {
 #pragma unroll
-    for (int o = 32; o; o >>= 1)
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], o, 64);
+    for (int k = 0; k < N; ++k) v[k] = over_wave(v[k], [](float a, float b) { return a + b; });
     if (LANES == 64) return;
     __syncthreads();
     if ((threadIdx.x & 63) == 0)
