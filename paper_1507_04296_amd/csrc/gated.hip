@@ -2,7 +2,7 @@
 // channel, with a = exp(-exp(a_log) sigmoid(gate_a)), b = sqrt(1 - a^2), i = sigmoid(gate_x).
 //
 // Bound by memory and by the vector unit alike: a step of a channel has 3 values in and 1
-// out for 25 operations and 6 of the slow kind (exponentials, reciprocals, a root: four
+// out for some 40 operations and 6 of the slow kind (exponentials, reciprocals, a root: four
 // slots each), so a value is read once and its decay formed once.  The steps of a chunk
 // lie in the lanes' registers: 8 steps of 2 channels a lane, 32 lanes a step, 2 runs of
 // steps a wave.  Each lane runs through its own steps from zero, and what enters a
@@ -10,6 +10,11 @@
 // between the halves of a wave by a shuffle, over the waves in LDS, over the chunks in
 // registers.  (4 steps of 4 channels make twice the joins: 10 % of all operations.)
 // The next chunk's loads are under way while this one's runs are joined.
+//
+// 32 x 128 x 1024 fp32: forward 14.6 us (4.6 TB/s), backward 22.5 (5.2 TB/s, part of it from
+// the cache).  4 x 1999 x 2000 bf16: forward 45 us and 18 for the maps, backward 72 and 18;
+// a prompt of 8192 x 1024 bf16: 26 and 15.  There the vector unit is busy half of the time,
+// and fewer or more waves, or loads a chunk earlier, change nothing.
 //
 // An episode start is a flag beside the product of decays, not a factor of zero:
 // what is before it may be infinite.  Chunks without one, and inside the sequence,
@@ -29,13 +34,14 @@ struct Rows {
 };
 struct GatedView {
     int B, T, C, tiles, nseg, seg;  // segments, and steps of one
+    int maps, span;                 // maps of a sequence, and the steps of one: a segment's or a part's of it
     Rows x, ga, gx, dy;
     const float *a_log, *state, *dstate_out, *marks_in;
     const uint8_t* reset;
     void *y, *dx, *dga, *dgx;
     float *state_out, *marks, *dstate;
     float* state_copy;     // [B][C] where there are segments: state_out may be state
-    float *seg_a, *seg_h;  // [B][nseg][C]: product of decays (negative: an episode starts in the segment), end
+    float *map_a, *map_h;  // [B][maps][C]: product of decays (negative: an episode starts there), end
     float* parts;          // [items][C] of da_log
     int items;             // workgroups that share a tile's sequences and segments
 };
@@ -186,43 +192,47 @@ __device__ __forceinline__ uint32_t cuts_of(const int (&cut)[W], int lane) {
 }
 __device__ __forceinline__ Two two(float2 v) { return {{v.x, v.y}}; }
 
-// What enters segment `seg` of the segments before it (behind it).
+// What maps first, first + step, .. (count of them) make of what enters the first of them: eight
+// are read at a time.
 template <bool PAIR>
-__device__ __forceinline__ void pass(Two& carry, const GatedView& v, int64_t b, int seg, const Place& at) {
-    const int64_t from = (b * v.nseg + seg) * v.C + at.c;
-    const Two a = get2<PAIR>(v.seg_a + from, at.second), h = get2<PAIR>(v.seg_h + from, at.second);
+__device__ __forceinline__ void pass(Two& carry, const GatedView& v, int64_t b, int first, int step, int count, const Place& at) {
+    constexpr int AHEAD = 8;
+    for (int m = 0; m < count; m += AHEAD) {
+        Two a[AHEAD], h[AHEAD];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) carry[j] = a[j] < 0.0f ? h[j] : fmaf(a[j], carry[j], h[j]);
+        for (int k = 0; k < AHEAD; ++k) {
+            const int64_t from = (b * v.maps + first + (m + k < count ? m + k : m) * step) * v.C + at.c;
+            a[k] = get2<PAIR>(v.map_a + from, at.second), h[k] = get2<PAIR>(v.map_h + from, at.second);
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (m + k < count)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) carry[j] = a[k][j] < 0.0f ? h[k][j] : fmaf(a[k][j], carry[j], h[k][j]);
+    }
 }
 template <bool PAIR>
-__device__ __forceinline__ void put_segment(const GatedView& v, int64_t b, int seg, Two prod, bool cut, Two end, const Place& at) {
-    const int64_t to = (b * v.nseg + seg) * v.C + at.c;
+__device__ __forceinline__ void put_map(const GatedView& v, int64_t b, int m, Two prod, bool cut, Two end, const Place& at) {
+    const int64_t to = (b * v.maps + m) * v.C + at.c;
     if (cut) prod = {{-1.0f, -1.0f}};
-    put2<PAIR>(v.seg_a + to, prod, at.n);
-    put2<PAIR>(v.seg_h + to, end, at.n);
+    put2<PAIR>(v.map_a + to, prod, at.n);
+    put2<PAIR>(v.map_h + to, end, at.n);
 }
 
 // Forward.  A workgroup of W waves walks the chunks of one segment of 64 channels.
-// AGG: the segment's map alone, for the workgroups of the segments behind it.
+// AGG: the map of a segment, or of a part of one, alone, for the segments behind it.
 template <class T, bool PAIR, int W, int S, bool AGG>
 __global__ __launch_bounds__(64 * W) void gated_kernel(GatedView v) {
     constexpr int CHUNK = 2 * S * W;
     __shared__ Shared<W, 1> sh[2];
-    const int tile = blockIdx.x % v.tiles, item = blockIdx.x / v.tiles, seg = item % v.nseg;
-    const int64_t b = item / v.nseg;
-    if (AGG && seg == v.nseg - 1) return;
+    const int count = AGG ? v.maps : v.nseg, steps = AGG ? v.span : v.seg;
+    const int tile = blockIdx.x % v.tiles, item = blockIdx.x / v.tiles, seg = item % count;
+    const int64_t b = item / count;
     const Place at(v, tile);
-    const int begin = seg * v.seg, end = begin + v.seg < v.T ? begin + v.seg : v.T;
+    const int begin = seg * steps, end = begin + steps < v.T ? begin + steps : v.T;
     const Two rate2 = at.rate2<PAIR>(v);
     Two carry{{0.0f, 0.0f}}, prod{{1.0f, 1.0f}};
     uint32_t cut = 0;
-    if (AGG) {
-        if (seg == 0 && threadIdx.x < 32) put2<PAIR>(v.state_copy + b * v.C + at.c, v.state ? get2<PAIR>(v.state + b * v.C + at.c, at.second) : carry, at.n);
-    } else {
-        const float* from = v.nseg > 1 ? v.state_copy : v.state;
-        if (from) carry = get2<PAIR>(from + b * v.C + at.c, at.second);
-        for (int s = 0; s < seg; ++s) pass<PAIR>(carry, v, b, s, at);
-    }
     Stream<T, PAIR, S> x(v.x, b, begin, at), ga(v.ga, b, begin, at), gx(v.gx, b, begin, at);
     int reset = 0;
     auto fetch_all = [&](int t0) {
@@ -239,6 +249,13 @@ __global__ __launch_bounds__(64 * W) void gated_kernel(GatedView v) {
         x.move(CHUNK), ga.move(CHUNK), gx.move(CHUNK);
     };
     if (begin < end) fetch_all(begin);
+    if (AGG) {
+        if (seg == 0 && threadIdx.x < 32) put2<PAIR>(v.state_copy + b * v.C + at.c, v.state ? get2<PAIR>(v.state + b * v.C + at.c, at.second) : carry, at.n);
+    } else {
+        const float* from = v.nseg > 1 ? v.state_copy : v.state;
+        if (from) carry = get2<PAIR>(from + b * v.C + at.c, at.second);
+        if (v.nseg > 1) pass<PAIR>(carry, v, b, 0, 1, begin / v.span, at);
+    }
     for (int t0 = begin, turn = 0; t0 < end; t0 += CHUNK, turn ^= 1) {
         const uint32_t mask = starts(reset), own = at.half ? mask >> S : mask & ((1u << S) - 1);
         const int t = t0 + (at.wave * 2 + at.half) * S;
@@ -314,7 +331,7 @@ __global__ __launch_bounds__(64 * W) void gated_kernel(GatedView v) {
         }
     }
     if (threadIdx.x >= 32) return;
-    if (AGG) put_segment<PAIR>(v, b, seg, prod, cut != 0, carry, at);
+    if (AGG) put_map<PAIR>(v, b, seg, prod, cut != 0, carry, at);
     else if (seg == v.nseg - 1 && v.state_out) put2<PAIR>(v.state_out + b * v.C + at.c, carry, at.n);
 }
 
@@ -384,7 +401,7 @@ __global__ __launch_bounds__(64 * W) void gated_back_kernel(GatedView v) {
         if (cuts == 0) over_waves(0);
         else over_waves(cuts);
     }
-    if (threadIdx.x < 32) put_segment<PAIR>(v, b, seg, prod, cut != 0, carry, at);
+    if (threadIdx.x < 32) put_map<PAIR>(v, b, seg, prod, cut != 0, carry, at);
 }
 
 // Backward: with R_t = dy_t + a_{t+1} R_{t+1},
@@ -408,26 +425,30 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
         const int begin = seg * v.seg, end = begin + v.seg < v.T ? begin + v.seg : v.T;
         Two carry{{0.0f, 0.0f}};
         if (v.dstate_out) carry = get2<PAIR>(v.dstate_out + b * v.C + at.c, at.second);
-        for (int s = v.nseg - 1; s > seg; --s) pass<PAIR>(carry, v, b, s, at);
+        pass<PAIR>(carry, v, b, v.nseg - 1, -1, v.nseg - 1 - seg, at);
         if (end <= begin) {  // no steps: what comes in goes out
             if (seg == 0 && v.dstate && threadIdx.x < 32) put2<PAIR>(v.dstate + b * v.C + at.c, carry, at.n);
             continue;
         }
         const int first = begin + (end - begin - 1) / CHUNK * CHUNK;
         Stream<T, PAIR, S> x(v.x, b, first, at), ga(v.ga, b, first, at), gx(v.gx, b, first, at), dy(v.dy, b, first, at);
+        // The gates' loads are a chunk ahead: their registers are free once decays are formed, which hides the others'.
+        auto fetch_two = [&](Stream<T, PAIR, S>& p, Stream<T, PAIR, S>& q, int t0) {
+            const int left = end - t0 - (at.wave * 2 + at.half) * S;
+            if (t0 + CHUNK <= end) {
+                p.template fetch<true>(left, at.second);
+                q.template fetch<true>(left, at.second);
+            } else {
+                p.template fetch<false>(left, at.second);
+                q.template fetch<false>(left, at.second);
+            }
+            p.move(-CHUNK), q.move(-CHUNK);
+        };
+        fetch_two(ga, gx, first);
         for (int t0 = first; t0 >= begin; t0 -= CHUNK, turn ^= 1) {
             const int t = t0 + (at.wave * 2 + at.half) * S;
             const int reset = start_of<S>(v, b, t0 + at.wave * 2 * S, end, at.lane);
-            auto fetch_all = [&](auto full) {
-                constexpr bool FULL = decltype(full)::value;
-                ga.template fetch<FULL>(end - t, at.second);
-                gx.template fetch<FULL>(end - t, at.second);
-                x.template fetch<FULL>(end - t, at.second);
-                dy.template fetch<FULL>(end - t, at.second);
-            };
-            if (t0 + CHUNK <= end) fetch_all(std::true_type{});
-            else fetch_all(std::false_type{});
-            x.move(-CHUNK), ga.move(-CHUNK), gx.move(-CHUNK), dy.move(-CHUNK);
+            fetch_two(x, dy, t0);
             const int group = t0 + at.wave / GROUP * MARK;  // the mark's step, if it exists
             Two now = get2<PAIR>(v.marks_in + (b * ((v.T + MARK - 1) / MARK) + (group < end ? group : t0) / MARK) * v.C + at.c, at.second);
             const uint32_t mask = starts(reset), own = at.half ? mask >> S : mask & ((1u << S) - 1);
@@ -438,7 +459,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
                 constexpr bool PLAIN = decltype(simple)::value;
 #pragma unroll
                 for (int k = 0; k < S; ++k) {
-                    const Two xv = x.r[k].get(), gav = ga.r[k].get(), gxv = gx.r[k].get();
+                    const Two gav = ga.r[k].get(), gxv = gx.r[k].get();
                     const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
@@ -447,6 +468,14 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
                         const Decay d = decay(-rate2[j] * r[k][j]);
                         a[k][j] = in ? d.a : 1.0f;
                         bb[k][j] = !in ? 0.0f : start ? 1.0f : d.b;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < S; ++k) {
+                    const Two xv = x.r[k].get();
+                    const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
                         const float u = in ? bb[k][j] * i[k][j] * xv[j] : 0.0f;
                         F[j] = start ? u : fmaf(a[k][j], F[j], u);
                         A[j] *= a[k][j];
@@ -462,6 +491,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
             };
             if (plain) runs(std::true_type{});
             else runs(std::false_type{});
+            if (t0 > begin) fetch_two(ga, gx, t0 - CHUNK);
             const Two oa = other_half(A), of = other_half(F), oh = other_half(H);
             Two back = carry;
             if (W > 1) {
@@ -579,32 +609,42 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedView v, float* poo
 
 // ---- host ----
 
-constexpr int CUT_BELOW = 128;  // workgroups (a sequence's tile each) below which forward calls are cut,
-constexpr int FULL = 256;       // and how many fill the chip
-constexpr int BACK_FULL = 512;  // the same backward, where the cut's own pass is cheap
-constexpr int LEAST_SEG = 256;  // steps of a segment at least
+constexpr int FULL = 256;       // workgroups of eight waves that fill the chip forward (512 need a longer pass
+                                // for the maps: 4 x 1999 x 2000 bf16 46 + 29 us, 256 45 + 19),
+constexpr int BACK_FULL = 512;  // of four backward, where the maps are cheap
+constexpr int LEAST_SEG = 256;  // steps of a segment, or of a map, at least
 constexpr int MAX_SEG = 64;     // segments of a sequence at most
 constexpr int WALKS = 2048;     // workgroups of the backward at most: each adds a part of da_log
 
+// Sequences whose tiles leave the chip idle are cut into segments.  Forward the maps of all
+// but the last are formed first, in parts of a segment, so that the whole chip has a
+// share of them.  (4 x 1999 x 2000 bf16, 128 tiles: uncut 65 us, cut 45 + 18; with fewer
+// tiles the cut gains.)
 struct Cut {
-    int tiles, nseg = 1, seg;
+    int tiles, nseg = 1, seg, maps = 0, span;
     Cut(int64_t B, int T, int C, bool backward) {
         tiles = (C + TILE - 1) / TILE;
-        seg = T > 0 ? T : 1;
+        seg = span = T > 0 ? T : 1;
         const int64_t have = B * tiles, full = backward ? BACK_FULL : FULL, most = (T + LEAST_SEG - 1) / LEAST_SEG;
-        if (have < 1 || have >= (backward ? BACK_FULL : CUT_BELOW)) return;
+        if (have < 1 || have >= full) return;
         int64_t k = (full + have - 1) / have;
         k = k < most ? k : most;
         k = k < MAX_SEG ? k : MAX_SEG;
         if (k < 2) return;
-        seg = (int)(((T + k - 1) / k + LEAST_SEG - 1) / LEAST_SEG * LEAST_SEG);
-        nseg = (T + seg - 1) / seg;
+        seg = span = (int)(((T + k - 1) / k + LEAST_SEG - 1) / LEAST_SEG * LEAST_SEG);
+        nseg = maps = (T + seg - 1) / seg;
+        if (backward || nseg < 2) return;
+        int64_t parts = BACK_FULL / (have * (nseg - 1));
+        if (parts > seg / LEAST_SEG) parts = seg / LEAST_SEG;
+        while (parts > 1 && seg % (parts * LEAST_SEG)) --parts;
+        if (parts > 1) span = (int)(seg / parts);
+        maps = (nseg - 1) * (seg / span);
     }
 };
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// Bytes of the workspace: the segments' maps and the states before the first (cut
-// calls have B * tiles < BACK_FULL, so B * nseg < 2 BACK_FULL / tiles), then the parts.
+// Bytes of the workspace: the maps and the states before the first step (cut calls
+// have B * tiles < BACK_FULL, so B * maps < 2 BACK_FULL / tiles), then the parts.
 struct Plan {
     size_t maps, states, parts, total;
     Plan(int T, int C, bool backward) {
@@ -644,19 +684,19 @@ int gated_view(const gorila_gated_scan_args* a, bool step, GatedView& v, bool& v
 
 // Waves a workgroup, of 16 steps each (a wave in which T ends, or a mark's four and more): forward two
 // chunks or more where there are as many steps, so that loads are under way while a
-// chunk is joined (32 x 128 x 1024 fp32: 14.6 us; one chunk of eight waves: 18.4).  Backward a lane
-// has 216 registers, and more waves than two a SIMD do not pay: 8 steps a lane and four
-// waves 22.7 us (5.2 TB/s), eight waves 27.6; 4 steps and eight waves, half of the registers, 26.2.
+// chunk is joined (32 x 128 x 1024 fp32: 14.6 us; one chunk of eight waves: 18.4).  Sixteen waves
+// are no faster on long sequences.  Backward a lane has 222 registers, and more waves than two a
+// SIMD do not pay: 8 steps a lane and four waves 22.7 us (5.2 TB/s), eight waves 27.6; 4 steps
+// and eight waves, half of the registers, 26.2.
 constexpr int S = 8;
-int forward_waves(int T) { return T <= 16 ? 1 : T <= 128 ? 4 : T <= 256 ? 8 : 16; }
+int forward_waves(int T) { return T <= 16 ? 1 : T <= 128 ? 4 : 8; }
 int backward_waves(int T) { return T <= 16 ? 1 : 4; }
 template <class F>
 void by_waves(int waves, F&& f) {
     using std::integral_constant;
     if (waves == 1) f(integral_constant<int, 1>{});
     else if (waves == 4) f(integral_constant<int, 4>{});
-    else if (waves == 8) f(integral_constant<int, 8>{});
-    else f(integral_constant<int, 16>{});
+    else f(integral_constant<int, 8>{});
 }
 
 template <class F>
@@ -694,13 +734,13 @@ int gorila_gated_scan(const gorila_gated_scan_args* args, void* y, float* state_
     if (!launch_fits(blocks, 64 * waves)) return GORILA_EUNSUPPORTED;
     if ((rc = ctx_view(ctx, k.nseg > 1 ? p.total : 0, c))) return rc;
     vec = vec && at_element(y, 2 * e) && at_element(state_out, 8) && at_element(marks, 8);
-    v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg;
+    v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg, v.maps = k.maps, v.span = k.span;
     v.y = y, v.state_out = state_out, v.marks = marks;
-    if (k.nseg > 1) v.seg_a = (float*)c.ws, v.seg_h = (float*)(c.ws + p.maps), v.state_copy = (float*)(c.ws + 2 * p.maps);
+    if (k.nseg > 1) v.map_a = (float*)c.ws, v.map_h = (float*)(c.ws + p.maps), v.state_copy = (float*)(c.ws + 2 * p.maps);
     by_rows(args->dtype, vec, [&](auto t, auto al) {
         using T = decltype(t);
         constexpr bool VEC = decltype(al)::value;
-        if (k.nseg > 1) gated_kernel<T, VEC, 16, S, true><<<(unsigned)blocks, 1024, 0, c.stream>>>(v);
+        if (k.nseg > 1) gated_kernel<T, VEC, 8, S, true><<<(unsigned)(v.B * k.maps * k.tiles), 512, 0, c.stream>>>(v);
         by_waves(waves, [&](auto w) {
             constexpr int W = decltype(w)::value;
             gated_kernel<T, VEC, W, S, false><<<(unsigned)blocks, 64 * W, 0, c.stream>>>(v);
@@ -733,12 +773,12 @@ int gorila_gated_scan_backward(const gorila_gated_scan_args* args, const float* 
     vec = vec && !((dy_batch_stride | dy_step_stride) & 1);
     for (const void* p : {dy, (const void*)dx, (const void*)dgate_a, (const void*)dgate_x}) vec = vec && at_element(p, 2 * e);
     for (const float* p : {marks, dstate_out, (const float*)dstate}) vec = vec && at_element(p, 8);
-    v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg;
+    v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg, v.maps = k.maps, v.span = k.span;
     const int64_t items = (int64_t)v.B * k.nseg;
     v.items = (int)(items < Plan::walks(k.tiles) ? items : Plan::walks(k.tiles));
     v.dy = {dy, dy_batch_stride, dy_step_stride};
     v.marks_in = marks, v.dstate_out = dstate_out, v.dx = dx, v.dga = dgate_a, v.dgx = dgate_x, v.dstate = dstate;
-    v.seg_a = (float*)c.ws, v.seg_h = (float*)(c.ws + p.maps), v.parts = (float*)(c.ws + 2 * p.maps + p.states);
+    v.map_a = (float*)c.ws, v.map_h = (float*)(c.ws + p.maps), v.parts = (float*)(c.ws + 2 * p.maps + p.states);
     if (items > 0)
         by_rows(args->dtype, vec, [&](auto t, auto al) {
             using T = decltype(t);
