@@ -369,8 +369,9 @@ int gorila_ps_apply(float* theta_plus, float* accum, int64_t n, const float* gra
  *  - Calls that use the workspace say so; after them the values behind
  *    gorila_learner_td are gone.
  *  - Sizes that a launch cannot hold (2^32 lanes; a norm's row has 64 or more, a
- *    scan's (sequence, head, 64 channels) 512, a step's four channels one) and
- *    lengths above 2^30: GORILA_EUNSUPPORTED.
+ *    scan's (sequence, head, 64 channels) 512, a gated scan's (sequence, 64 channels)
+ *    64 to 512, a step's four channels one) and lengths above 2^30:
+ *    GORILA_EUNSUPPORTED.
  *  - Zero rows, sequences or steps are a no-op that still writes the outputs that
  *    have elements (a carried state, zero parameter gradients). */
 
@@ -415,8 +416,8 @@ int gorila_add_rmsnorm_backward(const void* dy, int64_t dy_stride, const void* d
  * leaves, so that a row's common offset costs no more than its own values' rounding.
  * mean, rstd [rows] = mu, rho fp32; total, mean and rstd may be NULL.  EINVAL for
  * eps < 0.  Sums and squares are fp32: values whose sum is past its range make the
- * row NaN, deviations from about 2^63 on give rho 0.  A row of equal values is bias
- * (NaN where eps is 0). */
+ * row NaN, deviations from about 2^63 on give rho 0.  A row of equal values has no
+ * deviations, and y = bias, to what sqrt(1 / eps) makes of its values' rounding. */
 int gorila_add_layernorm(const void* x, int64_t x_stride, const void* residual,
                          int64_t residual_stride, const float* weight, const float* bias,
                          int64_t rows, int32_t width, int32_t dtype, float eps, void* y,
@@ -589,7 +590,7 @@ int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_
  *   (to fp32's precision).
  * `tensors` is a HOST array, read before the call returns; what its members point to is
  * on the device.  Elements are contiguous; grad is of grad_dtype (GORILA_F32 or
- * GORILA_BF16).  No two tensors of a call may overlap.  Any alignment of the element
+ * GORILA_BF16).  Nothing that a call writes may overlap anything else of it.  Any alignment of the element
  * types is accepted, 16 bytes (bf16 gradients: 8, codes: 4) is faster.
  *
  * state_bits 32: m and v are fp32 [n].  state_bits 8: m and v are codes u8 [n], and
@@ -653,7 +654,8 @@ int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float
  * above 0, or NaN: 0; 1 and more: the last).  All sums are of whole numbers, so no order of
  * addition shows.  probability_out (may be NULL) [rows] fp32: w / S.  A row without a value
  * above -infinity has action -1 and probability 0.
- * More than 2^20 actions: GORILA_EUNSUPPORTED.  Needs no workspace; few rows of more than
+ * More than 2^20 actions, and rows that a launch cannot hold (64 lanes each up to 64
+ * actions, 256 up to 2048, else 1024): GORILA_EUNSUPPORTED.  Needs no workspace; few rows of more than
  * 16384 actions are faster where the context has one (66 KB a row; the result is the
  * same, and the call then counts as one that uses it). */
 int gorila_sample_actions(const void* values, int64_t stride, int64_t rows, int32_t actions,

@@ -520,29 +520,35 @@ struct Listed {  // a list or tuple; it must outlive what is taken from it
         return THPVariable_Unpack((*this)[i]);
     }
 };
-struct Written {  // bytes that a call writes
-    std::vector<std::pair<const char*, const char*>> spans;
-    void add(const void* p, int64_t bytes) {
-        if (bytes > 0) spans.emplace_back((const char*)p, (const char*)p + bytes);
+struct Spans {  // bytes that a call writes, and others that it reads
+    typedef std::pair<const char*, const char*> Span;
+    std::vector<Span> written, read;
+    static void add(std::vector<Span>& to, const void* p, int64_t bytes) {
+        if (bytes > 0) to.emplace_back((const char*)p, (const char*)p + bytes);
     }
+    void write(const void* p, int64_t bytes) { add(written, p, bytes); }
     void check() {
-        std::sort(spans.begin(), spans.end());
-        for (size_t i = 1; i < spans.size(); ++i) want(spans[i].first >= spans[i - 1].second, "tensors and states must not overlap");
+        std::sort(written.begin(), written.end());
+        for (size_t i = 1; i < written.size(); ++i) want(written[i].first >= written[i - 1].second, "tensors and states must not overlap");
+        for (const Span& r : read) {  // the last written one that starts before its end
+            const auto w = std::lower_bound(written.begin(), written.end(), Span(r.second, nullptr));
+            if (w != written.begin()) want((w - 1)->second <= r.first, "gradients must not overlap tensors and states");
+        }
     }
 };
 // m and v of a state, and its scales where it has four members (8 bits).
-int state_of(const Call& c, PyObject* state, c10::IntArrayRef shape, int64_t n, gorila_adamw_tensor& t, Written& w) {
+int state_of(const Call& c, PyObject* state, c10::IntArrayRef shape, int64_t n, gorila_adamw_tensor& t, Spans& w) {
     const Listed s(state, "a state");
     want(s.n == 2 || s.n == 4, "a state is (m, v), or (m, v, m_scale, v_scale) in 8 bits");
     const auto typ = s.n == 2 ? F32 : at::kByte;
     const int64_t bytes = s.n == 2 ? 4 : 1, groups = (n + 255) / 256;
     t.m = c.at(s.tensor(0, "a state"), "m", shape, typ);
     t.v = c.at(s.tensor(1, "a state"), "v", shape, typ);
-    w.add(t.m, n * bytes), w.add(t.v, n * bytes);
+    w.write(t.m, n * bytes), w.write(t.v, n * bytes);
     if (s.n == 4) {
         t.m_scale = (float*)c.at(s.tensor(2, "a state"), "m_scale", {groups}, F32);
         t.v_scale = (float*)c.at(s.tensor(3, "a state"), "v_scale", {groups}, F32);
-        w.add(t.m_scale, groups * 4), w.add(t.v_scale, groups * 4);
+        w.write(t.m_scale, groups * 4), w.write(t.v_scale, groups * 4);
     }
     return s.n == 2 ? 32 : 8;
 }
@@ -556,7 +562,7 @@ PyObject* adamw(PyObject* const* args, Py_ssize_t n) {
     if (each) want(PySequence_Fast_GET_SIZE(args[11]) == thetas.n, "decay must be a number, or one for each tensor");
     const float all = each ? 0.0f : c.number(11);
     std::vector<gorila_adamw_tensor> ts((size_t)thetas.n);
-    Written w;
+    Spans w;
     int bits = 32;
     int32_t dtype = GORILA_F32;
     for (Py_ssize_t i = 0; i < thetas.n; ++i) {
@@ -567,7 +573,8 @@ PyObject* adamw(PyObject* const* args, Py_ssize_t n) {
         t.theta = (float*)c.at(theta, "theta", theta.sizes(), F32);
         const int32_t d = row_type(grad);
         t.grad = c.at(grad, "grad", theta.sizes(), grad.scalar_type());
-        w.add(t.theta, t.n * 4);
+        w.write(t.theta, t.n * 4);
+        Spans::add(w.read, t.grad, t.n * (d == GORILA_F32 ? 4 : 2));
         const int b = state_of(c, states[i], theta.sizes(), t.n, t, w);
         if (i == 0) bits = b, dtype = d;
         want(b == bits && d == dtype, "all states have the same bits and all gradients the same type");
@@ -579,12 +586,16 @@ PyObject* adamw(PyObject* const* args, Py_ssize_t n) {
         }
     }
     double* clock = (double*)c.at(c.tensor(6, "clock"), "clock", {3}, at::kDouble);
-    w.add(clock, 24);
+    w.write(clock, 24);
     w.check();
     const Tensor* keep = c.maybe(13, "keep");
     const uint8_t* pk = keep ? (const uint8_t*)c.at(keep, "keep", {1}, at::kByte) : nullptr;
     c.check(api.adamw(ts.data(), size32(thetas.n), dtype, bits, clock, pk, c.number(7), c.real(8), c.real(9), c.number(10), c.bits(12), c.ctx),
             "gorila_adamw");
+    for (Py_ssize_t i = 0; i < thetas.n; ++i) {  // as every update in place does, for graphs that still need the old values
+        const Tensor& theta = thetas.tensor(i, "thetas");
+        if (!theta.is_inference()) theta.unsafeGetTensorImpl()->bump_version();
+    }
     Py_RETURN_NONE;
 }
 
@@ -595,12 +606,14 @@ PyObject* adamw_values(PyObject* const* args, Py_ssize_t n) {
     std::vector<gorila_adamw_tensor> ts((size_t)states.n);
     std::vector<Tensor> m, v;
     std::vector<float*> pm, pv;
-    Written w;
+    Spans w;
     for (Py_ssize_t i = 0; i < states.n; ++i) {
-        const Tensor& first = Listed(states[i], "a state").n > 0 ? Listed(states[i], "a state").tensor(0, "a state") : Tensor();
+        const Listed state(states[i], "a state");
+        want(state.n == 4, "the states must be held in 8 bits");
+        const Tensor& first = state.tensor(0, "a state");
         ts[(size_t)i] = gorila_adamw_tensor{};
-        ts[(size_t)i].n = first.defined() ? first.numel() : 0;
-        want(state_of(c, states[i], first.sizes(), ts[(size_t)i].n, ts[(size_t)i], w) == 8, "the states must be held in 8 bits");
+        ts[(size_t)i].n = first.numel();
+        state_of(c, states[i], first.sizes(), ts[(size_t)i].n, ts[(size_t)i], w);
         m.push_back(make(first.sizes(), first, F32)), v.push_back(make(first.sizes(), first, F32));
         pm.push_back((float*)ptr(m.back())), pv.push_back((float*)ptr(v.back()));
     }

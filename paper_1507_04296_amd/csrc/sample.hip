@@ -227,6 +227,7 @@ struct Row {
     }
     __device__ __forceinline__ int action(int part, int j) const { return part * 256 + lane * 4 + j - shift; }
     __device__ __forceinline__ bool inside(int action) const { return action >= 0 && action < n; }
+    __device__ __forceinline__ bool whole(int part) const { return part * 256 >= shift && part * 256 + 256 - shift <= n; }
     // As it is read (outside the row: -infinity), and as values.
     __device__ __forceinline__ f32x4 load(int part) const {
         const int first = action(part, 0);
@@ -330,16 +331,26 @@ __device__ __forceinline__ uint64_t block_sum(S& sh, uint64_t v) {
     return v;
 }
 
-// A wave's values into a histogram of numbers (COUNT) or of weights.
+// A wave's values into a histogram of numbers (COUNT) or of weights.  Lanes that meet in an
+// address wait for each other: a wave in one bin adds once, and numbers in the last bin, where
+// all that is far below the largest value lies, are counted over the wave.
 template <int BINS, bool COUNT, class R, class W, class I>
 __device__ __forceinline__ void add_to_bins(const R& r, f32x4 v, int part, float most, float per, W&& weigh, I* bins) {
     uint64_t w[4];
+    const bool whole = r.whole(part);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = COUNT ? r.inside(r.action(part, j)) : weigh(v[j]);
+    for (int j = 0; j < 4; ++j) w[j] = COUNT ? whole || r.inside(r.action(part, j)) : weigh(v[j]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int b = bin_of<BINS>(v[j], most, per);
-        if (__all(b == __builtin_amdgcn_readfirstlane(b))) {  // a wave's values in one bin: one addition
+        if (COUNT) {
+            const uint64_t far = __ballot(w[j] && b == BINS - 1);
+            if (far) {
+                if (r.lane == 0) atomicAdd(bins + BINS - 1, (I)__popcll(far));
+                if (b == BINS - 1) w[j] = 0;
+            }
+        }
+        if (__all(b == __builtin_amdgcn_readfirstlane(b))) {
             const uint64_t s = COUNT ? __popcll(__ballot(w[j] != 0)) : wave_sum(w[j]);
             if (r.lane == 0 && s) atomicAdd(bins + b, (I)s);
         } else if (w[j]) {
@@ -351,22 +362,33 @@ __device__ __forceinline__ void add_to_bins(const R& r, f32x4 v, int part, float
 template <int BINS, int LIST, class R>
 __device__ __forceinline__ void add_to_list(const R& r, f32x4 v, int part, float most, float per, int first, int last, uint32_t* listed,
                                             uint32_t* key, uint32_t* act) {
+    bool is[4], any = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {  // as bin_of() says; what is no number is in the last bin
+        const float d = v[j] == most ? 0.0f : (most - v[j]) * per;
+        is[j] = last == BINS - 1 ? !(d < (float)first) : d >= (float)first && d < (float)(last + 1);
+    }
+    if (!r.whole(part)) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) is[j] = is[j] && r.inside(r.action(part, j));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) any = any || is[j];
+    if (!__any(any)) return;
     uint64_t who[4];
     int all = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int b = bin_of<BINS>(v[j], most, per);
-        who[j] = __ballot(b >= first && b <= last && r.inside(r.action(part, j)));
+        who[j] = __ballot(is[j]);
         all += __popcll(who[j]);
     }
-    if (all == 0) return;
     uint32_t base = 0;
     if (r.lane == 0) base = atomicAdd(listed, (uint32_t)all);
     base = __builtin_amdgcn_readfirstlane(base);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t at = base + __popcll(who[j] & ((1ull << r.lane) - 1));
-        if (who[j] >> r.lane & 1 && at < (uint32_t)LIST) key[at] = key_of(v[j]), act[at] = r.action(part, j);
+        const uint32_t at = base + __builtin_amdgcn_mbcnt_hi((uint32_t)(who[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who[j], 0));
+        if (is[j] && at < (uint32_t)LIST) key[at] = key_of(v[j]), act[at] = r.action(part, j);
         base += __popcll(who[j]);
     }
 }
@@ -810,8 +832,8 @@ int gorila_sample_actions(const void* values, int64_t stride, int64_t rows, int3
             sample_wave_kernel<T><<<(unsigned)((rows + 3) / 4), 256, 0, c.stream>>>(a);
         } else if (threads == 256) {
             sample_row_kernel<T, 256, 1, 512, 1024, 2048, WHOLE><<<(unsigned)rows, 256, 0, c.stream>>>(a, nullptr, 0);
-        } else if (actions <= 16384) {
-            sample_row_kernel<T, 1024, 1, 2048, 4096, 16384, WHOLE><<<(unsigned)rows, 1024, 0, c.stream>>>(a, nullptr, 0);
+        } else if (actions <= 65536 && !shared) {
+            sample_row_kernel<T, 1024, 1, 2048, 4096, 65536, WHOLE><<<(unsigned)rows, 1024, 0, c.stream>>>(a, nullptr, 0);
         } else if (shared) {
             RowSpace* space = (RowSpace*)c.ws;
             const unsigned blocks = (unsigned)(rows * shares);

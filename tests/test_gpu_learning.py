@@ -501,6 +501,18 @@ def test_adamw_extreme_gradients(g, ctx, bits):
         assert states[0][2].isnan().tolist() == [False] * 5 + [True] == states[0][3].isnan().tolist()
 
 
+def test_adamw_is_a_change_for_autograd(g, ctx):
+    """A tensor that a graph still needs is known to have changed, as by any update in place; one gradient may serve two tensors."""
+    theta, grad = torch.ones(10, device="cuda", requires_grad=True), rand(10, seed=1)
+    loss = (theta * theta).sum()
+    states = g.adamw_state([theta])
+    other = torch.ones(10, device="cuda")
+    g.adamw(ctx, [theta, other], [grad, grad], states + g.adamw_state([other]), g.adamw_clock(), 0.1)
+    assert torch.equal(theta.detach(), other)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
 def test_adamw_keep_and_no_tensors(g, ctx):
     thetas, grads = adamw_inputs([700], 8)
     states, clock = g.adamw_state(thetas, 8), g.adamw_clock()
@@ -582,6 +594,7 @@ def test_adamw_refusals(g, ctx):
     bad(ValueError, "overlap", [thetas[0], thetas[0].clone()], [grads[0]] * 2, [states[0], states[0]], clock, 0.1)
     bad(ValueError, "same bits", thetas, grads, [states[0], g.adamw_state(thetas, 8)[1]], clock, 0.1)
     bad(ValueError, "same type", thetas, [grads[0], grads[1].bfloat16()], states, clock, 0.1)
+    bad(ValueError, "overlap", thetas, [states[0][0], grads[1]], states, clock, 0.1)
     bad(ValueError, "grad must have shape", thetas, [grads[0], grads[0]], states, clock, 0.1)
     bad(ValueError, "decay", thetas, grads, states, clock, 0.1, decay=[0.1])
     bad(TypeError, "clock", thetas, grads, states, clock.float(), 0.1)
@@ -677,6 +690,31 @@ def test_sample_many_actions(g, ctx):
     for x in (0.0, 0.25, 0.9999999):
         action, p = g.sample_actions(ctx, big, torch.tensor([x], device="cuda"))
         assert int(action) == int(np.float32(x) * np.float64(1 << 20)) and float(p) == 2.0 ** -20
+
+
+@pytest.mark.parametrize("actions", [9000, 40000])
+@pytest.mark.parametrize("kind", ["equal", "two", "close", "spread"])
+def test_sample_of_long_rows_that_no_list_holds(g, ctx, actions, kind):
+    """More values at a border than the list of a row holds, large top_k, settings that leave one value or all; shared
+    rows (a workspace) and whole ones (none) agree."""
+    rows = 6
+    values, u, _ = sample_inputs(rows, actions, "", seed=80)
+    if kind == "equal":
+        values[:] = 0.25
+    elif kind == "two":
+        values = torch.where(values > 0, 1.0, -1.0)
+    elif kind == "close":
+        values = 1.0 + 1e-6 * values
+    bare = g.Context(0, 1)
+    k = torch.tensor([1, 2, actions // 2, actions - 1, actions, 5000], dtype=torch.int32, device="cuda")
+    p = torch.tensor([0.999, 0.5, 0.25, 1.0, 1e-7, 0.75], device="cuda")
+    t = torch.tensor([1.0, INF, 0.0, 1e-3, 50.0, 1.0], device="cuda")
+    for options in ({}, dict(top_k=k), dict(top_p=p), dict(top_k=k, top_p=p), dict(top_k=k, top_p=p, temperature=t, min_p=0.5 * p),
+                    dict(top_p=p, temperature=t)):
+        check_sample(g, ctx, values, u, options)
+        for a, b in zip(g.sample_actions(ctx, values, u, **options), g.sample_actions(bare, values, u, **options)):
+            assert torch.equal(a, b)
+    bare.close()
 
 
 @pytest.mark.parametrize("actions", [5, 300])
