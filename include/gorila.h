@@ -656,7 +656,7 @@ int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float
  * above -infinity has action -1 and probability 0.
  * More than 2^20 actions, and rows that a launch cannot hold (64 lanes each up to 64
  * actions, 256 up to 2048, else 1024): GORILA_EUNSUPPORTED.  Needs no workspace; few rows of more than
- * 16384 actions are faster where the context has one (66 KB a row; the result is the
+ * 16384 actions are faster where the context has one (90 KB a row; the result is the
  * same, and the call then counts as one that uses it). */
 int gorila_sample_actions(const void* values, int64_t stride, int64_t rows, int32_t actions,
                           int32_t dtype, const float* u, const float* temperature,

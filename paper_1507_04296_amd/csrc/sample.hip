@@ -19,11 +19,11 @@
 // What bounds a workgroup: a weight is some 25 operations in fp64, of 10 cycles each
 // as measured, so 32000 of them take it 13 us.  They are formed once for every value (top_p's
 // histogram) and once more for those that stay; under top_k for those alone.
-// 256 x 32000 bf16: 25 us without a filter, 30 with top_k, 58 with top_p, 34 with both.
+// 256 x 32000 bf16: 22 us without a filter, 29 with top_k, 55 with top_p, 31 with both.
 //
 // Few rows of many actions would leave the chip idle: each is shared by up to 64
 // workgroups, a launch for each step (largest value, histogram, list, sums, action).
-// 1 x 100003 fp32, top_p: 39 us, by one workgroup 94.
+// 1 x 100003 fp32, top_p: 26 us, by one workgroup 94.
 #include "seq.h"
 
 namespace gorila {
@@ -122,26 +122,38 @@ __device__ __forceinline__ uint64_t place_of(float u, uint64_t sum) {
     return at < sum ? at : sum - 1;
 }
 
-__device__ __forceinline__ uint64_t shuffle64(uint64_t v, int lane) { return (uint64_t)__shfl((unsigned long long)v, lane, 64); }
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += (uint64_t)__shfl_xor((unsigned long long)v, o, 64);
-    return v;
+__device__ __forceinline__ uint64_t lane64(uint64_t v, int lane) {  // of a lane that the wave agrees on
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, lane);
 }
-// Sum over the lanes up to this one.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ uint64_t plus_lane64(uint64_t v) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, CONTROL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), CONTROL, ROWS, 0xf, false);
+    return v + ((uint64_t)hi << 32 | lo);
+}
+// Sum over the lanes up to this one, as over_wave() goes.  (Twelve shuffles through LDS wait 0.6 us.)
 __device__ __forceinline__ uint64_t wave_running(uint64_t v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t p = shuffle64(v, lane >= o ? lane - o : lane);
-        if (lane >= o) v += p;
-    }
-    return v;
+    v = plus_lane64<0x111, 0xf>(v);
+    v = plus_lane64<0x112, 0xf>(v);
+    v = plus_lane64<0x114, 0xf>(v);
+    v = plus_lane64<0x118, 0xf>(v);
+    v = plus_lane64<0x142, 0xa>(v);
+    return plus_lane64<0x143, 0xc>(v);
+}
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) { return lane64(wave_running(v), 63); }
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ float most_lane(float v) {
+    const int b = __builtin_bit_cast(int, v);
+    return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, CONTROL, ROWS, 0xf, false)));
 }
 __device__ __forceinline__ float wave_most(float v) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+    v = most_lane<0x111, 0xf>(v);
+    v = most_lane<0x112, 0xf>(v);
+    v = most_lane<0x114, 0xf>(v);
+    v = most_lane<0x118, 0xf>(v);
+    v = most_lane<0x142, 0xa>(v);
+    v = most_lane<0x143, 0xc>(v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
 template <class T>
@@ -178,7 +190,7 @@ __global__ __launch_bounds__(256) void sample_wave_kernel(SampleArgs a) {
         if (ahead >= limit) w = 0;
     }
     if (w < f.least) w = 0;
-    const uint64_t running = wave_running(w), sum = shuffle64(running, 63), at = place_of(a.u[row], sum);
+    const uint64_t running = wave_running(w), sum = lane64(running, 63), at = place_of(a.u[row], sum);
     const int first = __ffsll((unsigned long long)__ballot(running > at)) - 1;
     if (lane == first) {
         a.action[row] = lane;
@@ -208,10 +220,10 @@ __device__ __forceinline__ Found find(const I* v, int n, uint64_t at) {
     }
     const int from = __ffsll((unsigned long long)__ballot(here)) - 1;
     Found f;
-    i = __shfl(i, from, 64);
+    i = __builtin_amdgcn_readlane(i, from);
     f.index = DOWN ? n - 1 - i : i;
-    f.above = shuffle64(sum, from);
-    f.level = shuffle64(level, from);
+    f.above = lane64(sum, from);
+    f.level = lane64(level, from);
     return f;
 }
 
@@ -258,16 +270,16 @@ __device__ __forceinline__ void each_part(const R& r, int first, int step, F&& f
 // What the workgroups that share a row tell each other, in the workspace.
 constexpr int SHARES = 64, ALL_BINS = 2048, ALL_LIST = 4096;
 struct RowSpace {
-    unsigned long long bins[ALL_BINS], pieces[MAX_SAMPLE / 1024 + 1];
+    unsigned long long bins[ALL_BINS], sums[MAX_SAMPLE / 256 + 1];
     uint32_t count[ALL_BINS], key[ALL_LIST], act[ALL_LIST];
     float most[SHARES];
-    uint32_t listed, done, border;  // done: the border is known, and pieces[] are the sums
+    uint32_t listed, done, border;  // done: the border and the parts' sums are known
     int end;
 };
 
-template <int BINS, int LIST, int PIECES>
+template <int BINS, int LIST, int PARTS>
 struct RowShared {
-    unsigned long long bins[BINS], weight[LIST], pieces[PIECES], digits[256], part[16];
+    unsigned long long bins[BINS], weight[LIST], sums[PARTS], digits[256], part[16];
     unsigned long long small_weight[SMALL];
     uint32_t count[BINS], key[LIST], act[LIST], small_key[SMALL], small_act[SMALL];
     float most[16];
@@ -476,53 +488,48 @@ __global__ __launch_bounds__(1024) void share_list_kernel(SampleArgs a, RowSpace
 }
 
 // A row's action by a workgroup (WHOLE), or where workgroups share it and its histogram and
-// list are in the workspace, the sums of the pieces (SUMS), and the action of them (PICK; a
+// list are in the workspace, the sums of its parts (SUMS), and the action of them (PICK; a
 // row whose list was too long is taken whole).
 enum Part { WHOLE, SUMS, PICK };
-template <class T, int THREADS, int SUB, int BINS, int LIST, int MOST, Part PART>
+template <class T, int THREADS, int BINS, int LIST, int MOST, Part PART>
 __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a, RowSpace* space, int shares) {
-    constexpr int NW = THREADS / 64, PIECE = 256 * SUB;  // a wave's piece of the running sums
-    __shared__ RowShared<BINS, LIST, MOST / PIECE + 1> sh;
+    constexpr int NW = THREADS / 64;
+    __shared__ RowShared<BINS, LIST, MOST / 256 + 1> sh;
     const int64_t row = PART == SUMS ? blockIdx.x / shares : blockIdx.x;
     const int share = PART == SUMS ? blockIdx.x % shares : 0;
     const Row<T> r(a, row);
-    const int lane = r.lane, wave = threadIdx.x >> 6, n = r.n, pieces = (r.parts + SUB - 1) / SUB;
+    const int lane = r.lane, wave = threadIdx.x >> 6, n = r.n, parts = r.parts;
     const Series series;
     Filter f = filter_of(a, row);
     auto weigh = [&](float v) { return weight(v, f, series); };
     auto each = [&](auto&& f) { each_part(r, wave, NW, f); };
-    // The sum of g(value) over a piece's values that stay(value, action); g is formed for all
-    // of a wave's four values or none, so that its long chains overlap.
-    auto piece_sum = [&](int piece, auto&& stay, auto&& g) {
-        uint64_t s = 0;
-        f32x4 next = r.load(piece * SUB);
-#pragma unroll 1
-        for (int part = piece * SUB; part < piece * SUB + SUB; ++part) {
-            const f32x4 v = values_of(next);
-            if (part + 1 < piece * SUB + SUB) next = r.load(part + 1);
+    // sums[] of parts first, first + step, ..: g(value) over the values that stay(value, action);
+    // g is formed for all of a wave's four values or none, so that its long chains overlap.
+    auto sum_parts = [&](int first, int step, unsigned long long* sums, auto&& stay, auto&& g) {
+        each_part(r, first, step, [&](f32x4 v, int part) {
             bool some[4], any = false;
 #pragma unroll
             for (int j = 0; j < 4; ++j) any |= some[j] = stay(v[j], r.action(part, j));
-            if (!__any(any)) continue;
+            uint64_t s = 0;
+            if (__any(any)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint64_t w = g(v[j]);
-                s += some[j] ? w : 0;
+                for (int j = 0; j < 4; ++j) {
+                    const uint64_t w = g(v[j]);
+                    s += some[j] ? w : 0;
+                }
+                s = wave_sum(s);
             }
-        }
-        return __any(s != 0) ? wave_sum(s) : 0;
+            if (lane == 0) sums[part] = s;
+        });
     };
-    auto sums = [&](auto&& stay, auto&& g) {  // pieces[] of all pieces
+    auto sums = [&](auto&& stay, auto&& g) {  // of all parts
         __syncthreads();
-        for (int piece = wave; piece < pieces; piece += NW) {
-            const uint64_t s = piece_sum(piece, stay, g);
-            if (lane == 0) sh.pieces[piece] = s;
-        }
+        sum_parts(wave, NW, sh.sums, stay, g);
         __syncthreads();
     };
-    auto total = [&]() -> uint64_t {  // of the pieces, for every lane
+    auto total = [&]() -> uint64_t {  // of the sums, for every lane
         uint64_t s = 0;
-        for (int i = lane; i < pieces; i += 64) s += sh.pieces[i];
+        for (int i = lane; i < parts; i += 64) s += sh.sums[i];
         return wave_sum(s);
     };
 
@@ -549,7 +556,7 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a, RowSp
     const bool known = PART == PICK && space[row].done;
     if (known) {
         key = space[row].border, end = space[row].end;
-        for (int i = threadIdx.x; i < pieces; i += THREADS) sh.pieces[i] = space[row].pieces[i];
+        for (int i = threadIdx.x; i < parts; i += THREADS) sh.sums[i] = space[row].sums[i];
         __syncthreads();
     } else if (by_count || by_sum) {
         const float per = (float)(f.per * (BINS / -GONE));
@@ -722,34 +729,27 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a, RowSp
                 end = sh.end;
             } else {
                 sums([&](float v, int i) { return key_of(v) == key && r.inside(i); }, [](float) -> uint64_t { return 1; });
-                const Found got = find<false>(sh.pieces, pieces, ties);
-                uint64_t before = got.above;
-#pragma unroll 1
-                for (int part = got.index * SUB; part < got.index * SUB + SUB; ++part) {
-                    const f32x4 v = values_of(r.load(part));
-                    uint64_t own = 0;
+                const Found got = find<false>(sh.sums, parts, ties);
+                const f32x4 v = values_of(r.load(got.index));
+                uint64_t own = 0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) own += key_of(v[j]) == key && r.inside(r.action(part, j));
-                    const uint64_t upto = before + wave_running(own);
-                    uint64_t at = upto - own;
-                    int here = -1;
+                for (int j = 0; j < 4; ++j) own += key_of(v[j]) == key && r.inside(r.action(got.index, j));
+                uint64_t at = got.above + wave_running(own) - own;
+                int here = -1;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (key_of(v[j]) == key && r.inside(r.action(part, j)) && at++ == ties) here = r.action(part, j);
-                    const uint64_t who = __ballot(here >= 0);
-                    if (who) end = __shfl(here, __ffsll((unsigned long long)who) - 1, 64);
-                    before = shuffle64(upto, 63);
-                }
+                for (int j = 0; j < 4; ++j)
+                    if (key_of(v[j]) == key && r.inside(r.action(got.index, j)) && at++ == ties) here = r.action(got.index, j);
+                end = __builtin_amdgcn_readlane(here, __ffsll((unsigned long long)__ballot(here >= 0)) - 1);
             }
         }
         if (complete && PART != SUMS) {
             __syncthreads();
-            for (int i = threadIdx.x; i < pieces; i += THREADS) sh.pieces[i] = 0;
+            for (int i = threadIdx.x; i < parts; i += THREADS) sh.sums[i] = 0;
             __syncthreads();
             for (uint32_t i = threadIdx.x; i < listed; i += THREADS) {
                 const uint64_t w = by_sum ? sh.weight[i] : weigh(value_of_key(sh.key[i]));
                 if (w >= f.least && w && (sh.key[i] > key || (sh.key[i] == key && (int)sh.act[i] < end)))
-                    atomicAdd(&sh.pieces[((int)sh.act[i] + r.shift) / PIECE], (unsigned long long)w);
+                    atomicAdd(&sh.sums[((int)sh.act[i] + r.shift) / 256], (unsigned long long)w);
             }
             __syncthreads();
         }
@@ -763,39 +763,30 @@ __global__ __launch_bounds__(THREADS) void sample_row_kernel(SampleArgs a, RowSp
         return w >= f.least ? w : 0;
     };
     if (PART == SUMS) {
-        for (int piece = share * NW + wave; piece < pieces; piece += shares * NW) {
-            const uint64_t s = piece_sum(piece, stays, enough);
-            if (lane == 0) space[row].pieces[piece] = s;
-        }
+        sum_parts(share * NW + wave, shares * NW, space[row].sums, stays, enough);
         if (share == 0 && threadIdx.x == 0) space[row].done = 1, space[row].border = key, space[row].end = end;
         return;
     }
     if (!known && !complete) sums(stays, enough);
     if (wave != 0) return;
     const uint64_t sum = total(), at = place_of(a.u[row], sum);
-    const Found got = find<false>(sh.pieces, pieces, at);
-    uint64_t before = got.above;
-#pragma unroll 1
-    for (int part = got.index * SUB; part < got.index * SUB + SUB; ++part) {
-        const f32x4 v = values_of(r.load(part));
-        uint64_t w[4], own = 0;
+    const Found got = find<false>(sh.sums, parts, at);
+    const f32x4 v = values_of(r.load(got.index));
+    uint64_t w[4], own = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            w[j] = enough(v[j]);
-            if (!stays(v[j], r.action(part, j))) w[j] = 0;
-            own += w[j];
-        }
-        const uint64_t upto = before + wave_running(own);
-        uint64_t run = upto - own;
+    for (int j = 0; j < 4; ++j) {
+        w[j] = enough(v[j]);
+        if (!stays(v[j], r.action(got.index, j))) w[j] = 0;
+        own += w[j];
+    }
+    uint64_t run = got.above + wave_running(own) - own;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (run <= at && at < run + w[j]) {
-                a.action[row] = r.action(part, j);
-                if (a.probability) a.probability[row] = (float)((double)w[j] / (double)sum);
-            }
-            run += w[j];
+    for (int j = 0; j < 4; ++j) {
+        if (run <= at && at < run + w[j]) {
+            a.action[row] = r.action(got.index, j);
+            if (a.probability) a.probability[row] = (float)((double)w[j] / (double)sum);
         }
-        before = shuffle64(upto, 63);
+        run += w[j];
     }
 }
 
@@ -822,7 +813,7 @@ int gorila_sample_actions(const void* values, int64_t stride, int64_t rows, int3
     const SampleArgs a{values, stride, rows, actions, u, temperature, top_p, min_p, top_k, action_out, probability_out};
     const int threads = actions <= 64 ? 64 : actions <= 2048 ? 256 : 1024;
     if (!(threads == 64 ? launch_fits((double)((rows + 3) / 4), 256) : launch_fits((double)rows, threads))) return GORILA_EUNSUPPORTED;
-    // few rows of many actions: each shared by workgroups of 16 pieces, if the workspace has the place
+    // few rows of many actions: each shared by workgroups of 16 parts, if the workspace has the place
     int shares = (actions + 3 + 16 * 256 - 1) / (16 * 256);
     if (shares > SHARES) shares = SHARES;
     const bool shared = actions > SHARED_FROM && rows * shares <= 2 * c.cus && ctx_view(ctx, (size_t)rows * sizeof(RowSpace), c) == GORILA_OK;
@@ -831,19 +822,19 @@ int gorila_sample_actions(const void* values, int64_t stride, int64_t rows, int3
         if (threads == 64) {
             sample_wave_kernel<T><<<(unsigned)((rows + 3) / 4), 256, 0, c.stream>>>(a);
         } else if (threads == 256) {
-            sample_row_kernel<T, 256, 1, 512, 1024, 2048, WHOLE><<<(unsigned)rows, 256, 0, c.stream>>>(a, nullptr, 0);
+            sample_row_kernel<T, 256, 512, 1024, 2048, WHOLE><<<(unsigned)rows, 256, 0, c.stream>>>(a, nullptr, 0);
         } else if (actions <= 65536 && !shared) {
-            sample_row_kernel<T, 1024, 1, 2048, 4096, 65536, WHOLE><<<(unsigned)rows, 1024, 0, c.stream>>>(a, nullptr, 0);
+            sample_row_kernel<T, 1024, 2048, 4096, 65536, WHOLE><<<(unsigned)rows, 1024, 0, c.stream>>>(a, nullptr, 0);
         } else if (shared) {
             RowSpace* space = (RowSpace*)c.ws;
             const unsigned blocks = (unsigned)(rows * shares);
             share_most_kernel<T><<<blocks, 1024, 0, c.stream>>>(a, space, shares);
             share_bins_kernel<T><<<blocks, 1024, 0, c.stream>>>(a, space, shares);
             share_list_kernel<T><<<blocks, 1024, 0, c.stream>>>(a, space, shares);
-            sample_row_kernel<T, 1024, 4, ALL_BINS, ALL_LIST, MAX_SAMPLE, SUMS><<<blocks, 1024, 0, c.stream>>>(a, space, shares);
-            sample_row_kernel<T, 1024, 4, ALL_BINS, ALL_LIST, MAX_SAMPLE, PICK><<<(unsigned)rows, 1024, 0, c.stream>>>(a, space, shares);
+            sample_row_kernel<T, 1024, ALL_BINS, ALL_LIST, MAX_SAMPLE, SUMS><<<blocks, 1024, 0, c.stream>>>(a, space, shares);
+            sample_row_kernel<T, 1024, ALL_BINS, ALL_LIST, MAX_SAMPLE, PICK><<<(unsigned)rows, 1024, 0, c.stream>>>(a, space, shares);
         } else {
-            sample_row_kernel<T, 1024, 4, 2048, 4096, MAX_SAMPLE, WHOLE><<<(unsigned)rows, 1024, 0, c.stream>>>(a, nullptr, 0);
+            sample_row_kernel<T, 1024, 2048, 4096, MAX_SAMPLE, WHOLE><<<(unsigned)rows, 1024, 0, c.stream>>>(a, nullptr, 0);
         }
     };
     dtype == GORILA_F32 ? go(float{}) : go(uint16_t{});
