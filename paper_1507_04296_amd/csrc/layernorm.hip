@@ -28,16 +28,116 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*sm)[N]) {
     }
 }
 
-// v - mean at the row's columns, zero past them.
-template <int W, int LANES, int QUADS>
-__device__ __forceinline__ void center(f32x4 (&v)[QUADS], float mean, int width, int l) {
+// 16 bytes of a row from column c on, zeros past its end.  EVEN: rows are whole loads at
+// multiples of 16 bytes.  Others are read where they are, and their end as the last 16 bytes
+// of the row, moved: no branch, so that all loads of a row are under way at once
+// (34571 x 781 bf16: 51 us forward, 54 backward; with a branch for the end 63 and 153, in
+// single values 132 and 225).
+template <class T> constexpr int PER = 16 / sizeof(T);  // values
+template <bool EVEN, class T>
+__device__ __forceinline__ uint4 load_piece(const T* p, int c, int width) {
+    constexpr int W = PER<T>;
+    uint4 u{0, 0, 0, 0};
+    if constexpr (EVEN) {
+        if (c < width) u = *(const uint4*)(p + c);
+    } else if (width >= W) {
+        u = load_any<uint4>(p + (c < width - W ? c : width - W));
+    } else if (c == 0) {
+        T t[W] = {};
 #pragma unroll
-    for (int i = 0; i < QUADS; ++i) {
-        const int n = width - column<W, LANES>(l, i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = (W == 1 ? j < n : 0 < n) ? v[i][j] - mean : 0.0f;
+        for (int j = 0; j < W - 1; ++j)
+            if (j < width) t[j] = p[j];
+        __builtin_memcpy(&u, t, 16);
+    }
+    return u;
+}
+template <bool EVEN, class T>
+__device__ __forceinline__ uint4 move_piece(uint4 u, int c, int width) {
+    constexpr int W = PER<T>;
+    if (EVEN || width < W) return u;
+    const int by = c - (width - W);  // 1 to W - 1 at the row's end, more past it
+    if (by > 0 && (by & (W / 2))) u = uint4{u.z, u.w, 0, 0};
+    if (by > 0 && (by & (W / 4))) u = uint4{u.y, u.z, u.w, 0};
+    if (W == 8 && by > 0 && (by & 1)) u = uint4{u.x >> 16 | u.y << 16, u.y >> 16 | u.z << 16, u.z >> 16 | u.w << 16, u.w >> 16};
+    return by >= W ? uint4{0, 0, 0, 0} : u;
+}
+template <bool EVEN, class T>
+__device__ __forceinline__ void store_piece(T* p, uint4 u, int c, int width) {
+    constexpr int W = PER<T>;
+    const int n = width - c;
+    p += c;
+    if constexpr (EVEN) {
+        if (n > 0) *(uint4*)p = u;
+    } else if (n >= W) {
+        store_any(p, u);
+    } else if (n > 0) {
+        if (n & (W / 2)) store_any(p, uint2{u.x, u.y}), u.x = u.z, u.y = u.w, p += W / 2;
+        if (n & (W / 4)) store_any(p, u.x), u.x = u.y, p += W / 4;
+        if (W == 8 && (n & 1)) *p = (T)u.x;
     }
 }
+__device__ __forceinline__ f32x4 floats(uint4 u) { return f32x4{__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)}; }
+__device__ __forceinline__ uint4 bits(f32x4 v) { return uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}; }
+
+// A row as it is read; its values as norm_rows.h holds them.
+template <class T, int LANES, int QUADS, bool EVEN>
+struct Row {
+    static constexpr int W = PER<T>, PIECES = QUADS * 4 / W;
+    uint4 u[PIECES];
+    __device__ __forceinline__ static int column_of(int l, int i) { return (l + i * LANES) * W; }
+    __device__ __forceinline__ Row(const T* p, int width, int l) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) u[i] = load_piece<EVEN>(p, column_of(l, i), width);
+    }
+    __device__ __forceinline__ void values(f32x4 (&v)[QUADS], int width, int l) const {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint4 m = move_piece<EVEN, T>(u[i], column_of(l, i), width);
+            if constexpr (W == 8) {
+                v[2 * i] = floats(uint4{m.x << 16, m.x & 0xffff0000u, m.y << 16, m.y & 0xffff0000u});
+                v[2 * i + 1] = floats(uint4{m.z << 16, m.z & 0xffff0000u, m.w << 16, m.w & 0xffff0000u});
+            } else {
+                v[i] = floats(m);
+            }
+        }
+    }
+    __device__ __forceinline__ static void store(const f32x4 (&v)[QUADS], T* p, int width, int l) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            uint4 m;
+            if constexpr (W == 8) {
+                const f32x4 &a = v[2 * i], &b = v[2 * i + 1];
+                m.x = row_round<T>(a[0]) | (uint32_t)row_round<T>(a[1]) << 16, m.y = row_round<T>(a[2]) | (uint32_t)row_round<T>(a[3]) << 16;
+                m.z = row_round<T>(b[0]) | (uint32_t)row_round<T>(b[1]) << 16, m.w = row_round<T>(b[2]) | (uint32_t)row_round<T>(b[3]) << 16;
+            } else {
+                m = bits(v[i]);
+            }
+            store_piece<EVEN>(p, m, column_of(l, i), width);
+        }
+    }
+    // the same columns of an fp32 vector
+    __device__ __forceinline__ static void columns(f32x4 (&v)[QUADS], const float* p, int width, int l) {
+        uint4 m[QUADS];
+#pragma unroll
+        for (int i = 0; i < QUADS; ++i) m[i] = load_piece<EVEN>(p, column<W, LANES>(l, i), width);
+#pragma unroll
+        for (int i = 0; i < QUADS; ++i) v[i] = floats(move_piece<EVEN, float>(m[i], column<W, LANES>(l, i), width));
+    }
+    __device__ __forceinline__ static void store_columns(const f32x4 (&v)[QUADS], float* p, int width, int l) {
+#pragma unroll
+        for (int i = 0; i < QUADS; ++i) store_piece<EVEN>(p, bits(v[i]), column<W, LANES>(l, i), width);
+    }
+    // v - mean at the row's columns, zero past them
+    __device__ __forceinline__ static void center(f32x4 (&v)[QUADS], float mean, int width, int l) {
+#pragma unroll
+        for (int i = 0; i < QUADS; ++i) {
+            const int n = width - column<W, LANES>(l, i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = (EVEN ? 0 < n : j < n) ? v[i][j] - mean : 0.0f;
+        }
+    }
+};
+
 __device__ __forceinline__ float sum4(f32x4 v) { return (v[0] + v[1]) + (v[2] + v[3]); }
 
 struct LayerArgs {
@@ -53,31 +153,36 @@ struct LayerArgs {
 
 // The mean is rounded, and a row's offset may be many times its deviations: the sum of
 // the deviations, which comes with the sum of their squares, is what it is off by.
-template <class T, int LANES, int QUADS, int W>
+template <class T, int LANES, int QUADS, bool EVEN>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layernorm_kernel(LayerArgs a) {
     __shared__ float sm1[LANES / 64][1], sm2[LANES / 64][2];
-    constexpr int PER = LANES < 256 ? 256 / LANES : 1;  // rows a workgroup
-    const int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / LANES;
+    constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;  // of a workgroup
+    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
     const int l = threadIdx.x % LANES;
     if (row >= a.rows) return;  // whole waves, and no barrier where a workgroup has several rows
+    using Row = Row<T, LANES, QUADS, EVEN>;
     f32x4 v[QUADS], w[QUADS];
-    load_row<W, LANES>(v, (const T*)a.x + row * a.xs, a.width, l);
+    const Row x((const T*)a.x + row * a.xs, a.width, l);
     if (a.residual) {
         f32x4 r[QUADS];
-        load_row<W, LANES>(r, (const T*)a.residual + row * a.rs, a.width, l);
+        const Row second((const T*)a.residual + row * a.rs, a.width, l);
+        x.values(v, a.width, l);
+        second.values(r, a.width, l);
 #pragma unroll
         for (int i = 0; i < QUADS; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[i][j] = row_value(row_round<T>(v[i][j] + r[i][j]));
+    } else {
+        x.values(v, a.width, l);
     }
-    load_weight<W, LANES>(w, a.weight, a.width, l);
+    Row::columns(w, a.weight, a.width, l);
     float sum[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) sum[0] += sum4(v[i]);
     row_sums<LANES>(sum, sm1);
-    if (a.total) store_row<W, LANES>(v, (T*)a.total + row * a.width, a.width, l);
+    if (a.total) Row::store(v, (T*)a.total + row * a.width, a.width, l);
     const float mean = sum[0] / (float)a.width;
-    center<W, LANES>(v, mean, a.width, l);
+    Row::center(v, mean, a.width, l);
     float two[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) two[0] += sum4(v[i]), two[1] += sum4(v[i] * v[i]);
@@ -91,34 +196,35 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layernorm_kernel(La
         if (a.rstd) a.rstd[row] = rho;
     }
     f32x4 b[QUADS];
-    if (a.bias) load_weight<W, LANES>(b, a.bias, a.width, l);
+    if (a.bias) Row::columns(b, a.bias, a.width, l);
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) {
         v[i] = (v[i] - off) * rho * w[i];
         if (a.bias) v[i] += b[i];
     }
-    store_row<W, LANES>(v, (T*)a.y + row * a.width, a.width, l);
+    Row::store(v, (T*)a.y + row * a.width, a.width, l);
 }
 
 // Backward: as the root-mean-square norm's, with both parameters' sums, and with the
 // saved mean's rounding taken out again: its part comes with the row's other sums.
-template <class T, int LANES, int QUADS, int W>
+template <class T, int LANES, int QUADS, bool EVEN>
 __global__ __launch_bounds__(LANES == 64 ? 512 : LANES) void layernorm_backward_kernel(LayerArgs a) {
-    constexpr int PER = LANES == 64 ? 8 : 1, COLS = LANES * QUADS * 4;
-    __shared__ __align__(16) float sums[PER > 1 ? PER / 2 * COLS : 4];
+    constexpr int ROWS = LANES == 64 ? 8 : 1, COLS = LANES * QUADS * 4;
+    __shared__ __align__(16) float sums[ROWS > 1 ? ROWS / 2 * COLS : 4];
     __shared__ float sm[LANES / 64][3];
     const int l = threadIdx.x % LANES, own = threadIdx.x / LANES;
+    using Row = Row<T, LANES, QUADS, EVEN>;
     f32x4 dw[QUADS], db[QUADS], w[QUADS];
-    load_weight<W, LANES>(w, a.weight, a.width, l);
+    Row::columns(w, a.weight, a.width, l);
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) dw[i] = db[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t row = (int64_t)blockIdx.x * PER + own; row < a.rows; row += (int64_t)gridDim.x * PER) {
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + own; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
         const float rho = a.rstd_in[row], mean = a.mean_in[row];
         f32x4 g[QUADS], v[QUADS], d[QUADS];
-        load_row<W, LANES>(g, (const T*)a.dy + row * a.dys, a.width, l);
-        load_row<W, LANES>(v, (const T*)a.total_in + row * a.width, a.width, l);
-        if (a.dtotal) load_row<W, LANES>(d, (const T*)a.dtotal + row * a.dts, a.width, l);
-        center<W, LANES>(v, mean, a.width, l);
+        const Row dy((const T*)a.dy + row * a.dys, a.width, l), total((const T*)a.total_in + row * a.width, a.width, l);
+        const Row dt((const T*)a.dtotal + row * a.dts, a.dtotal ? a.width : 0, l);
+        dy.values(g, a.width, l), total.values(v, a.width, l);
+        Row::center(v, mean, a.width, l);
         float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < QUADS; ++i) {
@@ -134,13 +240,17 @@ __global__ __launch_bounds__(LANES == 64 ? 512 : LANES) void layernorm_backward_
             dw[i] += g[i] * (v[i] * rho);
             db[i] += g[i];
             g[i] = (g[i] * w[i] - mg - v[i] * k) * rho;
-            if (a.dtotal) g[i] += d[i];
         }
-        store_row<W, LANES>(g, (T*)a.dx + row * a.width, a.width, l);
+        if (a.dtotal) {
+            dt.values(d, a.width, l);
+#pragma unroll
+            for (int i = 0; i < QUADS; ++i) g[i] += d[i];
+        }
+        Row::store(g, (T*)a.dx + row * a.width, a.width, l);
     }
     // the workgroup's rows joined: the upper half's sums to the lower half, and again
 #pragma unroll
-    for (int half = PER / 2; half; half >>= 1)
+    for (int half = ROWS / 2; half; half >>= 1)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             f32x4(&v)[QUADS] = k ? db : dw;
@@ -157,13 +267,8 @@ __global__ __launch_bounds__(LANES == 64 ? 512 : LANES) void layernorm_backward_
         }
     if (own != 0) return;
     float* part = a.parts + (int64_t)blockIdx.x * 2 * a.width;
-#pragma unroll
-    for (int i = 0; i < QUADS; ++i) {
-        const int c = column<W, LANES>(l, i);
-        if (c >= a.width) continue;
-        row_store<W != 1>(part + c, dw[i], a.width - c);
-        row_store<W != 1>(part + a.width + c, db[i], a.width - c);
-    }
+    Row::store_columns(dw, part, a.width, l);
+    Row::store_columns(db, part + a.width, a.width, l);
 }
 
 // Lanes and quads of the backward's rows: it holds six values a column, where the
@@ -179,6 +284,12 @@ void by_backward_width(int width, F&& f) {
     else if (width <= 8192) k(integral_constant<int, 512>{}, integral_constant<int, 4>{});
     else if (width <= 16384) k(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
     else k(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
+}
+
+template <class F>
+void by_rows(int dtype, bool even, F&& f) {
+    if (dtype == GORILA_F32) even ? f(float{}, std::true_type{}) : f(float{}, std::false_type{});
+    else even ? f(uint16_t{}, std::true_type{}) : f(uint16_t{}, std::false_type{});
 }
 
 int check_layer(const LayerArgs& a, int dtype) {
@@ -211,16 +322,15 @@ int gorila_add_layernorm(const void* x, int64_t x_stride, const void* residual, 
     for (const void* p : {x, residual, (const void*)y, (const void*)total})
         if (!at_element(p, e)) return GORILA_EINVAL;
     const int64_t strides = a.xs | a.rs | width;
-    const bool vec = !(strides & 3) && at_four(x, e) && at_four(residual, e) && at_four(y, e) && at_four(total, e) && at_four(weight, 4) &&
-                     at_four(bias, 4);
-    const bool pairs = vec && !(strides & 7) && aligned16(x) && aligned16(residual) && aligned16(y) && aligned16(total);
+    bool even = !(strides & (16 / e - 1)) && aligned16(weight) && aligned16(bias);
+    for (const void* p : {x, residual, (const void*)y, (const void*)total}) even = even && aligned16(p);
     bool fits = true;
     by_width(width, [&](auto lanes, auto quads) {
-        constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, PER = L < 256 ? 256 / L : 1;
-        fits = launch_fits((double)((rows + PER - 1) / PER), L < 256 ? 256 : L);
+        constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, ROWS = L < 256 ? 256 / L : 1;
+        fits = launch_fits((double)((rows + ROWS - 1) / ROWS), L < 256 ? 256 : L);
         if (!fits) return;
-        by_load(dtype, vec, pairs, [&](auto t, auto wide) {
-            layernorm_kernel<decltype(t), L, QD, decltype(wide)::value><<<(unsigned)((rows + PER - 1) / PER), L < 256 ? 256 : L, 0, c.stream>>>(a);
+        by_rows(dtype, even, [&](auto t, auto ev) {
+            layernorm_kernel<decltype(t), L, QD, decltype(ev)::value><<<(unsigned)((rows + ROWS - 1) / ROWS), L < 256 ? 256 : L, 0, c.stream>>>(a);
         });
     });
     return fits ? launched() : GORILA_EUNSUPPORTED;
@@ -248,16 +358,16 @@ int gorila_add_layernorm_backward(const void* dy, int64_t dy_stride, const void*
     if ((rc = ctx_view(ctx, (size_t)NORM_PARTS * width * 8, c))) return rc;
     a.parts = (float*)c.ws;
     const int64_t strides = a.dys | a.dts | width;
-    const bool vec = !(strides & 3) && at_four(dy, e) && at_four(dtotal, e) && at_four(total, e) && at_four(dx, e) && at_four(weight, 4);
-    const bool pairs = vec && !(strides & 7) && aligned16(dy) && aligned16(dtotal) && aligned16(total) && aligned16(dx);
+    bool even = !(strides & (16 / e - 1)) && aligned16(weight);
+    for (const void* p : {dy, dtotal, total, (const void*)dx}) even = even && aligned16(p);
     int parts = 0;
     by_backward_width(width, [&](auto lanes, auto quads) {
-        constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, THREADS = L == 64 ? 512 : L, PER = THREADS / L;
-        const int64_t need = (rows + PER - 1) / PER;
+        constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, THREADS = L == 64 ? 512 : L, ROWS = THREADS / L;
+        const int64_t need = (rows + ROWS - 1) / ROWS;
         parts = (int)(need < NORM_PARTS ? need : NORM_PARTS);
         if (parts == 0) return;
-        by_load(dtype, vec, pairs, [&](auto t, auto wide) {
-            layernorm_backward_kernel<decltype(t), L, QD, decltype(wide)::value><<<parts, THREADS, 0, c.stream>>>(a);
+        by_rows(dtype, even, [&](auto t, auto ev) {
+            layernorm_backward_kernel<decltype(t), L, QD, decltype(ev)::value><<<parts, THREADS, 0, c.stream>>>(a);
         });
     });
     launch_sum_parts(a.parts, parts, 2 * (int64_t)width, width, 1, dweight, dbias, c.stream);

@@ -65,6 +65,37 @@ __device__ __forceinline__ void row_store(T* p, f32x4 v, int n) {
     }
 }
 
+// A value at any address of its elements.  Global memory takes wide loads and stores there; those
+// that cross a line of the cache are two.
+template <class V>
+__device__ __forceinline__ V load_any(const void* p) {
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
+template <class V>
+__device__ __forceinline__ void store_any(void* p, V v) { __builtin_memcpy(p, &v, sizeof(V)); }
+// As row_load() and row_store() of quads, n of which exist: in one piece where all four do.
+__device__ __forceinline__ f32x4 quad_load(const float* p, int n) { return n >= 4 ? load_any<f32x4>(p) : row_load<false>(p, n); }
+__device__ __forceinline__ f32x4 quad_load(const uint16_t* p, int n) {
+    if (n < 4) return row_load<false>(p, n);
+    const uint2 v = load_any<uint2>(p);
+    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u)};
+}
+__device__ __forceinline__ void quad_store(float* p, f32x4 v, int n) {
+    if (n >= 4) store_any(p, v);
+    else row_store<false>(p, v, n);
+}
+__device__ __forceinline__ void quad_store(uint16_t* p, f32x4 v, int n) {
+    if (n >= 4) {
+        const uint32_t a = row_round<uint16_t>(v[0]), b = row_round<uint16_t>(v[1]);
+        const uint32_t c = row_round<uint16_t>(v[2]), d = row_round<uint16_t>(v[3]);
+        store_any(p, uint2{a | b << 16, c | d << 16});
+    } else {
+        row_store<false>(p, v, n);
+    }
+}
+
 // v of the lane that DPP's control names, 0 where there is none (or where the row of 16 lanes is
 // not in ROWS).
 template <int CONTROL, int ROWS>

@@ -170,6 +170,45 @@ def test_layernorm_odd_rows(g, ctx, dtype, width):
     assert dx.shape == (0, width) and float(dw.abs().max()) == 0 == float(db.abs().max())
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [2, 3, 4, 6, 7, 8, 9, 12, 15, 17, 511, 513, 781, 1027, 1690, 3001, 4100, 9003])
+def test_layernorm_ends_of_rows(g, ctx, width, dtype):
+    """Rows that end and begin anywhere, to the element: what lies around the outputs stays, and
+    what lies around the inputs (infinities) does not count."""
+    rows, bits, e = 5, 1 if dtype == BF16 else 0, 2 if dtype == BF16 else 4
+    sides, stream = 9, ctx.bind_stream()
+
+    def within(t, fill, off):  # t between values of `fill`, `off` elements past 16 bytes
+        flat = torch.full((t.numel() + 2 * sides + off,), fill, dtype=t.dtype, device="cuda")
+        flat[sides - 1 + off:sides - 1 + off + t.numel()] = t.reshape(-1)
+        return flat, flat.data_ptr() + (sides - 1 + off) * t.element_size()
+
+    x, r, dy, dt = (rand(rows, width, dtype=dtype, seed=k) for k in (1, 2, 3, 4))
+    w, b = 1 + rand(width, scale=0.1, seed=5), rand(width, scale=0.1, seed=6)
+    total, mean, rstd = (x.float() + r.float()).to(dtype), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    wy, _, rho = ref.layernorm(total, w, b, EPS)
+    wdx, wdw, wdb = ref.layernorm_backward(dy, total, w, EPS, dt)
+    size = float((rho[:, None] * (w.cpu().double() * dy.cpu().double()).abs()).norm()) + float(wdx.norm())
+    for off in (0, 1, 3):
+        held = [within(t, INF, off + k) for k, t in enumerate((x, r, w, b, dy, dt))]
+        px, pr, pw, pb, pdy, pdt = (h[1] for h in held)
+        (fy, y), (ft, tot), (fd, dx) = (within(torch.empty_like(x), 7.0, off + k) for k in range(3))
+        fw, fb = (torch.full((width + 2,), 7.0, device="cuda") for _ in range(2))
+        assert g.lib().gorila_add_layernorm(px, width, pr, width, pw, pb, rows, width, bits, EPS, y, tot, mean.data_ptr(), rstd.data_ptr(), stream) == 0
+        assert g.lib().gorila_add_layernorm_backward(pdy, width, pdt, width, tot, mean.data_ptr(), rstd.data_ptr(), pw, rows, width, bits, dx,
+                                                     fw.data_ptr() + 4, fb.data_ptr() + 4, stream) == 0
+        for flat, p in ((fy, y), (ft, tot), (fd, dx)):
+            at = (p - flat.data_ptr()) // e
+            assert bool((flat[:at] == 7).all()) and bool((flat[at + rows * width:] == 7).all())
+        cut = lambda flat, p: flat[(p - flat.data_ptr()) // e:][:rows * width].reshape(rows, width)  # noqa: E731
+        assert torch.equal(cut(ft, tot), total)
+        close(cut(fy, y), wy, tol_of(dtype, FWD), "y")
+        close(cut(fd, dx), wdx, tol_of(dtype, BWD), "dx", size=size)
+        for flat, want in ((fw, wdw), (fb, wdb)):
+            assert float(flat[0]) == 7 == float(flat[-1])
+            close(flat[1:-1], want, BWD, "sums", size=float(want.norm()) + float(dy.double().norm()))
+
+
 def test_layernorm_refusals(g, ctx):
     x, w = rand(3, 8), rand(8)
     y, total, mean, rstd = g.add_layernorm(ctx, x, w)
