@@ -265,6 +265,20 @@ def test_gated_scan(g, ctx, B, T, C, dtype):
     check_gated(g, ctx, args, reset, state, dy, dstate, dtype)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,C", [(1, 3), (20, 1), (130, 33), (600, 1), (700, 65), (65, 127), (3, 191)])
+def test_gated_scan_odd_channels(g, ctx, T, C, dtype):
+    """The last channel of an odd number, of one, and the first of a tile; views at one element's alignment."""
+    args, reset, state, dy, dstate = gated_inputs(2, T, C, dtype, seed=45)
+    check_gated(g, ctx, args, reset, state, dy, dstate, dtype)
+    want = g.gated_scan(ctx, *args, reset, state)
+    got = g.gated_scan(ctx, *[strided(a, 2, 2, k) for k, a in enumerate(args[:3])], strided(args[3], 0, 0, 1), reset, strided(state, 0, 0, 1))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    back = g.gated_scan_backward(ctx, dy, *args, want[2], reset, dstate)
+    got = g.gated_scan_backward(ctx, strided(dy, 2, 1, 1), *[strided(a, 2, 4, 1) for a in args[:3]], args[3], want[2], reset, strided(dstate, 0, 0, 1))
+    assert all(torch.equal(a, b) for a, b in zip(got, back))
+
+
 @pytest.mark.parametrize("resets", [0.0, 0.3, 1.0])
 @pytest.mark.parametrize("T", [63, 700])
 def test_gated_scan_starts(g, ctx, T, resets):
