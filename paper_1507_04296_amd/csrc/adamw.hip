@@ -34,7 +34,6 @@ struct Tensor {
 struct Tensors {
     Tensor t[MOST];
     int count;
-    uint64_t wide;  // bit i: tensor i is aligned for four elements a load
 };
 static_assert(sizeof(Tensors) <= 4032, "the arguments fit a launch's");
 
@@ -70,27 +69,19 @@ __device__ __forceinline__ int tensor_of(const Tensors& s, uint32_t chunk) {
     return lo;
 }
 
-__device__ __forceinline__ f32x4 load4(const float* p, int n, bool wide) { return wide ? row_load<true>(p, n) : row_load<false>(p, n); }
-__device__ __forceinline__ f32x4 load4(const uint16_t* p, int n, bool wide) { return wide ? row_load<true>(p, n) : row_load<false>(p, n); }
-__device__ __forceinline__ void store4(float* p, f32x4 v, int n, bool wide) {
-    if (wide) row_store<true>(p, v, n);
-    else row_store<false>(p, v, n);
-}
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n, bool wide) {
-    if (wide) return n > 0 ? *(const uint32_t*)p : 0u;
+// Four codes, n of which exist.
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n) {
+    if (n >= 4) return load_any<uint32_t>(p);
     uint32_t v = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 3; ++j)
         if (j < n) v |= (uint32_t)p[j] << (8 * j);
     return v;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t v, int n, bool wide) {
-    if (wide) {
-        if (n > 0) *(uint32_t*)p = v;
-        return;
-    }
+__device__ __forceinline__ void store_codes(uint8_t* p, uint32_t v, int n) {
+    if (n >= 4) return store_any(p, v);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 3; ++j)
         if (j < n) p[j] = (uint8_t)(v >> (8 * j));
 }
 
@@ -137,9 +128,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
     if (r.keep && !*r.keep) return;
     const int which = tensor_of(s, blockIdx.x);
     const Tensor& t = s.t[which];
-    const bool aligned = s.wide >> which & 1u;
     const int64_t first = (int64_t)(blockIdx.x - t.chunk) * CHUNK;
-    auto chunk = [&](auto whole) {  // a whole chunk of aligned elements, or any
+    auto chunk = [&](auto whole) {  // a whole chunk, or any
 #pragma clang fp contract(off)
         constexpr bool FULL = decltype(whole)::value;
         // all loads first: the stores between could lie anywhere, for the compiler
@@ -151,16 +141,15 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
         for (int k = 0; k < TURNS; ++k) {
             const int64_t at = first + k * 1024 + threadIdx.x * 4, left = t.n - at;
             const int n = FULL || left > 4 ? 4 : left > 0 ? (int)left : 0;
-            const bool wide = FULL || (aligned && (n == 4 || n == 0));
             const int64_t p = n > 0 ? at : 0;
-            theta[k] = load4(t.theta + p, n, wide);
-            g[k] = load4((const G*)t.grad + p, n, wide);
+            theta[k] = quad_load(t.theta + p, n);
+            g[k] = quad_load((const G*)t.grad + p, n);
             if (BITS == 32) {
-                m[k] = load4((const float*)t.m + p, n, wide);
-                v[k] = load4((const float*)t.v + p, n, wide);
+                m[k] = quad_load((const float*)t.m + p, n);
+                v[k] = quad_load((const float*)t.v + p, n);
             } else {
-                cm[k] = load_codes((const uint8_t*)t.m + p, n, wide);
-                cv[k] = load_codes((const uint8_t*)t.v + p, n, wide);
+                cm[k] = load_codes((const uint8_t*)t.m + p, n);
+                cv[k] = load_codes((const uint8_t*)t.v + p, n);
                 sm[k] = n > 0 ? t.m_scale[p / GROUP] : 0.0f;
                 sv[k] = n > 0 ? t.v_scale[p / GROUP] : 0.0f;
             }
@@ -171,7 +160,6 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
         for (int k = 0; k < TURNS; ++k) {
             const int64_t at = first + k * 1024 + threadIdx.x * 4, left = t.n - at;
             const int n = FULL || left > 4 ? 4 : left > 0 ? (int)left : 0;
-            const bool wide = FULL || (aligned && (n == 4 || n == 0));
             if (!FULL && __ballot(n > 0) == 0) break;
             const int64_t p = n > 0 ? at : 0;
             if (BITS == 8) {
@@ -189,10 +177,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
                 v[k][j] = r.beta2 * v[k][j] + r.rest2 * (g[k][j] * g[k][j]);
                 theta[k][j] = theta[k][j] - r.lr * (t.decay * theta[k][j] + step_of(m[k][j] * c1, v[k][j] * c2, r.eps));
             }
-            store4(t.theta + p, theta[k], n, wide);
+            quad_store(t.theta + p, theta[k], n);
             if (BITS == 32) {
-                store4((float*)t.m + p, m[k], n, wide);
-                store4((float*)t.v + p, v[k], n, wide);
+                quad_store((float*)t.m + p, m[k], n);
+                quad_store((float*)t.v + p, v[k], n);
             } else {
                 float mm = 0.0f, mv = 0.0f, bad_m = 0.0f, bad_v = 0.0f;
 #pragma unroll
@@ -221,8 +209,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
                         new_m |= a << (8 * j), new_v |= b << (8 * j);
                     }
                 }
-                store_codes((uint8_t*)t.m + p, new_m, n, wide);
-                store_codes((uint8_t*)t.v + p, new_v, n, wide);
+                store_codes((uint8_t*)t.m + p, new_m, n);
+                store_codes((uint8_t*)t.v + p, new_v, n);
                 if (n > 0 && (threadIdx.x & 63) == 0) {
                     t.m_scale[p / GROUP] = mm == INFINITY ? NAN : mm;
                     t.v_scale[p / GROUP] = mv == INFINITY ? NAN : mv;
@@ -230,7 +218,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
             }
         }
     };
-    if (aligned && first + CHUNK <= t.n) chunk(std::true_type{});
+    if (first + CHUNK <= t.n) chunk(std::true_type{});
     else chunk(std::false_type{});
 }
 
@@ -238,15 +226,13 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
 __global__ __launch_bounds__(256) void values_kernel(Tensors s) {
     const int which = tensor_of(s, blockIdx.x);
     const Tensor& t = s.t[which];
-    const bool aligned = s.wide >> which & 1u;
     const int64_t first = (int64_t)(blockIdx.x - t.chunk) * CHUNK;
 #pragma unroll
     for (int k = 0; k < CHUNK / 1024; ++k) {
         const int64_t p = first + k * 1024 + threadIdx.x * 4, left = t.n - p;
         if (left <= 0) return;
         const int n = left > 4 ? 4 : (int)left;
-        const bool wide = aligned && n == 4;
-        const uint32_t cm = load_codes((const uint8_t*)t.m + p, n, wide), cv = load_codes((const uint8_t*)t.v + p, n, wide);
+        const uint32_t cm = load_codes((const uint8_t*)t.m + p, n), cv = load_codes((const uint8_t*)t.v + p, n);
         const float sm = t.m_scale[p / GROUP], sv = t.v_scale[p / GROUP];
         f32x4 m, v;
 #pragma unroll
@@ -256,22 +242,22 @@ __global__ __launch_bounds__(256) void values_kernel(Tensors s) {
             m[j] = c & 128u ? -size : size;
             v[j] = value_of(cv >> (8 * j) & 255u, LEAST_V, sv);
         }
-        store4(t.theta + p, m, n, wide);
-        store4((float*)t.grad + p, v, n, wide);
+        quad_store(t.theta + p, m, n);
+        quad_store((float*)t.grad + p, v, n);
     }
 }
 
 // ---- host ----
 
 // Calls launch(tensors, chunks) for the tensors that have elements, MOST or as many chunks
-// as a launch holds at a time; fill(i, t) sets the addresses and says whether all are aligned.
+// as a launch holds at a time; fill(from, i, t) sets the addresses.
 template <class F, class L>
 void by_launch(const gorila_adamw_tensor* tensors, int count, F&& fill, L&& launch) {
     Tensors s{};
     uint64_t chunks = 0, place = 0;
     auto flush = [&] {
         if (s.count) launch(s, (unsigned)chunks);
-        s.count = 0, s.wide = 0, chunks = 0;
+        s.count = 0, chunks = 0;
     };
     for (int i = 0; i < count; ++i) {
         const int64_t n = tensors[i].n;
@@ -280,7 +266,7 @@ void by_launch(const gorila_adamw_tensor* tensors, int count, F&& fill, L&& laun
             if (s.count == MOST || !launch_fits((double)(chunks + need), 256)) flush();
             Tensor& t = s.t[s.count];
             t.n = n, t.place = place, t.chunk = (uint32_t)chunks, t.decay = tensors[i].decay;
-            if (fill(tensors[i], i, t)) s.wide |= 1ull << s.count;
+            fill(tensors[i], i, t);
             ++s.count;
             chunks += need;
         }
@@ -329,8 +315,6 @@ int gorila_adamw(const gorila_adamw_tensor* tensors, int32_t count, int32_t grad
         tensors, count,
         [&](const gorila_adamw_tensor& from, int, Tensor& t) {
             t.theta = from.theta, t.grad = from.grad, t.m = from.m, t.v = from.v, t.m_scale = from.m_scale, t.v_scale = from.v_scale;
-            const int bytes = state_bits == 8 ? 1 : 4;
-            return aligned16(t.theta) && at_four(t.grad, e) && at_four(t.m, bytes) && at_four(t.v, bytes);
         },
         [&](const Tensors& s, unsigned chunks) {
             if (grad_dtype == GORILA_F32) {
@@ -356,7 +340,6 @@ int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float
         tensors, count,
         [&](const gorila_adamw_tensor& from, int i, Tensor& t) {
             t.m = from.m, t.v = from.v, t.m_scale = from.m_scale, t.v_scale = from.v_scale, t.theta = m_out[i], t.grad = v_out[i];
-            return aligned16(t.theta) && aligned16(t.grad) && at_four(t.m, 1) && at_four(t.v, 1);
         },
         [&](const Tensors& s, unsigned chunks) { values_kernel<<<chunks, 256, 0, c.stream>>>(s); });
     return launched();
