@@ -612,25 +612,26 @@ __global__ __launch_bounds__(256) void gated_step_kernel(GatedView v, float* poo
 
 // ---- host ----
 
-constexpr int FULL = 256;       // workgroups of eight waves that fill the chip forward (512 need a longer pass
-                                // for the maps: 4 x 1999 x 2000 bf16 46 + 29 us, 256 45 + 19),
-constexpr int BACK_FULL = 512;  // of four backward, where the maps are cheap
+constexpr int FULL = 256;       // workgroups that fill the chip, one a compute unit: half as many are cut into segments
+constexpr int BACK_FULL = 512;  // what a backward's fewer than that are cut into: its workgroups of four waves lie two a unit
 constexpr int LEAST_SEG = 256;  // steps of a segment, or of a map, at least
 constexpr int MAX_SEG = 64;     // segments of a sequence at most
 constexpr int WALKS = 2048;     // workgroups of the backward at most: each adds a part of da_log
 
 // Sequences whose tiles leave the chip idle are cut into segments.  Forward the maps of all
 // but the last are formed first, in parts of a segment, so that the whole chip has a
-// share of them.  (4 x 1999 x 2000 bf16, 128 tiles: uncut 65 us, cut 45 + 18; with fewer
-// tiles the cut gains.)
+// share of them.  (4 x 1999 x 2000 bf16, 128 tiles: uncut 65 us, cut into 256 45 + 18, into
+// 512 46 + 29; 192 tiles of 2000 steps fp32 uncut 87, cut into 384 126.  Backward 128 tiles
+// of 2000 steps cut into 512 74 us, into 256 95; 256 tiles of 512 steps fp32 uncut 49, cut
+// 64; 400 of 300 steps 50 and 80; 185 of 600 steps cut into 555 61, into 370 73.)
 struct Cut {
     int tiles, nseg = 1, seg, maps = 0, span;
     Cut(int64_t B, int T, int C, bool backward) {
         tiles = (C + TILE - 1) / TILE;
         seg = span = T > 0 ? T : 1;
         const int64_t have = B * tiles, full = backward ? BACK_FULL : FULL, most = (T + LEAST_SEG - 1) / LEAST_SEG;
-        if (have < 1 || have >= full) return;
-        int64_t k = (full + have - 1) / have;
+        if (have < 1 || have >= FULL) return;
+        int64_t k = backward ? (full + have - 1) / have : full / have;
         k = k < most ? k : most;
         k = k < MAX_SEG ? k : MAX_SEG;
         if (k < 2) return;
@@ -680,14 +681,16 @@ int gated_view(const gorila_gated_scan_args* a, GatedView& v) {
     return GORILA_OK;
 }
 
-// Waves a workgroup, of 16 steps each (a wave in which T ends, or a mark's four and more): forward two
-// chunks or more where there are as many steps, so that loads are under way while a
-// chunk is joined (32 x 128 x 1024 fp32: 14.6 us; one chunk of eight waves: 18.4).  Sixteen waves
-// are no faster on long sequences.  Backward a lane has 222 registers, and more waves than two a
-// SIMD do not pay: 8 steps a lane and four waves 22.7 us (5.2 TB/s), eight waves 27.6; 4 steps
-// and eight waves, half of the registers, 26.2.
+// Waves a workgroup, of 16 steps each (a wave in which T ends, or a mark's four and more).  Forward
+// eight where that is one workgroup a compute unit (32 x 1000 x 512 fp32: 51 us, four waves 58),
+// else four: one of eight leaves no place for a second (300 x 200 x 128 fp32, 600
+// workgroups: 26 us, eight waves 34; 320 of 500 steps 39 and 43), and two chunks or
+// more have loads under way while one is joined (32 x 128 x 1024 fp32: 14.6 us; 18.4).
+// Backward a lane has 222 registers, and more waves than two a SIMD do not pay: 8 steps a lane
+// and four waves 22.7 us (5.2 TB/s), eight waves 27.6; 4 steps and eight waves, half of the
+// registers, 26.2.
 constexpr int S = 8;
-int forward_waves(int T) { return T <= 16 ? 1 : T <= 128 ? 4 : 8; }
+int forward_waves(int T, double blocks) { return T <= 16 ? 1 : T <= 128 || blocks > FULL ? 4 : 8; }
 int backward_waves(int T) { return T <= 16 ? 1 : 4; }
 template <class F>
 void by_waves(int waves, F&& f) {
@@ -727,7 +730,7 @@ int gorila_gated_scan(const gorila_gated_scan_args* args, void* y, float* state_
     const Cut k(v.B, v.T, v.C, false);
     const Plan p(v.T, v.C, false);
     const double blocks = (double)v.B * k.nseg * k.tiles;
-    const int waves = forward_waves(v.T);
+    const int waves = forward_waves(v.T, blocks);
     if (!launch_fits(blocks, 64 * waves)) return GORILA_EUNSUPPORTED;
     if ((rc = ctx_view(ctx, k.nseg > 1 ? p.total : 0, c))) return rc;
     v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg, v.maps = k.maps, v.span = k.span;
