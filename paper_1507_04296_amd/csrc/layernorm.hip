@@ -8,13 +8,25 @@
 namespace gorila {
 namespace {
 
+// The sum over a row's 4, 16 or 32 lanes, inside a wave: lanes beside one another, pairs, then
+// from half a row of DPP's 16 lanes to the other, and from row to row.
+template <int LANES>
+__device__ __forceinline__ float over_lanes(float v) {
+    v += lane_of<0xb1, 0xf>(v);
+    v += lane_of<0x4e, 0xf>(v);
+    if (LANES > 4) v += lane_of<0x141, 0xf>(v), v += lane_of<0x140, 0xf>(v);
+    if (LANES > 16) v += __shfl_xor(v, 16, 64);
+    return v;
+}
 // The sums of N values over the LANES lanes of a row (all of them get them); sm: LDS, N
 // for each wave, used where a row has more than one.
 template <int LANES, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float (*sm)[N]) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = over_wave(v[k], [](float a, float b) { return a + b; });
-    if (LANES == 64) return;
+    for (int k = 0; k < N; ++k)
+        if constexpr (LANES < 64) v[k] = over_lanes<LANES>(v[k]);
+        else v[k] = over_wave(v[k], [](float a, float b) { return a + b; });
+    if (LANES <= 64) return;
     __syncthreads();
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -155,11 +167,11 @@ struct LayerArgs {
 // the deviations, which comes with the sum of their squares, is what it is off by.
 template <class T, int LANES, int QUADS, bool EVEN>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layernorm_kernel(LayerArgs a) {
-    __shared__ float sm1[LANES / 64][1], sm2[LANES / 64][2];
+    __shared__ float sm1[(LANES + 63) / 64][1], sm2[(LANES + 63) / 64][2];
     constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;  // of a workgroup
     const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
     const int l = threadIdx.x % LANES;
-    if (row >= a.rows) return;  // whole waves, and no barrier where a workgroup has several rows
+    if (row >= a.rows) return;  // all lanes of a row, and no barrier where a workgroup has several
     using Row = Row<T, LANES, QUADS, EVEN>;
     f32x4 v[QUADS], w[QUADS];
     const Row x((const T*)a.x + row * a.xs, a.width, l);
@@ -208,10 +220,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layernorm_kernel(La
 // Backward: as the root-mean-square norm's, with both parameters' sums, and with the
 // saved mean's rounding taken out again: its part comes with the row's other sums.
 template <class T, int LANES, int QUADS, bool EVEN>
-__global__ __launch_bounds__(LANES == 64 ? 512 : LANES) void layernorm_backward_kernel(LayerArgs a) {
-    constexpr int ROWS = LANES == 64 ? 8 : 1, COLS = LANES * QUADS * 4;
+__global__ __launch_bounds__(LANES <= 64 ? 512 : LANES) void layernorm_backward_kernel(LayerArgs a) {
+    constexpr int ROWS = LANES <= 64 ? 512 / LANES : 1, COLS = LANES * QUADS * 4;
     __shared__ __align__(16) float sums[ROWS > 1 ? ROWS / 2 * COLS : 4];
-    __shared__ float sm[LANES / 64][3];
+    __shared__ float sm[(LANES + 63) / 64][3];
     const int l = threadIdx.x % LANES, own = threadIdx.x / LANES;
     using Row = Row<T, LANES, QUADS, EVEN>;
     f32x4 dw[QUADS], db[QUADS], w[QUADS];
@@ -271,13 +283,18 @@ __global__ __launch_bounds__(LANES == 64 ? 512 : LANES) void layernorm_backward_
     Row::store_columns(db, part + a.width, a.width, l);
 }
 
-// Lanes and quads of the backward's rows: it holds six values a column, where the
-// root-mean-square norm's holds five.
-template <class F>
-void by_backward_width(int width, F&& f) {
+// Lanes and quads of a row: narrow rows share a wave, 8 values a lane (125000 x 64 bf16: 17 us
+// forward, 19 backward; a wave each 51 and 50).  The backward holds six values a column, where
+// the root-mean-square norm's holds five.
+template <bool BACKWARD, class F>
+void by_layer_width(int width, F&& f) {
     auto k = [&](auto lanes, auto quads) { f(lanes, quads); };
     using std::integral_constant;
-    if (width <= 512) k(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    if (width <= 32) k(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    else if (width <= 128) k(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    else if (width <= 256) k(integral_constant<int, 32>{}, integral_constant<int, 2>{});
+    else if constexpr (!BACKWARD) by_width(width, f);
+    else if (width <= 512) k(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     else if (width <= 1024) k(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else if (width <= 2048) k(integral_constant<int, 256>{}, integral_constant<int, 2>{});
     else if (width <= 4096) k(integral_constant<int, 256>{}, integral_constant<int, 4>{});
@@ -325,7 +342,7 @@ int gorila_add_layernorm(const void* x, int64_t x_stride, const void* residual, 
     bool even = !(strides & (16 / e - 1)) && aligned16(weight) && aligned16(bias);
     for (const void* p : {x, residual, (const void*)y, (const void*)total}) even = even && aligned16(p);
     bool fits = true;
-    by_width(width, [&](auto lanes, auto quads) {
+    by_layer_width<false>(width, [&](auto lanes, auto quads) {
         constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, ROWS = L < 256 ? 256 / L : 1;
         fits = launch_fits((double)((rows + ROWS - 1) / ROWS), L < 256 ? 256 : L);
         if (!fits) return;
@@ -361,8 +378,8 @@ int gorila_add_layernorm_backward(const void* dy, int64_t dy_stride, const void*
     bool even = !(strides & (16 / e - 1)) && aligned16(weight);
     for (const void* p : {dy, dtotal, total, (const void*)dx}) even = even && aligned16(p);
     int parts = 0;
-    by_backward_width(width, [&](auto lanes, auto quads) {
-        constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, THREADS = L == 64 ? 512 : L, ROWS = THREADS / L;
+    by_layer_width<true>(width, [&](auto lanes, auto quads) {
+        constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, THREADS = L <= 64 ? 512 : L, ROWS = THREADS / L;
         const int64_t need = (rows + ROWS - 1) / ROWS;
         parts = (int)(need < NORM_PARTS ? need : NORM_PARTS);
         if (parts == 0) return;

@@ -130,6 +130,30 @@ def test_layernorm(g, ctx, rows, width, dtype):
     close(y2, ref.layernorm(x, w, None, EPS)[0], tol_of(dtype, FWD), "no bias, no residual")
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width", [(1, 32), (15, 33), (16, 128), (17, 97), (63, 8), (64, 32), (130, 31), (9, 129), (8, 256), (33, 200),
+                                        (20000, 64), (70001, 16)])
+def test_layernorm_narrow_rows(g, ctx, rows, width, dtype):
+    """Rows that share a wave: the last ones alone in it, and more of them than workgroups."""
+    x, w, b = rand(rows, width, dtype=dtype, seed=1), 1 + rand(width, scale=0.1, seed=3), rand(width, scale=0.1, seed=6)
+    dy, dt = rand(rows, width, dtype=dtype, seed=4), rand(rows, width, dtype=dtype, seed=5)
+    y, total, mean, rstd = g.add_layernorm(ctx, x, w, b)
+    want, wmean, rho = ref.layernorm(x, w, b, EPS)
+    close(y, want, tol_of(dtype, FWD), "y")
+    close(mean, wmean, FWD, "mean", size=float(x.double().norm()) / math.sqrt(width))
+    close(rstd, rho, FWD, "rstd")
+    dx, dw, db = g.add_layernorm_backward(ctx, dy, total, mean, rstd, w, dt)
+    wdx, wdw, wdb = ref.layernorm_backward(dy, x, w, EPS, dt)
+    size = float((rho[:, None] * (w.cpu().double() * dy.cpu().double()).abs()).norm()) + float(wdx.norm())
+    close(dx, wdx, tol_of(dtype, BWD), "dx", size=size)
+    xh = (x.cpu().double() - wmean[:, None]) * rho[:, None]
+    close(dw, wdw, BWD, "dweight", size=float((dy.cpu().double() * xh).norm()))
+    close(db, wdb, BWD, "dbias", size=float(dy.double().norm()))
+    x[0, 0] = NAN  # of the first row alone
+    again = g.add_layernorm(ctx, x, w, b)[0]
+    assert bool(again[0].isnan().all()) and torch.equal(again[1:], y[1:])
+
+
 @pytest.mark.parametrize("width", [64, 512, 2000, 9000])
 @pytest.mark.parametrize("offset", [1e3, -3e5])
 def test_layernorm_of_rows_with_a_large_offset(g, ctx, width, offset):
