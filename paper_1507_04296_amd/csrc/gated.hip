@@ -42,7 +42,7 @@ struct GatedView {
     float *state_out, *marks, *dstate;
     float* state_copy;     // [B][C] where there are segments: state_out may be state
     float *map_a, *map_h;  // [B][maps][C]: product of decays (negative: an episode starts there), end
-    float* parts;          // [items][C] of da_log
+    float *parts, *dal;    // [items][C] of da_log, and where a lone one goes
     int items;             // workgroups that share a tile's sequences and segments
 };
 
@@ -573,7 +573,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
         const float2 s = sums[k][at.lane];
         dal[0] += s.x, dal[1] += s.y;
     }
-    put2<PAIR>(v.parts + (int64_t)(blockIdx.x / v.tiles) * v.C + at.c, dal, at.n);
+    put2<PAIR>((v.items == 1 ? v.dal : v.parts + (int64_t)(blockIdx.x / v.tiles) * v.C) + at.c, dal, at.n);
 }
 
 // One step of every row: four channels a lane.
@@ -771,6 +771,7 @@ int gorila_gated_scan_backward(const gorila_gated_scan_args* args, const float* 
     v.tiles = k.tiles, v.nseg = k.nseg, v.seg = k.seg, v.maps = k.maps, v.span = k.span;
     const int64_t items = (int64_t)v.B * k.nseg;
     v.items = (int)(items < Plan::walks(k.tiles) ? items : Plan::walks(k.tiles));
+    v.dal = da_log;
     v.dy = {dy, dy_batch_stride, dy_step_stride};
     v.marks_in = marks, v.dstate_out = dstate_out, v.dx = dx, v.dga = dgate_a, v.dgx = dgate_x, v.dstate = dstate;
     v.map_a = (float*)c.ws, v.map_h = (float*)(c.ws + p.maps), v.parts = (float*)(c.ws + 2 * p.maps + p.states);
@@ -782,7 +783,7 @@ int gorila_gated_scan_backward(const gorila_gated_scan_args* args, const float* 
             if (waves == 1) gated_backward_kernel<T, PAIR, 1, S><<<(unsigned)(v.items * k.tiles), 64, 0, c.stream>>>(v);
             else gated_backward_kernel<T, PAIR, 4, S><<<(unsigned)(v.items * k.tiles), 256, 0, c.stream>>>(v);
         });
-    launch_sum_parts(v.parts, v.items, v.C, v.C, 1, da_log, nullptr, c.stream);
+    if (v.items != 1) launch_sum_parts(v.parts, v.items, v.C, v.C, 1, da_log, nullptr, c.stream);
     return launched();
 }
 

@@ -160,7 +160,7 @@ struct LayerArgs {
     int width;
     float eps;
     void *y, *total, *dx;
-    float *mean, *rstd, *parts;
+    float *mean, *rstd, *parts, *dweight, *dbias;
 };
 
 // The mean is rounded, and a row's offset may be many times its deviations: the sum of
@@ -278,10 +278,20 @@ __global__ __launch_bounds__(LANES <= 64 ? 512 : LANES) void layernorm_backward_
             }
         }
     if (own != 0) return;
+    if (gridDim.x == 1) {  // no other workgroup's to add
+        using Any = gorila::Row<T, LANES, QUADS, false>;
+        Any::store_columns(dw, a.dweight, a.width, l);
+        if (a.dbias) Any::store_columns(db, a.dbias, a.width, l);
+        return;
+    }
     float* part = a.parts + (int64_t)blockIdx.x * 2 * a.width;
     Row::store_columns(dw, part, a.width, l);
     Row::store_columns(db, part + a.width, a.width, l);
 }
+
+// Turns over the rows up to which one workgroup takes all of them, so that no launch adds sums: a
+// turn is 0.7 us (1.4 where rows are wide), the launch 2.2 us in a graph and 3 outside.
+constexpr int ALONE = 4, ALONE_WIDE = 3;
 
 // Lanes and quads of a row: narrow rows share a wave, 8 values a lane (125000 x 64 bf16: 17 us
 // forward, 19 backward; a wave each 51 and 50).  The backward holds six values a column, where
@@ -363,7 +373,7 @@ int gorila_add_layernorm_backward(const void* dy, int64_t dy_stride, const void*
                                   void* dx, float* dweight, float* dbias, gorila_ctx* ctx) {
     LayerArgs a{};
     a.dy = dy, a.dys = dy_stride, a.dtotal = dtotal, a.dts = dtotal ? dtotal_stride : 0, a.total_in = total, a.mean_in = mean;
-    a.rstd_in = rstd, a.weight = weight, a.rows = rows, a.width = width, a.dx = dx;
+    a.rstd_in = rstd, a.weight = weight, a.rows = rows, a.width = width, a.dx = dx, a.dweight = dweight, a.dbias = dbias;
     CtxView c;
     int rc = ctx_view(ctx, 0, c);
     if (rc || (rc = check_layer(a, dtype))) return rc;
@@ -381,13 +391,13 @@ int gorila_add_layernorm_backward(const void* dy, int64_t dy_stride, const void*
     by_layer_width<true>(width, [&](auto lanes, auto quads) {
         constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, THREADS = L <= 64 ? 512 : L, ROWS = THREADS / L;
         const int64_t need = (rows + ROWS - 1) / ROWS;
-        parts = (int)(need < NORM_PARTS ? need : NORM_PARTS);
+        parts = need <= (L <= 256 ? ALONE : ALONE_WIDE) ? rows > 0 : (int)(need < NORM_PARTS ? need : NORM_PARTS);
         if (parts == 0) return;
         by_rows(dtype, even, [&](auto t, auto ev) {
             layernorm_backward_kernel<decltype(t), L, QD, decltype(ev)::value><<<parts, THREADS, 0, c.stream>>>(a);
         });
     });
-    launch_sum_parts(a.parts, parts, 2 * (int64_t)width, width, 1, dweight, dbias, c.stream);
+    if (parts != 1) launch_sum_parts(a.parts, parts, 2 * (int64_t)width, width, 1, dweight, dbias, c.stream);
     return launched();
 }
 

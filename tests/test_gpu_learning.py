@@ -149,6 +149,9 @@ def test_layernorm_narrow_rows(g, ctx, rows, width, dtype):
     xh = (x.cpu().double() - wmean[:, None]) * rho[:, None]
     close(dw, wdw, BWD, "dweight", size=float((dy.cpu().double() * xh).norm()))
     close(db, wdb, BWD, "dbias", size=float(dy.double().norm()))
+    dx2, dw2, _ = g.add_layernorm_backward(ctx, dy, x, mean, rstd, w)
+    close(dx2, ref.layernorm_backward(dy, x, w, EPS)[0], tol_of(dtype, BWD), "dx", size=size)
+    assert torch.equal(dw2, dw)
     x[0, 0] = NAN  # of the first row alone
     again = g.add_layernorm(ctx, x, w, b)[0]
     assert bool(again[0].isnan().all()) and torch.equal(again[1:], y[1:])
