@@ -46,14 +46,14 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*sm)[N]) {
 // (34571 x 781 bf16: 51 us forward, 54 backward; with a branch for the end 63 and 153, in
 // single values 132 and 225).
 template <class T> constexpr int PER = 16 / sizeof(T);  // values
-template <bool EVEN, class T>
+template <bool EVEN, bool PAST, class T>
 __device__ __forceinline__ uint4 load_piece(const T* p, int c, int width) {
     constexpr int W = PER<T>;
     uint4 u{0, 0, 0, 0};
     if constexpr (EVEN) {
         if (c < width) u = *(const uint4*)(p + c);
     } else if (width >= W) {
-        u = load_any<uint4>(p + (c < width - W ? c : width - W));
+        if (PAST || c < width) u = load_any<uint4>(p + (c < width - W ? c : width - W));
     } else if (c == 0) {
         T t[W] = {};
 #pragma unroll
@@ -63,15 +63,16 @@ __device__ __forceinline__ uint4 load_piece(const T* p, int c, int width) {
     }
     return u;
 }
-template <bool EVEN, class T>
+template <bool EVEN, bool PAST, class T>
 __device__ __forceinline__ uint4 move_piece(uint4 u, int c, int width) {
     constexpr int W = PER<T>;
     if (EVEN || width < W) return u;
     const int by = c - (width - W);  // 1 to W - 1 at the row's end, more past it
+    if (W == 8 && __ballot(by > 0) == 0) return u;
     if (by > 0 && (by & (W / 2))) u = uint4{u.z, u.w, 0, 0};
     if (by > 0 && (by & (W / 4))) u = uint4{u.y, u.z, u.w, 0};
     if (W == 8 && by > 0 && (by & 1)) u = uint4{u.x >> 16 | u.y << 16, u.y >> 16 | u.z << 16, u.z >> 16 | u.w << 16, u.w >> 16};
-    return by >= W ? uint4{0, 0, 0, 0} : u;
+    return PAST && by >= W ? uint4{0, 0, 0, 0} : u;
 }
 template <bool EVEN, class T>
 __device__ __forceinline__ void store_piece(T* p, uint4 u, int c, int width) {
@@ -92,19 +93,19 @@ __device__ __forceinline__ f32x4 floats(uint4 u) { return f32x4{__uint_as_float(
 __device__ __forceinline__ uint4 bits(f32x4 v) { return uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}; }
 
 // A row as it is read; its values as norm_rows.h holds them.
-template <class T, int LANES, int QUADS, bool EVEN>
+template <class T, int LANES, int QUADS, bool EVEN, bool PAST = false>
 struct Row {
     static constexpr int W = PER<T>, PIECES = QUADS * 4 / W;
     uint4 u[PIECES];
     __device__ __forceinline__ static int column_of(int l, int i) { return (l + i * LANES) * W; }
     __device__ __forceinline__ Row(const T* p, int width, int l) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) u[i] = load_piece<EVEN>(p, column_of(l, i), width);
+        for (int i = 0; i < PIECES; ++i) u[i] = load_piece<EVEN, PAST>(p, column_of(l, i), width);
     }
     __device__ __forceinline__ void values(f32x4 (&v)[QUADS], int width, int l) const {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint4 m = move_piece<EVEN, T>(u[i], column_of(l, i), width);
+            const uint4 m = move_piece<EVEN, PAST, T>(u[i], column_of(l, i), width);
             if constexpr (W == 8) {
                 v[2 * i] = floats(uint4{m.x << 16, m.x & 0xffff0000u, m.y << 16, m.y & 0xffff0000u});
                 v[2 * i + 1] = floats(uint4{m.z << 16, m.z & 0xffff0000u, m.w << 16, m.w & 0xffff0000u});
@@ -131,9 +132,9 @@ struct Row {
     __device__ __forceinline__ static void columns(f32x4 (&v)[QUADS], const float* p, int width, int l) {
         uint4 m[QUADS];
 #pragma unroll
-        for (int i = 0; i < QUADS; ++i) m[i] = load_piece<EVEN>(p, column<W, LANES>(l, i), width);
+        for (int i = 0; i < QUADS; ++i) m[i] = load_piece<EVEN, PAST>(p, column<W, LANES>(l, i), width);
 #pragma unroll
-        for (int i = 0; i < QUADS; ++i) v[i] = floats(move_piece<EVEN, float>(m[i], column<W, LANES>(l, i), width));
+        for (int i = 0; i < QUADS; ++i) v[i] = floats(move_piece<EVEN, PAST, float>(m[i], column<W, LANES>(l, i), width));
     }
     __device__ __forceinline__ static void store_columns(const f32x4 (&v)[QUADS], float* p, int width, int l) {
 #pragma unroll
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(LANES <= 64 ? 512 : LANES) void layernorm_backward_
     __shared__ __align__(16) float sums[ROWS > 1 ? ROWS / 2 * COLS : 4];
     __shared__ float sm[(LANES + 63) / 64][3];
     const int l = threadIdx.x % LANES, own = threadIdx.x / LANES;
-    using Row = Row<T, LANES, QUADS, EVEN>;
+    using Row = Row<T, LANES, QUADS, EVEN, sizeof(T) == 4>;
     f32x4 dw[QUADS], db[QUADS], w[QUADS];
     Row::columns(w, a.weight, a.width, l);
 #pragma unroll
@@ -294,16 +295,16 @@ __global__ __launch_bounds__(LANES <= 64 ? 512 : LANES) void layernorm_backward_
 constexpr int ALONE = 4, ALONE_WIDE = 3;
 
 // Lanes and quads of a row: narrow rows share a wave, 8 values a lane (125000 x 64 bf16: 17 us
-// forward, 19 backward; a wave each 51 and 50).  The backward holds six values a column, where
-// the root-mean-square norm's holds five.
-template <bool BACKWARD, class F>
+// forward, 19 backward; a wave each 51 and 50), wide ones have 8 or 16 values a lane: with 32,
+// as the root-mean-square norm's forward, uneven rows have few waves a unit (10494 x 2001
+// fp32 72 us, so 64; even ones of 1200 bf16 34 and 37).
+template <class F>
 void by_layer_width(int width, F&& f) {
     auto k = [&](auto lanes, auto quads) { f(lanes, quads); };
     using std::integral_constant;
     if (width <= 32) k(integral_constant<int, 4>{}, integral_constant<int, 2>{});
     else if (width <= 128) k(integral_constant<int, 16>{}, integral_constant<int, 2>{});
     else if (width <= 256) k(integral_constant<int, 32>{}, integral_constant<int, 2>{});
-    else if constexpr (!BACKWARD) by_width(width, f);
     else if (width <= 512) k(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     else if (width <= 1024) k(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else if (width <= 2048) k(integral_constant<int, 256>{}, integral_constant<int, 2>{});
@@ -352,7 +353,7 @@ int gorila_add_layernorm(const void* x, int64_t x_stride, const void* residual, 
     bool even = !(strides & (16 / e - 1)) && aligned16(weight) && aligned16(bias);
     for (const void* p : {x, residual, (const void*)y, (const void*)total}) even = even && aligned16(p);
     bool fits = true;
-    by_layer_width<false>(width, [&](auto lanes, auto quads) {
+    by_layer_width(width, [&](auto lanes, auto quads) {
         constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, ROWS = L < 256 ? 256 / L : 1;
         fits = launch_fits((double)((rows + ROWS - 1) / ROWS), L < 256 ? 256 : L);
         if (!fits) return;
@@ -388,10 +389,11 @@ int gorila_add_layernorm_backward(const void* dy, int64_t dy_stride, const void*
     bool even = !(strides & (16 / e - 1)) && aligned16(weight);
     for (const void* p : {dy, dtotal, total, (const void*)dx}) even = even && aligned16(p);
     int parts = 0;
-    by_layer_width<true>(width, [&](auto lanes, auto quads) {
+    by_layer_width(width, [&](auto lanes, auto quads) {
         constexpr int L = decltype(lanes)::value, QD = decltype(quads)::value, THREADS = L <= 64 ? 512 : L, ROWS = THREADS / L;
         const int64_t need = (rows + ROWS - 1) / ROWS;
-        parts = need <= (L <= 256 ? ALONE : ALONE_WIDE) ? rows > 0 : (int)(need < NORM_PARTS ? need : NORM_PARTS);
+        constexpr int MOST = L < 512 ? NORM_PARTS : NORM_PARTS / 2;  // one a compute unit; a part's sums are 8 bytes a column
+        parts = need <= (L <= 256 ? ALONE : ALONE_WIDE) ? rows > 0 : (int)(need < MOST ? need : MOST);
         if (parts == 0) return;
         by_rows(dtype, even, [&](auto t, auto ev) {
             layernorm_backward_kernel<decltype(t), L, QD, decltype(ev)::value><<<parts, THREADS, 0, c.stream>>>(a);
