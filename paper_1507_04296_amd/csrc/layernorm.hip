@@ -10,13 +10,14 @@
 namespace gorila {
 namespace {
 
-// The sum over a row's 4, 16 or 32 lanes, inside a wave: lanes beside one another, pairs, then
+// The sum over a row's 4, 8, 16 or 32 lanes, inside a wave: lanes beside one another, pairs, then
 // from half a row of DPP's 16 lanes to the other, and from row to row.
 template <int LANES>
 __device__ __forceinline__ float over_lanes(float v) {
     v += lane_of<0xb1, 0xf>(v);
     v += lane_of<0x4e, 0xf>(v);
-    if (LANES > 4) v += lane_of<0x141, 0xf>(v), v += lane_of<0x140, 0xf>(v);
+    if (LANES > 4) v += lane_of<0x141, 0xf>(v);
+    if (LANES > 8) v += lane_of<0x140, 0xf>(v);
     if (LANES > 16) v += __shfl_xor(v, 16, 64);
     return v;
 }
@@ -296,15 +297,17 @@ __global__ __launch_bounds__(LANES <= 64 ? 512 : LANES) void layernorm_backward_
 // turn is 0.7 us (1.4 where rows are wide), the launch 2.2 us in a graph and 3 outside.
 constexpr int ALONE = 4, ALONE_WIDE = 3;
 
-// Lanes and quads of a row: narrow rows share a wave, 8 values a lane (125000 x 64 bf16: 17 us
-// forward, 19 backward; a wave each 51 and 50), wide ones have 8 or 16 values a lane: with 32,
-// as the root-mean-square norm's forward, uneven rows have few waves a unit (10494 x 2001
-// fp32 72 us, so 64; even ones of 1200 bf16 34 and 37).
+// Lanes and quads of a row: narrow rows share a wave, 8 values a lane (421875 x 64 bf16: 37 us
+// forward, 43 backward, with 16 lanes a row 51 and 50; a wave each takes three times as
+// long), wide ones have 8 or 16 values a lane: with 32, as the root-mean-square norm's
+// forward, uneven rows have few waves a unit (10494 x 2001 fp32 72 us, so 64; even ones of
+// 1200 bf16 34 and 37).
 template <class F>
 void by_layer_width(int width, F&& f) {
     auto k = [&](auto lanes, auto quads) { f(lanes, quads); };
     using std::integral_constant;
     if (width <= 32) k(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+    else if (width <= 64) k(integral_constant<int, 8>{}, integral_constant<int, 2>{});
     else if (width <= 128) k(integral_constant<int, 16>{}, integral_constant<int, 2>{});
     else if (width <= 256) k(integral_constant<int, 32>{}, integral_constant<int, 2>{});
     else if (width <= 512) k(integral_constant<int, 64>{}, integral_constant<int, 2>{});
