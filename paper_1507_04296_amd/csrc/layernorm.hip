@@ -301,7 +301,7 @@ constexpr int ALONE = 4, ALONE_WIDE = 3;
 // forward, 43 backward, with 16 lanes a row 51 and 50; a wave each takes three times as
 // long), wide ones have 8 or 16 values a lane: with 32, as the root-mean-square norm's
 // forward, uneven rows have few waves a unit (10494 x 2001 fp32 72 us, so 64; even ones of
-// 1200 bf16 34 and 37).
+// 1200 bf16 34 and 37).  Backward of 4797 x 4377: 65 us bf16 and 78 fp32, with 16 values 70 and 87.
 template <class F>
 void by_layer_width(int width, F&& f) {
     auto k = [&](auto lanes, auto quads) { f(lanes, quads); };
@@ -314,7 +314,8 @@ void by_layer_width(int width, F&& f) {
     else if (width <= 1024) k(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else if (width <= 2048) k(integral_constant<int, 256>{}, integral_constant<int, 2>{});
     else if (width <= 4096) k(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    else if (width <= 8192) k(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+    else if (width <= 6144) k(integral_constant<int, 768>{}, integral_constant<int, 2>{});
+    else if (width <= 8192) k(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
     else if (width <= 16384) k(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
     else k(integral_constant<int, 1024>{}, integral_constant<int, 16>{});
 }
