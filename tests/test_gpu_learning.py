@@ -236,6 +236,19 @@ def test_layernorm_ends_of_rows(g, ctx, width, dtype):
             close(flat[1:-1], want, BWD, "sums", size=float(want.norm()) + float(dy.double().norm()))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,width", [(3, 20), (200, 53), (9, 512), (70, 781), (40, 4377), (7, 8000)])
+def test_layernorm_in_a_graph(g, ctx, rows, width, dtype):
+    """Sums by one workgroup and by many, replayed."""
+    x, r, dy, dt = (rand(rows, width, dtype=dtype, seed=k) for k in (1, 2, 3, 4))
+    w, b = 1 + rand(width, scale=0.1, seed=5), rand(width, scale=0.1, seed=6)
+
+    def call():
+        y, total, mean, rstd = g.add_layernorm(ctx, x, w, b, r, EPS)
+        return (y, total, mean, rstd, *g.add_layernorm_backward(ctx, dy, total, mean, rstd, w, dt))
+    replayed(call, lambda o: o, [v.clone() for v in call()])
+
+
 def test_layernorm_refusals(g, ctx):
     x, w = rand(3, 8), rand(8)
     y, total, mean, rstd = g.add_layernorm(ctx, x, w)
@@ -471,6 +484,16 @@ def test_gated_scan_refusals(g, ctx):
         with pytest.raises(g.GorilaError, match="EWORKSPACE"):
             call()
     bare.close()
+
+
+@pytest.mark.parametrize("T", [1, 100])
+def test_gated_scan_of_one_sequence_in_a_graph(g, ctx, T):
+    args, reset, state, dy, dstate = gated_inputs(1, T, 65, seed=98)
+
+    def call():
+        y, out, marks = g.gated_scan(ctx, *args, reset, state)
+        return (y, out, *g.gated_scan_backward(ctx, dy, *args, marks, reset, dstate))
+    replayed(call, lambda o: o, [v.clone() for v in call()])
 
 
 def test_gated_scan_in_a_graph(g, ctx):
