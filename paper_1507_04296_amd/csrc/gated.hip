@@ -49,6 +49,15 @@ struct GatedView {
 __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -LOG2E));
 }
+// A sigmoid and what it leaves to 1, which is not formed as the difference where the gate is
+// open: nothing is left of that (at a gate of 8 it is off by 1e-4 of itself, at 17 it is 0).
+struct Gate {
+    float open, rest;
+};
+__device__ __forceinline__ Gate gate_of(float v) {
+    const float e = __builtin_amdgcn_exp2f(v * -LOG2E), open = __builtin_amdgcn_rcpf(1.0f + e);
+    return {open, v < 0.0f ? 1.0f - open : e * open};
+}
 // exp(a_log) for a base of two: log2 a = -rate2 sigmoid(gate_a).
 __device__ __forceinline__ float rate2_of(float a_log) {
     const float e = expf(a_log);
@@ -408,8 +417,10 @@ __global__ __launch_bounds__(64 * W) void gated_back_kernel(GatedView v) {
 //   dgate_a = G (1 - r),   da_log = sum of G      (at a start G is zero).
 // Chunks are walked from the last on; the state before every fourth wave's steps is a
 // mark, so that both directions are in registers at once and every value is read once.
+// What the gates give is held as the outputs take it (u = b i x, b i, a log a, its quotient by
+// b^2 and a, 1 - r and 1 - i): two waves a SIMD have room for it.  One wave has one chunk.
 template <class T, bool PAIR, int W, int S>
-__global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
+__global__ __launch_bounds__(64 * W, 2) void gated_backward_kernel(GatedView v) {
     constexpr int CHUNK = 2 * S * W, GROUP = MARK / (2 * S);  // steps, waves that share a mark
     __shared__ Shared<W, 2> sh[2];
     __shared__ float2 sums[2 * W][32];
@@ -453,7 +464,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
             const uint32_t mask = starts(reset), own = at.half ? mask >> S : mask & ((1u << S) - 1);
             const bool plain = mask == 0 && t0 + CHUNK <= end;
             const bool cut0 = mask & ((1u << S) - 1), cut1 = mask >> S;
-            Two r[S], i[S], a[S], bb[S], A{{1.0f, 1.0f}}, F{{0.0f, 0.0f}}, H{{0.0f, 0.0f}};
+            Two a[S], w[S], over[S], bi[S], rr[S], ri[S], u[S], A{{1.0f, 1.0f}}, F{{0.0f, 0.0f}}, H{{0.0f, 0.0f}};
             auto runs = [&](auto simple) {
                 constexpr bool PLAIN = decltype(simple)::value;
 #pragma unroll
@@ -462,11 +473,17 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
                     const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        r[k][j] = sigmoid(gav[j]);
-                        i[k][j] = sigmoid(gxv[j]);
-                        const Decay d = decay(-rate2[j] * r[k][j]);
+                        const Gate r = gate_of(gav[j]), i = gate_of(gxv[j]);
+                        const float l = -rate2[j] * r.open;
+                        const Decay d = decay(l);
+                        rr[k][j] = r.rest, ri[k][j] = i.rest;
+                        // a log a before any other factor: log a may be as large as fp32 goes where a is 0;
+                        // its quotient by b twice is 1/2 at most
+                        w[k][j] = d.a * (l * LN2);
                         a[k][j] = in ? d.a : 1.0f;
-                        bb[k][j] = !in ? 0.0f : start ? 1.0f : d.b;
+                        const float b = !in ? 0.0f : start ? 1.0f : d.b, per = __builtin_amdgcn_rcpf(b);
+                        over[k][j] = b > 0.0f ? w[k][j] * a[k][j] * per * per : 0.0f;
+                        bi[k][j] = b * i.open;
                     }
                 }
 #pragma unroll
@@ -475,8 +492,8 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
                     const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float u = in ? bb[k][j] * i[k][j] * xv[j] : 0.0f;
-                        F[j] = start ? u : fmaf(a[k][j], F[j], u);
+                        u[k][j] = in ? bi[k][j] * xv[j] : 0.0f;
+                        F[j] = start ? u[k][j] : fmaf(a[k][j], F[j], u[k][j]);
                         A[j] *= a[k][j];
                     }
                 }
@@ -490,7 +507,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
             };
             if (plain) runs(std::true_type{});
             else runs(std::false_type{});
-            if (t0 > begin) fetch_two(ga, gx, t0 - CHUNK);
+            if (W > 1 && t0 > begin) fetch_two(ga, gx, t0 - CHUNK);
             const Two oa = other_half(A), of = other_half(F), oh = other_half(H);
             Two back = carry;
             if (W > 1) {
@@ -525,31 +542,21 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
                 Two h[S];  // the state before the step
 #pragma unroll
                 for (int k = 0; k < S; ++k) {
-                    const Two xv = x.r[k].get(at);
-                    const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
                     h[k] = now;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float u = in ? bb[k][j] * i[k][j] * xv[j] : 0.0f;
-                        now[j] = start ? u : fmaf(a[k][j], now[j], u);
-                    }
+                    now = through(a[k], u[k], !PLAIN && (own >> k & 1u), now);
                 }
 #pragma unroll
                 for (int k = S - 1; k >= 0; --k) {
-                    const Two xv = x.r[k].get(at), d = dy.r[k].get(at);
+                    const Two d = dy.r[k].get(at);
                     const bool start = !PLAIN && (own >> k & 1u), in = PLAIN || t + k < end;
                     Two dx, dga, dgx;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float R = (in ? d[j] : 0.0f) + back[j], Ri = R * i[k][j];
-                        dx[j] = Ri * bb[k][j];
-                        dgx[j] = dx[j] * xv[j] * (1.0f - i[k][j]);
-                        // log a times a, before any other factor: log a may be as large as fp32 goes where a is 0;
-                        // with log a, its quotient by b goes to zero as a root
-                        const float l = a[k][j] * (-rate2[j] * LN2 * r[k][j]);
-                        const float over = bb[k][j] > 0.0f ? l * a[k][j] * __builtin_amdgcn_rcpf(bb[k][j]) : 0.0f;
-                        const float G = start ? 0.0f : R * (l * h[k][j]) - Ri * xv[j] * over;
-                        dga[j] = G * (1.0f - r[k][j]);
+                        const float R = (in ? d[j] : 0.0f) + back[j], Ru = R * u[k][j];
+                        dx[j] = R * bi[k][j];
+                        dgx[j] = Ru * ri[k][j];
+                        const float G = start ? 0.0f : R * (w[k][j] * h[k][j]) - Ru * over[k][j];
+                        dga[j] = G * rr[k][j];
                         if (in) dal[j] += G;
                         back[j] = start ? 0.0f : a[k][j] * R;
                     }
@@ -562,6 +569,7 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(GatedView v) {
             };
             if (plain) outputs(std::true_type{});
             else outputs(std::false_type{});
+            if (W == 1) break;  // (T is at most a chunk)
         }
         if (seg == 0 && v.dstate && threadIdx.x < 32) put2<PAIR>(v.dstate + b * v.C + at.c, carry, at.n);
     }
@@ -686,7 +694,7 @@ int gated_view(const gorila_gated_scan_args* a, GatedView& v) {
 // else four: one of eight leaves no place for a second (300 x 200 x 128 fp32, 600
 // workgroups: 26 us, eight waves 34; 320 of 500 steps 39 and 43), and two chunks or
 // more have loads under way while one is joined (32 x 128 x 1024 fp32: 14.6 us; 18.4).
-// Backward a lane has 222 registers, and more waves than two a SIMD do not pay: 8 steps a lane
+// Backward a lane has up to 247 registers, and more waves than two a SIMD do not pay: 8 steps a lane
 // and four waves 22.7 us (5.2 TB/s), eight waves 27.6; 4 steps and eight waves, half of the
 // registers, 26.2.
 constexpr int S = 8;
