@@ -110,18 +110,22 @@ __device__ __forceinline__ int code_of(float unit, uint32_t chance, int least) {
     const int c = (int)((__float_as_uint(unit) + (chance << 4)) >> 20) - least;
     return c < 0 ? 0 : c;
 }
-// m / (sqrt(v) + eps) to three units of the last place, v from the smallest fp32 value on.
+// m / (sqrt(v) + eps) to three units of the last place, v from the smallest fp32 value on.  The
+// reciprocal takes and gives normal numbers alone: an eps that may lie outside (ODD; a root is
+// 0 or 2^-75 to 2^64) has a copy of the code that divides.
+bool odd(float eps) { return (eps > 0.0f && eps < 0x1p-126f) || eps > 0x1p125f; }
+template <bool ODD>
 __device__ __forceinline__ float step_of(float m, float v, float eps) {
     const bool tiny = v < 0x1p-100f;
     const float root = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p-32f : 1.0f);
-    return m * __builtin_amdgcn_rcpf(root + eps);
+    return ODD ? m / (root + eps) : m * __builtin_amdgcn_rcpf(root + eps);
 }
 __device__ __forceinline__ float wave_max(float v) {  // of sizes
     return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // G: the gradients' type; BITS: the states'.
-template <class G, int BITS>
+template <class G, int BITS, bool ODD>
 __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
 // m' and v' are held to the bit as the header says: products and sums are rounded apart
 #pragma clang fp contract(off)
@@ -175,7 +179,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(Tensors s, Rule r) {
             for (int j = 0; j < 4; ++j) {
                 m[k][j] = r.beta1 * m[k][j] + r.rest1 * g[k][j];
                 v[k][j] = r.beta2 * v[k][j] + r.rest2 * (g[k][j] * g[k][j]);
-                theta[k][j] = theta[k][j] - r.lr * (t.decay * theta[k][j] + step_of(m[k][j] * c1, v[k][j] * c2, r.eps));
+                theta[k][j] = theta[k][j] - r.lr * (t.decay * theta[k][j] + step_of<ODD>(m[k][j] * c1, v[k][j] * c2, r.eps));
             }
             quad_store(t.theta + p, theta[k], n);
             if (BITS == 32) {
@@ -317,13 +321,16 @@ int gorila_adamw(const gorila_adamw_tensor* tensors, int32_t count, int32_t grad
             t.theta = from.theta, t.grad = from.grad, t.m = from.m, t.v = from.v, t.m_scale = from.m_scale, t.v_scale = from.v_scale;
         },
         [&](const Tensors& s, unsigned chunks) {
-            if (grad_dtype == GORILA_F32) {
-                if (state_bits == 32) adamw_kernel<float, 32><<<chunks, 256, 0, c.stream>>>(s, r);
-                else adamw_kernel<float, 8><<<chunks, 256, 0, c.stream>>>(s, r);
-            } else {
-                if (state_bits == 32) adamw_kernel<uint16_t, 32><<<chunks, 256, 0, c.stream>>>(s, r);
-                else adamw_kernel<uint16_t, 8><<<chunks, 256, 0, c.stream>>>(s, r);
-            }
+            auto go = [&](auto g, auto bits, auto odd_eps) {
+                adamw_kernel<decltype(g), decltype(bits)::value, decltype(odd_eps)::value><<<chunks, 256, 0, c.stream>>>(s, r);
+            };
+            auto by_bits = [&](auto g, auto odd_eps) {
+                using std::integral_constant;
+                if (state_bits == 32) go(g, integral_constant<int, 32>{}, odd_eps);
+                else go(g, integral_constant<int, 8>{}, odd_eps);
+            };
+            auto by_type = [&](auto odd_eps) { grad_dtype == GORILA_F32 ? by_bits(float{}, odd_eps) : by_bits(uint16_t{}, odd_eps); };
+            odd(eps) ? by_type(std::true_type{}) : by_type(std::false_type{});
         });
     return launched();
 }

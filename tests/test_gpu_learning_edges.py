@@ -1,10 +1,10 @@
-"""The gated scan's gates far from zero.  Tolerances are those of test_gpu_learning.py
-where nothing else is said."""
+"""The gated scan's gates far from zero and AdamW's eps at both ends of fp32.  Tolerances
+are those of test_gpu_learning.py where nothing else is said."""
 import pytest
 import torch
 
 import learning_ref as ref
-from test_gpu_learning import BF16, BWD, F32, FWD, close, ctx, g, gated_inputs, tol_of, uniform  # noqa: F401
+from test_gpu_learning import BF16, BWD, F32, FWD, check_step, close, ctx, g, gated_inputs, rand, tol_of, uniform  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,18 @@ def test_gated_scan_gradients_of_saturated_gates(g, ctx, T, sign, dtype):  # noq
     for k, name in ((1, "dgate_a"), (2, "dgate_x")):
         slope = torch.sigmoid(-args[k].cpu().double().abs())
         close(got[k].cpu().double() / slope, want[k] / slope, tol_of(dtype, BWD), name)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-45, 1e-40, 1e38, 3e38])
+def test_adamw_eps_at_the_ends(g, ctx, bits, eps):  # noqa: F811
+    """An eps below and far above the normal numbers, beside v of zero (no gradient at all, and squares that underflow) and not."""
+    theta = rand(1024, seed=1, scale=0.05)
+    theta[700:] = 0
+    grad = rand(1024, seed=2)
+    grad[:256], grad[256:512], grad[512:768] = 0, 1e-30, 1e18
+    states, clock = g.adamw_state([theta], bits), g.adamw_clock()
+    was = theta[:256].clone()
+    for _ in range(2):
+        check_step(g, ctx, [theta], [grad], states, clock, 0.0, seed=5, eps=eps)
+    assert torch.equal(theta[:256], was)
