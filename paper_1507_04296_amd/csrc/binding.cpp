@@ -147,6 +147,11 @@ int32_t row_type(const Tensor& x) {
 Tensor make(c10::IntArrayRef shape, const Tensor& like, at::ScalarType dtype) { return at::empty(shape, like.options().dtype(dtype)); }
 Tensor same(const Tensor& t) { return at::empty(t.sizes(), t.options()); }
 void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+// What a call has written in place counts a new version, as after every such update, for
+// graphs that still need the old values.
+void changed(const Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 
 // A tuple of tensors; an undefined one is None.
 PyObject* tuple(std::initializer_list<const Tensor*> ts) {
@@ -287,6 +292,7 @@ PyObject* causal_conv_step(PyObject* const* args, Py_ssize_t n) {
     const int32_t* slot = (const int32_t*)c.at(c.maybe(8, "slot"), "slot", {v.a.batch}, at::kInt);
     const Tensor y = same(v.x);
     c.check(api.causal_conv_step(&v.a, p, slots, slot, ptr(y), c.ctx), "gorila_causal_conv_step");
+    changed(pool);
     return one(y);
 }
 
@@ -359,6 +365,7 @@ PyObject* scan_step(PyObject* const* args, Py_ssize_t n) {
     const int32_t* slot = (const int32_t*)c.at(c.maybe(12, "slot"), "slot", {v.a.batch}, at::kInt);
     const Tensor y = same(v.x);
     c.check(api.scan_step(&v.a, p, slots, slot, ptr(y), c.ctx), "gorila_scan_step");
+    changed(pool);
     return one(y);
 }
 
@@ -502,6 +509,7 @@ PyObject* gated_scan_step(PyObject* const* args, Py_ssize_t n) {
     const int32_t* slot = (const int32_t*)c.at(c.maybe(8, "slot"), "slot", {(int64_t)v.a.batch}, at::kInt);
     const Tensor y = same(v.x);
     c.check(api.gated_scan_step(&v.a, p, slots, slot, ptr(y), c.ctx), "gorila_gated_scan_step");
+    changed(pool);
     return one(y);
 }
 
@@ -592,9 +600,11 @@ PyObject* adamw(PyObject* const* args, Py_ssize_t n) {
     const uint8_t* pk = keep ? (const uint8_t*)c.at(keep, "keep", {1}, at::kByte) : nullptr;
     c.check(api.adamw(ts.data(), size32(thetas.n), dtype, bits, clock, pk, c.number(7), c.real(8), c.real(9), c.number(10), c.bits(12), c.ctx),
             "gorila_adamw");
-    for (Py_ssize_t i = 0; i < thetas.n; ++i) {  // as every update in place does, for graphs that still need the old values
-        const Tensor& theta = thetas.tensor(i, "thetas");
-        if (!theta.is_inference()) theta.unsafeGetTensorImpl()->bump_version();
+    changed(c.tensor(6, "clock"));
+    for (Py_ssize_t i = 0; i < thetas.n; ++i) {
+        changed(thetas.tensor(i, "thetas"));
+        const Listed state(states[i], "a state");
+        for (Py_ssize_t k = 0; k < state.n; ++k) changed(state.tensor(k, "a state"));
     }
     Py_RETURN_NONE;
 }

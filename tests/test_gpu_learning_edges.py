@@ -1,5 +1,6 @@
-"""The gated scan's gates far from zero and AdamW's eps at both ends of fp32.  Tolerances
-are those of test_gpu_learning.py where nothing else is said."""
+"""The gated scan's gates far from zero, AdamW's eps at both ends of fp32 and what the
+operators that write in place tell autograd.  Tolerances are those of
+test_gpu_learning.py where nothing else is said."""
 import pytest
 import torch
 
@@ -45,3 +46,35 @@ def test_adamw_eps_at_the_ends(g, ctx, bits, eps):  # noqa: F811
     for _ in range(2):
         check_step(g, ctx, [theta], [grad], states, clock, 0.0, seed=5, eps=eps)
     assert torch.equal(theta[:256], was)
+
+
+def test_what_is_written_in_place_is_a_change_for_autograd(g, ctx):  # noqa: F811
+    """States, clocks and pools count a new version with each call that writes them, as by any operation in place."""
+    theta, grad = rand(300, seed=1), rand(300, seed=2)
+    for bits in (32, 8):
+        states, clock = g.adamw_state([theta], bits), g.adamw_clock()
+        written = [theta, clock, *states[0]]
+        before = [v._version for v in written]
+        g.adamw(ctx, [theta], [grad], states, clock, 0.1)
+        assert all(v._version > b for v, b in zip(written, before)) and grad._version == 0
+    x, w = rand(2, 8, seed=3), rand(8, 4, seed=4)
+    pool = torch.zeros(2, 8, device="cuda", requires_grad=True)
+    kept = (pool * pool).sum()
+    version = pool._version
+    g.gated_scan_step(ctx, x, x, x, rand(8, seed=5), pool)
+    assert pool._version > version
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.backward()
+    window = torch.zeros(2, 3, 8, device="cuda")
+    version = window._version
+    g.causal_conv_step(ctx, x, window, w)
+    assert window._version > version
+    pool = torch.zeros(2, 1, 8, 4, device="cuda")
+    version = pool._version
+    one = torch.ones(1, device="cuda")
+    g.scan_step(ctx, x[:, None], rand(2, 1, seed=6), rand(2, 1, 4, seed=7), rand(2, 1, 4, seed=8), one, one, one, pool)
+    assert pool._version > version
+    with torch.inference_mode():  # such tensors have no versions
+        pool = torch.zeros(2, 8, device="cuda")
+        g.gated_scan_step(ctx, x, x, x, rand(8, seed=5), pool)
+        assert bool(pool.any())
