@@ -1,5 +1,6 @@
-// What the sequence operators (norm.hip, shortconv.hip, scan.hip, qmatvec.hip)
-// share: the context as they see it, and rows of fp32 or bf16 values.
+// What the sequence operators (norm.hip, layernorm.hip, shortconv.hip, scan.hip, gated.hip,
+// qmatvec.hip), adamw.hip and sample.hip share: the context as they see it, rows of fp32
+// or bf16 values, and sums over a wave.
 #pragma once
 #include "common.h"
 #include "kernels.h"
