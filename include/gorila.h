@@ -417,7 +417,9 @@ int gorila_add_rmsnorm_backward(const void* dy, int64_t dy_stride, const void* d
  * mean, rstd [rows] = mu, rho fp32; total, mean and rstd may be NULL.  EINVAL for
  * eps < 0.  Sums and squares are fp32: values whose sum is past its range make the
  * row NaN, deviations from about 2^63 on give rho 0.  A row of equal values has no
- * deviations, and y = bias, to what sqrt(1 / eps) makes of its values' rounding. */
+ * deviations, and y = bias, to what sqrt(1 / eps) makes of its values' rounding; with
+ * eps 0 such a row, and one of deviations below 2^-75, has rho infinite, and one of
+ * deviations below 2^-60 loses precision. */
 int gorila_add_layernorm(const void* x, int64_t x_stride, const void* residual,
                          int64_t residual_stride, const float* weight, const float* bias,
                          int64_t rows, int32_t width, int32_t dtype, float eps, void* y,
@@ -516,7 +518,9 @@ int gorila_scan_step(const gorila_scan_args* args, float* state_pool, int64_t sl
  * scan's state is head_dim x state_dim a head).
  *   L = -exp(a_log[c]) * sigmoid(gate_a),   a = exp(L), 0 at a reset,
  *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) * sigmoid(gate_x) * x_t   (from `state`),   y = h.
- * (At a reset the root is 1.)  1 - a^2 is formed from L, without cancellation.
+ * (At a reset the root is 1.)  1 - a^2 is formed from L, without cancellation, and in the
+ * gradients 1 - sigmoid(gate) from exp(-|gate|); a sigmoid is right to about
+ * (6 + 2 |gate|) 2^-24 of itself, and 0 below 2^-126.
  * exp(a_log) above 2^127 counts as 2^127.
  * x, gate_a, gate_x, y [batch][length][channels]; state and state_out
  * [batch][channels] (NULL: zeros / not wanted; state_out may be state).  marks
@@ -611,7 +615,7 @@ int gorila_qmatvec(const void* x, int64_t x_stride, const float* x_scale, int32_
  *
  * clock [3] fp64 (device, 8-byte aligned, zero before the first call): the number of
  * steps taken, 1 - beta1^t and 1 - beta2^t; the call advances it, so that a captured
- * call can be replayed.  keep (u8 device scalar, NULL = 1; e.g. of gorila_loss_filter):
+ * call can be replayed (with its own lr, betas, eps, decays and seed, which are the host's).  keep (u8 device scalar, NULL = 1; e.g. of gorila_loss_filter):
  * 0 leaves everything as it was, the clock included.
  * EINVAL for beta outside [0, 1), eps < 0, lr < 0, n < 0.  n of 2^35 and more, and
  * more than GORILA_ADAMW_MAX_TENSORS: GORILA_EUNSUPPORTED.  Uses no workspace. */
@@ -641,8 +645,8 @@ int gorila_adamw_values(const gorila_adamw_tensor* tensors, int32_t count, float
  * fp32 in [0, 1).  temperature, top_p, min_p [rows] fp32 and top_k [rows] int32 may be
  * NULL: 1, 1, 0 and all.  NaN counts as -infinity; with `most` the row's largest value,
  *   w = round to nearest even of 2^40 exp((value - most) / temperature),
- * formed in fp64, to about 2^-50 of itself (2^40 where value = most, also if that is infinite; 0 for
- * -infinity and beside an infinite `most`).  In the order of values, the lowest action
+ * formed in fp64, to about (1 + |log2(w / 2^40)|) 2^-52 of itself (2^40 where value = most, also if that
+ * is infinite; 0 for -infinity and beside an infinite `most`).  In the order of values, the lowest action
  * first among equal ones:
  *   top_k: the first k stay (k outside 1 .. actions: all; temperature not above 0:
  *     one, the greedy action);

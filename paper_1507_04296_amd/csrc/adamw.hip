@@ -7,10 +7,11 @@
 // which travel in the kernel's arguments: a launch for 48 tensors, and nothing to copy.
 // The clock is a launch of its own, before: all workgroups read it.
 //
-// The Q-network's ten tensors (1.69 M elements, fp32): 10.5 us (4.5 TB/s, part of it from
-// the cache) and 2.3 for the clock.  52 M elements in 8 bits, bf16 gradients: 165 us (4.45
-// TB/s; a large copy reaches 4.64), 217 with divisions, branches for the tail in every
-// chunk and sums through LDS.  Their values: 92 us (5.7 TB/s).
+// The Q-network's ten tensors (1.69 M elements, fp32): 10.2 us (4.6 TB/s, part of it from
+// the cache) and 2.2 for the clock.  52 M elements in 8 bits, bf16 gradients, three sets in
+// turn: 144 us with the clock (5.1 TB/s; a large copy, half of whose bytes are written,
+// reaches 4.65), a third more with divisions, branches for the tail in every chunk and sums
+// through LDS.  Their values: 99 us (5.3 TB/s).
 #include "seq.h"
 
 namespace gorila {

@@ -11,10 +11,12 @@
 // registers.  (4 steps of 4 channels make twice the joins: 10 % of all operations.)
 // The next chunk's loads are under way while this one's runs are joined.
 //
-// 32 x 128 x 1024 fp32: forward 14.6 us (4.6 TB/s), backward 22.5 (5.2 TB/s, part of it from
-// the cache).  4 x 1999 x 2000 bf16: forward 45 us and 18 for the maps, backward 72 and 18;
-// a prompt of 8192 x 1024 bf16: 26 and 15.  There the vector unit is busy half of the time,
-// and fewer or more waves, or loads a chunk earlier, change nothing.
+// 32 x 128 x 1024 fp32: forward 13.8 us (4.9 TB/s), backward 22.6 (5.2 TB/s, part of it from
+// the cache).  4 x 1999 x 2000 bf16: forward 46 us and 18 for the maps, backward 71 and 18;
+// a prompt of 8192 x 1024 bf16: 26 and 15.  There the vector unit is busy a third to a half of
+// the time, and fewer or more waves, or loads a chunk earlier, change nothing.  A wave
+// forms 16 steps and a tile has 64 channels, however few there are: 256 x 1 x 4096 fp32
+// 24 us forward (0.7 TB/s) and 60 backward (0.5), 512 x 200 x 16 fp32 17 and 32 (1.5).
 //
 // An episode start is a flag beside the product of decays, not a factor of zero:
 // what is before it may be infinite.  Chunks without one, and inside the sequence,

@@ -2,9 +2,12 @@
 //
 // Memory bound, as the root-mean-square norm: every value is read once and written once,
 // a row stays in the registers of its lanes between its sums and the output.  (Where it
-// fits: widths above 16384, backward 8192, keep part of it in scratch memory.)
-// 40007 x 1000 bf16: forward 60 us, backward 62 (5.3 and 5.2 TB/s) and 5 for its parts'
-// sums; 4096 x 512 fp32: 8.6 and 8.6, all rows in flight at once.
+// fits: widths above 16384, backward 8192, keep part of it in scratch memory, up to 680 and
+// 2400 bytes a lane, and uneven fp32 rows of 6145 to 8192 keep 12 bytes of it backward.  Such
+// widths are taken for completeness: 1281 x 16384 bf16 39 us forward (4.3 TB/s) and 92
+// backward (1.8), 320 x 65536 bf16 112 (1.5) and 495 (0.3).)
+// 40007 x 1000 bf16: forward 60 us, backward 61 (5.4 and 5.2 TB/s) and 5 for its parts'
+// sums; 4096 x 512 fp32: 8.6 and 8.7, all rows in flight at once.
 #include "norm_rows.h"
 
 namespace gorila {

@@ -5,7 +5,7 @@
 // filters' borders and the drawn action do not depend on how a row is cut.
 //
 // Rows of up to 64 actions have a wave each, a value a lane: a walk over the lanes
-// gives every action's rank and the sum before it (1024 x 18: 4.9 us, most of it the
+// gives every action's rank and the sum before it (1024 x 18: 5.3 us, most of it the
 // launch).  Longer rows have a workgroup.  The border of top_k (top_p) is the value at
 // which the count (the sum of weights) from the largest on reaches its target.  A
 // histogram over 2048 even bins of (most - value) / temperature, which spreads a row's
@@ -19,11 +19,11 @@
 // What bounds a workgroup: a weight is some 25 operations in fp64, of 10 cycles each
 // as measured, so 32000 of them take it 13 us.  They are formed once for every value (top_p's
 // histogram) and once more for those that stay; under top_k for those alone.
-// 256 x 32000 bf16: 22 us without a filter, 29 with top_k, 55 with top_p, 31 with both.
+// 256 x 32000 bf16: 21 us without a filter, 27 with top_k, 54 with top_p, 33 with all.
 //
 // Few rows of many actions would leave the chip idle: each is shared by up to 64
 // workgroups, a launch for each step (largest value, histogram, list, sums, action).
-// 1 x 100003 fp32, top_p: 26 us, by one workgroup 94.
+// 1 x 100003 fp32, top_p: 28 us, by one workgroup 100.
 #include "seq.h"
 
 namespace gorila {
